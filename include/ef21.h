@@ -283,6 +283,95 @@ const char *ef21_kernel_name(int kernel_class);
 int ef21_hbm_read(const void *src, int64_t bytes, float *sink, void *hip_stream);
 int ef21_hbm_copy(void *dst, const void *src, int64_t bytes, void *hip_stream);
 
+/*
+ * ---- The two ends of a language model ----
+ * The lookup of an embedding table and the losses on a model's logits, with the gradients that ef21_step takes.  Stateless:
+ * every call works on the arrays and the stream it is given, allocates and synchronises nothing (so it may be captured into a
+ * HIP graph), and where it needs scratch memory the caller passes a workspace, of which a second call of the same function tells the size.
+ * Tables, activations, logits and their gradients are fp32, bf16 or fp16 (EF21_F32, EF21_BF16, EF21_F16); arithmetic is fp32 and
+ * results are rounded once, to nearest.  Tokens and labels are int32 or int64 (EF21_I32, EF21_I64).  Two-dimensional arrays
+ * have contiguous rows `stride` entries apart, of any alignment that their type has.  Zero rows or tokens are allowed (then
+ * the arrays that would be empty may be NULL).  Every result is bitwise reproducible.
+ * EF21_EINVAL: a size or stride out of range, an unknown type, a NULL or misaligned pointer, a workspace that is too small.
+ */
+enum { EF21_F32 = 0, EF21_BF16 = 1, EF21_F16 = 2 };
+enum { EF21_I32 = 0, EF21_I64 = 1 };
+
+/*
+ * Embedding lookup: out[t] = scale * table[tokens[t]] for `count` tokens, table [vocab][width], out [count][width].  A token
+ * outside [0, vocab) is never dereferenced and gives a row of zeros.  out must not overlap the table.
+ */
+int ef21_embed(const void *table, int table_type, int64_t vocab, int64_t width, int64_t table_stride, const void *tokens,
+               int token_type, int64_t count, float scale, void *out, int out_type, int64_t out_stride, void *hip_stream);
+
+/*
+ * Its gradient for n workers at once, each with `count` tokens: for worker i
+ *   G_i[v] = scale * sum over t with tokens[i][t] = v of grad_out[i][t]          v = 0 .. vocab - 1
+ * grad_out: [n][count] rows of `width` entries, grad_stride apart;  tokens [n][count];  G_i: fp32 [vocab][width], contiguous, at
+ * table_grad + i * worker_stride -- with worker_stride = d a block of the rows [n][d] that ef21_step takes.  accumulate != 0
+ * adds to what is there (a table shared with the output layer) and leaves rows without a token untouched; 0 writes every row.
+ * Tokens outside [0, vocab) contribute nothing.  The positions are sorted by token and a token's rows are added in an order
+ * that the tokens alone fix.  n in [1, 65535], count and vocab below 2^31.
+ * workspace: 256-byte aligned device memory of at least the bytes that ef21_embed_grad_workspace says.
+ */
+int ef21_embed_grad_workspace(int32_t n, int64_t count, int64_t vocab, int64_t width, int64_t *bytes);
+int ef21_embed_grad(const void *grad_out, int type, int64_t grad_stride, const void *tokens, int token_type, int32_t n,
+                    int64_t count, int64_t vocab, int64_t width, float scale, float *table_grad, int64_t worker_stride,
+                    int accumulate, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Log-probabilities of the labels under the softmax of each row of logits [rows][vocab]:
+ *   lse[r] = log sum_v exp(x_v),   logp[r] = x_label - lse[r]
+ * A row whose label is outside [0, vocab) (a prompt's token, padding) is ignored here and in the calls below: it is not read,
+ * its logp and lse are 0, its gradient is a row of zeros.  Entries of -inf have probability zero; a row with nothing above
+ * -inf has lse = logp = -inf and a gradient of zeros.  A NaN or +inf in a row with a label makes that row's results NaN.
+ */
+int ef21_token_logps(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
+                     int label_type, float *logp, float *lse, void *hip_stream);
+
+/*
+ * The gradient of the logits from that of the log-probabilities, grad_logp [rows] (read where there is a label):
+ *   grad_logits[r][v] = grad_logp[r] * ([v = label] - exp(x_v - lse[r]))
+ * lse as ef21_token_logps gave it.  grad_logits has the logits' type; it may be the logits themselves (same stride) and must
+ * otherwise not overlap them, here and in the calls below.
+ */
+int ef21_token_logps_grad(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
+                          int label_type, const float *lse, const float *grad_logp, void *grad_logits, int64_t grad_stride,
+                          void *hip_stream);
+
+/*
+ * Preference loss of `pairs` pairs of sequences, the logistic or least squares loss of the difference of their log ratios to
+ * a reference model.  Sequence s is the rows seq_start[s] .. seq_start[s + 1] - 1 of the logits (int64 [2 pairs + 1], device, not
+ * decreasing, within [0, rows]; a sequence may be empty, and rows in none have a gradient of zeros); pair p prefers sequence
+ * 2p to 2p + 1.  With S(s) the sum (mean != 0: the mean) over its labelled rows of logp - ref_logp and D = S(2p) - S(2p + 1):
+ *   EF21_LOSS_LOGISTIC       out_loss[p] = -(1 - smoothing) log sigma(beta D) - smoothing log sigma(-beta D)
+ *   EF21_LOSS_LEAST_SQUARES  out_loss[p] = (D - 1 / (2 beta))^2                      (smoothing plays no part)
+ * ref_logp [rows]: the reference's log-probabilities per token (ef21_token_logps on its logits), read where there is a label;
+ * per token, since of the sums over long sequences fp32 keeps too little.  logp [rows]: out.  grad_logits: the gradient of
+ * sum_p pair_weight[p] out_loss[p], or NULL for the loss alone; pair_weight [pairs] or NULL for 1 / pairs.
+ * EF21_EINVAL also: pairs < 1, beta not finite and > 0, smoothing outside [0, 1).
+ * workspace: 256-byte aligned device memory of at least the bytes that ef21_preference_loss_workspace says.
+ */
+int ef21_preference_loss_workspace(int64_t rows, int32_t pairs, int64_t *bytes);
+int ef21_preference_loss(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
+                         int label_type, const int64_t *seq_start, int32_t pairs, const float *ref_logp, float beta,
+                         float smoothing, int loss, int mean, const float *pair_weight, float *out_loss, float *logp,
+                         void *grad_logits, int64_t grad_stride, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Clipped policy loss with a KL term, per token: with q = exp(logp - old_logp), A = advantages, o = ref_logp - logp
+ *   token_loss[r] = -min(q A, clip(q, 1 - clip_low, 1 + clip_high) A) + kl (exp(o) - 1 - o)
+ *   out_loss[0]   = sum_r weight[r] token_loss[r]
+ * old_logp, advantages, ref_logp, weight: fp32 [rows], read where there is a label.  ref_logp NULL: no KL term (kl must be 0);
+ * weight NULL: 1 / rows.  grad_logits: the gradient of out_loss, or NULL for the loss alone; where the two sides of the
+ * minimum are equal it is that of q A.  token_loss and logp: fp32 [rows], out.
+ * EF21_EINVAL also: clip_low outside [0, 1], clip_high or kl negative or not finite.
+ */
+int ef21_policy_loss(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
+                     int label_type, const float *old_logp, const float *advantages, const float *ref_logp,
+                     const float *weight, float clip_low, float clip_high, float kl, float *out_loss, float *token_loss,
+                     float *logp, void *grad_logits, int64_t grad_stride, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,9 +24,12 @@ SYMBOLS = (
     "ef21_set_problem_dense", "ef21_set_problem_csr", "ef21_set_state", "ef21_get_state",
     "ef21_get_messages", "ef21_local_grad", "ef21_step", "ef21_set_timing", "ef21_get_timing", "ef21_kernel_name",
     "ef21_hbm_read", "ef21_hbm_copy", "ef21_get_choices", "ef21_set_loss", "ef21_set_minibatch", "ef21_theory_stepsize",
-    "ef21_topk_static",
+    "ef21_topk_static", "ef21_embed", "ef21_embed_grad_workspace", "ef21_embed_grad", "ef21_token_logps", "ef21_token_logps_grad",
+    "ef21_preference_loss_workspace", "ef21_preference_loss", "ef21_policy_loss",
 )
 K_COUNT = 11
+VALUE_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # EF21_F32, EF21_BF16, EF21_F16
+TOKEN_TYPES = {torch.int32: 0, torch.int64: 1}                          # EF21_I32, EF21_I64
 
 
 class EF21Error(RuntimeError):
@@ -73,6 +76,15 @@ def load_library() -> C.CDLL:
     lib.ef21_theory_stepsize.argtypes = [p, C.c_int32, p, p, p]
     lib.ef21_hbm_read.argtypes = [p, C.c_int64, p, p]
     lib.ef21_hbm_copy.argtypes = [p, p, C.c_int64, p]
+    lib.ef21_embed.argtypes = [p, C.c_int, i64, i64, i64, p, C.c_int, i64, f32, p, C.c_int, i64, p]
+    lib.ef21_embed_grad_workspace.argtypes = [i32, i64, i64, i64, p]
+    lib.ef21_embed_grad.argtypes = [p, C.c_int, i64, p, C.c_int, i32, i64, i64, i64, f32, p, i64, C.c_int, p, i64, p]
+    logits = [p, C.c_int, i64, i64, i64, p, C.c_int]
+    lib.ef21_token_logps.argtypes = [*logits, p, p, p]
+    lib.ef21_token_logps_grad.argtypes = [*logits, p, p, p, i64, p]
+    lib.ef21_preference_loss_workspace.argtypes = [i64, i32, p]
+    lib.ef21_preference_loss.argtypes = [*logits, p, i32, p, f32, f32, C.c_int, C.c_int, p, p, p, p, i64, p, i64, p]
+    lib.ef21_policy_loss.argtypes = [*logits, p, p, p, p, f32, f32, f32, p, p, p, p, i64, p]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = C.c_int
     lib.ef21_kernel_name.restype = C.c_char_p
@@ -139,6 +151,199 @@ def ef21_hbm_copy(dst: torch.Tensor, src: torch.Tensor) -> None:
     if dst.numel() * dst.element_size() != src.numel() * src.element_size():
         raise ValueError("dst and src must have the same size in bytes")
     _check(lib.ef21_hbm_copy(dst.data_ptr(), src.data_ptr(), src.numel() * src.element_size(), _current_stream_ptr()))
+
+
+# -- the two ends of a language model (stateless, on torch's current stream; see include/ef21.h)
+def _matrix(t: torch.Tensor, what: str, types=VALUE_TYPES):
+    """(address, type, rows, width, stride) of a matrix whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what}: expected a tensor in GPU memory")
+    kind = types.get(t.dtype)
+    if kind is None:
+        raise TypeError(f"{what}: unsupported type {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{what}: expected two dimensions, got {tuple(t.shape)}")
+    rows, width = t.shape
+    if width > 1 and rows > 0 and t.stride(1) != 1:
+        raise TypeError(f"{what}: rows must be contiguous")
+    return t.data_ptr(), kind, rows, width, t.stride(0) if rows > 1 else width
+
+
+def _token_list(t: torch.Tensor, what: str):
+    """(address, type) of contiguous tokens or labels."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what}: expected a tensor in GPU memory")
+    if t.dtype not in TOKEN_TYPES or not t.is_contiguous():
+        raise TypeError(f"{what}: expected contiguous int32 or int64, got {t.dtype} (contiguous={t.is_contiguous()})")
+    return t.data_ptr(), TOKEN_TYPES[t.dtype]
+
+
+def _vector(t, length: int, device, dtype=torch.float32):
+    """`t`, checked, or a new vector."""
+    if t is None:
+        return torch.empty(length, dtype=dtype, device=device)
+    _dev(t, dtype, (length,))
+    return t
+
+
+def _same_device(*tensors) -> None:
+    first = tensors[0].device
+    if any(t is not None and t.device != first for t in tensors):
+        raise ValueError("all tensors must be on one device")
+    if first.index is not None and torch.cuda.current_device() != first.index:
+        raise ValueError(f"the tensors are on {first}, which is not the current device")
+
+
+def _workspace(t, need: int, device):
+    if t is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    return t
+
+
+def ef21_embed(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None,
+               dtype: torch.dtype | None = None) -> torch.Tensor:
+    """scale * table[tokens] (ef21_embed): table [vocab][width], tokens of any shape (contiguous); out [..., width] of the
+    table's type, of `dtype`, or as given."""
+    lib = load_library()
+    at, kind, vocab, width, stride = _matrix(table, "table")
+    ids, id_type = _token_list(tokens, "tokens")
+    if out is None:
+        out = torch.empty(*tokens.shape, width, dtype=dtype or table.dtype, device=table.device)
+    flat = out if out.dim() == 2 else out.view(-1, width)
+    to, out_type, rows, cols, out_stride = _matrix(flat, "out")
+    if (rows, cols) != (tokens.numel(), width):
+        raise ValueError(f"out must have {tokens.numel()} rows of {width} entries")
+    _same_device(table, tokens, out)
+    _check(lib.ef21_embed(at, kind, vocab, width, stride, ids, id_type, rows, scale, to, out_type, out_stride, _current_stream_ptr()))
+    return out
+
+
+def ef21_embed_grad_workspace(n: int, count: int, vocab: int, width: int) -> int:
+    """Bytes of workspace that ef21_embed_grad needs."""
+    size = C.c_int64()
+    _check(load_library().ef21_embed_grad_workspace(n, count, vocab, width, C.byref(size)))
+    return size.value
+
+
+def ef21_embed_grad(grad_out: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float = 1.0, out: torch.Tensor | None = None,
+                    accumulate: bool = False, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradients of the table (ef21_embed_grad): grad_out [n][count][width], tokens [n][count]; returns fp32 [n][vocab][width]
+    (`out`, whose workers may lie further apart, for example a block of columns of the rows that EF21.step takes)."""
+    lib = load_library()
+    if grad_out.dim() != 3 or tuple(grad_out.shape[:2]) != tuple(tokens.shape):
+        raise ValueError("grad_out must be [n][count][width] and tokens [n][count]")
+    n, count, width = grad_out.shape
+    ids, id_type = _token_list(tokens, "tokens")
+    # the workers' rows as one matrix
+    if not grad_out.is_cuda or grad_out.dtype not in VALUE_TYPES:
+        raise TypeError(f"grad_out: expected float32, bfloat16 or float16 in GPU memory, got {grad_out.dtype}")
+    stride = grad_out.stride(1) if count > 1 else grad_out.stride(0) if n > 1 else width
+    if n * count == 0:
+        stride = width
+    elif (width > 1 and grad_out.stride(2) != 1) or (n > 1 and grad_out.stride(0) != count * stride):
+        raise TypeError("grad_out: entries of a row must be contiguous and the workers' rows follow one another at one stride")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the gradient to add to")
+        out = torch.empty(n, vocab, width, dtype=torch.float32, device=grad_out.device)
+    if out.dtype != torch.float32 or not out.is_cuda or tuple(out.shape) != (n, vocab, width) or not out[0].is_contiguous():
+        raise TypeError(f"out must be float32 [{n}][{vocab}][{width}] in GPU memory, each worker's table contiguous")
+    need = ef21_embed_grad_workspace(n, count, vocab, width)
+    workspace = _workspace(workspace, need, grad_out.device)
+    _same_device(grad_out, tokens, out, workspace)
+    _check(lib.ef21_embed_grad(grad_out.data_ptr(), VALUE_TYPES[grad_out.dtype], stride, ids, id_type, n, count, vocab, width, scale, out.data_ptr(), out.stride(0), int(accumulate),
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _current_stream_ptr()))
+    return out
+
+
+def _logit_rows(logits, labels):
+    at, kind, rows, vocab, stride = _matrix(logits, "logits")
+    ids, id_type = _token_list(labels, "labels")
+    if tuple(labels.shape) != (rows,):
+        raise ValueError(f"labels must be [{rows}]")
+    return (at, kind, rows, vocab, stride, ids, id_type), rows
+
+
+def _logit_grad(grad, logits):
+    """(tensor or None, address, stride) of the gradient: `grad` is a tensor to write, True for a new one, False or None for none."""
+    if grad is None or grad is False:
+        return None, None, 0
+    if grad is True:
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    at, _, _, _, stride = _matrix(grad, "grad")
+    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+        raise ValueError("grad must have the logits' type and shape")
+    return grad, at, stride
+
+
+def ef21_token_logps(logits: torch.Tensor, labels: torch.Tensor, logp: torch.Tensor | None = None, lse: torch.Tensor | None = None):
+    """(logp [rows], lse [rows]) of the labels under the softmax of each row of logits [rows][vocab] (ef21_token_logps)."""
+    lib = load_library()
+    args, rows = _logit_rows(logits, labels)
+    logp, lse = _vector(logp, rows, logits.device), _vector(lse, rows, logits.device)
+    _same_device(logits, labels, logp, lse)
+    _check(lib.ef21_token_logps(*args, logp.data_ptr(), lse.data_ptr(), _current_stream_ptr()))
+    return logp, lse
+
+
+def ef21_token_logps_grad(logits: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, grad_logp: torch.Tensor,
+                          out: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient of the logits from that of the log-probabilities (ef21_token_logps_grad); `out` may be the logits."""
+    lib = load_library()
+    args, rows = _logit_rows(logits, labels)
+    out, to, stride = _logit_grad(True if out is None else out, logits)
+    _same_device(logits, labels, lse, grad_logp, out)
+    _check(lib.ef21_token_logps_grad(*args, _dev(lse, torch.float32, (rows,)), _dev(grad_logp, torch.float32, (rows,)), to, stride,
+                                     _current_stream_ptr()))
+    return out
+
+
+def ef21_preference_loss_workspace(rows: int, pairs: int) -> int:
+    """Bytes of workspace that ef21_preference_loss needs."""
+    size = C.c_int64()
+    _check(load_library().ef21_preference_loss_workspace(rows, pairs, C.byref(size)))
+    return size.value
+
+
+def ef21_preference_loss(logits: torch.Tensor, labels: torch.Tensor, seq_start: torch.Tensor, ref_logp: torch.Tensor, beta: float,
+                         smoothing: float = 0.0, loss: int = LOSS_LOGISTIC, mean: bool = False, pair_weight: torch.Tensor | None = None,
+                         out_loss: torch.Tensor | None = None, logp: torch.Tensor | None = None, grad: "torch.Tensor | bool | None" = True,
+                         workspace: torch.Tensor | None = None):
+    """(loss [pairs], logp [rows], grad [rows][vocab] or None) of ef21_preference_loss; seq_start int64 [2 pairs + 1] on the
+    device.  grad: a tensor to write (the logits themselves if they are not needed again), True for a new one, False for none."""
+    lib = load_library()
+    args, rows = _logit_rows(logits, labels)
+    starts = _dev(seq_start, torch.int64)
+    pairs = (seq_start.numel() - 1) // 2
+    if seq_start.dim() != 1 or seq_start.numel() != 2 * pairs + 1 or pairs < 1:
+        raise ValueError("seq_start must be [2 pairs + 1]")
+    out_loss, logp = _vector(out_loss, pairs, logits.device), _vector(logp, rows, logits.device)
+    grad, to, stride = _logit_grad(grad, logits)
+    workspace = _workspace(workspace, ef21_preference_loss_workspace(rows, pairs), logits.device)
+    _same_device(logits, labels, seq_start, ref_logp, pair_weight, out_loss, logp, grad, workspace)
+    _check(lib.ef21_preference_loss(*args, starts, pairs, _dev(ref_logp, torch.float32, (rows,)), beta, smoothing, int(loss), int(mean),
+                                    _opt(pair_weight, torch.float32, (pairs,)), out_loss.data_ptr(), logp.data_ptr(), to, stride,
+                                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), _current_stream_ptr()))
+    return out_loss, logp, grad
+
+
+def ef21_policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, clip_low: float,
+                     clip_high: float, ref_logp: torch.Tensor | None = None, kl: float = 0.0, weight: torch.Tensor | None = None,
+                     out_loss: torch.Tensor | None = None, token_loss: torch.Tensor | None = None, logp: torch.Tensor | None = None,
+                     grad: "torch.Tensor | bool | None" = True):
+    """(loss [1], token_loss [rows], logp [rows], grad [rows][vocab] or None) of ef21_policy_loss; grad as in
+    ef21_preference_loss."""
+    lib = load_library()
+    args, rows = _logit_rows(logits, labels)
+    f32, shape = torch.float32, (rows,)
+    out_loss = _vector(out_loss, 1, logits.device)
+    token_loss, logp = _vector(token_loss, rows, logits.device), _vector(logp, rows, logits.device)
+    grad, to, stride = _logit_grad(grad, logits)
+    _same_device(logits, labels, old_logp, advantages, ref_logp, weight, out_loss, token_loss, logp, grad)
+    _check(lib.ef21_policy_loss(*args, _dev(old_logp, f32, shape), _dev(advantages, f32, shape), _opt(ref_logp, f32, shape),
+                                _opt(weight, f32, shape), clip_low, clip_high, kl, out_loss.data_ptr(), token_loss.data_ptr(),
+                                logp.data_ptr(), to, stride, _current_stream_ptr()))
+    return out_loss, token_loss, logp, grad
 
 
 class EF21:

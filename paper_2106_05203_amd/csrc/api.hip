@@ -9,6 +9,7 @@
 #include "../../include/ef21.h"
 #include "gram_way.h"
 #include "kernels.h"
+#include "lm.h"
 
 // Workspace of ef21_topk_static: device memory that exists from the moment the library is loaded, so that call
 // never allocates.  Every GPU holds its own copy at its own address; host code reaches it only through the address
@@ -34,6 +35,28 @@ int fail_hip(hipError_t st, const char *what) {
         hipError_t st__ = (call);                                \
         if (st__ != hipSuccess) return fail_hip(st__, #call);    \
     } while (0)
+
+}  // namespace
+
+// The same for the entry points in lm_api.hip; a text that cannot be kept is left out.
+int ef21::report_error(int code, const char *text) {
+    try {
+        g_last_error = text;
+    } catch (...) {
+        g_last_error.clear();
+    }
+    return code;
+}
+int ef21::report_hip_error(hipError_t st, const char *what) {
+    try {
+        return fail_hip(st, what);
+    } catch (...) {
+        g_last_error.clear();
+        return EF21_EHIP;
+    }
+}
+
+namespace {
 
 static_assert((int)ef21::K_COUNT == (int)EF21_K_COUNT, "kernel classes of kernels.h and ef21.h must agree");
 
