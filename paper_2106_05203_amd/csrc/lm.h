@@ -36,11 +36,12 @@ struct LogitGrad {                                         // [rows] rows, may b
     int64_t stride = 0;
 };
 
-// logp[r] = x[label] - lse[r]; coef (may be nullptr) <- 0, the coefficient of a row in no sequence.
-hipError_t launch_token_logps(const LogitRows &in, float *logp, float *lse, float *coef, hipStream_t stream);
+// logp[r] = x[label] - lse[r].  ls not nullptr: lse in two parts, the row's maximum in `lse` and the logarithm of its sum in `ls`.  coef (may be
+// nullptr) <- 0, the coefficient of a row in no sequence.
+hipError_t launch_token_logps(const LogitRows &in, float *logp, float *lse, float *ls, float *coef, hipStream_t stream);
 
-// grad[r][v] = coef[r] ([v = label] - exp(x - lse[r]))
-hipError_t launch_token_grad(const LogitRows &in, const float *lse, const float *coef, const LogitGrad &out, hipStream_t stream);
+// grad[r][v] = coef[r] ([v = label] - exp(x - lse[r])); ls as above, or nullptr
+hipError_t launch_token_grad(const LogitRows &in, const float *lse, const float *ls, const float *coef, const LogitGrad &out, hipStream_t stream);
 
 struct PairArgs {
     const int64_t *seq_start;                              // [2 pairs + 1]

@@ -66,8 +66,8 @@ int check_workspace(const void *workspace, int64_t have, size_t need) {
 
 int launched(hipError_t st, const char *what) { return st == hipSuccess ? EF21_OK : ef21::report_hip_error(st, what); }
 
-// Workspace of the preference loss: lse and the coefficients of the rows.
-size_t preference_bytes(int64_t rows) { return 2 * (((size_t)rows * sizeof(float) + 255) / 256 * 256); }
+// Workspace of the preference loss: the rows' maxima, logarithms of their sums, coefficients.
+size_t preference_bytes(int64_t rows) { return 3 * (((size_t)rows * sizeof(float) + 255) / 256 * 256); }
 
 int check_embed_grad_sizes(int32_t n, int64_t count, int64_t vocab, int64_t width) {
     if (n < 1 || n > 65535) return invalid("n must be in [1, 65535]");
@@ -125,7 +125,7 @@ int ef21_token_logps(const void *logits, int type, int64_t rows, int64_t vocab, 
     ef21::LogitRows in;
     if (int rc = check_logits(logits, type, rows, vocab, stride, labels, label_type, &in)) return rc;
     if (int rc = check_vectors(rows, {logp, lse})) return rc;
-    return launched(ef21::launch_token_logps(in, logp, lse, nullptr, (hipStream_t)hip_stream), "log-probability kernel launch");
+    return launched(ef21::launch_token_logps(in, logp, lse, nullptr, nullptr, (hipStream_t)hip_stream), "log-probability kernel launch");
 }
 
 int ef21_token_logps_grad(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
@@ -135,7 +135,7 @@ int ef21_token_logps_grad(const void *logits, int type, int64_t rows, int64_t vo
     if (int rc = check_logits(logits, type, rows, vocab, stride, labels, label_type, &in)) return rc;
     if (int rc = check_vectors(rows, {lse, grad_logp})) return rc;
     if (int rc = check_grad(in, grad_logits, grad_stride)) return rc;
-    return launched(ef21::launch_token_grad(in, lse, grad_logp, {grad_logits, grad_stride}, (hipStream_t)hip_stream), "logit gradient launch");
+    return launched(ef21::launch_token_grad(in, lse, nullptr, grad_logp, {grad_logits, grad_stride}, (hipStream_t)hip_stream), "logit gradient launch");
 }
 
 int ef21_preference_loss_workspace(int64_t rows, int32_t pairs, int64_t *bytes) {
@@ -162,14 +162,14 @@ int ef21_preference_loss(const void *logits, int type, int64_t rows, int64_t voc
     if (!(smoothing >= 0.f && smoothing < 1.f)) return invalid("smoothing must be in [0, 1)");
     if (loss != EF21_LOSS_LOGISTIC && loss != EF21_LOSS_LEAST_SQUARES) return invalid("unknown loss");
     if (int rc = check_workspace(workspace, workspace_bytes, preference_bytes(rows))) return rc;
-    float *lse = static_cast<float *>(workspace);
-    float *coef = lse + preference_bytes(rows) / 2 / sizeof(float);
+    const size_t each = preference_bytes(rows) / 3 / sizeof(float);
+    float *top = static_cast<float *>(workspace), *ls = top + each, *coef = ls + each;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    hipError_t st = ef21::launch_token_logps(in, logp, lse, coef, stream);
+    hipError_t st = ef21::launch_token_logps(in, logp, top, ls, coef, stream);
     const ef21::PairArgs p{seq_start, pairs,       rows,     logp, ref_logp,    in.labels, vocab,
                            beta,      smoothing,   loss,     mean, pair_weight, out_loss,  grad_logits ? coef : nullptr};
     if (st == hipSuccess) st = ef21::launch_preference_pairs(p, stream);
-    if (st == hipSuccess && grad_logits) st = ef21::launch_token_grad(in, lse, coef, {grad_logits, grad_stride}, stream);
+    if (st == hipSuccess && grad_logits) st = ef21::launch_token_grad(in, top, ls, coef, {grad_logits, grad_stride}, stream);
     return launched(st, "preference loss launch");
 }
 
