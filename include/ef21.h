@@ -366,11 +366,14 @@ int ef21_preference_loss(const void *logits, int type, int64_t rows, int64_t voc
  * weight NULL: 1 / rows.  grad_logits: the gradient of out_loss, or NULL for the loss alone; where the two sides of the
  * minimum are equal it is that of q A.  token_loss and logp: fp32 [rows], out.
  * EF21_EINVAL also: clip_low outside [0, 1], clip_high or kl negative or not finite.
+ * workspace: 256-byte aligned device memory of at least the bytes that ef21_policy_loss_workspace says.
  */
+int ef21_policy_loss_workspace(int64_t rows, int64_t *bytes);
 int ef21_policy_loss(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
                      int label_type, const float *old_logp, const float *advantages, const float *ref_logp,
                      const float *weight, float clip_low, float clip_high, float kl, float *out_loss, float *token_loss,
-                     float *logp, void *grad_logits, int64_t grad_stride, void *hip_stream);
+                     float *logp, void *grad_logits, int64_t grad_stride, void *workspace, int64_t workspace_bytes,
+                     void *hip_stream);
 
 #ifdef __cplusplus
 }

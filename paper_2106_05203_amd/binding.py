@@ -25,7 +25,7 @@ SYMBOLS = (
     "ef21_get_messages", "ef21_local_grad", "ef21_step", "ef21_set_timing", "ef21_get_timing", "ef21_kernel_name",
     "ef21_hbm_read", "ef21_hbm_copy", "ef21_get_choices", "ef21_set_loss", "ef21_set_minibatch", "ef21_theory_stepsize",
     "ef21_topk_static", "ef21_embed", "ef21_embed_grad_workspace", "ef21_embed_grad", "ef21_token_logps", "ef21_token_logps_grad",
-    "ef21_preference_loss_workspace", "ef21_preference_loss", "ef21_policy_loss",
+    "ef21_preference_loss_workspace", "ef21_preference_loss", "ef21_policy_loss_workspace", "ef21_policy_loss",
 )
 K_COUNT = 11
 VALUE_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # EF21_F32, EF21_BF16, EF21_F16
@@ -84,7 +84,8 @@ def load_library() -> C.CDLL:
     lib.ef21_token_logps_grad.argtypes = [*logits, p, p, p, i64, p]
     lib.ef21_preference_loss_workspace.argtypes = [i64, i32, p]
     lib.ef21_preference_loss.argtypes = [*logits, p, i32, p, f32, f32, C.c_int, C.c_int, p, p, p, p, i64, p, i64, p]
-    lib.ef21_policy_loss.argtypes = [*logits, p, p, p, p, f32, f32, f32, p, p, p, p, i64, p]
+    lib.ef21_policy_loss_workspace.argtypes = [i64, p]
+    lib.ef21_policy_loss.argtypes = [*logits, p, p, p, p, f32, f32, f32, p, p, p, p, i64, p, i64, p]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = C.c_int
     lib.ef21_kernel_name.restype = C.c_char_p
@@ -327,10 +328,17 @@ def ef21_preference_loss(logits: torch.Tensor, labels: torch.Tensor, seq_start: 
     return out_loss, logp, grad
 
 
+def ef21_policy_loss_workspace(rows: int) -> int:
+    """Bytes of workspace that ef21_policy_loss needs."""
+    size = C.c_int64()
+    _check(load_library().ef21_policy_loss_workspace(rows, C.byref(size)))
+    return size.value
+
+
 def ef21_policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, clip_low: float,
                      clip_high: float, ref_logp: torch.Tensor | None = None, kl: float = 0.0, weight: torch.Tensor | None = None,
                      out_loss: torch.Tensor | None = None, token_loss: torch.Tensor | None = None, logp: torch.Tensor | None = None,
-                     grad: "torch.Tensor | bool | None" = True):
+                     grad: "torch.Tensor | bool | None" = True, workspace: torch.Tensor | None = None):
     """(loss [1], token_loss [rows], logp [rows], grad [rows][vocab] or None) of ef21_policy_loss; grad as in
     ef21_preference_loss."""
     lib = load_library()
@@ -339,10 +347,12 @@ def ef21_policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch
     out_loss = _vector(out_loss, 1, logits.device)
     token_loss, logp = _vector(token_loss, rows, logits.device), _vector(logp, rows, logits.device)
     grad, to, stride = _logit_grad(grad, logits)
-    _same_device(logits, labels, old_logp, advantages, ref_logp, weight, out_loss, token_loss, logp, grad)
+    workspace = _workspace(workspace, ef21_policy_loss_workspace(rows), logits.device)
+    _same_device(logits, labels, old_logp, advantages, ref_logp, weight, out_loss, token_loss, logp, grad, workspace)
     _check(lib.ef21_policy_loss(*args, _dev(old_logp, f32, shape), _dev(advantages, f32, shape), _opt(ref_logp, f32, shape),
                                 _opt(weight, f32, shape), clip_low, clip_high, kl, out_loss.data_ptr(), token_loss.data_ptr(),
-                                logp.data_ptr(), to, stride, _current_stream_ptr()))
+                                logp.data_ptr(), to, stride, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                _current_stream_ptr()))
     return out_loss, token_loss, logp, grad
 
 

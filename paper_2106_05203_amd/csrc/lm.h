@@ -36,18 +36,18 @@ struct LogitGrad {                                         // [rows] rows, may b
     int64_t stride = 0;
 };
 
-// logp[r] = x[label] - lse[r].  ls not nullptr: lse in two parts, the row's maximum in `lse` and the logarithm of its sum in `ls`.  coef (may be
-// nullptr) <- 0, the coefficient of a row in no sequence.
-hipError_t launch_token_logps(const LogitRows &in, float *logp, float *lse, float *ls, float *coef, hipStream_t stream);
+// logp[r] = x[label] - lse[r]
+hipError_t launch_token_logps(const LogitRows &in, float *logp, float *lse, hipStream_t stream);
 
-// grad[r][v] = coef[r] ([v = label] - exp(x - lse[r])); ls as above, or nullptr
-hipError_t launch_token_grad(const LogitRows &in, const float *lse, const float *ls, const float *coef, const LogitGrad &out, hipStream_t stream);
+// grad[r][v] = coef[r] ([v = label] - exp(x - lse[r]))
+hipError_t launch_token_grad(const LogitRows &in, const float *lse, const float *coef, const LogitGrad &out, hipStream_t stream);
 
 struct PairArgs {
     const int64_t *seq_start;                              // [2 pairs + 1]
     int32_t pairs;
     int64_t rows;
-    const float *logp, *ref;
+    float *logp;                                           // [rows], written by the sums
+    const float *ref;
     Tokens labels;
     int64_t vocab;
     float beta, smoothing;
@@ -56,14 +56,17 @@ struct PairArgs {
     float *out_loss;                                       // [pairs]
     float *coef;                                           // [rows] or nullptr
 };
-hipError_t launch_preference_pairs(const PairArgs &p, hipStream_t stream);
+// pairs.coef is set from the workspace.
+size_t preference_workspace_bytes(int64_t rows);
+hipError_t launch_preference(const LogitRows &in, PairArgs pairs, const LogitGrad &out, void *workspace, hipStream_t stream);
 
 struct PolicyArgs {
     const float *old_logp, *ref_logp, *advantages, *weight;  // [rows]; ref_logp nullptr: no KL term; weight nullptr: 1 / rows
     float clip_low, clip_high, kl;
     float *out_loss, *token_loss, *logp;                   // [1], [rows], [rows]
 };
-hipError_t launch_policy(const LogitRows &in, const PolicyArgs &p, const LogitGrad &out, hipStream_t stream);
+size_t policy_workspace_bytes(int64_t rows);
+hipError_t launch_policy(const LogitRows &in, const PolicyArgs &p, const LogitGrad &out, void *workspace, hipStream_t stream);
 
 struct EmbedArgs {
     const void *table;

@@ -66,9 +66,6 @@ int check_workspace(const void *workspace, int64_t have, size_t need) {
 
 int launched(hipError_t st, const char *what) { return st == hipSuccess ? EF21_OK : ef21::report_hip_error(st, what); }
 
-// Workspace of the preference loss: the rows' maxima, logarithms of their sums, coefficients.
-size_t preference_bytes(int64_t rows) { return 3 * (((size_t)rows * sizeof(float) + 255) / 256 * 256); }
-
 int check_embed_grad_sizes(int32_t n, int64_t count, int64_t vocab, int64_t width) {
     if (n < 1 || n > 65535) return invalid("n must be in [1, 65535]");
     if (count < 0 || count > kMostRows || count > ((int64_t)1 << 40) / n) return invalid("count must be in [0, 2^31), and n count at most 2^40");
@@ -125,7 +122,7 @@ int ef21_token_logps(const void *logits, int type, int64_t rows, int64_t vocab, 
     ef21::LogitRows in;
     if (int rc = check_logits(logits, type, rows, vocab, stride, labels, label_type, &in)) return rc;
     if (int rc = check_vectors(rows, {logp, lse})) return rc;
-    return launched(ef21::launch_token_logps(in, logp, lse, nullptr, nullptr, (hipStream_t)hip_stream), "log-probability kernel launch");
+    return launched(ef21::launch_token_logps(in, logp, lse, (hipStream_t)hip_stream), "log-probability kernel launch");
 }
 
 int ef21_token_logps_grad(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
@@ -135,14 +132,14 @@ int ef21_token_logps_grad(const void *logits, int type, int64_t rows, int64_t vo
     if (int rc = check_logits(logits, type, rows, vocab, stride, labels, label_type, &in)) return rc;
     if (int rc = check_vectors(rows, {lse, grad_logp})) return rc;
     if (int rc = check_grad(in, grad_logits, grad_stride)) return rc;
-    return launched(ef21::launch_token_grad(in, lse, nullptr, grad_logp, {grad_logits, grad_stride}, (hipStream_t)hip_stream), "logit gradient launch");
+    return launched(ef21::launch_token_grad(in, lse, grad_logp, {grad_logits, grad_stride}, (hipStream_t)hip_stream), "logit gradient launch");
 }
 
 int ef21_preference_loss_workspace(int64_t rows, int32_t pairs, int64_t *bytes) {
     if (rows < 0 || rows > kMostRows) return invalid("rows must be in [0, 2^31)");
     if (pairs < 1) return invalid("pairs must be at least 1");
     if (!bytes) return invalid("bytes is NULL");
-    *bytes = (int64_t)preference_bytes(rows);
+    *bytes = (int64_t)ef21::preference_workspace_bytes(rows);
     return EF21_OK;
 }
 
@@ -161,22 +158,22 @@ int ef21_preference_loss(const void *logits, int type, int64_t rows, int64_t voc
     if (!(beta > 0.f) || !std::isfinite(beta)) return invalid("beta must be finite and > 0");
     if (!(smoothing >= 0.f && smoothing < 1.f)) return invalid("smoothing must be in [0, 1)");
     if (loss != EF21_LOSS_LOGISTIC && loss != EF21_LOSS_LEAST_SQUARES) return invalid("unknown loss");
-    if (int rc = check_workspace(workspace, workspace_bytes, preference_bytes(rows))) return rc;
-    const size_t each = preference_bytes(rows) / 3 / sizeof(float);
-    float *top = static_cast<float *>(workspace), *ls = top + each, *coef = ls + each;
-    const hipStream_t stream = (hipStream_t)hip_stream;
-    hipError_t st = ef21::launch_token_logps(in, logp, top, ls, coef, stream);
-    const ef21::PairArgs p{seq_start, pairs,       rows,     logp, ref_logp,    in.labels, vocab,
-                           beta,      smoothing,   loss,     mean, pair_weight, out_loss,  grad_logits ? coef : nullptr};
-    if (st == hipSuccess) st = ef21::launch_preference_pairs(p, stream);
-    if (st == hipSuccess && grad_logits) st = ef21::launch_token_grad(in, top, ls, coef, {grad_logits, grad_stride}, stream);
-    return launched(st, "preference loss launch");
+    if (int rc = check_workspace(workspace, workspace_bytes, ef21::preference_workspace_bytes(rows))) return rc;
+    const ef21::PairArgs p{seq_start, pairs, rows, logp, ref_logp, in.labels, vocab, beta, smoothing, loss, mean, pair_weight, out_loss, nullptr};
+    return launched(ef21::launch_preference(in, p, {grad_logits, grad_stride}, workspace, (hipStream_t)hip_stream), "preference loss launch");
+}
+
+int ef21_policy_loss_workspace(int64_t rows, int64_t *bytes) {
+    if (rows < 0 || rows > kMostRows) return invalid("rows must be in [0, 2^31)");
+    if (!bytes) return invalid("bytes is NULL");
+    *bytes = (int64_t)ef21::policy_workspace_bytes(rows);
+    return EF21_OK;
 }
 
 int ef21_policy_loss(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
                      int label_type, const float *old_logp, const float *advantages, const float *ref_logp,
                      const float *weight, float clip_low, float clip_high, float kl, float *out_loss, float *token_loss,
-                     float *logp, void *grad_logits, int64_t grad_stride, void *hip_stream) {
+                     float *logp, void *grad_logits, int64_t grad_stride, void *workspace, int64_t workspace_bytes, void *hip_stream) {
     ef21::LogitRows in;
     if (int rc = check_logits(logits, type, rows, vocab, stride, labels, label_type, &in)) return rc;
     if (int rc = check_vectors(rows, {old_logp, advantages, token_loss, logp})) return rc;
@@ -188,8 +185,9 @@ int ef21_policy_loss(const void *logits, int type, int64_t rows, int64_t vocab, 
     if (!(clip_high >= 0.f) || !std::isfinite(clip_high)) return invalid("clip_high must be finite and >= 0");
     if (!(kl >= 0.f) || !std::isfinite(kl)) return invalid("kl must be finite and >= 0");
     if (kl > 0.f && rows > 0 && !ref_logp) return invalid("a KL term needs ref_logp");
+    if (int rc = check_workspace(workspace, workspace_bytes, ef21::policy_workspace_bytes(rows))) return rc;
     const ef21::PolicyArgs p{old_logp, kl > 0.f ? ref_logp : nullptr, advantages, weight, clip_low, clip_high, kl, out_loss, token_loss, logp};
-    return launched(ef21::launch_policy(in, p, {grad_logits, grad_stride}, (hipStream_t)hip_stream), "policy loss launch");
+    return launched(ef21::launch_policy(in, p, {grad_logits, grad_stride}, workspace, (hipStream_t)hip_stream), "policy loss launch");
 }
 
 }  // extern "C"

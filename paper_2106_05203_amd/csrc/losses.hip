@@ -1,0 +1,387 @@
+// The preference loss and the clipped policy loss on rows of logits, with the gradient of the logits (token_rows.h has the rows).
+//
+// Preference: for pair p with the sequences 2p (preferred) and 2p + 1,
+//   D = S(2p) - S(2p + 1),  S = the sum, or the mean, of logp - ref over a sequence's labelled rows
+//   logistic       L = -(1 - e) log sigma(beta D) - e log sigma(-beta D),   dL/dD = beta (sigma(beta D) - (1 - e))
+//   least squares  L = (D - 1 / (2 beta))^2,                                dL/dD = 2 (D - 1 / (2 beta))
+// The differences logp - ref are taken per token: sums of log-probabilities of long sequences are thousands and would keep
+// little of a margin near one in fp32.  Sums over sequences in 64 bits, in a fixed order.
+//
+// Policy, per token: q = exp(logp - old), L = -min(q A, clip(q) A) + kl (exp(o) - 1 - o), o = ref - logp.
+#include "token_rows.h"
+
+namespace ef21 {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---------------------------------------------------------------- the losses, from log-probabilities
+// Loss of one token and its derivative in logp.
+struct TokenLoss {
+    float loss, slope;
+};
+// What the loss of a token needs, read before it is needed.
+struct TokenIn {
+    float old_logp, advantage, ref_logp, weight;
+};
+__device__ __forceinline__ TokenIn token_in(const PolicyArgs &p, int64_t r, int64_t rows) {
+    return {p.old_logp[r], p.advantages[r], p.ref_logp ? p.ref_logp[r] : 0.f, p.weight ? p.weight[r] : 1.f / (float)rows};
+}
+__device__ __forceinline__ TokenLoss policy_token(const PolicyArgs &p, const TokenIn &in, float logp) {
+    const float q = expf(logp - in.old_logp), a = in.advantage;
+    const float one = q * a, two = fminf(fmaxf(q, 1.f - p.clip_low), 1.f + p.clip_high) * a;
+    TokenLoss t = one > two ? TokenLoss{-two, 0.f} : TokenLoss{-one, -one};   // a NaN is neither above nor dropped
+    if (p.ref_logp) {
+        const float off = in.ref_logp - logp, e = expm1f(off);
+        t.loss += p.kl * (e - off);
+        t.slope -= p.kl * e;
+    }
+    return t;
+}
+
+// Sums of (a, b) over the workgroup, the same bits in every thread.
+__device__ void block_sum2(double &a, double &b, double (*lds)[2]) {
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+        a += __shfl_xor(a, o, kWave);
+        b += __shfl_xor(b, o, kWave);
+    }
+    __syncthreads();
+    if (lane_id() == 0) {
+        lds[wave_id()][0] = a;
+        lds[wave_id()][1] = b;
+    }
+    __syncthreads();
+    a = b = 0.0;
+    for (int w = 0; w < kThreads / kWave; ++w) {
+        a += lds[w][0];
+        b += lds[w][1];
+    }
+}
+
+// Margin, loss and coefficients of one pair.
+__device__ void preference_pair(const PairArgs &p, int64_t pair, double (*lds)[2]) {
+    int64_t from[2], to[2];
+    double ratio[2], per[2];
+    for (int side = 0; side < 2; ++side) {
+        const int64_t s = 2 * pair + side;
+        from[side] = min(max(p.seq_start[s], (int64_t)0), p.rows);
+        to[side] = min(max(p.seq_start[s + 1], from[side]), p.rows);
+        double sum = 0.0, count = 0.0;
+        for (int64_t r = from[side] + threadIdx.x; r < to[side]; r += kThreads) {
+            const int64_t label = token_at(p.labels, r);
+            if (label < 0 || label >= p.vocab) continue;
+            sum += (double)p.logp[r] - (double)p.ref[r];
+            count += 1.0;
+        }
+        block_sum2(sum, count, lds);
+        per[side] = p.mean && count > 0.0 ? 1.0 / count : 1.0;
+        ratio[side] = sum * per[side];
+    }
+    const double margin = ratio[0] - ratio[1], beta = (double)p.beta;
+    double loss, slope;
+    if (p.loss == 0) {                                           // EF21_LOSS_LOGISTIC
+        const double z = beta * margin, e = (double)p.smoothing, soft = log1p(exp(-fabs(z)));
+        loss = (1.0 - e) * (soft + fmax(-z, 0.0)) + e * (soft + fmax(z, 0.0));
+        slope = beta * (1.0 / (1.0 + exp(-z)) - (1.0 - e));
+    } else {
+        const double off = margin - 0.5 / beta;
+        loss = off * off;
+        slope = 2.0 * off;
+    }
+    if (threadIdx.x == 0) p.out_loss[pair] = (float)loss;
+    if (!p.coef) return;
+    slope *= p.weight ? (double)p.weight[pair] : 1.0 / (double)p.pairs;
+    for (int side = 0; side < 2; ++side) {
+        const float c = (float)((side == 0 ? slope : -slope) * per[side]);
+        for (int64_t r = from[side] + threadIdx.x; r < to[side]; r += kThreads) p.coef[r] = c;
+    }
+}
+
+// What the sums leave for the gradient: the rows' maxima, logarithms of their sums, coefficients.
+struct RowSpace {
+    float *top, *ls, *coef;
+};
+
+// ---------------------------------------------------------------- the sums, and then the gradient
+// POLICY: the tokens' losses and the rows' coefficients too; else the coefficient of a row in no pair.
+template <class T, int WAVES, bool POLICY>
+__global__ __launch_bounds__(Team<WAVES>::kBlock) void loss_forward_kernel(LogitRows in, PolicyArgs pol, float *logp_out, RowSpace out) {
+    typedef Team<WAVES> G;
+    __shared__ TeamShared<WAVES> shared[2];
+    int turn = 0;
+    for (int64_t r = G::first(); r < in.rows; r += G::step()) {
+        const int32_t label = label_of(in, r);
+        RowStat st{0.f, 0.f};
+        TokenLoss t{0.f, 0.f};
+        float logp = 0.f, coef = 0.f;
+        if (label >= 0) {
+            const T *x = static_cast<const T *>(in.x) + r * in.stride;
+            TokenIn ti{};
+            if (POLICY) ti = token_in(pol, r, in.rows);
+            const float at_label = (float)x[label];
+            st = row_stat<T, WAVES>(x, cut_row(x, (int32_t)in.vocab), G::thread(), shared[turn]);
+            turn ^= 1;
+            logp = st.log_prob(at_label);
+            if (POLICY) {
+                t = policy_token(pol, ti, logp);
+                coef = t.slope * ti.weight;
+            }
+        }
+        if (G::thread() == 0) {
+            logp_out[r] = logp;
+            out.top[r] = st.m;
+            out.ls[r] = st.ls;
+            out.coef[r] = coef;
+            if (POLICY) pol.token_loss[r] = t.loss;
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void preference_pairs_kernel(PairArgs p) {
+    __shared__ double lds[kThreads / kWave][2];
+    for (int64_t pair = blockIdx.x; pair < p.pairs; pair += gridDim.x) preference_pair(p, pair, lds);
+}
+
+// Rows that one wavefront takes.
+template <class T>
+__global__ __launch_bounds__(Team<1>::kBlock) void loss_grad_short_kernel(LogitRows in, RowSpace s, LogitGrad out) {
+    typedef Team<1> G;
+    for (int64_t r = G::first(); r < in.rows; r += G::step()) {
+        const int32_t label = label_of(in, r);
+        const T *x = static_cast<const T *>(in.x) + r * in.stride;
+        T *g = static_cast<T *>(out.ptr) + r * out.stride;
+        if (label >= 0) stream_grad<T, kWave>(x, g, cut_row(x, (int32_t)in.vocab), GradOf(RowStat{s.top[r], s.ls[r]}, s.coef[r], label), G::thread());
+        else zero_row<T, kWave>(g, (int32_t)in.vocab, G::thread());
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(kGradThreads) void loss_grad_kernel(LogitRows in, RowSpace s, LogitGrad out, int32_t tiles) {
+    for (int64_t w = blockIdx.x; w < in.rows * tiles; w += gridDim.x) {
+        const int64_t r = w / tiles;
+        const int32_t label = label_of(in, r);
+        grad_tile<T>(static_cast<const T *>(in.x) + r * in.stride, static_cast<T *>(out.ptr) + r * out.stride, (int32_t)in.vocab, label,
+                     label >= 0 ? s.coef[r] : 0.f, (int32_t)(w % tiles), [&](const Cut &) { return RowStat{s.top[r], s.ls[r]}; });
+    }
+}
+
+template <class T, bool POLICY>
+hipError_t loss_forward(const LogitRows &in, const PolicyArgs &pol, float *logp, const RowSpace &s, hipStream_t stream) {
+    return with_team<T>(in.vocab, [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        hipLaunchKernelGGL((loss_forward_kernel<T, W, POLICY>), dim3(grid_of(in.rows, Team<W>::kPerBlock, kManyBlocks)), dim3(Team<W>::kBlock), 0, stream, in, pol,
+                           logp, s);
+        return hipGetLastError();
+    });
+}
+
+template <class T>
+hipError_t loss_grad(const LogitRows &in, const RowSpace &s, const LogitGrad &out, hipStream_t stream) {
+    if (team_waves<T>(in.vocab) == 1) {
+        hipLaunchKernelGGL(loss_grad_short_kernel<T>, dim3(grid_of(in.rows, Team<1>::kPerBlock, kManyBlocks)), dim3(Team<1>::kBlock), 0, stream, in, s, out);
+    } else {
+        const int32_t tiles = grad_tiles<T>(in.vocab);
+        hipLaunchKernelGGL(loss_grad_kernel<T>, dim3(grid_of(in.rows * tiles, 1, kManyBlocks)), dim3(kGradThreads), 0, stream, in, s, out, tiles);
+    }
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- the policy loss with the row held in registers
+// The row stays in the team's registers between the sum and the gradient, so it is read once: thread t holds the pieces t, t + TEAM, ..., and -inf
+// behind the last one.
+template <class T, int WAVES, int PIECES>
+__global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void policy_held_kernel(LogitRows in, PolicyArgs pol, LogitGrad out) {
+    typedef Team<WAVES> G;
+    constexpr int N = Piece<T>::N, K = Piece<T>::kGroup, TEAM = G::kSize;
+    static_assert(PIECES % K == 0, "whole groups");
+    __shared__ TeamShared<WAVES> shared[2];
+    int turn = 0;
+    for (int64_t r = G::first(); r < in.rows; r += G::step()) {
+        const int32_t label = label_of(in, r), thread = G::thread(), vocab = (int32_t)in.vocab;
+        T *g = static_cast<T *>(out.ptr) + r * out.stride;
+        if (label < 0) {
+            if (out.ptr) zero_row<T, TEAM>(g, vocab, thread);
+            if (thread == 0) {
+                pol.logp[r] = 0.f;
+                pol.token_loss[r] = 0.f;
+            }
+            continue;
+        }
+        const T *x = static_cast<const T *>(in.x) + r * in.stride;
+        const Cut c = cut_row(x, vocab);
+        // the same 32-bit offset of the thread from bases that all threads share
+        const char *from = reinterpret_cast<const char *>(x + c.head);
+        const uint32_t mine = (uint32_t)thread * 16u;
+        float at_label = (float)x[label];
+        Raw held[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            held[i] = nothing<T>();
+            if (thread < c.pieces - i * TEAM) held[i] = load_piece(reinterpret_cast<const T *>(from + (int64_t)i * TEAM * 16 + mine));
+        }
+        const int32_t edge_at = thread < c.edges() ? c.edge<T>(thread) : -1;
+        const float edge = edge_at >= 0 ? (float)x[edge_at] : -INFINITY;
+        const TokenIn ti = token_in(pol, r, in.rows);
+        ExpSum e;
+#pragma unroll
+        for (int i = 0; i < PIECES; i += K) {
+            float f[K * N];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                asm("" : "+v"(held[i + k]));                       // held as it was loaded: left alone, the compiler unpacks it first
+                float(&one)[N] = reinterpret_cast<float(&)[N]>(f[k * N]);
+                unpack<T>(held[i + k], one);
+            }
+            e.add(f);
+            asm volatile("" : "+v"(e.m), "+v"(e.s));               // here and now: one group unpacked at a time
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (edge_at >= 0) {
+            const float f[1] = {edge};
+            e.add(f);
+        }
+        asm volatile("" : "+v"(at_label));                         // has arrived, like all of the row, before any wavefront may write over it
+        const RowStat st = team_stat<WAVES>(e, shared[turn]);
+        turn ^= 1;
+        const float logp = st.log_prob(at_label);
+        const TokenLoss t = policy_token(pol, ti, logp);
+        if (out.ptr) {
+            const GradOf d(st, t.slope * ti.weight, label);
+            char *to = reinterpret_cast<char *>(g + c.head);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                if (thread < c.pieces - i * TEAM) {
+                    Raw raw = held[i];
+                    asm("" : "+v"(raw));                           // or the entries unpacked for the sum would be kept, twice the registers
+                    float f[N];
+                    unpack<T>(raw, f);
+                    d.piece((uint32_t)(label - c.head - i * TEAM * N - thread * N), f);
+                    store_piece(reinterpret_cast<T *>(to + (int64_t)i * TEAM * 16 + mine), f);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (edge_at >= 0) g[edge_at] = stored<T>(d.entry(edge_at, edge));
+        }
+        if (thread == 0) {
+            pol.logp[r] = logp;
+            pol.token_loss[r] = t.loss;
+        }
+    }
+}
+
+// out_loss = sum_r weight[r] token_loss[r] over the rows with a label, in 64 bits and in an order that the number of rows alone fixes: slices of
+// kSumSlice rows, a workgroup each, then the slices.
+constexpr int kSumThreads = 256, kSumRows = 16, kSumSlice = kSumThreads * kSumRows;
+
+__device__ __forceinline__ double block_sum(double v, double *lds) {
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+    if (lane_id() == 0) lds[wave_id()] = v;
+    __syncthreads();
+    v = 0.0;
+    for (int w = 0; w < kSumThreads / kWave; ++w) v += lds[w];
+    return v;
+}
+
+// sums nullptr: one slice, straight to out_loss.
+__global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(LogitRows in, const float *token_loss, const float *weight, double *sums, float *out_loss) {
+    __shared__ double lds[kSumThreads / kWave];
+    const int64_t first = (int64_t)blockIdx.x * kSumSlice + threadIdx.x;
+    const float even = 1.f / (float)in.rows;
+    float l[kSumRows], w[kSumRows];
+#pragma unroll
+    for (int i = 0; i < kSumRows; ++i) {
+        const int64_t r = first + i * kSumThreads;
+        const bool has = r < in.rows && label_of(in, r) >= 0;
+        l[i] = has ? token_loss[r] : 0.f;
+        w[i] = !has ? 0.f : weight ? weight[r] : even;
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kSumRows; ++i) sum += (double)l[i] * (double)w[i];
+    sum = block_sum(sum, lds);
+    if (threadIdx.x == 0) {
+        if (sums) sums[blockIdx.x] = sum;
+        else *out_loss = (float)sum;
+    }
+}
+__global__ __launch_bounds__(kSumThreads) void policy_slices_kernel(const double *sums, int64_t slices, float *out_loss) {
+    __shared__ double lds[kSumThreads / kWave];
+    double sum = 0.0;
+#pragma unroll 8
+    for (int64_t i = threadIdx.x; i < slices; i += kSumThreads) sum += sums[i];
+    sum = block_sum(sum, lds);
+    if (threadIdx.x == 0) *out_loss = (float)sum;
+}
+
+template <class T, int WAVES, int PIECES>
+hipError_t policy_held(const LogitRows &in, const PolicyArgs &p, const LogitGrad &out, hipStream_t stream) {
+    typedef Team<WAVES> G;
+    hipLaunchKernelGGL((policy_held_kernel<T, WAVES, PIECES>), dim3(grid_of(in.rows, G::kPerBlock, kManyBlocks)), dim3(G::kBlock), 0, stream, in, p, out);
+    return hipGetLastError();
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Workspaces: RowSpace, and for the policy loss the slices' sums before it.
+size_t row_space_bytes(int64_t rows) { return 3 * padded((size_t)rows * sizeof(float)); }
+RowSpace row_space(int64_t rows, void *space) {
+    char *at = static_cast<char *>(space);
+    const size_t each = padded((size_t)rows * sizeof(float));
+    return {reinterpret_cast<float *>(at), reinterpret_cast<float *>(at + each), reinterpret_cast<float *>(at + 2 * each)};
+}
+
+template <class T>
+hipError_t policy(const LogitRows &in, const PolicyArgs &p, const LogitGrad &out, void *space, hipStream_t stream) {
+    const int64_t pieces = ceil_div(in.vocab, Piece<T>::N);
+    switch (team_waves<T>(in.vocab)) {
+        case 1: return pieces <= 64 * 4 ? policy_held<T, 1, 4>(in, p, out, stream) : policy_held<T, 1, 8>(in, p, out, stream);
+        case 4: return pieces <= 256 * 4 ? policy_held<T, 4, 4>(in, p, out, stream) : policy_held<T, 4, 8>(in, p, out, stream);
+        case 8: return policy_held<T, 8, 8>(in, p, out, stream);
+        default: break;
+    }
+    if (pieces <= 1024 * 8) return policy_held<T, 16, 8>(in, p, out, stream);
+    if (pieces <= 1024 * 16) return policy_held<T, 16, 16>(in, p, out, stream);
+    const RowSpace s = row_space(in.rows, space);
+    const hipError_t st = loss_forward<T, true>(in, p, p.logp, s, stream);
+    return st != hipSuccess || !out.ptr ? st : loss_grad<T>(in, s, out, stream);
+}
+
+}  // namespace
+
+size_t preference_workspace_bytes(int64_t rows) { return row_space_bytes(rows); }
+
+hipError_t launch_preference(const LogitRows &in, PairArgs pairs, const LogitGrad &out, void *workspace, hipStream_t stream) {
+    const RowSpace s = row_space(in.rows, workspace);
+    pairs.coef = out.ptr ? s.coef : nullptr;
+    return with_type(in.type, [&](auto type) {
+        typedef typename ValueOf<decltype(type)::value>::type T;
+        hipError_t st = in.rows > 0 ? loss_forward<T, false>(in, PolicyArgs(), pairs.logp, s, stream) : hipSuccess;
+        if (st != hipSuccess) return st;
+        hipLaunchKernelGGL(preference_pairs_kernel, dim3(grid_of(pairs.pairs, 1, kManyBlocks)), dim3(kThreads), 0, stream, pairs);
+        st = hipGetLastError();
+        return st != hipSuccess || !out.ptr || in.rows == 0 ? st : loss_grad<T>(in, s, out, stream);
+    });
+}
+
+size_t policy_workspace_bytes(int64_t rows) { return padded((size_t)ceil_div(rows, kSumSlice) * sizeof(double)) + row_space_bytes(rows); }
+
+hipError_t launch_policy(const LogitRows &in, const PolicyArgs &p, const LogitGrad &out, void *workspace, hipStream_t stream) {
+    const int64_t slices = ceil_div(in.rows, kSumSlice);
+    double *sums = static_cast<double *>(workspace);
+    if (in.rows > 0) {
+        void *space = static_cast<char *>(workspace) + padded((size_t)slices * sizeof(double));
+        const hipError_t st = with_type(in.type, [&](auto type) {
+            return policy<typename ValueOf<decltype(type)::value>::type>(in, p, out, space, stream);
+        });
+        if (st != hipSuccess) return st;
+    }
+    hipLaunchKernelGGL(policy_sum_kernel, dim3((unsigned)(slices > 1 ? slices : 1)), dim3(kSumThreads), 0, stream, in, p.token_loss, p.weight,
+                       slices > 1 ? sums : nullptr, p.out_loss);
+    if (slices > 1) hipLaunchKernelGGL(policy_slices_kernel, dim3(1), dim3(kSumThreads), 0, stream, sums, slices, p.out_loss);
+    return hipGetLastError();
+}
+
+}  // namespace ef21

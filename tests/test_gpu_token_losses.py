@@ -329,11 +329,12 @@ def test_another_stream_and_a_graph(gpu):
     start = torch.tensor([0, 10, 25, 30, 40], device="cuda")
     bufs = dict(l1=torch.empty(2, device="cuda"), l2=torch.empty(1, device="cuda"), t=torch.empty(rows, device="cuda"),
                 p1=torch.empty(rows, device="cuda"), p2=torch.empty(rows, device="cuda"), g1=torch.empty_like(x), g2=torch.empty_like(x),
-                ws=torch.empty(b.ef21_preference_loss_workspace(rows, 2), dtype=torch.uint8, device="cuda"))
+                ws=torch.empty(b.ef21_preference_loss_workspace(rows, 2), dtype=torch.uint8, device="cuda"),
+                ws2=torch.empty(b.ef21_policy_loss_workspace(rows), dtype=torch.uint8, device="cuda"))
 
     def calls():
         b.ef21_preference_loss(x, dl, start, ref, 0.1, out_loss=bufs["l1"], logp=bufs["p1"], grad=bufs["g1"], workspace=bufs["ws"])
-        b.ef21_policy_loss(x, dl, ref, adv, 0.2, 0.2, ref_logp=ref, kl=0.1, out_loss=bufs["l2"], token_loss=bufs["t"], logp=bufs["p2"], grad=bufs["g2"])
+        b.ef21_policy_loss(x, dl, ref, adv, 0.2, 0.2, ref_logp=ref, kl=0.1, out_loss=bufs["l2"], token_loss=bufs["t"], logp=bufs["p2"], grad=bufs["g2"], workspace=bufs["ws2"])
 
     side = torch.cuda.Stream()
     torch.cuda.synchronize()
@@ -348,7 +349,7 @@ def test_another_stream_and_a_graph(gpu):
         torch.cuda.synchronize()
         graph.replay()
         torch.cuda.synchronize()
-        got = {k: v.clone() for k, v in bufs.items() if k != "ws"}
+        got = {k: v.clone() for k, v in bufs.items() if not k.startswith("ws")}
         l1, p1, g1 = b.ef21_preference_loss(x, dl, start, ref, 0.1)
         l2, t, p2, g2 = b.ef21_policy_loss(x, dl, ref, adv, 0.2, 0.2, ref_logp=ref, kl=0.1)
         for k, v in dict(l1=l1, l2=l2, t=t, p1=p1, p2=p2, g1=g1, g2=g2).items():

@@ -89,12 +89,17 @@ def test_preference_loss(lib, ptr):
 
 
 def test_policy_loss(lib, ptr):
+    size = C.c_int64()
+    assert lib.ef21_policy_loss_workspace(5, C.byref(size)) == binding.EF21_OK
+    need = size.value
     other = ptr + 512
-    good = [ptr, 1, 5, 7, 7, ptr, 0, ptr, ptr, ptr, ptr, 0.2, 0.2, 0.1, ptr, ptr, ptr, other, 7, None]
+    good = [ptr, 1, 5, 7, 7, ptr, 0, ptr, ptr, ptr, ptr, 0.2, 0.2, 0.1, ptr, ptr, ptr, other, 7, ptr, need, None]
     for args in [*bad_logits(good, ptr)] + [swap(good, at, v) for at, v in [
             (7, None), (8, None), (9, None), (9, ptr + 2), (10, ptr + 1), (11, -0.1), (11, 1.1), (11, math.nan), (12, -0.1), (12, math.inf), (13, -1.0),
-            (13, math.nan), (14, None), (15, None), (16, None), (17, ptr + 1), (18, 6)]]:
+            (13, math.nan), (14, None), (15, None), (16, None), (17, ptr + 1), (18, 6), (19, None), (19, ptr + 8), (20, need - 1)]]:
         refused(lib, lib.ef21_policy_loss(*args))
+    for args in [(-1, C.byref(size)), (2 ** 31, C.byref(size)), (5, None)]:
+        refused(lib, lib.ef21_policy_loss_workspace(*args))
 
 
 def test_binding_refuses_host_tensors():
