@@ -10,31 +10,53 @@
 
 namespace ef21 {
 namespace {
+#ifndef FL
+#define FL 8
+#endif
 
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------- pieces of rows
 typedef uint32_t Loose4 __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any address that a type here has
 
-// N entries from p on, converted to fp32.
+// N entries from p on, as they lie in memory, and converted to fp32.  ONCE: the row is read once (non-temporal).
 template <class T, int N>
-__device__ __forceinline__ void load_entries(const T *p, float (&f)[N]) {
+struct Held {
+    static constexpr int kWords = N * (int)sizeof(T) / 16;
     static_assert(N * sizeof(T) % 16 == 0, "whole loads");
-    constexpr int PER = 16 / (int)sizeof(T);
+    Loose4 w[kWords];
+    template <bool ONCE>
+    __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-    for (int i = 0; i < N / PER; ++i) {
-        const Loose4 r = __builtin_nontemporal_load(reinterpret_cast<const Loose4 *>(p + i * PER));
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[4 * i + j] = __uint_as_float(r[j]);
-        } else {
-            typedef T T8 __attribute__((ext_vector_type(8)));
-            const T8 h = __builtin_bit_cast(T8, r);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[8 * i + j] = (float)h[j];
+        for (int i = 0; i < kWords; ++i) {
+            const Loose4 *at = reinterpret_cast<const Loose4 *>(p) + i;
+            w[i] = ONCE ? __builtin_nontemporal_load(at) : *at;
         }
     }
-}
+    __device__ __forceinline__ void get(float (&f)[N]) const {
+        constexpr int PER = 16 / (int)sizeof(T);
+        typedef T TN __attribute__((ext_vector_type(PER)));
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const TN h = __builtin_bit_cast(TN, w[i]);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) f[PER * i + j] = (float)h[j];
+        }
+    }
+    // the first `count` entries, one by one
+    __device__ __forceinline__ void load_few(const T *p, int count) {
+        constexpr int PER = 16 / (int)sizeof(T);
+        typedef T TN __attribute__((ext_vector_type(PER)));
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            TN h = {};
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                if (PER * i + j < count) h[j] = p[PER * i + j];
+            w[i] = __builtin_bit_cast(Loose4, h);
+        }
+    }
+};
 template <class T, int N>
 __device__ __forceinline__ void store_entries(T *p, const float (&f)[N]) {
     constexpr int PER = 16 / (int)sizeof(T);
@@ -69,14 +91,16 @@ __device__ __forceinline__ Columns columns_of(int64_t first, int64_t width) {
     const int64_t at = first + N <= width ? first : width - N;
     return {at, (int32_t)(first - at), N};
 }
-template <class T, int N>
+template <bool ONCE, class T, int N>
+__device__ __forceinline__ void hold_columns(const T *row, const Columns &c, Held<T, N> &h) {
+    if (c.count == N) h.template load<ONCE>(row + c.at);
+    else h.load_few(row, c.count);
+}
+template <bool ONCE, class T, int N>
 __device__ __forceinline__ void load_columns(const T *row, const Columns &c, float (&f)[N]) {
-    if (c.count == N) {
-        load_entries(row + c.at, f);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = i < c.count ? (float)row[i] : 0.f;
-    }
+    Held<T, N> h;
+    hold_columns<ONCE>(row, c, h);
+    h.get(f);
 }
 // own: write only what no other lane writes.
 template <class T, int N>
@@ -106,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs p, int64_t co
         for (int i = 0; i < kLookupRows; ++i) {
             const int64_t token = first + i < p.count ? token_at(p.tokens, first + i) : -1;
             has[i] = token >= 0 && token < p.vocab;
-            if (has[i] && c.at >= 0) load_columns(static_cast<const TIN *>(p.table) + token * p.table_stride, c, f[i]);
+            if (has[i] && c.at >= 0) load_columns<false>(static_cast<const TIN *>(p.table) + token * p.table_stride, c, f[i]);
         }
 #pragma unroll
         for (int i = 0; i < kLookupRows; ++i) {
@@ -122,9 +146,9 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs p, int64_t co
 // Stable radix sort of (token, position), digit by digit from the lowest.  Up to kLdsSort entries of a worker are sorted in the LDS of one
 // workgroup in one launch; more go tile by tile, a histogram and a scatter per digit.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-constexpr int kMostDigits = 256;
+constexpr int kDigitBits = 9, kMostDigits = 1 << kDigitBits;
 constexpr int kLdsSort = 16 * kSortThreads;
-constexpr int kTileItems = 8, kTile = kTileItems * kSortThreads;
+constexpr int kTileItems = 4, kTile = kTileItems * kSortThreads;
 constexpr uint32_t kNoKey = 0xffffffffu;                           // behind every key, in every digit
 
 // Key of a token: itself, or vocab (behind all others) where it is none.
@@ -133,14 +157,30 @@ __device__ __forceinline__ uint32_t token_key(const Tokens &t, int64_t i, int64_
     return v >= 0 && v < vocab ? (uint32_t)v : (uint32_t)vocab;
 }
 
+// First of a worker's sorted keys that is not below v, by the whole wavefront: 64 places are compared at a time.
+__device__ __forceinline__ int64_t wave_lower_bound(const uint32_t *key, int64_t count, uint32_t v) {
+    int64_t a = 0, b = count;                                      // every key before a is below v, none from b on is
+    while (a < b) {
+        const int64_t step = (b - a + kWave - 1) / kWave, at = a + lane_id() * step;
+        const uint32_t below = popc64(__ballot(at < b && key[at] < v));   // of the places a, a + step, ...
+        if (below == 0u) return a;
+        const int64_t last = a + (int64_t)(below - 1u) * step;     // the last place that is below
+        b = last + step < b ? last + step : b;
+        a = last + 1;
+    }
+    return a;
+}
+
+// Rows of a table are marked in words of 32, so many words at a time.
+constexpr int kMarkedWords = 1024;
+
 struct Digit {
     int shift, bits;
     __device__ uint32_t of(uint32_t key) const { return key >> shift & ((1u << bits) - 1u); }
-    __device__ int count() const { return 1 << bits; }
 };
 
 struct SortShared {
-    uint32_t before[kSortWaves][kMostDigits];                      // entries of the digit in the wavefront so far; then: in the wavefronts before it
+    uint16_t before[kSortWaves][kMostDigits];                      // entries of the digit in the wavefront so far; then: in the wavefronts before it
     uint32_t base[kMostDigits];                                    // entries of lower digits (or where the digit's entries go)
     uint32_t wave_total[kSortWaves];
 };
@@ -148,9 +188,9 @@ struct SortShared {
 // rank[i]: how many entries of the same digit the wavefront has before entry (i, lane), entries in the order of i, then of the lane.
 template <int ITEMS>
 __device__ __forceinline__ void rank_items(const uint32_t (&key)[ITEMS], uint32_t (&rank)[ITEMS], Digit digit, SortShared &s) {
-    for (int i = (int)threadIdx.x; i < kSortWaves * kMostDigits; i += kSortThreads) (&s.before[0][0])[i] = 0u;
+    for (int i = (int)threadIdx.x; i < kSortWaves * kMostDigits / 2; i += kSortThreads) reinterpret_cast<uint32_t *>(s.before)[i] = 0u;
     __syncthreads();
-    volatile uint32_t *mine = s.before[wave_id()];
+    volatile uint16_t *mine = s.before[wave_id()];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const uint32_t d = digit.of(key[i]);
@@ -163,7 +203,7 @@ __device__ __forceinline__ void rank_items(const uint32_t (&key)[ITEMS], uint32_
         const uint32_t below = lanes_below(peers), old = mine[d];
         rank[i] = old + below;
         __builtin_amdgcn_wave_barrier();                           // all lanes have read before the first of each digit writes
-        if (below == 0u) mine[d] = old + popc64(peers);
+        if (below == 0u) mine[d] = (uint16_t)(old + popc64(peers));
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
@@ -176,7 +216,7 @@ __device__ __forceinline__ void scan_digits(SortShared &s) {
     if (d < kMostDigits) {
         for (int w = 0; w < kSortWaves; ++w) {
             const uint32_t c = s.before[w][d];
-            s.before[w][d] = total;
+            s.before[w][d] = (uint16_t)total;
             total += c;
         }
     }
@@ -195,9 +235,30 @@ __device__ __forceinline__ void scan_digits(SortShared &s) {
 template <int ITEMS>
 __device__ __forceinline__ int item_index(int i) { return wave_id() * (kWave * ITEMS) + i * kWave + lane_id(); }
 
+// Tables that are cleared whole before the sums.
+struct ClearArgs {
+    float *table;
+    int64_t entries, stride;                                       // of a worker's table, from one worker's to the next
+    int64_t blocks_per_worker;                                     // of 4 kSortThreads entries
+};
+__device__ __forceinline__ void clear_block(const ClearArgs &c, int64_t block) {
+    float *table = c.table + block / c.blocks_per_worker * c.stride;
+    const int64_t at = (block % c.blocks_per_worker * kSortThreads + threadIdx.x) * 4;
+    if (at + 4 <= c.entries) {
+        store4_any(table + at, make_float4(0.f, 0.f, 0.f, 0.f));
+    } else {
+        for (int64_t i = at; i < c.entries; ++i) table[i] = 0.f;
+    }
+}
+
+// Workgroups 0 .. n - 1 sort; those behind them clear tables meanwhile, which the memory is free for.
 template <int ITEMS>
-__global__ __launch_bounds__(kSortThreads) void sort_in_lds_kernel(Tokens tokens, int32_t count, int64_t vocab, int bits, int passes, uint32_t *key_out,
-                                                                   uint32_t *pos_out) {
+__global__ __launch_bounds__(kSortThreads) void sort_in_lds_kernel(Tokens tokens, int32_t n, int32_t count, int64_t vocab, int bits, int passes,
+                                                                   uint32_t *key_out, uint32_t *pos_out, uint32_t *named, int64_t named_words, ClearArgs clear) {
+    if ((int32_t)blockIdx.x >= n) {
+        for (int64_t b = (int64_t)blockIdx.x - n; b < (int64_t)n * clear.blocks_per_worker; b += (int64_t)gridDim.x - n) clear_block(clear, b);
+        return;
+    }
     extern __shared__ uint32_t lds_keys[];                         // [ITEMS * kSortThreads], then as many 16-bit positions
     __shared__ SortShared s;
     uint16_t *lds_pos = reinterpret_cast<uint16_t *>(lds_keys + ITEMS * kSortThreads);
@@ -234,6 +295,41 @@ __global__ __launch_bounds__(kSortThreads) void sort_in_lds_kernel(Tokens tokens
         key_out[first + at] = lds_keys[at];
         pos_out[first + at] = lds_pos[at];
     }
+    if (!named) return;
+    // a bit for every row that a token names, kMarked rows at a time
+    __shared__ uint32_t marks[kMarkedWords];
+    uint32_t *mine = named + (int64_t)blockIdx.x * named_words;
+    int at = (int)threadIdx.x;                                     // of this thread's entries, the first that is not marked yet
+    for (int64_t word = 0; word < named_words; word += kMarkedWords) {
+        const int words = (int)(named_words - word < kMarkedWords ? named_words - word : kMarkedWords);
+        __syncthreads();
+        for (int i = (int)threadIdx.x; i < words; i += kSortThreads) marks[i] = 0u;
+        __syncthreads();
+        for (; at < count; at += kSortThreads) {
+            const int64_t in = (int64_t)lds_keys[at] - word * 32;
+            if (in >= (int64_t)words * 32) break;
+            atomicOr(&marks[in / 32], 1u << (in & 31));
+        }
+        __syncthreads();
+        for (int i = (int)threadIdx.x; i < words; i += kSortThreads) mine[word + i] = marks[i];
+    }
+}
+
+// The same from sorted keys in memory: a workgroup per kMarkedWords words of a worker.
+__global__ __launch_bounds__(kThreads) void mark_named_kernel(const uint32_t *keys, int64_t count, uint32_t *named, int64_t named_words) {
+    __shared__ uint32_t marks[kMarkedWords];
+    const uint32_t *key = keys + (int64_t)blockIdx.y * count;
+    const int64_t word = (int64_t)blockIdx.x * kMarkedWords;
+    const int words = (int)(named_words - word < kMarkedWords ? named_words - word : kMarkedWords);
+    for (int i = (int)threadIdx.x; i < words; i += kThreads) marks[i] = 0u;
+    __syncthreads();
+    for (int64_t i = wave_lower_bound(key, count, (uint32_t)(word * 32)) + threadIdx.x; i < count; i += kThreads) {
+        const int64_t in = (int64_t)key[i] - word * 32;
+        if (in >= (int64_t)words * 32) break;
+        atomicOr(&marks[in / 32], 1u << (in & 31));
+    }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < words; i += kThreads) named[(int64_t)blockIdx.y * named_words + word + i] = marks[i];
 }
 
 struct SortArgs {
@@ -254,10 +350,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_histogram_kernel(SortArgs a
     const int64_t first = (int64_t)blockIdx.y * a.count, start = (int64_t)blockIdx.x * kTile;
     if (threadIdx.x < kMostDigits) hist[threadIdx.x] = 0u;
     __syncthreads();
+    uint32_t key[kTileItems];
+#pragma unroll
     for (int i = 0; i < kTileItems; ++i) {
         const int64_t at = start + i * kSortThreads + threadIdx.x;
-        if (at < a.count) atomicAdd(&hist[a.digit.of(sort_key(a, first, at))], 1u);
+        key[i] = at < a.count ? sort_key(a, first, at) : kNoKey;
     }
+#pragma unroll
+    for (int i = 0; i < kTileItems; ++i)
+        if (start + i * kSortThreads + threadIdx.x < a.count) atomicAdd(&hist[a.digit.of(key[i])], 1u);
     __syncthreads();
     if (threadIdx.x < kMostDigits) a.counts[((int64_t)blockIdx.y * a.tiles + blockIdx.x) * kMostDigits + threadIdx.x] = hist[threadIdx.x];
 }
@@ -278,6 +379,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
     uint32_t total = 0u, earlier = 0u;
     if (threadIdx.x < kMostDigits) {
         const uint32_t *c = a.counts + (int64_t)blockIdx.y * a.tiles * kMostDigits + threadIdx.x;
+#pragma unroll 8
         for (int t = 0; t < a.tiles; ++t) {
             const uint32_t v = c[(int64_t)t * kMostDigits];
             total += v;
@@ -305,14 +407,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
 }
 
 // ---------------------------------------------------------------- sums
-constexpr int kChunk = 64;                                         // sorted entries that a wavefront adds
-constexpr int kFlight = 8;                                         // rows that it has in flight
-
 struct SumArgs {
     EmbedGradArgs p;
     const uint32_t *key, *pos;                                     // [n][count], sorted
+    const uint32_t *named;                                         // [n][named_words]
     float *partial;                                                // [n][chunks][2][width]: what a chunk has of the token that it begins with, and of the last one
-    int64_t chunks, column_tiles;
+    int64_t chunks, column_tiles, named_words;
+    int32_t chunk;                                                 // sorted entries that a wavefront adds, at most 64
     int64_t sum_blocks;                                            // workgroups of the sums; those behind them write the rows without a token
     int64_t fill_rows, fill_blocks_per_worker;
 };
@@ -320,182 +421,313 @@ struct SumArgs {
 template <class T>
 constexpr int sum_columns() { return 16 / (int)sizeof(T); }        // columns of a lane
 
-// First of a worker's sorted keys that is not below v, by the whole wavefront: 64 places are compared at a time.
-__device__ __forceinline__ int64_t wave_lower_bound(const uint32_t *key, int64_t count, uint32_t v) {
-    int64_t a = 0, b = count;                                      // every key before a is below v, none from b on is
-    while (a < b) {
-        const int64_t step = (b - a + kWave - 1) / kWave, at = a + lane_id() * step;
-        const uint32_t below = popc64(__ballot(at < b && key[at] < v));   // of the places a, a + step, ...
-        if (below == 0u) return a;
-        const int64_t last = a + (int64_t)(below - 1u) * step;     // the last place that is below
-        b = last + step < b ? last + step : b;
-        a = last + 1;
-    }
-    return a;
-}
+constexpr int kShort = kWave;                                      // a token of up to so many entries is added by one wavefront
 
-template <class T, bool ADD>
+// The chunk's wavefront adds the tokens that begin in the chunk, those with at most kShort entries to their end.  Of a longer token it adds what lies
+// in the chunk and leaves a partial sum.  FLIGHT rows of grad_out, and with ADD the rows that they are added to, are in flight.
+template <class T, bool ADD, int FLIGHT>
 __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int64_t chunk, int64_t column_tile) {
     constexpr int N = sum_columns<T>();
     const EmbedGradArgs &p = s.p;
     const Columns c = columns_of<N>(column_tile * (kWave * N) + lane_id() * N, p.width);
     const uint32_t *key = s.key + worker * p.count, *pos = s.pos + worker * p.count;
-    const int64_t first = chunk * kChunk;
-    const int here = (int)(p.count - first < kChunk ? p.count - first : kChunk);
+    const int64_t first = chunk * s.chunk, mine = first + lane_id();
+    const int here = (int)(p.count - first < s.chunk ? p.count - first : s.chunk);
     const T *grad = static_cast<const T *>(p.grad_out) + worker * p.count * p.grad_stride;
     float *table = p.table_grad + worker * p.worker_stride;
     float *part = s.partial + (worker * s.chunks + chunk) * 2 * p.width;
     const uint32_t none = (uint32_t)p.vocab;                       // the key of what is no token
-    uint32_t k = none, q = 0u;
+    uint32_t k = kNoKey, q = 0u, k_next = kNoKey, k_before = kNoKey, k_behind = kNoKey, q_behind = 0u;
     if (lane_id() < here) {
-        k = key[first + lane_id()];
-        q = pos[first + lane_id()];
+        k = key[mine];
+        q = pos[mine];
+        if (mine + 1 < p.count) k_next = key[mine + 1];
     }
-    const uint32_t before = first > 0 ? key[first - 1] : kNoKey, behind = first + here < p.count ? key[first + here] : kNoKey;
+    if (mine >= kWave) k_before = key[mine - kWave];
+    if (mine + here < p.count) {
+        k_behind = key[mine + here];
+        q_behind = pos[mine + here];
+    }
+    const uint32_t k_first = __builtin_amdgcn_readfirstlane(k), k_last = __builtin_amdgcn_readlane(k, here - 1);
+    // entries of the first token before the chunk and of the last one behind it (at most 64 of each are looked at), and of the first one in the chunk
+    const int before = (int)popc64(__ballot(k_before == k_first)), behind = (int)popc64(__ballot(k_behind == k_last));
+    const int lead = (int)popc64(__ballot(k == k_first)), tail = (int)popc64(__ballot(k == k_last));
+    int at = 0, stop = here;
+    bool open = false;                                             // the first token is a long one that began before
+    if (before > 0) {
+        open = before + lead + (lead == here ? behind : 0) > kShort;
+        if (!open) at = lead;                                      // the wavefront of the chunk that it began in adds it
+    }
+    const bool began_here = !(before > 0 && lead == here);
+    const uint64_t ends = __ballot(k != k_next);                   // entries that are the last of their token
+    if (began_here && behind > 0 && tail + behind <= kShort) stop += behind;
     float acc[N] = {};
-    uint32_t current = __builtin_amdgcn_readlane(k, 0);
-    bool open = current == before;                                 // the token has entries in the chunk before
-    for (int base = 0; base < here; base += kFlight) {
-        float f[kFlight][N];
+    while (at < stop) {
+        Held<T, N> f[FLIGHT];
+        float old[ADD ? FLIGHT : 1][N];
 #pragma unroll
-        for (int j = 0; j < kFlight; ++j) {
-            const int at = base + j < here ? base + j : here - 1;
-            const int64_t row = __builtin_amdgcn_readlane(q, at);
-            if (c.at >= 0) load_columns(grad + row * p.grad_stride, c, f[j]);
+        for (int j = 0; j < FLIGHT; ++j) {
+            const int e = at + j < stop ? at + j : stop - 1;
+            const int64_t row = e < here ? __builtin_amdgcn_readlane(q, e) : __builtin_amdgcn_readlane(q_behind, e - here);
+            if (c.at >= 0) hold_columns<true>(grad + row * p.grad_stride, c, f[j]);
+            if (ADD && (e < here ? (ends >> e & 1u) != 0 : e + 1 == stop)) {
+                const uint32_t token = e < here ? __builtin_amdgcn_readlane(k, e) : k_last;
+                if (token != none && c.at >= 0) load_columns<true>(table + (int64_t)token * p.width, c, old[j]);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < kFlight; ++j) {
-            if (base + j >= here) continue;
+        for (int j = 0; j < FLIGHT; ++j) {
+            const int e = at + j;
+            if (e >= stop) continue;
+            float g[N];
+            f[j].get(g);
 #pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] += f[j][i];
-            const int at = base + j;
-            const uint32_t next = at + 1 < here ? __builtin_amdgcn_readlane(k, at + 1 < kWave ? at + 1 : 0) : behind;
-            const bool last = at + 1 == here;
-            if (next == current && !last) continue;
-            const bool goes_on = last && next == current;
-            if (current != none && c.at >= 0) {
-                if (open || goes_on) {
+            for (int i = 0; i < N; ++i) acc[i] += g[i];
+            const bool over = e < here ? (ends >> e & 1u) != 0 : e + 1 == stop;
+            if (!over && e + 1 < stop) continue;
+            const uint32_t token = e < here ? __builtin_amdgcn_readlane(k, e) : k_last;
+            if (token != none && c.at >= 0) {
+                if (open || !over) {
                     store_columns(part + (open ? 0 : p.width), c, acc, true);
                 } else {
-                    float *out = table + (int64_t)current * p.width;
-                    if (ADD) {
-                        float old[N];
-                        load_columns(out, c, old);
 #pragma unroll
-                        for (int i = 0; i < N; ++i) acc[i] = fmaf(p.scale, acc[i], old[i]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < N; ++i) acc[i] *= p.scale;
-                    }
-                    store_columns(out, c, acc, true);
+                    for (int i = 0; i < N; ++i) acc[i] = ADD ? fmaf(p.scale, acc[i], old[ADD ? j : 0][i]) : p.scale * acc[i];
+                    store_columns(table + (int64_t)token * p.width, c, acc, true);
                 }
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) acc[i] = 0.f;
-            current = next;
             open = false;
         }
+        at += FLIGHT;
     }
 }
-
-constexpr int kMostFillRows = 1024;
 
 // Rows of a table that no token names are written as zeros.
-__device__ void fill_rows(const SumArgs &s, int64_t worker, int64_t block, uint32_t *named) {
+__device__ __forceinline__ void fill_rows(const SumArgs &s, int64_t worker, int64_t block) {
     const EmbedGradArgs &p = s.p;
     const int64_t from = block * s.fill_rows, to = from + s.fill_rows < p.vocab ? from + s.fill_rows : p.vocab;
-    const uint32_t *key = s.key + worker * p.count;
-    for (int i = (int)threadIdx.x; i < kMostFillRows / 32; i += kThreads) named[i] = 0u;
-    __syncthreads();
-    for (int64_t i = wave_lower_bound(key, p.count, (uint32_t)from) + threadIdx.x; i < p.count; i += kThreads) {
-        const uint32_t k = key[i];
-        if (k >= (uint32_t)to) break;
-        atomicOr(&named[(k - (uint32_t)from) / 32], 1u << (k - (uint32_t)from) % 32);
-    }
-    __syncthreads();
+    const uint32_t *named = s.named + worker * s.named_words;
+    float *table = p.table_grad + worker * p.worker_stride;
     const float none[4] = {};
     for (int64_t v = from + wave_id(); v < to; v += kThreads / kWave) {
-        if (named[(v - from) / 32] >> (v - from) % 32 & 1u) continue;
-        float *out = p.table_grad + worker * p.worker_stride + v * p.width;
-        for (int64_t j = lane_id() * 4; j < p.width; j += kWave * 4) {
-            const Columns c = columns_of<4>(j, p.width);
-            store_columns(out, c, none, false);
-        }
+        if (named[v / 32] >> (v & 31) & 1u) continue;
+        for (int64_t j = lane_id() * 4; j < p.width; j += kWave * 4) store_columns(table + v * p.width, columns_of<4>(j, p.width), none, false);
     }
 }
 
-template <class T, bool ADD>
-__global__ __launch_bounds__(kThreads) void embed_grad_kernel(SumArgs s) {
-    __shared__ uint32_t named[kMostFillRows / 32];
+// What is done with the rows that no token names, and with those that one does.
+enum SumMode { kStoreAndFill, kStore, kAdd };
+
+// (Beside the filling at most 64 registers, so that the workgroups that only write fill the compute units.)
+template <class T, int MODE>
+__global__ __launch_bounds__(kThreads, MODE == kStoreAndFill ? 8 : 4) void embed_grad_kernel(SumArgs s) {
     if ((int64_t)blockIdx.x < s.sum_blocks) {
         const int64_t tasks = (int64_t)s.p.n * s.chunks * s.column_tiles;
         for (int64_t task = (int64_t)blockIdx.x * (kThreads / kWave) + wave_id(); task < tasks; task += s.sum_blocks * (kThreads / kWave)) {
             const int64_t chunk = task / s.column_tiles;
-            sum_chunk<T, ADD>(s, chunk / s.chunks, chunk % s.chunks, task % s.column_tiles);
+            sum_chunk<T, MODE == kAdd, (MODE == kStoreAndFill ? 4 : FL)>(s, chunk / s.chunks, chunk % s.chunks, task % s.column_tiles);
         }
-    } else if (!ADD) {
+    } else if (MODE == kStoreAndFill) {
         const int64_t blocks = (int64_t)s.p.n * s.fill_blocks_per_worker;
-        for (int64_t b = (int64_t)blockIdx.x - s.sum_blocks; b < blocks; b += (int64_t)gridDim.x - s.sum_blocks) {
-            fill_rows(s, b / s.fill_blocks_per_worker, b % s.fill_blocks_per_worker, named);
-            __syncthreads();
-        }
+        for (int64_t b = (int64_t)blockIdx.x - s.sum_blocks; b < blocks; b += (int64_t)gridDim.x - s.sum_blocks)
+            fill_rows(s, b / s.fill_blocks_per_worker, b % s.fill_blocks_per_worker);
     }
 }
 
-// The tokens that begin in a chunk and go on behind it: their partial sums in order.  A workgroup per chunk and 256 columns.
+// The tokens of more than kShort entries that begin in a chunk and go on behind it: their partial sums in order.  A workgroup per chunk and kJoinColumns columns; of a long run
+// each quarter of the workgroup takes a quarter.
+constexpr int kJoinThreads = 512, kJoinParts = 4, kJoinColumns = kJoinThreads / kJoinParts * 4;
+
 template <bool ADD>
-__global__ __launch_bounds__(kThreads) void embed_grad_join_kernel(SumArgs s, int64_t tiles) {
-    __shared__ float lds[kThreads / kWave][kWave * 4];
+__global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s, int64_t tiles) {
+    __shared__ float lds[kJoinParts][kJoinColumns];
     const EmbedGradArgs &p = s.p;
     const int64_t tasks = (int64_t)p.n * (s.chunks - 1) * tiles;
     for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
         const int64_t tile = task % tiles, chunk = task / tiles % (s.chunks - 1), worker = task / tiles / (s.chunks - 1);
         const uint32_t *key = s.key + worker * p.count;
-        const int64_t first = chunk * kChunk, end = first + kChunk;
-        const uint32_t k = key[end - 1];
-        if (k != key[end] || k == (uint32_t)p.vocab) continue;                            // ends here
-        if (first > 0 && key[first] == k && key[first - 1] == k) continue;                // began before
-        const int64_t last = (end + wave_lower_bound(key + end, p.count - end, k + 1u) - 1) / kChunk;   // the chunk it ends in
-        const int64_t each = (last - chunk + 1 + kThreads / kWave - 1) / (kThreads / kWave);
-        const int64_t from = chunk + wave_id() * each, to = from + each < last + 1 ? from + each : last + 1;
-        const Columns c = columns_of<4>(tile * (kWave * 4) + lane_id() * 4, p.width);
+        const int64_t first = chunk * s.chunk, end = first + s.chunk;
+        const uint32_t k = key[end - 1], behind = key[end], begin = key[first], before = first > 0 ? key[first - 1] : kNoKey;
+        const uint32_t k_here = lane_id() < s.chunk ? key[first + lane_id()] : kNoKey, k_behind = end + lane_id() < p.count ? key[end + lane_id()] : kNoKey;
+        if (k != behind || k == (uint32_t)p.vocab) continue;                              // ends here
+        if (begin == k && before == k) continue;                                          // began before
+        if (popc64(__ballot(k_here == k)) + popc64(__ballot(k_behind == k)) <= (uint32_t)kShort) continue;
+        const int64_t last = (end + wave_lower_bound(key + end, p.count - end, k + 1u) - 1) / s.chunk;   // the chunk it ends in
+        const int64_t run = last - chunk + 1, each = run <= 8 ? run : (run + kJoinParts - 1) / kJoinParts;
+        const int quarter = (int)threadIdx.x / (kJoinThreads / kJoinParts), column = (int)threadIdx.x % (kJoinThreads / kJoinParts) * 4;
+        const int64_t from = chunk + quarter * each, to = from + each < last + 1 ? from + each : last + 1;
+        const Columns c = columns_of<4>(tile * kJoinColumns + column, p.width);
         const float *part = s.partial + worker * s.chunks * 2 * p.width;
-        float acc[4] = {};
+        float *out = p.table_grad + worker * p.worker_stride + (int64_t)k * p.width;
+        float acc[4] = {}, old[4] = {};
         if (c.at >= 0) {
+            if (ADD && quarter == 0) load_columns<true>(out, c, old);
 #pragma unroll 8
             for (int64_t i = from; i < to; ++i) {
                 float f[4];
-                load_columns(part + (2 * i + (i == chunk ? 1 : 0)) * p.width, c, f);
+                load_columns<true>(part + (2 * i + (i == chunk ? 1 : 0)) * p.width, c, f);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[j] += f[j];
             }
         }
-        __syncthreads();
+        if (each < run) {
+            __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) lds[wave_id()][lane_id() * 4 + j] = acc[j];
-        __syncthreads();
-        if (wave_id() == 0 && c.at >= 0) {
-            float *out = p.table_grad + worker * p.worker_stride + (int64_t)k * p.width;
-            float old[4] = {};
-            if (ADD) load_columns(out, c, old);
+            for (int j = 0; j < 4; ++j) lds[quarter][column + j] = acc[j];
+            __syncthreads();
+            for (int w = 1; w < kJoinParts; ++w) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                for (int w = 1; w < kThreads / kWave; ++w) acc[j] += lds[w][lane_id() * 4 + j];
-                acc[j] = ADD ? fmaf(p.scale, acc[j], old[j]) : p.scale * acc[j];
+                for (int j = 0; j < 4; ++j) acc[j] += lds[w][column + j];
             }
+        }
+        if (quarter == 0 && c.at >= 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = ADD ? fmaf(p.scale, acc[j], old[j]) : p.scale * acc[j];
             store_columns(out, c, acc, true);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- few tokens
+// One launch without a sort: a workgroup per worker, `rows` rows of the table and a wavefront's columns reads all tokens, keeps in order those
+// that name its rows, and adds (or clears) row by row.
+constexpr int64_t kFewTokens = 1024;
+constexpr int kFewHeavy = 32;                                      // from so many entries on a row is added by the whole workgroup
+
+template <class T, bool ADD>
+__global__ __launch_bounds__(kThreads) void embed_grad_few_kernel(EmbedGradArgs p, int32_t rows, int64_t groups, int64_t column_tiles) {
+    constexpr int N = sum_columns<T>(), FLIGHT = 8, WAVES = kThreads / kWave;
+    __shared__ uint32_t list[kFewTokens];                          // row within the group << 16 | position
+    __shared__ uint32_t found[WAVES];
+    __shared__ float joined[WAVES][kWave * N];
+    const int64_t column_tile = blockIdx.x % column_tiles, group = blockIdx.x / column_tiles % groups, worker = blockIdx.x / column_tiles / groups;
+    const int64_t low = group * rows, first = worker * p.count;
+    const int here = (int)(p.vocab - low < rows ? p.vocab - low : rows);
+    // each wavefront looks through its quarter of the tokens
+    const int count = (int)p.count, each = (count + WAVES - 1) / WAVES, start = wave_id() * each, stop = min(start + each, count);
+    uint32_t mine = 0u;
+    for (int base = start; base < stop; base += kWave) {
+        const int at = base + lane_id();
+        const int64_t in = at < stop ? token_at(p.tokens, first + at) - low : -1;
+        const bool hit = in >= 0 && in < here;
+        const uint64_t hits = __ballot(hit);
+        if (hit) list[start + mine + lanes_below(hits)] = (uint32_t)in << 16 | (uint32_t)at;
+        mine += popc64(hits);
+    }
+    if (lane_id() == 0) found[wave_id()] = mine;
+    __syncthreads();
+    const Columns c = columns_of<N>(column_tile * (kWave * N) + lane_id() * N, p.width);
+    const T *grad = static_cast<const T *>(p.grad_out) + first * p.grad_stride;
+    float *table = p.table_grad + worker * p.worker_stride + low * p.width;
+    uint32_t total = 0u;
+    for (int w = 0; w < WAVES; ++w) total += found[w];
+    if (ADD && total == 0u) return;
+
+    // Adds the entries number from .. to - 1 of a row, in order.
+    auto add = [&](uint32_t row, uint32_t from, uint32_t to, float(&acc)[N]) {
+        uint32_t seen = 0u;
+        for (int w = 0; w < WAVES; ++w) {
+            for (uint32_t base = 0u; base < found[w]; base += kWave) {
+                const uint32_t e = base + lane_id() < found[w] ? list[w * each + base + lane_id()] : ~0u;
+                uint64_t hits = __ballot(e >> 16 == row);
+                while (hits) {
+                    float f[FLIGHT][N];
+                    bool take[FLIGHT];
+#pragma unroll
+                    for (int j = 0; j < FLIGHT; ++j) {
+                        take[j] = hits != 0 && seen >= from && seen < to;
+                        if (hits != 0) {
+                            const int lane = __ffsll((long long)hits) - 1;
+                            const int64_t at = __builtin_amdgcn_readlane(e, lane) & 0xffffu;
+                            if (take[j] && c.at >= 0) load_columns<true>(grad + at * p.grad_stride, c, f[j]);
+                            hits &= hits - 1u;
+                            ++seen;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < FLIGHT; ++j) {
+                        if (!take[j]) continue;
+#pragma unroll
+                        for (int i = 0; i < N; ++i) acc[i] += f[j][i];
+                    }
+                }
+            }
+        }
+    };
+    auto entries = [&](uint32_t row) {
+        uint32_t n = 0u;
+        for (int w = 0; w < WAVES; ++w)
+            for (uint32_t base = 0u; base < found[w]; base += kWave)
+                n += popc64(__ballot(base + lane_id() < found[w] && list[w * each + base + lane_id()] >> 16 == row));
+        return n;
+    };
+    auto finish = [&](uint32_t row, float(&acc)[N], const float(&old)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = ADD ? fmaf(p.scale, acc[i], old[i]) : p.scale * acc[i];
+        store_columns(table + (int64_t)row * p.width, c, acc, true);
+    };
+    uint64_t heavy = 0u;                                           // rows wave + 4 b of the group that are left for the whole workgroup
+    for (uint32_t row = wave_id(); row < (uint32_t)here; row += WAVES) {
+        const uint32_t n = total > 0u ? entries(row) : 0u;
+        if (n >= kFewHeavy) {
+            heavy |= 1ull << (row / WAVES);
+            continue;
+        }
+        if (ADD && n == 0u) continue;
+        float acc[N] = {}, old[N] = {};
+        if (n > 0u) {
+            if (ADD && c.at >= 0) load_columns<true>(table + (int64_t)row * p.width, c, old);
+            add(row, 0u, n, acc);                                  // by all lanes, those without columns too: they hold entries of the list
+        }
+        if (c.at >= 0) finish(row, acc, old);
+    }
+    if (total < kFewHeavy) return;
+    __shared__ uint64_t heavies[WAVES];
+    if (lane_id() == 0) heavies[wave_id()] = heavy;
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) {
+        for (uint64_t left = heavies[w]; left != 0; left &= left - 1u) {
+            const uint32_t row = (uint32_t)(__ffsll((long long)left) - 1) * WAVES + w, n = entries(row), part = (n + WAVES - 1) / WAVES;
+            float acc[N] = {}, old[N] = {};
+            if (ADD && c.at >= 0 && wave_id() == 0) load_columns<true>(table + (int64_t)row * p.width, c, old);
+            add(row, wave_id() * part, min(n, (wave_id() + 1) * part), acc);
+#pragma unroll
+            for (int i = 0; i < N; ++i) joined[wave_id()][lane_id() * N + i] = acc[i];
+            __syncthreads();
+            if (wave_id() == 0 && c.at >= 0) {
+                for (int v = 1; v < WAVES; ++v) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) acc[i] += joined[v][lane_id() * N + i];
+                }
+                finish(row, acc, old);
+            }
+            __syncthreads();
         }
     }
 }
 
 // ---------------------------------------------------------------- the workspace
 struct GradSpace {
-    uint32_t *key[2], *pos[2], *counts;
+    uint32_t *key[2], *pos[2], *counts, *named;
     float *partial;
 };
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t kManyBlocks = 1 << 20;
+unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)(blocks < most ? blocks : most); }
 
-size_t grad_layout(int32_t n, int64_t count, int64_t width, void *ws, GradSpace *out) {
+// Sorted entries of a chunk: 64 (fewer partial sums) where that gives wavefronts enough for the chip, else 16.
+#ifndef CHK
+#define CHK 64
+#endif
+int32_t chunk_entries(int32_t n, int64_t count, int64_t width) { return (int64_t)n * count * ceil_div(width, 512) / CHK >= 4096 ? CHK : 16; }
+
+// Whether the tables are cleared whole, beside the sort, and rows with a token written twice, or the rows without one are written beside the sums.
+// The plain clearing writes faster (6.5 TB/s against 5, 1 GB) and hides the sort, but only up to so many tokens there are few rows to write twice.
+bool clears_first(const EmbedGradArgs &p) { return !p.accumulate && p.count <= 8 * kSortThreads && 3 * p.count <= p.vocab; }
+
+size_t grad_layout(int32_t n, int64_t count, int64_t vocab, int64_t width, void *ws, GradSpace *out) {
+    if (count <= kFewTokens) return 256;                           // not used; never zero, so that callers need no case of their own for it
     char *at = static_cast<char *>(ws);
     size_t used = 0;
     auto take = [&](size_t bytes) {
@@ -511,33 +743,37 @@ size_t grad_layout(int32_t n, int64_t count, int64_t width, void *ws, GradSpace 
         g.pos[i] = reinterpret_cast<uint32_t *>(take(entries * sizeof(uint32_t)));
     }
     if (count > kLdsSort) g.counts = reinterpret_cast<uint32_t *>(take((size_t)n * (size_t)ceil_div(count, kTile) * kMostDigits * sizeof(uint32_t)));
-    if (count > kChunk) g.partial = reinterpret_cast<float *>(take((size_t)n * (size_t)ceil_div(count, kChunk) * 2 * (size_t)width * sizeof(float)));
+    g.named = reinterpret_cast<uint32_t *>(take((size_t)n * (size_t)ceil_div(vocab, 32) * sizeof(uint32_t)));
+    g.partial = reinterpret_cast<float *>(take((size_t)n * (size_t)ceil_div(count, chunk_entries(n, count, width)) * 2 * (size_t)width * sizeof(float)));
     if (out) *out = g;
     return used;
 }
 
 template <int ITEMS>
-hipError_t sort_in_lds(const EmbedGradArgs &p, int bits, int passes, const GradSpace &g, hipStream_t stream) {
+hipError_t sort_in_lds(const EmbedGradArgs &p, int bits, int passes, const GradSpace &g, bool clear, hipStream_t stream) {
     constexpr size_t kBytes = (size_t)ITEMS * kSortThreads * (sizeof(uint32_t) + sizeof(uint16_t));
     static PerDeviceOnce once;
     const hipError_t st = once([] {
         return hipFuncSetAttribute(reinterpret_cast<const void *>(&sort_in_lds_kernel<ITEMS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
     });
     if (st != hipSuccess) return st;
-    hipLaunchKernelGGL(sort_in_lds_kernel<ITEMS>, dim3((unsigned)p.n), dim3(kSortThreads), kBytes, stream, p.tokens, (int32_t)p.count, p.vocab, bits, passes,
-                       g.key[0], g.pos[0]);
+    ClearArgs c{p.table_grad, p.vocab * p.width, p.worker_stride, 0};
+    if (clear) c.blocks_per_worker = ceil_div(c.entries, 4 * kSortThreads);
+    hipLaunchKernelGGL(sort_in_lds_kernel<ITEMS>, dim3((unsigned)p.n + at_most((int64_t)p.n * c.blocks_per_worker, kManyBlocks)), dim3(kSortThreads), kBytes,
+                       stream, p.tokens, p.n, (int32_t)p.count, p.vocab, bits, passes, g.key[0], g.pos[0], p.accumulate || clear ? nullptr : g.named,
+                       ceil_div(p.vocab, 32), c);
     return hipGetLastError();
 }
 
-// Sorts; *in: the buffer of g that holds the result.
-hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, int *in, hipStream_t stream) {
+// Sorts; *in: the buffer of g that holds the result.  clear: the tables are cleared too (clears_first), else the rows with a token marked.
+hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, bool clear, int *in, hipStream_t stream) {
     int key_bits = 1;                                              // of vocab, the largest key
     while (p.vocab >> key_bits) ++key_bits;
-    const int passes = (key_bits + 7) / 8, bits = (key_bits + passes - 1) / passes;
+    const int passes = (key_bits + kDigitBits - 1) / kDigitBits, bits = (key_bits + passes - 1) / passes;
     *in = 0;
-    if (p.count <= 2 * kSortThreads) return sort_in_lds<2>(p, bits, passes, g, stream);
-    if (p.count <= 8 * kSortThreads) return sort_in_lds<8>(p, bits, passes, g, stream);
-    if (p.count <= kLdsSort) return sort_in_lds<16>(p, bits, passes, g, stream);
+    if (p.count <= 2 * kSortThreads) return sort_in_lds<2>(p, bits, passes, g, clear, stream);
+    if (p.count <= 8 * kSortThreads) return sort_in_lds<8>(p, bits, passes, g, clear, stream);
+    if (p.count <= kLdsSort) return sort_in_lds<16>(p, bits, passes, g, clear, stream);
     SortArgs a{};
     a.tokens = p.tokens;
     a.count = p.count;
@@ -554,11 +790,13 @@ hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, int *in, hipS
         hipLaunchKernelGGL(sort_histogram_kernel, grid, dim3(kSortThreads), 0, stream, a);
         hipLaunchKernelGGL(sort_scatter_kernel, grid, dim3(kSortThreads), 0, stream, a);
     }
+    if (!p.accumulate) {
+        const int64_t words = ceil_div(p.vocab, 32);
+        hipLaunchKernelGGL(mark_named_kernel, dim3((unsigned)ceil_div(words, kMarkedWords), (unsigned)p.n), dim3(kThreads), 0, stream, g.key[*in], p.count, g.named,
+                           words);
+    }
     return hipGetLastError();
 }
-
-constexpr int64_t kManyBlocks = 1 << 20;
-unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)(blocks < most ? blocks : most); }
 
 }  // namespace
 
@@ -576,43 +814,58 @@ hipError_t launch_embed(const EmbedArgs &p, hipStream_t stream) {
     });
 }
 
-size_t embed_grad_workspace_bytes(int32_t n, int64_t count, int64_t vocab, int64_t width) {
-    (void)vocab;
-    return grad_layout(n, count, width, nullptr, nullptr);
+size_t embed_grad_workspace_bytes(int32_t n, int64_t count, int64_t vocab, int64_t width) { return grad_layout(n, count, vocab, width, nullptr, nullptr); }
+
+template <class T>
+static hipError_t embed_grad_few(const EmbedGradArgs &p, hipStream_t stream) {
+    const int64_t column_tiles = ceil_div(p.width, kWave * sum_columns<T>());
+    // some 16 KB of a table to a workgroup, but no more rows than its list and its heavy bits number, and workgroups enough for the chip
+    int64_t rows = (16 << 10) / (4 * (p.width < kWave * sum_columns<T>() ? p.width : kWave * sum_columns<T>()));
+    const int64_t all = p.vocab * p.n * column_tiles;
+    if (rows > all / 1024) rows = all / 1024;
+    rows = rows < 4 ? 4 : rows > 256 ? 256 : rows;
+    const int64_t groups = ceil_div(p.vocab, rows), blocks = groups * p.n * column_tiles;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (p.accumulate) hipLaunchKernelGGL((embed_grad_few_kernel<T, true>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p, (int32_t)rows, groups, column_tiles);
+    else hipLaunchKernelGGL((embed_grad_few_kernel<T, false>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p, (int32_t)rows, groups, column_tiles);
+    return hipGetLastError();
 }
 
 hipError_t launch_embed_grad(const EmbedGradArgs &p, void *workspace, hipStream_t stream) {
     if (p.count == 0 && p.accumulate) return hipSuccess;
+    if (p.count <= kFewTokens)
+        return with_type(p.type, [&](auto type) { return embed_grad_few<typename ValueOf<decltype(type)::value>::type>(p, stream); });
     GradSpace g;
-    grad_layout(p.n, p.count, p.width, workspace, &g);
+    grad_layout(p.n, p.count, p.vocab, p.width, workspace, &g);
     int in = 0;
-    if (p.count > 0) {
-        const hipError_t st = sort_tokens(p, g, &in, stream);
-        if (st != hipSuccess) return st;
-    }
+    const bool cleared = clears_first(p);
+    const hipError_t st = sort_tokens(p, g, cleared, &in, stream);
+    if (st != hipSuccess) return st;
     SumArgs s{};
     s.p = p;
     s.key = g.key[in];
     s.pos = g.pos[in];
+    s.named = g.named;
+    s.named_words = ceil_div(p.vocab, 32);
     s.partial = g.partial;
-    s.chunks = ceil_div(p.count, kChunk);
+    s.chunk = chunk_entries(p.n, p.count, p.width);
+    s.chunks = ceil_div(p.count, s.chunk);
     return with_type(p.type, [&](auto type) {
         typedef typename ValueOf<decltype(type)::value>::type T;
         s.column_tiles = ceil_div(p.width, kWave * sum_columns<T>());
         s.sum_blocks = at_most(ceil_div((int64_t)p.n * s.chunks * s.column_tiles, kThreads / kWave), kManyBlocks);
-        const int64_t wanted = ceil_div(1 << 17, 4 * p.width);     // rows of some 128 KB in all
-        s.fill_rows = wanted > kMostFillRows ? kMostFillRows : wanted;
+        const int64_t wanted = (16 << 10) / (4 * p.width);         // rows of some 16 KB in all: workgroups that run together write one stretch of memory
+        s.fill_rows = wanted < 4 ? 4 : wanted;
         s.fill_blocks_per_worker = ceil_div(p.vocab, s.fill_rows);
-        const int64_t fill = p.accumulate ? 0 : at_most((int64_t)p.n * s.fill_blocks_per_worker, kManyBlocks);
+        const int64_t fill = p.accumulate || cleared ? 0 : at_most((int64_t)p.n * s.fill_blocks_per_worker, 8 * kManyBlocks);
         const dim3 grid((unsigned)(s.sum_blocks + fill));
-        if (p.accumulate) hipLaunchKernelGGL((embed_grad_kernel<T, true>), grid, dim3(kThreads), 0, stream, s);
-        else hipLaunchKernelGGL((embed_grad_kernel<T, false>), grid, dim3(kThreads), 0, stream, s);
-        const int64_t tiles = ceil_div(p.width, kWave * 4);
-        if (s.chunks > 1) {
-            const dim3 join(at_most((int64_t)p.n * (s.chunks - 1) * tiles, kManyBlocks));
-            if (p.accumulate) hipLaunchKernelGGL((embed_grad_join_kernel<true>), join, dim3(kThreads), 0, stream, s, tiles);
-            else hipLaunchKernelGGL((embed_grad_join_kernel<false>), join, dim3(kThreads), 0, stream, s, tiles);
-        }
+        if (p.accumulate) hipLaunchKernelGGL((embed_grad_kernel<T, kAdd>), grid, dim3(kThreads), 0, stream, s);
+        else if (cleared) hipLaunchKernelGGL((embed_grad_kernel<T, kStore>), grid, dim3(kThreads), 0, stream, s);
+        else hipLaunchKernelGGL((embed_grad_kernel<T, kStoreAndFill>), grid, dim3(kThreads), 0, stream, s);
+        const int64_t tiles = ceil_div(p.width, kJoinColumns);
+        const dim3 join(at_most((int64_t)p.n * (s.chunks - 1) * tiles, kManyBlocks));
+        if (p.accumulate) hipLaunchKernelGGL((embed_grad_join_kernel<true>), join, dim3(kJoinThreads), 0, stream, s, tiles);
+        else hipLaunchKernelGGL((embed_grad_join_kernel<false>), join, dim3(kJoinThreads), 0, stream, s, tiles);
         return hipGetLastError();
     });
 }
