@@ -98,9 +98,9 @@ __device__ void preference_pair(const PairArgs &p, int64_t pair, double (*lds)[2
     }
 }
 
-// What the sums leave for the gradient: the rows' maxima, logarithms of their sums, coefficients.
+// What the sums leave for the gradient: the rows' RowStat and coefficients.
 struct RowSpace {
-    float *top, *ls, *coef;
+    float *m, *l, *coef;
 };
 
 // ---------------------------------------------------------------- the sums, and then the gradient
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void loss_forward_kernel(Logit
             TokenIn ti{};
             if (POLICY) ti = token_in(pol, r, in.rows);
             const float at_label = (float)x[label];
-            st = row_stat<T, WAVES>(x, cut_row(x, (int32_t)in.vocab), G::thread(), shared[turn]);
+            st = row_stat<T, WAVES>(x, cut_row(x, (int32_t)in.vocab), (int32_t)in.vocab, G::thread(), shared[turn]);
             turn ^= 1;
             logp = st.log_prob(at_label);
             if (POLICY) {
@@ -130,8 +130,8 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void loss_forward_kernel(Logit
         }
         if (G::thread() == 0) {
             logp_out[r] = logp;
-            out.top[r] = st.m;
-            out.ls[r] = st.ls;
+            out.m[r] = st.m;
+            out.l[r] = st.l;
             out.coef[r] = coef;
             if (POLICY) pol.token_loss[r] = t.loss;
         }
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(Team<1>::kBlock) void loss_grad_short_kernel(LogitR
         const int32_t label = label_of(in, r);
         const T *x = static_cast<const T *>(in.x) + r * in.stride;
         T *g = static_cast<T *>(out.ptr) + r * out.stride;
-        if (label >= 0) stream_grad<T, kWave>(x, g, cut_row(x, (int32_t)in.vocab), GradOf(RowStat{s.top[r], s.ls[r]}, s.coef[r], label), G::thread());
+        if (label >= 0) stream_grad<T, kWave>(x, g, cut_row(x, (int32_t)in.vocab), GradOf<T>(RowStat{s.m[r], s.l[r]}, s.coef[r], label), G::thread());
         else zero_row<T, kWave>(g, (int32_t)in.vocab, G::thread());
     }
 }
@@ -161,8 +161,11 @@ __global__ __launch_bounds__(kGradThreads) void loss_grad_kernel(LogitRows in, R
     for (int64_t w = blockIdx.x; w < in.rows * tiles; w += gridDim.x) {
         const int64_t r = w / tiles;
         const int32_t label = label_of(in, r);
-        grad_tile<T>(static_cast<const T *>(in.x) + r * in.stride, static_cast<T *>(out.ptr) + r * out.stride, (int32_t)in.vocab, label,
-                     label >= 0 ? s.coef[r] : 0.f, (int32_t)(w % tiles), [&](const Cut &) { return RowStat{s.top[r], s.ls[r]}; });
+        T *g = static_cast<T *>(out.ptr) + r * out.stride;
+        GradTile<T> t;
+        t.load(static_cast<const T *>(in.x) + r * in.stride, g, (int32_t)in.vocab, label >= 0, (int32_t)(w % tiles));
+        if (label >= 0) t.store(g, GradOf<T>(RowStat{s.m[r], s.l[r]}, s.coef[r], label));
+        else t.zero(g);
     }
 }
 
@@ -224,8 +227,10 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void poli
         const float edge = edge_at >= 0 ? (float)x[edge_at] : -INFINITY;
         const TokenIn ti = token_in(pol, r, in.rows);
         ExpSum e;
+        const int32_t wave_first = __builtin_amdgcn_readfirstlane(thread);
 #pragma unroll
         for (int i = 0; i < PIECES; i += K) {
+            if (wave_first >= c.pieces - i * TEAM && i > 0) break;
             float f[K * N];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -233,35 +238,41 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void poli
                 float(&one)[N] = reinterpret_cast<float(&)[N]>(f[k * N]);
                 unpack<T>(held[i + k], one);
             }
+            if (i == 0 && c.pieces > 0) e.start(f);
             e.add(f);
             asm volatile("" : "+v"(e.m), "+v"(e.s));               // here and now: one group unpacked at a time
             __builtin_amdgcn_sched_barrier(0);
         }
         if (edge_at >= 0) {
             const float f[1] = {edge};
+            if (c.pieces == 0) e.start(f);
             e.add(f);
         }
         asm volatile("" : "+v"(at_label));                         // has arrived, like all of the row, before any wavefront may write over it
-        const RowStat st = team_stat<WAVES>(e, shared[turn]);
+        const RowStat st = team_stat<T, WAVES>(e, x, vocab, thread, shared[turn]);
         turn ^= 1;
         const float logp = st.log_prob(at_label);
         const TokenLoss t = policy_token(pol, ti, logp);
         if (out.ptr) {
-            const GradOf d(st, t.slope * ti.weight, label);
-            char *to = reinterpret_cast<char *>(g + c.head);
+            const GradOf<T> d(st, t.slope * ti.weight, label);
+            if (d.way != GradOf<T>::kUsual) {
+                entrywise_grad<T, TEAM>(x, g, vocab, d, thread);   // all of the row has been read
+            } else {
+                char *to = reinterpret_cast<char *>(g + c.head);
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                if (thread < c.pieces - i * TEAM) {
-                    Raw raw = held[i];
-                    asm("" : "+v"(raw));                           // or the entries unpacked for the sum would be kept, twice the registers
-                    float f[N];
-                    unpack<T>(raw, f);
-                    d.piece((uint32_t)(label - c.head - i * TEAM * N - thread * N), f);
-                    store_piece(reinterpret_cast<T *>(to + (int64_t)i * TEAM * 16 + mine), f);
+                for (int i = 0; i < PIECES; ++i) {
+                    if (thread < c.pieces - i * TEAM) {
+                        Raw raw = held[i];
+                        asm("" : "+v"(raw));                       // or the entries unpacked for the sum would be kept, twice the registers
+                        float f[N];
+                        unpack<T>(raw, f);
+                        d.template piece_by<GradOf<T>::kUsual>((uint32_t)(label - c.head - i * TEAM * N - thread * N), f);
+                        store_piece(reinterpret_cast<T *>(to + (int64_t)i * TEAM * 16 + mine), f);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                if (edge_at >= 0) g[edge_at] = stored<T>(d.entry(edge_at, edge));
             }
-            if (edge_at >= 0) g[edge_at] = stored<T>(d.entry(edge_at, edge));
         }
         if (thread == 0) {
             pol.logp[r] = logp;

@@ -1,9 +1,17 @@
 // Rows of logits: what the kernels of token_rows.hip and losses.hip share.
 //
-//   lse = m + log sum_v exp(x_v - m), m = max_v x_v;   logp = x_label - lse;   d logp / d x_v = [v = label] - exp(x_v - lse)
+//   lse = log sum_v exp(x_v);   logp = x_label - lse;   d logp / d x_v = [v = label] - exp(x_v - lse)
 //
-// A team of wavefronts takes a row.  Every thread keeps the running maximum and sum of its own entries, (m, s) meaning s e^m, and the
-// team joins them once, so that lse costs one pass.  Rows start at any address: a row is taken as 16-byte pieces between a head and
+// in base 2: with z_v = x_v log2 e - M (one fused multiply-add, whole numbers M), l = log2 sum_v 2^z_v,
+//
+//   lse = (M + l) ln 2,   logp = (z_label - l) ln 2,   exp(x_v - lse) = 2^(z_v - l)
+//
+// for any M: log2 e rounded to fp32 means a softmax at another temperature by 10^-8, and everything else cancels.  M only has to keep the sum in fp32's range,
+// so a running maximum is not needed: every thread takes M from the first entries that it sees and adds up; fp32 holds 2^127 of them, an entry 88 above those
+// it started from.  A sum that leaves the range after all (or a NaN) shows in the joint sum, and the row is taken again with its maximum.  That
+// is four instructions an entry (unpack, multiply-add, exponential, add) instead of six, for rows whose sums are bound by instructions as much as by memory.
+//
+// A team of wavefronts takes a row and joins its threads' sums once, so that lse costs one pass.  Rows start at any address: a row is taken as 16-byte pieces between a head and
 // a tail of a few entries, which go one to a thread.
 #pragma once
 #include "device_utils.h"
@@ -12,8 +20,6 @@
 namespace ef21 {
 
 constexpr float kLowest = -3.402823466e38f;                        // fp32's lowest value
-
-__device__ __forceinline__ float exp2_of(float natural) { return __builtin_amdgcn_exp2f(natural * kLog2E); }
 
 // ---------------------------------------------------------------- sixteen bytes of a row
 typedef uint32_t Raw __attribute__((ext_vector_type(4)));
@@ -93,29 +99,46 @@ __device__ __forceinline__ Cut cut_row(const T *x, int32_t vocab) {
     return c;
 }
 
-// ---------------------------------------------------------------- the running maximum and sum
-// sum of exponentials s e^m.  m is never below fp32's lowest value, so that no difference of two infinities arises; s = 0 where there was nothing above -inf.
+// ---------------------------------------------------------------- sums of exponentials
+// s 2^m
 struct ExpSum {
-    float m = kLowest, s = 0.f;
+    float m = 0.f, s = 0.f;
+    // M from the thread's first entries.  Below kMasked they are masks rather than logits, and zero is as good a guess as any.
+    template <int N>
+    __device__ __forceinline__ void start(const float (&f)[N]) {
+        constexpr float kMasked = -5000.f;
+        float top = f[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) top = fmaxf(top, f[i]);
+        m = top > kMasked ? __builtin_rintf(top * kLog2E) : 0.f;
+    }
     template <int N>
     __device__ __forceinline__ void add(const float (&f)[N]) {
-        float top = m;
 #pragma unroll
-        for (int i = 0; i < N; ++i) top = fmaxf(top, f[i]);
-        s *= exp2_of(m - top);
-#pragma unroll
-        for (int i = 0; i < N; ++i) s += exp2_of(f[i] - top);
-        m = top;
+        for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(f[i], kLog2E, -m));
     }
 };
 
-// log sum exp of a row as m + ls.  The two are kept apart where the row is still at hand: where |m| is large their sum has lost ls.
-// ls = -inf: no entry above -inf.
+// log2 sum exp of a row.  Two kinds of rows: with z = x log2 e - 2 m the sum is 2 m + l; where the numbers are so large that this product's rounding is
+// no longer small (or that it is infinite: a row of the lowest number everywhere), z = (x - m) log2 e, and it is m log2 e + l.  Which one it is shows in
+// m: half of a whole number below 2^22, or a maximum of 2.9e6 and more.  l = -inf: no entry above -inf.
+constexpr float kMostM = 4194304.f, kLargeTop = 2.9e6f;
 struct RowStat {
-    float m, ls;
-    __device__ bool empty() const { return ls == -INFINITY; }
-    __device__ float lse() const { return empty() ? -INFINITY : m + ls; }
-    __device__ float log_prob(float x) const { return empty() ? -INFINITY : (x - m) - ls; }
+    float m, l;
+    __device__ bool empty() const { return l == -INFINITY; }
+    __device__ bool large() const { return fabsf(m) >= kMostM / 2.f; }
+    __device__ float z(float x) const { return large() ? (x - m) * kLog2E : fmaf(x, kLog2E, -2.f * m); }
+    __device__ float lse() const {
+        constexpr double kLn2 = 0.69314718055994530942;
+        return empty() ? -INFINITY : large() ? (float)((double)m + kLn2 * (double)l) : (float)((2.0 * (double)m + (double)l) * kLn2);
+    }
+    __device__ float log_prob(float x) const { return empty() ? -INFINITY : (z(x) - l) * 0.693147181f; }
+    // of a row whose lse is known, |lse| < 10^6
+    static __device__ RowStat of(float lse) {
+        const double both = (double)lse * 1.44269504088896340736;
+        const float m = (float)both;
+        return {0.5f * m, (float)(both - (double)m)};
+    }
 };
 
 // The largest value of each group of 16 or 64 lanes, in every lane of the group (group_sum with another operation).
@@ -140,40 +163,63 @@ struct TeamShared {
     float m[WAVES], s[WAVES], label;
 };
 
-// A wavefront's joint sum, the same in every lane.
+// A wavefront's joint sum, the same in every lane.  A thread without a sum has no say in what M is.
 __device__ __forceinline__ ExpSum join_wave(ExpSum e) {
     ExpSum w;
+    if (e.s == 0.f) e.m = kLowest;
     w.m = group_max<64>(e.m);
-    w.s = group_sum<64>(e.s * exp2_of(e.m - w.m));
+    w.s = group_sum<64>(e.s * __builtin_amdgcn_exp2f(e.m - w.m));
     return w;
 }
 
 // ---------------------------------------------------------------- gradient of a row
+template <class T>
 struct GradOf {
-    float m, shift, minus_coef;                                    // entry: minus_coef 2^((x - m) log2 e + shift)
+    // kOne: 2^(x log2 e - (2 m + l)), where that sum's rounding is far below the type's (but not for the label, where 1 - p may cancel); kTwo: 2^(z - l); kLarge: z of such a row; kZero: nothing to give
+    enum Way { kOne, kTwo, kLarge, kZero };
+    static constexpr Way kUsual = sizeof(T) == 2 ? kOne : kTwo;
+    Way way;
+    float m, l, both, coef;                                        // m: what z subtracts; both: m + l
     int32_t label;
-    float label_coef;
-    bool zero;
-    __device__ GradOf(RowStat st, float coef, int32_t label_)
-        : m(st.m), shift(-st.ls * kLog2E), minus_coef(-coef), label(label_), label_coef(coef), zero(st.empty()) {}
-    __device__ __forceinline__ float prob(float x) const { return __builtin_amdgcn_exp2f(fmaf(x - m, kLog2E, shift)); }
-    __device__ __forceinline__ float at_label(float x) const { return zero ? 0.f : label_coef * (1.f - prob(x)); }
-    __device__ __forceinline__ float entry(int32_t v, float x) const { return v == label ? at_label(x) : zero ? 0.f : minus_coef * prob(x); }
-    // A piece in which the label is entry `at`, if at < N.
-    template <int N>
-    __device__ __forceinline__ void piece(uint32_t at, float (&f)[N]) const {
+    __device__ GradOf(RowStat st, float coef_, int32_t label_) : m(st.m), l(st.l), coef(coef_), label(label_) {
+        way = st.empty() ? kZero : st.large() ? kLarge : sizeof(T) == 2 && fabsf(st.m) <= 2048.f ? kOne : kTwo;
+        if (way != kLarge) m *= 2.f;
+        both = m + l;
+    }
+    template <Way WAY>
+    __device__ __forceinline__ float prob(float x) const {
+        if constexpr (WAY == kOne) return __builtin_amdgcn_exp2f(fmaf(x, kLog2E, -both));
+        else if constexpr (WAY == kTwo) return __builtin_amdgcn_exp2f(fmaf(x, kLog2E, -m) - l);
+        else if constexpr (WAY == kLarge) return __builtin_amdgcn_exp2f((x - m) * kLog2E - l);
+        else return 0.f;
+    }
+    template <Way WAY, int N>
+    __device__ __forceinline__ void piece_by(uint32_t at, float (&f)[N]) const {
         float hot = 0.f;
         if (at < (uint32_t)N) {
 #pragma unroll
             for (int i = 0; i < N; ++i) hot = (int)at == i ? f[i] : hot;
-            hot = at_label(hot);
+            hot = WAY == kZero ? 0.f : coef * (1.f - prob<(WAY == kOne ? kTwo : WAY)>(hot));
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = zero ? 0.f : minus_coef * prob(f[i]);
+        for (int i = 0; i < N; ++i) f[i] = WAY == kZero ? 0.f : -coef * prob<WAY>(f[i]);
         if (at < (uint32_t)N) {
 #pragma unroll
             for (int i = 0; i < N; ++i) f[i] = (int)at == i ? hot : f[i];
         }
+    }
+    // A piece in which the label is entry `at`, if at < N.
+    template <int N>
+    __device__ __forceinline__ void piece(uint32_t at, float (&f)[N]) const {
+        if (sizeof(T) == 2 && way == kOne) piece_by<kOne>(at, f);
+        else if (way == kTwo) piece_by<kTwo>(at, f);
+        else if (way == kLarge) piece_by<kLarge>(at, f);
+        else piece_by<kZero>(at, f);
+    }
+    __device__ __forceinline__ float entry(int32_t v, float x) const {
+        float f[1] = {x};
+        piece((uint32_t)(label - v), f);
+        return f[0];
     }
 };
 
@@ -195,6 +241,7 @@ __device__ ExpSum stream_sum(const T *x, const Cut &c, int32_t thread) {
     ExpSum e;
     const char *from = reinterpret_cast<const char *>(x + c.head);
     const uint32_t mine = (uint32_t)thread * 16u;
+    const int32_t wave_first = __builtin_amdgcn_readfirstlane(thread);
     for (int32_t base = 0; base < c.pieces; base += U * K * TEAM, from += (int64_t)U * K * TEAM * 16) {
         Raw r[U * K];
         if (base + U * K * TEAM <= c.pieces) {
@@ -209,22 +256,24 @@ __device__ ExpSum stream_sum(const T *x, const Cut &c, int32_t thread) {
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (wave_first >= c.pieces - base - u * K * TEAM) break;   // none of the wavefront's threads has more
             float f[K * N];
 #pragma unroll
             for (int k = 0; k < K; ++k) unpack<T>(r[u * K + k], reinterpret_cast<float(&)[N]>(f[k * N]));
+            if (u == 0 && base == 0) e.start(f);
             e.add(f);
         }
     }
     if (thread < c.edges()) {
         const float f[1] = {(float)x[c.edge<T>(thread)]};
+        if (c.pieces == 0) e.start(f);
         e.add(f);
     }
     return e;
 }
 
-// The team's joint stat of its threads' sums, the same bits in every thread.
 template <int WAVES>
-__device__ __forceinline__ RowStat team_stat(ExpSum e, TeamShared<WAVES> &sh) {
+__device__ __forceinline__ ExpSum join_team(ExpSum e, TeamShared<WAVES> &sh) {
     e = join_wave(e);
     if constexpr (WAVES > 1) {
         if (lane_id() == 0) {
@@ -235,17 +284,55 @@ __device__ __forceinline__ RowStat team_stat(ExpSum e, TeamShared<WAVES> &sh) {
         const int w = (int)threadIdx.x & (WAVES - 1);
         const float mw = sh.m[w];
         e.m = group_max<16>(mw);
-        e.s = group_sum<16>(sh.s[w] * exp2_of(mw - e.m)) * ((float)WAVES / 16.f);
+        e.s = group_sum<16>(sh.s[w] * __builtin_amdgcn_exp2f(mw - e.m)) * ((float)WAVES / 16.f);
     }
-    return e.s == 0.f ? RowStat{0.f, -INFINITY} : RowStat{e.m, logf(e.s)};
+    return e;
+}
+
+// The row again, its maximum first.  By the whole team; all of the row has been read when a thread returns.
+template <class T, int WAVES>
+__device__ __forceinline__ RowStat careful_stat(const T *x, int32_t vocab, int32_t thread, TeamShared<WAVES> &sh) {
+    constexpr int TEAM = WAVES * kWave;
+    float top = -INFINITY;
+#pragma unroll 1
+    for (int32_t v = thread; v < vocab; v += TEAM) top = fmaxf(top, (float)x[v]);
+    top = group_max<64>(top);
+    if constexpr (WAVES > 1) {
+        __syncthreads();                                           // the sums in sh have been read
+        if (lane_id() == 0) sh.m[wave_id()] = top;
+        __syncthreads();
+        top = group_max<16>(sh.m[(int)threadIdx.x & (WAVES - 1)]);
+        __syncthreads();
+    }
+    RowStat st{fabsf(top) >= kLargeTop ? top : 0.5f * __builtin_rintf(top * kLog2E), 0.f};
+    if (top == -INFINITY) st.m = 0.f;
+    ExpSum e;
+#pragma unroll 1
+    for (int32_t v = thread; v < vocab; v += TEAM) e.s += __builtin_amdgcn_exp2f(st.z((float)x[v]));
+    float s = group_sum<64>(e.s);
+    if constexpr (WAVES > 1) {
+        if (lane_id() == 0) sh.s[wave_id()] = s;
+        __syncthreads();
+        s = group_sum<16>(sh.s[(int)threadIdx.x & (WAVES - 1)]) * ((float)WAVES / 16.f);
+    }
+    st.l = s == 0.f ? -INFINITY : log2f(s);
+    return st;
+}
+
+// The team's joint stat of its threads' sums of row x, the same bits in every thread.
+template <class T, int WAVES>
+__device__ __forceinline__ RowStat team_stat(ExpSum e, const T *x, int32_t vocab, int32_t thread, TeamShared<WAVES> &sh) {
+    e = join_team<WAVES>(e, sh);
+    if (e.s > 0.f && e.s < INFINITY && fabsf(e.m) < kMostM) return {0.5f * e.m, log2f(e.s)};
+    return careful_stat<T, WAVES>(x, vocab, thread, sh);
 }
 template <class T, int WAVES>
-__device__ __forceinline__ RowStat row_stat(const T *x, const Cut &c, int32_t thread, TeamShared<WAVES> &sh) {
-    return team_stat<WAVES>(stream_sum<T, WAVES * kWave>(x, c, thread), sh);
+__device__ __forceinline__ RowStat row_stat(const T *x, const Cut &c, int32_t vocab, int32_t thread, TeamShared<WAVES> &sh) {
+    return team_stat<T, WAVES>(stream_sum<T, WAVES * kWave>(x, c, thread), x, vocab, thread, sh);
 }
 
 template <class T, int TEAM>
-__device__ void stream_grad(const T *x, T *g, const Cut &c, const GradOf &d, int32_t thread) {
+__device__ void stream_grad(const T *x, T *g, const Cut &c, const GradOf<T> &d, int32_t thread) {
     constexpr int N = Piece<T>::N, U = 4;
     int32_t i = thread;
     for (; i + (U - 1) * TEAM < c.pieces; i += U * TEAM) {
@@ -272,6 +359,13 @@ __device__ void stream_grad(const T *x, T *g, const Cut &c, const GradOf &d, int
         const int32_t v = c.edge<T>(thread);
         g[v] = stored<T>(d.entry(v, (float)x[v]));
     }
+}
+
+// The gradient of an unusual row, entry by entry: few registers, beside code that needs them.
+template <class T, int TEAM>
+__device__ __forceinline__ void entrywise_grad(const T *x, T *g, int32_t vocab, const GradOf<T> &d, int32_t thread) {
+#pragma unroll 1
+    for (int32_t v = thread; v < vocab; v += TEAM) g[v] = stored<T>(d.entry(v, (float)x[v]));
 }
 
 // ---------------------------------------------------------------- teams
@@ -316,40 +410,48 @@ constexpr int kGradThreads = 256, kGradFlight = 2, kGradPieces = kGradThreads * 
 template <class T>
 inline int32_t grad_tiles(int64_t vocab) { return (int32_t)((vocab / Piece<T>::N + kGradPieces - 1) / kGradPieces); }
 
-// stat_at(x, cut) gives the row's stat, once the tile's loads are under way.
-template <class T, class F>
-__device__ __forceinline__ void grad_tile(const T *x, T *g, int32_t vocab, int32_t label, float coef, int32_t tile, F stat_at) {
-    constexpr int N = Piece<T>::N;
-    const int32_t thread = (int32_t)threadIdx.x, first = tile * kGradPieces + thread;
-    const Cut c = cut_row(label >= 0 ? x : g, vocab);
-    const bool at_edge = tile == 0 && thread < c.edges();
-    if (label >= 0) {
-        Raw raw[kGradFlight];
-        float edge = 0.f;
+template <class T>
+struct GradTile {
+    static constexpr int N = Piece<T>::N;
+    Raw raw[kGradFlight];
+    float edge;
+    int32_t thread, first;
+    Cut c;
+    bool at_edge;
+    // labelled: x is read, into raw; else it is g's pieces that will be written
+    __device__ __forceinline__ void load(const T *x, const T *g, int32_t vocab, bool labelled, int32_t tile) {
+        thread = (int32_t)threadIdx.x;
+        first = tile * kGradPieces + thread;
+        c = cut_row(labelled ? x : g, vocab);
+        at_edge = tile == 0 && thread < c.edges();
+        edge = 0.f;
+        if (!labelled) return;
 #pragma unroll
         for (int u = 0; u < kGradFlight; ++u)
             if (first + u * kGradThreads < c.pieces) raw[u] = load_piece(x + c.head + (first + u * kGradThreads) * N);
         if (at_edge) edge = (float)x[c.edge<T>(thread)];
-        const GradOf d(stat_at(c), coef, label);
+    }
+    __device__ __forceinline__ void store(T *g, const GradOf<T> &d) const {
 #pragma unroll
         for (int u = 0; u < kGradFlight; ++u) {
             if (first + u * kGradThreads < c.pieces) {
                 const int32_t v = c.head + (first + u * kGradThreads) * N;
                 float f[N];
                 unpack<T>(raw[u], f);
-                d.piece((uint32_t)(label - v), f);
+                d.piece((uint32_t)(d.label - v), f);
                 store_piece(g + v, f);
             }
         }
         if (at_edge) g[c.edge<T>(thread)] = stored<T>(d.entry(c.edge<T>(thread), edge));
-    } else {
-        float none[N] = {};
+    }
+    __device__ __forceinline__ void zero(T *g) const {
+        const float none[N] = {};
 #pragma unroll
         for (int u = 0; u < kGradFlight; ++u)
             if (first + u * kGradThreads < c.pieces) store_piece(g + c.head + (first + u * kGradThreads) * N, none);
         if (at_edge) g[c.edge<T>(thread)] = (T)0.f;
     }
-}
+};
 
 inline unsigned grid_of(int64_t items, int64_t per_block, int64_t most) {
     const int64_t blocks = (items + per_block - 1) / per_block;

@@ -354,3 +354,47 @@ def test_another_stream_and_a_graph(gpu):
         l2, t, p2, g2 = b.ef21_policy_loss(x, dl, ref, adv, 0.2, 0.2, ref_logp=ref, kl=0.1)
         for k, v in dict(l1=l1, l2=l2, t=t, p1=p1, p2=p2, g1=g1, g2=g2).items():
             assert torch.equal(got[k], v), f"replay {seed}: {k} differs"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [70, 1500, 9001, 40000, 70001, 200000])
+def test_rows_of_every_size_and_spread(gpu, vocab, dtype):
+    """Rows far from zero, rows whose entries lie hundreds apart, rows that begin with masks: sums that leave fp32's range unless they are
+    taken relative to the row's maximum."""
+    torch, b = gpu
+    print(f"spread vocab={vocab} {dtype}", flush=True)
+    rng = np.random.default_rng(vocab)
+    base = rng.standard_normal(vocab)
+    half = np.arange(vocab) < vocab // 2
+    kinds = [40 * base, 300 * base, 1000 + base, -300 + 2 * base, -6000 + base, 20000 + 40 * base, np.where(half, -10000.0, base), np.where(half, -30000.0, 3 * base),
+             np.where(half, base, 900 + base), np.where(half[::-1], -60000.0, -100 + base), np.where(np.arange(vocab) == vocab - 2, 500.0, base)]
+    if dtype != "f16":
+        kinds += [1e6 + 100 * base, -2.8e6 + 1e4 * base, 3.5e6 + 1e5 * base, -5e6 + base, 1e9 * base, 1e20 * base, -1e30 + 0 * base, 1e37 * base, -2.5e38 + 0 * base]
+    x = torch.from_numpy(np.stack(kinds)).to(lm.TORCH[dtype]).cuda()
+    x64 = as64(x)
+    rows = len(kinds)
+    labels = rng.integers(0, vocab, rows)
+    labels[::3] = np.argmax(x64, axis=1)[::3]
+    dl = torch.from_numpy(labels).cuda()
+    R = lm.Rows(x64, labels)
+    logp, lse = b.ef21_token_logps(x, dl)
+    lm.inside(as64(lse), R.lse, R.d_lse, "lse")
+    lm.inside(as64(logp), R.logp, R.d_logp, "logp")
+    one = torch.ones(rows, device="cuda")
+    g, bound = R.grad(np.ones(rows), np.zeros(rows), dtype)
+    lm.inside(as64(b.ef21_token_logps_grad(x, dl, lse, one)), g, bound, "gradient")
+    # one sequence a row, empty ones beside them: the gradient of row r is -w_r times that of logp
+    start = torch.arange(rows + 1, device="cuda").repeat_interleave(2)[1:]
+    ref = logp.clone()
+    _, logp2, grad2 = b.ef21_preference_loss(x, dl, start, ref, 1.0, pair_weight=one * 2)
+    assert torch.equal(logp2, logp)
+    ratio = np.where(np.isfinite(as64(logp)), 1.0, np.nan)
+    keep = np.isfinite(ratio)
+    # beta 1, margin 0: the slope of the loss is -1/2, twice that -1; its own error is the margin's over 4
+    lm.inside(as64(grad2)[keep], -g[keep], bound[keep] + (np.abs(R.grad(np.ones(rows), np.ones(rows), "f32")[0]) * 1e-7)[keep], "preference gradient")
+    total, tokens, logp3, grad3 = b.ef21_policy_loss(x, dl, logp, one, 0.2, 0.2, weight=one)
+    assert torch.equal(logp3, logp)
+    lm.inside(as64(grad3)[keep], -g[keep], bound[keep] + (np.abs(g) * 1e-7)[keep], "policy gradient")
+    over = x.clone()
+    b.ef21_token_logps_grad(over, dl, lse, one, out=over)
+    lm.inside(as64(over), g, bound, "gradient over the logits")
