@@ -7,6 +7,7 @@ failing call raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -155,50 +156,70 @@ def ef21_hbm_copy(dst: torch.Tensor, src: torch.Tensor) -> None:
 
 
 # -- the two ends of a language model (stateless, on torch's current stream; see include/ef21.h)
-def _matrix(t: torch.Tensor, what: str, types=VALUE_TYPES):
-    """(address, type, rows, width, stride) of a matrix whose rows are contiguous."""
+# A call on a few tokens takes as long as its checks here, so they touch every tensor few times.
+_F32 = torch.float32
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _gpu(t, what: str) -> None:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what}: expected a tensor in GPU memory")
-    kind = types.get(t.dtype)
+
+
+def _matrix(t: torch.Tensor, what: str):
+    """(address, type, rows, width, stride) of a matrix whose rows are contiguous."""
+    _gpu(t, what)
+    kind = VALUE_TYPES.get(t.dtype)
     if kind is None:
         raise TypeError(f"{what}: unsupported type {t.dtype}")
-    if t.dim() != 2:
-        raise ValueError(f"{what}: expected two dimensions, got {tuple(t.shape)}")
-    rows, width = t.shape
-    if width > 1 and rows > 0 and t.stride(1) != 1:
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{what}: expected two dimensions, got {tuple(shape)}")
+    rows, width = shape
+    step, unit = t.stride()
+    if unit != 1 and width > 1 and rows > 0:
         raise TypeError(f"{what}: rows must be contiguous")
-    return t.data_ptr(), kind, rows, width, t.stride(0) if rows > 1 else width
+    return t.data_ptr(), kind, rows, width, step if rows > 1 else width
 
 
 def _token_list(t: torch.Tensor, what: str):
     """(address, type) of contiguous tokens or labels."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{what}: expected a tensor in GPU memory")
-    if t.dtype not in TOKEN_TYPES or not t.is_contiguous():
+    _gpu(t, what)
+    kind = TOKEN_TYPES.get(t.dtype)
+    if kind is None or not t.is_contiguous():
         raise TypeError(f"{what}: expected contiguous int32 or int64, got {t.dtype} (contiguous={t.is_contiguous()})")
-    return t.data_ptr(), TOKEN_TYPES[t.dtype]
+    return t.data_ptr(), kind
 
 
-def _vector(t, length: int, device, dtype=torch.float32):
-    """`t`, checked, or a new vector."""
-    if t is None:
-        return torch.empty(length, dtype=dtype, device=device)
-    _dev(t, dtype, (length,))
-    return t
+def _vector(t, length: int, what: str, dtype=_F32) -> int:
+    """Address of a contiguous vector."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == (length,) and t.is_contiguous():
+        return t.data_ptr()
+    _gpu(t, what)
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise TypeError(f"{what}: expected contiguous {dtype}, got {t.dtype} (contiguous={t.is_contiguous()})")
+    raise ValueError(f"{what}: expected shape ({length},), got {tuple(t.shape)}")
 
 
-def _same_device(*tensors) -> None:
-    first = tensors[0].device
-    if any(t is not None and t.device != first for t in tensors):
-        raise ValueError("all tensors must be on one device")
-    if first.index is not None and torch.cuda.current_device() != first.index:
-        raise ValueError(f"the tensors are on {first}, which is not the current device")
+def _optional(t, length: int, what: str):
+    return None if t is None else _vector(t, length, what)
 
 
-def _workspace(t, need: int, device):
-    if t is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
-    return t
+def _stream_of(*tensors) -> int:
+    """The current stream of the device that all tensors are on, which must be the current one."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("all tensors must be on one device")
+    if _raw_device() != device:
+        raise ValueError(f"the tensors are on device {device}, which is not the current one")
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _size(call, *sizes) -> int:
+    size = C.c_int64()
+    _check(call(*sizes, C.byref(size)))
+    return size.value
 
 
 def ef21_embed(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None,
@@ -210,20 +231,17 @@ def ef21_embed(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, ou
     ids, id_type = _token_list(tokens, "tokens")
     if out is None:
         out = torch.empty(*tokens.shape, width, dtype=dtype or table.dtype, device=table.device)
-    flat = out if out.dim() == 2 else out.view(-1, width)
-    to, out_type, rows, cols, out_stride = _matrix(flat, "out")
-    if (rows, cols) != (tokens.numel(), width):
+    to, out_type, rows, cols, out_stride = _matrix(out if out.dim() == 2 else out.view(-1, width), "out")
+    if cols != width or rows != tokens.numel():
         raise ValueError(f"out must have {tokens.numel()} rows of {width} entries")
-    _same_device(table, tokens, out)
-    _check(lib.ef21_embed(at, kind, vocab, width, stride, ids, id_type, rows, scale, to, out_type, out_stride, _current_stream_ptr()))
+    _check(lib.ef21_embed(at, kind, vocab, width, stride, ids, id_type, rows, scale, to, out_type, out_stride, _stream_of(table, tokens, out)))
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def ef21_embed_grad_workspace(n: int, count: int, vocab: int, width: int) -> int:
     """Bytes of workspace that ef21_embed_grad needs."""
-    size = C.c_int64()
-    _check(load_library().ef21_embed_grad_workspace(n, count, vocab, width, C.byref(size)))
-    return size.value
+    return _size(load_library().ef21_embed_grad_workspace, n, count, vocab, width)
 
 
 def ef21_embed_grad(grad_out: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float = 1.0, out: torch.Tensor | None = None,
@@ -231,36 +249,42 @@ def ef21_embed_grad(grad_out: torch.Tensor, tokens: torch.Tensor, vocab: int, sc
     """Gradients of the table (ef21_embed_grad): grad_out [n][count][width], tokens [n][count]; returns fp32 [n][vocab][width]
     (`out`, whose workers may lie further apart, for example a block of columns of the rows that EF21.step takes)."""
     lib = load_library()
-    if grad_out.dim() != 3 or tuple(grad_out.shape[:2]) != tuple(tokens.shape):
+    _gpu(grad_out, "grad_out")
+    shape = grad_out.shape
+    if len(shape) != 3 or tokens.shape != shape[:2]:
         raise ValueError("grad_out must be [n][count][width] and tokens [n][count]")
-    n, count, width = grad_out.shape
+    n, count, width = shape
+    kind = VALUE_TYPES.get(grad_out.dtype)
+    if kind is None:
+        raise TypeError(f"grad_out: unsupported type {grad_out.dtype}")
     ids, id_type = _token_list(tokens, "tokens")
     # the workers' rows as one matrix
-    if not grad_out.is_cuda or grad_out.dtype not in VALUE_TYPES:
-        raise TypeError(f"grad_out: expected float32, bfloat16 or float16 in GPU memory, got {grad_out.dtype}")
-    stride = grad_out.stride(1) if count > 1 else grad_out.stride(0) if n > 1 else width
+    across, down, unit = grad_out.stride()
+    stride = down if count > 1 else across if n > 1 else width
     if n * count == 0:
         stride = width
-    elif (width > 1 and grad_out.stride(2) != 1) or (n > 1 and grad_out.stride(0) != count * stride):
+    elif (unit != 1 and width > 1) or (n > 1 and across != count * stride):
         raise TypeError("grad_out: entries of a row must be contiguous and the workers' rows follow one another at one stride")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the gradient to add to")
-        out = torch.empty(n, vocab, width, dtype=torch.float32, device=grad_out.device)
-    if out.dtype != torch.float32 or not out.is_cuda or tuple(out.shape) != (n, vocab, width) or not out[0].is_contiguous():
-        raise TypeError(f"out must be float32 [{n}][{vocab}][{width}] in GPU memory, each worker's table contiguous")
-    need = ef21_embed_grad_workspace(n, count, vocab, width)
-    workspace = _workspace(workspace, need, grad_out.device)
-    _same_device(grad_out, tokens, out, workspace)
-    _check(lib.ef21_embed_grad(grad_out.data_ptr(), VALUE_TYPES[grad_out.dtype], stride, ids, id_type, n, count, vocab, width, scale, out.data_ptr(), out.stride(0), int(accumulate),
-                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _current_stream_ptr()))
+        out = torch.empty(n, vocab, width, dtype=_F32, device=grad_out.device)
+    if out.dtype is not _F32 or not out.is_cuda or out.shape != (n, vocab, width):
+        raise TypeError(f"out must be float32 [{n}][{vocab}][{width}] in GPU memory")
+    apart, row, one = out.stride()
+    if (row != width and vocab > 1) or (one != 1 and width > 1):
+        raise TypeError("out: each worker's table must be contiguous")
+    if workspace is None:
+        workspace = torch.empty(ef21_embed_grad_workspace(n, count, vocab, width), dtype=torch.uint8, device=grad_out.device)
+    _check(lib.ef21_embed_grad(grad_out.data_ptr(), kind, stride, ids, id_type, n, count, vocab, width, scale, out.data_ptr(), apart, int(accumulate),
+                               workspace.data_ptr(), workspace.nbytes, _stream_of(grad_out, tokens, out, workspace)))
     return out
 
 
 def _logit_rows(logits, labels):
     at, kind, rows, vocab, stride = _matrix(logits, "logits")
     ids, id_type = _token_list(labels, "labels")
-    if tuple(labels.shape) != (rows,):
+    if labels.shape != (rows,):
         raise ValueError(f"labels must be [{rows}]")
     return (at, kind, rows, vocab, stride, ids, id_type), rows
 
@@ -272,18 +296,21 @@ def _logit_grad(grad, logits):
     if grad is True:
         grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     at, _, _, _, stride = _matrix(grad, "grad")
-    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+    if grad.dtype is not logits.dtype or grad.shape != logits.shape:
         raise ValueError("grad must have the logits' type and shape")
     return grad, at, stride
+
+
+def _new(t, length: int, like):
+    return torch.empty(length, dtype=_F32, device=like.device) if t is None else t
 
 
 def ef21_token_logps(logits: torch.Tensor, labels: torch.Tensor, logp: torch.Tensor | None = None, lse: torch.Tensor | None = None):
     """(logp [rows], lse [rows]) of the labels under the softmax of each row of logits [rows][vocab] (ef21_token_logps)."""
     lib = load_library()
     args, rows = _logit_rows(logits, labels)
-    logp, lse = _vector(logp, rows, logits.device), _vector(lse, rows, logits.device)
-    _same_device(logits, labels, logp, lse)
-    _check(lib.ef21_token_logps(*args, logp.data_ptr(), lse.data_ptr(), _current_stream_ptr()))
+    logp, lse = _new(logp, rows, logits), _new(lse, rows, logits)
+    _check(lib.ef21_token_logps(*args, _vector(logp, rows, "logp"), _vector(lse, rows, "lse"), _stream_of(logits, labels, logp, lse)))
     return logp, lse
 
 
@@ -293,17 +320,15 @@ def ef21_token_logps_grad(logits: torch.Tensor, labels: torch.Tensor, lse: torch
     lib = load_library()
     args, rows = _logit_rows(logits, labels)
     out, to, stride = _logit_grad(True if out is None else out, logits)
-    _same_device(logits, labels, lse, grad_logp, out)
-    _check(lib.ef21_token_logps_grad(*args, _dev(lse, torch.float32, (rows,)), _dev(grad_logp, torch.float32, (rows,)), to, stride,
-                                     _current_stream_ptr()))
+    _check(lib.ef21_token_logps_grad(*args, _vector(lse, rows, "lse"), _vector(grad_logp, rows, "grad_logp"), to, stride,
+                                     _stream_of(logits, labels, lse, grad_logp, out)))
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def ef21_preference_loss_workspace(rows: int, pairs: int) -> int:
     """Bytes of workspace that ef21_preference_loss needs."""
-    size = C.c_int64()
-    _check(load_library().ef21_preference_loss_workspace(rows, pairs, C.byref(size)))
-    return size.value
+    return _size(load_library().ef21_preference_loss_workspace, rows, pairs)
 
 
 def ef21_preference_loss(logits: torch.Tensor, labels: torch.Tensor, seq_start: torch.Tensor, ref_logp: torch.Tensor, beta: float,
@@ -314,25 +339,25 @@ def ef21_preference_loss(logits: torch.Tensor, labels: torch.Tensor, seq_start: 
     device.  grad: a tensor to write (the logits themselves if they are not needed again), True for a new one, False for none."""
     lib = load_library()
     args, rows = _logit_rows(logits, labels)
-    starts = _dev(seq_start, torch.int64)
     pairs = (seq_start.numel() - 1) // 2
-    if seq_start.dim() != 1 or seq_start.numel() != 2 * pairs + 1 or pairs < 1:
+    if pairs < 1:
         raise ValueError("seq_start must be [2 pairs + 1]")
-    out_loss, logp = _vector(out_loss, pairs, logits.device), _vector(logp, rows, logits.device)
+    starts = _vector(seq_start, 2 * pairs + 1, "seq_start", torch.int64)
+    out_loss, logp = _new(out_loss, pairs, logits), _new(logp, rows, logits)
     grad, to, stride = _logit_grad(grad, logits)
-    workspace = _workspace(workspace, ef21_preference_loss_workspace(rows, pairs), logits.device)
-    _same_device(logits, labels, seq_start, ref_logp, pair_weight, out_loss, logp, grad, workspace)
-    _check(lib.ef21_preference_loss(*args, starts, pairs, _dev(ref_logp, torch.float32, (rows,)), beta, smoothing, int(loss), int(mean),
-                                    _opt(pair_weight, torch.float32, (pairs,)), out_loss.data_ptr(), logp.data_ptr(), to, stride,
-                                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), _current_stream_ptr()))
+    if workspace is None:
+        workspace = torch.empty(ef21_preference_loss_workspace(rows, pairs), dtype=torch.uint8, device=logits.device)
+    _check(lib.ef21_preference_loss(*args, starts, pairs, _vector(ref_logp, rows, "ref_logp"), beta, smoothing, int(loss), int(mean),
+                                    _optional(pair_weight, pairs, "pair_weight"), _vector(out_loss, pairs, "out_loss"), _vector(logp, rows, "logp"), to,
+                                    stride, workspace.data_ptr(), workspace.nbytes,
+                                    _stream_of(logits, labels, seq_start, ref_logp, pair_weight, out_loss, logp, grad, workspace)))
     return out_loss, logp, grad
 
 
+@functools.lru_cache(maxsize=256)
 def ef21_policy_loss_workspace(rows: int) -> int:
     """Bytes of workspace that ef21_policy_loss needs."""
-    size = C.c_int64()
-    _check(load_library().ef21_policy_loss_workspace(rows, C.byref(size)))
-    return size.value
+    return _size(load_library().ef21_policy_loss_workspace, rows)
 
 
 def ef21_policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, clip_low: float,
@@ -343,16 +368,15 @@ def ef21_policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch
     ef21_preference_loss."""
     lib = load_library()
     args, rows = _logit_rows(logits, labels)
-    f32, shape = torch.float32, (rows,)
-    out_loss = _vector(out_loss, 1, logits.device)
-    token_loss, logp = _vector(token_loss, rows, logits.device), _vector(logp, rows, logits.device)
+    out_loss, token_loss, logp = _new(out_loss, 1, logits), _new(token_loss, rows, logits), _new(logp, rows, logits)
     grad, to, stride = _logit_grad(grad, logits)
-    workspace = _workspace(workspace, ef21_policy_loss_workspace(rows), logits.device)
-    _same_device(logits, labels, old_logp, advantages, ref_logp, weight, out_loss, token_loss, logp, grad, workspace)
-    _check(lib.ef21_policy_loss(*args, _dev(old_logp, f32, shape), _dev(advantages, f32, shape), _opt(ref_logp, f32, shape),
-                                _opt(weight, f32, shape), clip_low, clip_high, kl, out_loss.data_ptr(), token_loss.data_ptr(),
-                                logp.data_ptr(), to, stride, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                _current_stream_ptr()))
+    if workspace is None:
+        workspace = torch.empty(ef21_policy_loss_workspace(rows), dtype=torch.uint8, device=logits.device)
+    _check(lib.ef21_policy_loss(*args, _vector(old_logp, rows, "old_logp"), _vector(advantages, rows, "advantages"),
+                                _optional(ref_logp, rows, "ref_logp"), _optional(weight, rows, "weight"), clip_low, clip_high, kl,
+                                _vector(out_loss, 1, "out_loss"), _vector(token_loss, rows, "token_loss"), _vector(logp, rows, "logp"), to, stride,
+                                workspace.data_ptr(), workspace.nbytes,
+                                _stream_of(logits, labels, old_logp, advantages, ref_logp, weight, out_loss, token_loss, logp, grad, workspace)))
     return out_loss, token_loss, logp, grad
 
 
