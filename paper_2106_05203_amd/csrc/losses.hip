@@ -13,8 +13,6 @@
 namespace ef21 {
 namespace {
 
-constexpr int kThreads = 256;
-
 // ---------------------------------------------------------------- the losses, from log-probabilities
 // Loss of one token and its derivative in logp.
 struct TokenLoss {
@@ -39,48 +37,59 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyArgs &p, const Tok
     return t;
 }
 
-// Sums of (a, b) over the workgroup, the same bits in every thread.
-__device__ void block_sum2(double &a, double &b, double (*lds)[2]) {
+// Sums of V[] over the workgroup, the same bits in every thread.
+constexpr int kPairThreads = 1024;
+template <int N>
+__device__ void block_sums(double (&v)[N], double (*lds)[N]) {
 #pragma unroll
     for (int o = kWave / 2; o > 0; o >>= 1) {
-        a += __shfl_xor(a, o, kWave);
-        b += __shfl_xor(b, o, kWave);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o, kWave);
     }
     __syncthreads();
     if (lane_id() == 0) {
-        lds[wave_id()][0] = a;
-        lds[wave_id()][1] = b;
+#pragma unroll
+        for (int i = 0; i < N; ++i) lds[wave_id()][i] = v[i];
     }
     __syncthreads();
-    a = b = 0.0;
-    for (int w = 0; w < kThreads / kWave; ++w) {
-        a += lds[w][0];
-        b += lds[w][1];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = lds[lane_id() % (kPairThreads / kWave)][i];
+#pragma unroll
+    for (int o = kPairThreads / kWave / 2; o > 0; o >>= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o, kWave);
     }
 }
 
-// Margin, loss and coefficients of one pair.
-__device__ void preference_pair(const PairArgs &p, int64_t pair, double (*lds)[2]) {
-    int64_t from[2], to[2];
-    double ratio[2], per[2];
-    for (int side = 0; side < 2; ++side) {
-        const int64_t s = 2 * pair + side;
-        from[side] = min(max(p.seq_start[s], (int64_t)0), p.rows);
-        to[side] = min(max(p.seq_start[s + 1], from[side]), p.rows);
-        double sum = 0.0, count = 0.0;
-        for (int64_t r = from[side] + threadIdx.x; r < to[side]; r += kThreads) {
-            const int64_t label = token_at(p.labels, r);
-            if (label < 0 || label >= p.vocab) continue;
-            sum += (double)p.logp[r] - (double)p.ref[r];
-            count += 1.0;
-        }
-        block_sum2(sum, count, lds);
-        per[side] = p.mean && count > 0.0 ? 1.0 / count : 1.0;
-        ratio[side] = sum * per[side];
+// What a pair's rows need: where its two sequences begin and end, and their coefficients.
+struct PairTerms {
+    int64_t at[3];
+    float loss, chosen, other;
+};
+// By a workgroup; the same in every thread.  The two sequences' rows follow one another, so one pass takes both.
+__device__ __forceinline__ PairTerms pair_terms(const PairArgs &p, int64_t pair, double (*lds)[4]) {
+    PairTerms t;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) t.at[i] = min(max(p.seq_start[2 * pair + i], i ? t.at[i ? i - 1 : 0] : (int64_t)0), p.rows);
+    double v[4] = {0.0, 0.0, 0.0, 0.0};                              // sum and count of the first sequence, of the second one
+#pragma unroll 4
+    for (int64_t r = t.at[0] + threadIdx.x; r < t.at[2]; r += kPairThreads) {
+        const int64_t label = token_at(p.labels, r);
+        const float logp = p.logp[r], ref = p.ref[r];
+        const bool has = label >= 0 && label < p.vocab, first = r < t.at[1];
+        const double d = has ? (double)logp - (double)ref : 0.0, one = has ? 1.0 : 0.0;
+        v[0] += first ? d : 0.0;
+        v[1] += first ? one : 0.0;
+        v[2] += first ? 0.0 : d;
+        v[3] += first ? 0.0 : one;
     }
-    const double margin = ratio[0] - ratio[1], beta = (double)p.beta;
+    block_sums<4>(v, lds);
+    double per[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) per[side] = p.mean && v[2 * side + 1] > 0.0 ? 1.0 / v[2 * side + 1] : 1.0;
+    const double margin = v[0] * per[0] - v[2] * per[1], beta = (double)p.beta;
     double loss, slope;
-    if (p.loss == 0) {                                           // EF21_LOSS_LOGISTIC
+    if (p.loss == 0) {                                               // EF21_LOSS_LOGISTIC
         const double z = beta * margin, e = (double)p.smoothing, soft = log1p(exp(-fabs(z)));
         loss = (1.0 - e) * (soft + fmax(-z, 0.0)) + e * (soft + fmax(z, 0.0));
         slope = beta * (1.0 / (1.0 + exp(-z)) - (1.0 - e));
@@ -89,12 +98,20 @@ __device__ void preference_pair(const PairArgs &p, int64_t pair, double (*lds)[2
         loss = off * off;
         slope = 2.0 * off;
     }
-    if (threadIdx.x == 0) p.out_loss[pair] = (float)loss;
-    if (!p.coef) return;
     slope *= p.weight ? (double)p.weight[pair] : 1.0 / (double)p.pairs;
-    for (int side = 0; side < 2; ++side) {
-        const float c = (float)((side == 0 ? slope : -slope) * per[side]);
-        for (int64_t r = from[side] + threadIdx.x; r < to[side]; r += kThreads) p.coef[r] = c;
+    t.loss = (float)loss;
+    t.chosen = (float)(slope * per[0]);
+    t.other = (float)(-slope * per[1]);
+    return t;
+}
+
+__global__ __launch_bounds__(kPairThreads) void preference_pairs_kernel(PairArgs p) {
+    __shared__ double lds[kPairThreads / kWave][4];
+    for (int64_t pair = blockIdx.x; pair < p.pairs; pair += gridDim.x) {
+        const PairTerms t = pair_terms(p, pair, lds);
+        if (threadIdx.x == 0) p.out_loss[pair] = t.loss;
+        if (!p.coef) continue;
+        for (int64_t r = t.at[0] + threadIdx.x; r < t.at[2]; r += kPairThreads) p.coef[r] = r < t.at[1] ? t.chosen : t.other;
     }
 }
 
@@ -138,11 +155,6 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void loss_forward_kernel(Logit
     }
 }
 
-__global__ __launch_bounds__(kThreads) void preference_pairs_kernel(PairArgs p) {
-    __shared__ double lds[kThreads / kWave][2];
-    for (int64_t pair = blockIdx.x; pair < p.pairs; pair += gridDim.x) preference_pair(p, pair, lds);
-}
-
 // Rows that one wavefront takes.
 template <class T>
 __global__ __launch_bounds__(Team<1>::kBlock) void loss_grad_short_kernel(LogitRows in, RowSpace s, LogitGrad out) {
@@ -166,6 +178,33 @@ __global__ __launch_bounds__(kGradThreads) void loss_grad_kernel(LogitRows in, R
         t.load(static_cast<const T *>(in.x) + r * in.stride, g, (int32_t)in.vocab, label >= 0, (int32_t)(w % tiles));
         if (label >= 0) t.store(g, GradOf<T>(RowStat{s.m[r], s.l[r]}, s.coef[r], label));
         else t.zero(g);
+    }
+}
+
+// The pairs and the gradient of few logits in one launch: `share` workgroups per pair, each of which forms the pair's terms for itself.  The first
+// pair's workgroups take the rows before it too, the last one's those behind it (coefficient 0).
+template <class T>
+__global__ __launch_bounds__(kPairThreads) void preference_few_kernel(LogitRows in, PairArgs p, RowSpace s, LogitGrad out, int32_t share, bool short_rows) {
+    __shared__ double lds[kPairThreads / kWave][4];
+    const int64_t pair = blockIdx.x / share, part = blockIdx.x % share;
+    const PairTerms t = pair_terms(p, pair, lds);
+    if (part == 0 && threadIdx.x == 0) p.out_loss[pair] = t.loss;
+    const int64_t begin = pair == 0 ? 0 : t.at[0], end = pair + 1 == p.pairs ? in.rows : t.at[2];
+    const int32_t vocab = (int32_t)in.vocab, thread = short_rows ? lane_id() : (int32_t)threadIdx.x;
+    const int64_t teams = short_rows ? kPairThreads / kWave : 1;
+    for (int64_t r = begin + part * teams + (short_rows ? wave_id() : 0); r < end; r += share * teams) {
+        const int32_t label = label_of(in, r);
+        const T *x = static_cast<const T *>(in.x) + r * in.stride;
+        T *g = static_cast<T *>(out.ptr) + r * out.stride;
+        const float coef = r < t.at[0] || r >= t.at[2] ? 0.f : r < t.at[1] ? t.chosen : t.other;
+        const GradOf<T> d(RowStat{s.m[r], s.l[r]}, coef, label);
+        if (short_rows) {
+            if (label >= 0) stream_grad<T, kWave>(x, g, cut_row(x, vocab), d, thread);
+            else zero_row<T, kWave>(g, vocab, thread);
+        } else {
+            if (label >= 0) stream_grad<T, kPairThreads>(x, g, cut_row(x, vocab), d, thread);
+            else zero_row<T, kPairThreads>(g, vocab, thread);
+        }
     }
 }
 
@@ -362,6 +401,10 @@ hipError_t policy(const LogitRows &in, const PolicyArgs &p, const LogitGrad &out
 
 }  // namespace
 
+// us a call, three launches and two: 256 x 1000 bf16, 4 pairs 15.3 and 12.7; 256 x 4000 fp32 15.2 and 12.6; 8 x 32000 fp32 15.2 and 14.6; beyond, 64 x 32000 bf16 15.2 and
+// 15.8, 1024 x 4000 fp32 19.1 and 32, 8 x 131072 bf16 18.0 and 21.6.  (Rows of 8 KB by one wavefront each, 64 x 4000 bf16: 15.3 and 15.9.)
+constexpr int64_t kFewBytes = (int64_t)4 << 20, kFewRowBytes = 64 << 10, kFewShortBytes = 4 << 10;
+
 size_t preference_workspace_bytes(int64_t rows) { return row_space_bytes(rows); }
 
 hipError_t launch_preference(const LogitRows &in, PairArgs pairs, const LogitGrad &out, void *workspace, hipStream_t stream) {
@@ -371,7 +414,19 @@ hipError_t launch_preference(const LogitRows &in, PairArgs pairs, const LogitGra
         typedef typename ValueOf<decltype(type)::value>::type T;
         hipError_t st = in.rows > 0 ? loss_forward<T, false>(in, PolicyArgs(), pairs.logp, s, stream) : hipSuccess;
         if (st != hipSuccess) return st;
-        hipLaunchKernelGGL(preference_pairs_kernel, dim3(grid_of(pairs.pairs, 1, kManyBlocks)), dim3(kThreads), 0, stream, pairs);
+        // Up to kFewBytes a launch less counts for more than the pairs' terms formed again by every workgroup.
+        const int64_t row_bytes = in.vocab * (int64_t)sizeof(T);
+        if (out.ptr && in.rows * row_bytes <= kFewBytes && row_bytes <= kFewRowBytes) {
+            const bool short_rows = row_bytes <= kFewShortBytes;
+            const int64_t share = ceil_div(ceil_div(in.rows, pairs.pairs), short_rows ? kPairThreads / kWave : 1);
+            const int64_t blocks = pairs.pairs * (share < 1 ? 1 : share);
+            if (blocks <= 4096) {
+                hipLaunchKernelGGL(preference_few_kernel<T>, dim3((unsigned)blocks), dim3(kPairThreads), 0, stream, in, pairs, s, out,
+                                   (int32_t)(blocks / pairs.pairs), short_rows);
+                return hipGetLastError();
+            }
+        }
+        hipLaunchKernelGGL(preference_pairs_kernel, dim3(grid_of(pairs.pairs, 1, kManyBlocks)), dim3(kPairThreads), 0, stream, pairs);
         st = hipGetLastError();
         return st != hipSuccess || !out.ptr || in.rows == 0 ? st : loss_grad<T>(in, s, out, stream);
     });
