@@ -289,6 +289,17 @@ __device__ __forceinline__ ExpSum join_team(ExpSum e, TeamShared<WAVES> &sh) {
     return e;
 }
 
+// log2 of 2^whole s in a whole and a part in [-1/2, 1/2]: the whole is exact and goes into M, so that the label's z - l is rounded at about
+// the size of log p itself and not at that of the two numbers it is the difference of (a sum over a long reply adds those roundings up).
+__device__ __forceinline__ RowStat stat_of(float whole, float s) {
+    float f = __builtin_amdgcn_frexp_mantf(s), k = (float)__builtin_amdgcn_frexp_expf(s);
+    if (f < 0.70710678f) {
+        f += f;
+        k -= 1.f;
+    }
+    return {0.5f * (whole + k), log2f(f)};
+}
+
 // The row again, its maximum first.  By the whole team; all of the row has been read when a thread returns.
 template <class T, int WAVES>
 __device__ __forceinline__ RowStat careful_stat(const T *x, int32_t vocab, int32_t thread, TeamShared<WAVES> &sh) {
@@ -315,7 +326,9 @@ __device__ __forceinline__ RowStat careful_stat(const T *x, int32_t vocab, int32
         __syncthreads();
         s = group_sum<16>(sh.s[(int)threadIdx.x & (WAVES - 1)]) * ((float)WAVES / 16.f);
     }
-    st.l = s == 0.f ? -INFINITY : log2f(s);
+    if (s == 0.f) st.l = -INFINITY;
+    else if (st.large()) st.l = log2f(s);
+    else st = stat_of(2.f * st.m, s);
     return st;
 }
 
@@ -323,7 +336,7 @@ __device__ __forceinline__ RowStat careful_stat(const T *x, int32_t vocab, int32
 template <class T, int WAVES>
 __device__ __forceinline__ RowStat team_stat(ExpSum e, const T *x, int32_t vocab, int32_t thread, TeamShared<WAVES> &sh) {
     e = join_team<WAVES>(e, sh);
-    if (e.s > 0.f && e.s < INFINITY && fabsf(e.m) < kMostM) return {0.5f * e.m, log2f(e.s)};
+    if (e.s > 0.f && e.s < INFINITY && fabsf(e.m) < kMostM - 256.f) return stat_of(e.m, e.s);
     return careful_stat<T, WAVES>(x, vocab, thread, sh);
 }
 template <class T, int WAVES>
