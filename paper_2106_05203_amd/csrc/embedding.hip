@@ -10,9 +10,6 @@
 
 namespace ef21 {
 namespace {
-#ifndef FL
-#define FL 8
-#endif
 
 constexpr int kThreads = 256;
 
@@ -526,7 +523,7 @@ __global__ __launch_bounds__(kThreads, MODE == kStoreAndFill ? 8 : 4) void embed
         const int64_t tasks = (int64_t)s.p.n * s.chunks * s.column_tiles;
         for (int64_t task = (int64_t)blockIdx.x * (kThreads / kWave) + wave_id(); task < tasks; task += s.sum_blocks * (kThreads / kWave)) {
             const int64_t chunk = task / s.column_tiles;
-            sum_chunk<T, MODE == kAdd, (MODE == kStoreAndFill ? 4 : FL)>(s, chunk / s.chunks, chunk % s.chunks, task % s.column_tiles);
+            sum_chunk<T, MODE == kAdd, (MODE == kStoreAndFill ? 4 : 8)>(s, chunk / s.chunks, chunk % s.chunks, task % s.column_tiles);
         }
     } else if (MODE == kStoreAndFill) {
         const int64_t blocks = (int64_t)s.p.n * s.fill_blocks_per_worker;
@@ -590,120 +587,170 @@ __global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s
 }
 
 // ---------------------------------------------------------------- few tokens
-// One launch without a sort: a workgroup per worker, `rows` rows of the table and a wavefront's columns reads all tokens, keeps in order those
-// that name its rows, and adds (or clears) row by row.
-constexpr int64_t kFewTokens = 1024;
-constexpr int kFewHeavy = 32;                                      // from so many entries on a row is added by the whole workgroup
+// One launch without a sort.  A workgroup has all of its worker's tokens in its LDS; a wavefront takes an entry and, if it is the first that names its row, looks through
+// the others and adds them in order.  A token of many entries is added by the whole workgroup, each wavefront those of a stretch of time.  Behind
+// these workgroups are others that clear stretches of the tables around the named rows.
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / kWave;
+constexpr int64_t kFewTokens = 4096;
+constexpr int64_t kFewBlocks = 4096;                               // workgroups that fill the chip several times over
+constexpr int64_t kFewStretch = 8 * kFewThreads, kFewMostStretch = 128 * kFewThreads;   // entries of a table: 16 KB, 256 KB
+constexpr uint32_t kFewHeavy = 32;                                 // from so many entries on a row is added by the whole workgroup
 
-template <class T, bool ADD>
-__global__ __launch_bounds__(kThreads) void embed_grad_few_kernel(EmbedGradArgs p, int32_t rows, int64_t groups, int64_t column_tiles) {
-    constexpr int N = sum_columns<T>(), FLIGHT = 8, WAVES = kThreads / kWave;
-    __shared__ uint32_t list[kFewTokens];                          // row within the group << 16 | position
-    __shared__ uint32_t found[WAVES];
-    __shared__ float joined[WAVES][kWave * N];
-    const int64_t column_tile = blockIdx.x % column_tiles, group = blockIdx.x / column_tiles % groups, worker = blockIdx.x / column_tiles / groups;
-    const int64_t low = group * rows, first = worker * p.count;
-    const int here = (int)(p.vocab - low < rows ? p.vocab - low : rows);
-    // each wavefront looks through its quarter of the tokens
-    const int count = (int)p.count, each = (count + WAVES - 1) / WAVES, start = wave_id() * each, stop = min(start + each, count);
-    uint32_t mine = 0u;
-    for (int base = start; base < stop; base += kWave) {
-        const int at = base + lane_id();
-        const int64_t in = at < stop ? token_at(p.tokens, first + at) - low : -1;
-        const bool hit = in >= 0 && in < here;
-        const uint64_t hits = __ballot(hit);
-        if (hit) list[start + mine + lanes_below(hits)] = (uint32_t)in << 16 | (uint32_t)at;
-        mine += popc64(hits);
-    }
-    if (lane_id() == 0) found[wave_id()] = mine;
+struct FewArgs {
+    EmbedGradArgs p;
+    int64_t column_tiles, sum_blocks;
+    int32_t blocks_each;                                           // workgroups of a worker and column tile: entry t is taken by number t mod blocks_each
+    int64_t stretch, stretches;                                    // entries of a table that a workgroup clears; so many a worker
+};
+
+__device__ __forceinline__ void clear_unnamed(const FewArgs &a, int64_t block, uint32_t *marks) {
+    const EmbedGradArgs &p = a.p;
+    const int64_t worker = block / a.stretches, from = block % a.stretches * a.stretch, all = p.vocab * p.width;
+    const int64_t to = from + a.stretch < all ? from + a.stretch : all, low = from / p.width, rows = (to - 1) / p.width + 1 - low;
+    for (int i = (int)threadIdx.x; i < (rows + 31) / 32; i += kFewThreads) marks[i] = 0u;
     __syncthreads();
-    const Columns c = columns_of<N>(column_tile * (kWave * N) + lane_id() * N, p.width);
-    const T *grad = static_cast<const T *>(p.grad_out) + first * p.grad_stride;
-    float *table = p.table_grad + worker * p.worker_stride + low * p.width;
-    uint32_t total = 0u;
-    for (int w = 0; w < WAVES; ++w) total += found[w];
-    if (ADD && total == 0u) return;
-
-    // Adds the entries number from .. to - 1 of a row, in order.
-    auto add = [&](uint32_t row, uint32_t from, uint32_t to, float(&acc)[N]) {
-        uint32_t seen = 0u;
-        for (int w = 0; w < WAVES; ++w) {
-            for (uint32_t base = 0u; base < found[w]; base += kWave) {
-                const uint32_t e = base + lane_id() < found[w] ? list[w * each + base + lane_id()] : ~0u;
-                uint64_t hits = __ballot(e >> 16 == row);
-                while (hits) {
-                    float f[FLIGHT][N];
-                    bool take[FLIGHT];
-#pragma unroll
-                    for (int j = 0; j < FLIGHT; ++j) {
-                        take[j] = hits != 0 && seen >= from && seen < to;
-                        if (hits != 0) {
-                            const int lane = __ffsll((long long)hits) - 1;
-                            const int64_t at = __builtin_amdgcn_readlane(e, lane) & 0xffffu;
-                            if (take[j] && c.at >= 0) load_columns<true>(grad + at * p.grad_stride, c, f[j]);
-                            hits &= hits - 1u;
-                            ++seen;
-                        }
-                    }
-#pragma unroll
-                    for (int j = 0; j < FLIGHT; ++j) {
-                        if (!take[j]) continue;
-#pragma unroll
-                        for (int i = 0; i < N; ++i) acc[i] += f[j][i];
-                    }
+    for (int i = (int)threadIdx.x; i < (int)p.count; i += kFewThreads) {
+        const int64_t in = token_at(p.tokens, worker * p.count + i) - low;
+        if (in >= 0 && in < rows) atomicOr(&marks[in / 32], 1u << (in & 31));
+    }
+    __syncthreads();
+    constexpr int64_t kStep = 4 * kFewThreads;
+    const int64_t step_rows = kStep / p.width, step_column = kStep % p.width;
+    int64_t at = from + 4 * (int64_t)threadIdx.x, row = at / p.width, column = at % p.width;
+    row -= low;
+    float *table = p.table_grad + worker * p.worker_stride;
+    for (; at < to; at += kStep) {
+        if (column + 4 <= p.width && at + 4 <= to) {
+            if (!(marks[row / 32] >> (row & 31) & 1u)) store4_any(table + at, make_float4(0.f, 0.f, 0.f, 0.f));
+        } else {
+            int64_t r = row, c = column;
+            for (int j = 0; j < 4 && at + j < to; ++j) {
+                if (!(marks[r / 32] >> (r & 31) & 1u)) table[at + j] = 0.f;
+                if (++c == p.width) {
+                    c = 0;
+                    ++r;
                 }
             }
         }
-    };
-    auto entries = [&](uint32_t row) {
-        uint32_t n = 0u;
-        for (int w = 0; w < WAVES; ++w)
-            for (uint32_t base = 0u; base < found[w]; base += kWave)
-                n += popc64(__ballot(base + lane_id() < found[w] && list[w * each + base + lane_id()] >> 16 == row));
-        return n;
+        row += step_rows;
+        column += step_column;
+        if (column >= p.width) {
+            column -= p.width;
+            ++row;
+        }
+    }
+}
+
+template <class T, bool ADD>
+__global__ __launch_bounds__(kFewThreads, 6) void embed_grad_few_kernel(FewArgs a) {
+    constexpr int N = sum_columns<T>(), FLIGHT = 8;
+    __shared__ uint32_t keys[kFewTokens];
+    if (!ADD && (int64_t)blockIdx.x >= a.sum_blocks) {
+        clear_unnamed(a, (int64_t)blockIdx.x - a.sum_blocks, keys);
+        return;
+    }
+    __shared__ volatile uint16_t lists[kFewWaves][2 * kWave];      // a wavefront's entries of its row
+    __shared__ float joined[kFewWaves][kWave * N];
+    __shared__ uint16_t heavy[kFewTokens / kFewHeavy];             // first entries of heavy tokens
+    __shared__ uint32_t heavies;
+    const EmbedGradArgs &p = a.p;
+    const int64_t column_tile = blockIdx.x % a.column_tiles, worker = blockIdx.x / a.column_tiles / a.blocks_each;
+    const int count = (int)p.count, block = (int)(blockIdx.x / a.column_tiles % a.blocks_each);
+    if (threadIdx.x == 0) heavies = 0u;
+    for (int i = (int)threadIdx.x; i < (count + 4 * kWave - 1) / (4 * kWave) * (4 * kWave); i += kFewThreads)
+        keys[i] = i < count ? token_key(p.tokens, worker * count + i, p.vocab) : kNoKey;
+    __syncthreads();
+    const Columns c = columns_of<N>(column_tile * (kWave * N) + lane_id() * N, p.width);
+    const T *grad = static_cast<const T *>(p.grad_out) + worker * p.count * p.grad_stride;
+    float *table = p.table_grad + worker * p.worker_stride;
+    volatile uint16_t *list = lists[wave_id()];
+
+    // what entries of the list name are added, the first `n`
+    auto add_listed = [&](int n, float(&acc)[N]) {
+        __builtin_amdgcn_wave_barrier();
+        for (int i = 0; i < n; i += FLIGHT) {
+            Held<T, N> f[FLIGHT];
+#pragma unroll
+            for (int j = 0; j < FLIGHT; ++j) {
+                if (i + j >= n) break;
+                const int64_t at = __builtin_amdgcn_readfirstlane((int)list[i + j]);
+                if (c.at >= 0) hold_columns<true>(grad + at * p.grad_stride, c, f[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < FLIGHT; ++j) {
+                if (i + j >= n) break;
+                float g[N];
+                f[j].get(g);
+#pragma unroll
+                for (int k = 0; k < N; ++k) acc[k] += g[k];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     };
     auto finish = [&](uint32_t row, float(&acc)[N], const float(&old)[N]) {
+        if (c.at < 0) return;
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[i] = ADD ? fmaf(p.scale, acc[i], old[i]) : p.scale * acc[i];
         store_columns(table + (int64_t)row * p.width, c, acc, true);
     };
-    uint64_t heavy = 0u;                                           // rows wave + 4 b of the group that are left for the whole workgroup
-    for (uint32_t row = wave_id(); row < (uint32_t)here; row += WAVES) {
-        const uint32_t n = total > 0u ? entries(row) : 0u;
-        if (n >= kFewHeavy) {
-            heavy |= 1ull << (row / WAVES);
+
+    for (int t = block + a.blocks_each * wave_id(); t < count; t += a.blocks_each * kFewWaves) {
+        const uint32_t row = __builtin_amdgcn_readfirstlane(keys[t]);
+        if (row == (uint32_t)p.vocab) continue;
+        int n = 0;
+        bool first = true, light = true;
+        for (int base = 0; base < count && first && light; base += 4 * kWave) {
+            uint64_t hits[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) hits[j] = __ballot(keys[base + j * kWave + lane_id()] == row);
+            if (!(hits[0] | hits[1] | hits[2] | hits[3])) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int from = base + j * kWave, more = (int)popc64(hits[j]);
+                if (more == 0 || !first || !light) continue;
+                first = n > 0 || from + __ffsll((long long)hits[j]) - 1 == t;
+                light = n + more < (int)kFewHeavy;
+                if (first && light && (hits[j] >> lane_id() & 1u)) list[n + lanes_below(hits[j])] = (uint16_t)(from + lane_id());
+                n += more;
+            }
+        }
+        if (!first) continue;
+        if (!light) {
+            if (lane_id() == 0) heavy[atomicAdd(&heavies, 1u)] = (uint16_t)t;
             continue;
         }
-        if (ADD && n == 0u) continue;
         float acc[N] = {}, old[N] = {};
-        if (n > 0u) {
-            if (ADD && c.at >= 0) load_columns<true>(table + (int64_t)row * p.width, c, old);
-            add(row, 0u, n, acc);                                  // by all lanes, those without columns too: they hold entries of the list
-        }
-        if (c.at >= 0) finish(row, acc, old);
+        if (ADD && c.at >= 0) load_columns<true>(table + (int64_t)row * p.width, c, old);
+        add_listed(n, acc);
+        finish(row, acc, old);
     }
-    if (total < kFewHeavy) return;
-    __shared__ uint64_t heavies[WAVES];
-    if (lane_id() == 0) heavies[wave_id()] = heavy;
     __syncthreads();
-    for (int w = 0; w < WAVES; ++w) {
-        for (uint64_t left = heavies[w]; left != 0; left &= left - 1u) {
-            const uint32_t row = (uint32_t)(__ffsll((long long)left) - 1) * WAVES + w, n = entries(row), part = (n + WAVES - 1) / WAVES;
-            float acc[N] = {}, old[N] = {};
-            if (ADD && c.at >= 0 && wave_id() == 0) load_columns<true>(table + (int64_t)row * p.width, c, old);
-            add(row, wave_id() * part, min(n, (wave_id() + 1) * part), acc);
-#pragma unroll
-            for (int i = 0; i < N; ++i) joined[wave_id()][lane_id() * N + i] = acc[i];
-            __syncthreads();
-            if (wave_id() == 0 && c.at >= 0) {
-                for (int v = 1; v < WAVES; ++v) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) acc[i] += joined[v][lane_id() * N + i];
-                }
-                finish(row, acc, old);
+    const int left = (int)heavies, each = (count + kFewWaves - 1) / kFewWaves, start = wave_id() * each, stop = min(start + each, count);
+    for (int h = 0; h < left; ++h) {
+        const uint32_t row = __builtin_amdgcn_readfirstlane(keys[heavy[h]]);
+        float acc[N] = {}, old[N] = {};
+        if (ADD && c.at >= 0 && wave_id() == 0) load_columns<true>(table + (int64_t)row * p.width, c, old);
+        int n = 0;
+        for (int base = start; base < stop; base += kWave) {
+            const uint64_t hits = __ballot(base + lane_id() < stop && keys[base + lane_id()] == row);
+            if (hits >> lane_id() & 1u) list[n + lanes_below(hits)] = (uint16_t)(base + lane_id());
+            n += (int)popc64(hits);
+            if (n >= kWave || base + kWave >= stop) {
+                add_listed(n, acc);
+                n = 0;
             }
-            __syncthreads();
         }
+#pragma unroll
+        for (int i = 0; i < N; ++i) joined[wave_id()][lane_id() * N + i] = acc[i];
+        __syncthreads();
+        if (wave_id() == 0) {
+            for (int v = 1; v < kFewWaves; ++v) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc[i] += joined[v][lane_id() * N + i];
+            }
+            finish(row, acc, old);
+        }
+        __syncthreads();
     }
 }
 
@@ -717,17 +764,18 @@ constexpr int64_t kManyBlocks = 1 << 20;
 unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)(blocks < most ? blocks : most); }
 
 // Sorted entries of a chunk: 64 (fewer partial sums) where that gives wavefronts enough for the chip, else 16.
-#ifndef CHK
-#define CHK 64
-#endif
-int32_t chunk_entries(int32_t n, int64_t count, int64_t width) { return (int64_t)n * count * ceil_div(width, 512) / CHK >= 4096 ? CHK : 16; }
+int32_t chunk_entries(int32_t n, int64_t count, int64_t width) { return (int64_t)n * count * ceil_div(width, 512) / 64 >= 4096 ? 64 : 16; }
 
 // Whether the tables are cleared whole, beside the sort, and rows with a token written twice, or the rows without one are written beside the sums.
 // The plain clearing writes faster (6.5 TB/s against 5, 1 GB) and hides the sort, but only up to so many tokens there are few rows to write twice.
 bool clears_first(const EmbedGradArgs &p) { return !p.accumulate && p.count <= 8 * kSortThreads && 3 * p.count <= p.vocab; }
 
+// One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^25 of them.  (n, tokens, rows of 512 columns:
+// 2, 1374, 22283 of 64: 12 us, 30 by sorting; 1, 2117, 97230 of 33: 11 and 41; 14, 1033, 1327 of 1072, 2^25.4: 84 and 60.)
+bool few_tokens(int32_t n, int64_t count, int64_t width) { return count <= kFewTokens && n * count * count * ceil_div(width, 512) <= (int64_t)1 << 25; }
+
 size_t grad_layout(int32_t n, int64_t count, int64_t vocab, int64_t width, void *ws, GradSpace *out) {
-    if (count <= kFewTokens) return 256;                           // not used; never zero, so that callers need no case of their own for it
+    if (few_tokens(n, count, width)) return 256;                           // not used; never zero, so that callers need no case of their own for it
     char *at = static_cast<char *>(ws);
     size_t used = 0;
     auto take = [&](size_t bytes) {
@@ -819,21 +867,25 @@ size_t embed_grad_workspace_bytes(int32_t n, int64_t count, int64_t vocab, int64
 template <class T>
 static hipError_t embed_grad_few(const EmbedGradArgs &p, hipStream_t stream) {
     const int64_t column_tiles = ceil_div(p.width, kWave * sum_columns<T>());
-    // some 16 KB of a table to a workgroup, but no more rows than its list and its heavy bits number, and workgroups enough for the chip
-    int64_t rows = (16 << 10) / (4 * (p.width < kWave * sum_columns<T>() ? p.width : kWave * sum_columns<T>()));
-    const int64_t all = p.vocab * p.n * column_tiles;
-    if (rows > all / 1024) rows = all / 1024;
-    rows = rows < 4 ? 4 : rows > 256 ? 256 : rows;
-    const int64_t groups = ceil_div(p.vocab, rows), blocks = groups * p.n * column_tiles;
+    FewArgs a{p, column_tiles, 0, 0, 0, 1};
+    // a wavefront per entry, or more where that gives many thousand workgroups, each of which reads all of the worker's tokens
+    const int64_t each = ceil_div(p.count, kFewWaves), wanted = ceil_div(kFewBlocks, p.n * column_tiles);
+    a.blocks_each = (int32_t)(each < wanted ? each : wanted);
+    a.sum_blocks = p.n * column_tiles * a.blocks_each;
+    const int64_t all = p.vocab * p.width;
+    a.stretch = ceil_div(ceil_div(p.n * all, kFewBlocks), kFewStretch) * kFewStretch;
+    if (a.stretch > kFewMostStretch) a.stretch = kFewMostStretch;
+    a.stretches = ceil_div(all, a.stretch);
+    const int64_t blocks = a.sum_blocks + (p.accumulate ? 0 : p.n * a.stretches);
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    if (p.accumulate) hipLaunchKernelGGL((embed_grad_few_kernel<T, true>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p, (int32_t)rows, groups, column_tiles);
-    else hipLaunchKernelGGL((embed_grad_few_kernel<T, false>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p, (int32_t)rows, groups, column_tiles);
+    if (p.accumulate) hipLaunchKernelGGL((embed_grad_few_kernel<T, true>), dim3((unsigned)blocks), dim3(kFewThreads), 0, stream, a);
+    else hipLaunchKernelGGL((embed_grad_few_kernel<T, false>), dim3((unsigned)blocks), dim3(kFewThreads), 0, stream, a);
     return hipGetLastError();
 }
 
 hipError_t launch_embed_grad(const EmbedGradArgs &p, void *workspace, hipStream_t stream) {
     if (p.count == 0 && p.accumulate) return hipSuccess;
-    if (p.count <= kFewTokens)
+    if (few_tokens(p.n, p.count, p.width))
         return with_type(p.type, [&](auto type) { return embed_grad_few<typename ValueOf<decltype(type)::value>::type>(p, stream); });
     GradSpace g;
     grad_layout(p.n, p.count, p.vocab, p.width, workspace, &g);
