@@ -168,9 +168,6 @@ __device__ __forceinline__ int64_t wave_lower_bound(const uint32_t *key, int64_t
     return a;
 }
 
-// Rows of a table are marked in words of 32, so many words at a time.
-constexpr int kMarkedWords = 1024;
-
 struct Digit {
     int shift, bits;
     __device__ uint32_t of(uint32_t key) const { return key >> shift & ((1u << bits) - 1u); }
@@ -232,28 +229,32 @@ __device__ __forceinline__ void scan_digits(SortShared &s) {
 template <int ITEMS>
 __device__ __forceinline__ int item_index(int i) { return wave_id() * (kWave * ITEMS) + i * kWave + lane_id(); }
 
-// Tables that are cleared whole before the sums.
+// Tables that are cleared whole while the tokens are sorted: the sort leaves the memory idle.  Rows with a token are written twice.
 struct ClearArgs {
     float *table;
     int64_t entries, stride;                                       // of a worker's table, from one worker's to the next
     int64_t blocks_per_worker;                                     // of 4 kSortThreads entries
+    int64_t from, to;                                              // the blocks that this launch clears
 };
-__device__ __forceinline__ void clear_block(const ClearArgs &c, int64_t block) {
-    float *table = c.table + block / c.blocks_per_worker * c.stride;
-    const int64_t at = (block % c.blocks_per_worker * kSortThreads + threadIdx.x) * 4;
-    if (at + 4 <= c.entries) {
-        store4_any(table + at, make_float4(0.f, 0.f, 0.f, 0.f));
-    } else {
-        for (int64_t i = at; i < c.entries; ++i) table[i] = 0.f;
+// By workgroup `block` of `blocks`.
+__device__ __forceinline__ void clear_blocks(const ClearArgs &c, int64_t block, int64_t blocks) {
+    for (int64_t b = c.from + block; b < c.to; b += blocks) {
+        float *table = c.table + b / c.blocks_per_worker * c.stride;
+        const int64_t at = (b % c.blocks_per_worker * kSortThreads + threadIdx.x) * 4;
+        if (at + 4 <= c.entries) {
+            store4_any(table + at, make_float4(0.f, 0.f, 0.f, 0.f));
+        } else {
+            for (int64_t i = at; i < c.entries; ++i) table[i] = 0.f;
+        }
     }
 }
 
-// Workgroups 0 .. n - 1 sort; those behind them clear tables meanwhile, which the memory is free for.
+// Workgroups 0 .. n - 1 sort; those behind them clear.
 template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void sort_in_lds_kernel(Tokens tokens, int32_t n, int32_t count, int64_t vocab, int bits, int passes,
-                                                                   uint32_t *key_out, uint32_t *pos_out, uint32_t *named, int64_t named_words, ClearArgs clear) {
+                                                                   uint32_t *key_out, uint32_t *pos_out, ClearArgs clear) {
     if ((int32_t)blockIdx.x >= n) {
-        for (int64_t b = (int64_t)blockIdx.x - n; b < (int64_t)n * clear.blocks_per_worker; b += (int64_t)gridDim.x - n) clear_block(clear, b);
+        clear_blocks(clear, (int64_t)blockIdx.x - n, (int64_t)gridDim.x - n);
         return;
     }
     extern __shared__ uint32_t lds_keys[];                         // [ITEMS * kSortThreads], then as many 16-bit positions
@@ -292,41 +293,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_in_lds_kernel(Tokens tokens
         key_out[first + at] = lds_keys[at];
         pos_out[first + at] = lds_pos[at];
     }
-    if (!named) return;
-    // a bit for every row that a token names, kMarked rows at a time
-    __shared__ uint32_t marks[kMarkedWords];
-    uint32_t *mine = named + (int64_t)blockIdx.x * named_words;
-    int at = (int)threadIdx.x;                                     // of this thread's entries, the first that is not marked yet
-    for (int64_t word = 0; word < named_words; word += kMarkedWords) {
-        const int words = (int)(named_words - word < kMarkedWords ? named_words - word : kMarkedWords);
-        __syncthreads();
-        for (int i = (int)threadIdx.x; i < words; i += kSortThreads) marks[i] = 0u;
-        __syncthreads();
-        for (; at < count; at += kSortThreads) {
-            const int64_t in = (int64_t)lds_keys[at] - word * 32;
-            if (in >= (int64_t)words * 32) break;
-            atomicOr(&marks[in / 32], 1u << (in & 31));
-        }
-        __syncthreads();
-        for (int i = (int)threadIdx.x; i < words; i += kSortThreads) mine[word + i] = marks[i];
-    }
-}
-
-// The same from sorted keys in memory: a workgroup per kMarkedWords words of a worker.
-__global__ __launch_bounds__(kThreads) void mark_named_kernel(const uint32_t *keys, int64_t count, uint32_t *named, int64_t named_words) {
-    __shared__ uint32_t marks[kMarkedWords];
-    const uint32_t *key = keys + (int64_t)blockIdx.y * count;
-    const int64_t word = (int64_t)blockIdx.x * kMarkedWords;
-    const int words = (int)(named_words - word < kMarkedWords ? named_words - word : kMarkedWords);
-    for (int i = (int)threadIdx.x; i < words; i += kThreads) marks[i] = 0u;
-    __syncthreads();
-    for (int64_t i = wave_lower_bound(key, count, (uint32_t)(word * 32)) + threadIdx.x; i < count; i += kThreads) {
-        const int64_t in = (int64_t)key[i] - word * 32;
-        if (in >= (int64_t)words * 32) break;
-        atomicOr(&marks[in / 32], 1u << (in & 31));
-    }
-    __syncthreads();
-    for (int i = (int)threadIdx.x; i < words; i += kThreads) named[(int64_t)blockIdx.y * named_words + word + i] = marks[i];
 }
 
 struct SortArgs {
@@ -337,14 +303,24 @@ struct SortArgs {
     uint32_t *key_out, *pos_out;
     uint32_t *counts;                                              // [n][tiles][kMostDigits]
     Digit digit;
+    ClearArgs clear;
+    int64_t sort_blocks;                                           // n tiles; workgroups behind them clear
+    __device__ __forceinline__ bool clears() const {
+        if (blockIdx.x < sort_blocks) return false;
+        clear_blocks(clear, blockIdx.x - sort_blocks, gridDim.x - sort_blocks);
+        return true;
+    }
+    __device__ __forceinline__ int64_t worker() const { return blockIdx.x / (uint32_t)tiles; }
+    __device__ __forceinline__ int32_t tile() const { return (int32_t)(blockIdx.x % (uint32_t)tiles); }
 };
 __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t first, int64_t at) {
     return a.digit.shift == 0 ? token_key(a.tokens, first + at, a.vocab) : a.key[first + at];
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_histogram_kernel(SortArgs a) {
+    if (a.clears()) return;
     __shared__ uint32_t hist[kMostDigits];
-    const int64_t first = (int64_t)blockIdx.y * a.count, start = (int64_t)blockIdx.x * kTile;
+    const int64_t first = a.worker() * a.count, start = (int64_t)a.tile() * kTile;
     if (threadIdx.x < kMostDigits) hist[threadIdx.x] = 0u;
     __syncthreads();
     uint32_t key[kTileItems];
@@ -357,13 +333,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_histogram_kernel(SortArgs a
     for (int i = 0; i < kTileItems; ++i)
         if (start + i * kSortThreads + threadIdx.x < a.count) atomicAdd(&hist[a.digit.of(key[i])], 1u);
     __syncthreads();
-    if (threadIdx.x < kMostDigits) a.counts[((int64_t)blockIdx.y * a.tiles + blockIdx.x) * kMostDigits + threadIdx.x] = hist[threadIdx.x];
+    if (threadIdx.x < kMostDigits) a.counts[(int64_t)blockIdx.x * kMostDigits + threadIdx.x] = hist[threadIdx.x];
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) {
+    if (a.clears()) return;
     __shared__ SortShared s;
     __shared__ uint32_t goes[kMostDigits];
-    const int64_t first = (int64_t)blockIdx.y * a.count, start = (int64_t)blockIdx.x * kTile;
+    const int64_t first = a.worker() * a.count, start = (int64_t)a.tile() * kTile;
     uint32_t key[kTileItems], rank[kTileItems], pos[kTileItems];
 #pragma unroll
     for (int i = 0; i < kTileItems; ++i) {
@@ -375,12 +352,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
     // where the tile's entries of a digit go: behind all of lower digits, and those of the same digit in the tiles before
     uint32_t total = 0u, earlier = 0u;
     if (threadIdx.x < kMostDigits) {
-        const uint32_t *c = a.counts + (int64_t)blockIdx.y * a.tiles * kMostDigits + threadIdx.x;
+        const uint32_t *c = a.counts + a.worker() * a.tiles * kMostDigits + threadIdx.x;
 #pragma unroll 8
         for (int t = 0; t < a.tiles; ++t) {
             const uint32_t v = c[(int64_t)t * kMostDigits];
             total += v;
-            if (t < (int)blockIdx.x) earlier += v;
+            if (t < a.tile()) earlier += v;
         }
     }
     const uint32_t sum = wave_inclusive_scan(total);
@@ -407,12 +384,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
 struct SumArgs {
     EmbedGradArgs p;
     const uint32_t *key, *pos;                                     // [n][count], sorted
-    const uint32_t *named;                                         // [n][named_words]
     float *partial;                                                // [n][chunks][2][width]: what a chunk has of the token that it begins with, and of the last one
-    int64_t chunks, column_tiles, named_words;
+    int64_t chunks, column_tiles;
     int32_t chunk;                                                 // sorted entries that a wavefront adds, at most 64
-    int64_t sum_blocks;                                            // workgroups of the sums; those behind them write the rows without a token
-    int64_t fill_rows, fill_blocks_per_worker;
 };
 
 template <class T>
@@ -421,10 +395,13 @@ constexpr int sum_columns() { return 16 / (int)sizeof(T); }        // columns of
 constexpr int kShort = kWave;                                      // a token of up to so many entries is added by one wavefront
 
 // The chunk's wavefront adds the tokens that begin in the chunk, those with at most kShort entries to their end.  Of a longer token it adds what lies
-// in the chunk and leaves a partial sum.  FLIGHT rows of grad_out, and with ADD the rows that they are added to, are in flight.
-template <class T, bool ADD, int FLIGHT>
+// in the chunk and leaves a partial sum.  Eight rows of grad_out, and with ADD the rows that they are added to, are in flight.
+template <class T, bool ADD>
 __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int64_t chunk, int64_t column_tile) {
-    constexpr int N = sum_columns<T>();
+    #ifndef FL
+#define FL 8
+#endif
+    constexpr int N = sum_columns<T>(), FLIGHT = FL;
     const EmbedGradArgs &p = s.p;
     const Columns c = columns_of<N>(column_tile * (kWave * N) + lane_id() * N, p.width);
     const uint32_t *key = s.key + worker * p.count, *pos = s.pos + worker * p.count;
@@ -500,35 +477,15 @@ __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int6
     }
 }
 
-// Rows of a table that no token names are written as zeros.
-__device__ __forceinline__ void fill_rows(const SumArgs &s, int64_t worker, int64_t block) {
-    const EmbedGradArgs &p = s.p;
-    const int64_t from = block * s.fill_rows, to = from + s.fill_rows < p.vocab ? from + s.fill_rows : p.vocab;
-    const uint32_t *named = s.named + worker * s.named_words;
-    float *table = p.table_grad + worker * p.worker_stride;
-    const float none[4] = {};
-    for (int64_t v = from + wave_id(); v < to; v += kThreads / kWave) {
-        if (named[v / 32] >> (v & 31) & 1u) continue;
-        for (int64_t j = lane_id() * 4; j < p.width; j += kWave * 4) store_columns(table + v * p.width, columns_of<4>(j, p.width), none, false);
-    }
-}
-
-// What is done with the rows that no token names, and with those that one does.
-enum SumMode { kStoreAndFill, kStore, kAdd };
-
-// (Beside the filling at most 64 registers, so that the workgroups that only write fill the compute units.)
-template <class T, int MODE>
-__global__ __launch_bounds__(kThreads, MODE == kStoreAndFill ? 8 : 4) void embed_grad_kernel(SumArgs s) {
-    if ((int64_t)blockIdx.x < s.sum_blocks) {
-        const int64_t tasks = (int64_t)s.p.n * s.chunks * s.column_tiles;
-        for (int64_t task = (int64_t)blockIdx.x * (kThreads / kWave) + wave_id(); task < tasks; task += s.sum_blocks * (kThreads / kWave)) {
-            const int64_t chunk = task / s.column_tiles;
-            sum_chunk<T, MODE == kAdd, (MODE == kStoreAndFill ? 4 : 8)>(s, chunk / s.chunks, chunk % s.chunks, task % s.column_tiles);
-        }
-    } else if (MODE == kStoreAndFill) {
-        const int64_t blocks = (int64_t)s.p.n * s.fill_blocks_per_worker;
-        for (int64_t b = (int64_t)blockIdx.x - s.sum_blocks; b < blocks; b += (int64_t)gridDim.x - s.sum_blocks)
-            fill_rows(s, b / s.fill_blocks_per_worker, b % s.fill_blocks_per_worker);
+#ifndef EU
+#define EU 4
+#endif
+template <class T, bool ADD>
+__global__ __launch_bounds__(kThreads, EU) void embed_grad_kernel(SumArgs s) {
+    const int64_t tasks = (int64_t)s.p.n * s.chunks * s.column_tiles;
+    for (int64_t task = (int64_t)blockIdx.x * (kThreads / kWave) + wave_id(); task < tasks; task += (int64_t)gridDim.x * (kThreads / kWave)) {
+        const int64_t chunk = task / s.column_tiles;
+        sum_chunk<T, ADD>(s, chunk / s.chunks, chunk % s.chunks, task % s.column_tiles);
     }
 }
 
@@ -620,9 +577,10 @@ __device__ __forceinline__ void clear_unnamed(const FewArgs &a, int64_t block, u
     row -= low;
     float *table = p.table_grad + worker * p.worker_stride;
     for (; at < to; at += kStep) {
-        if (column + 4 <= p.width && at + 4 <= to) {
-            if (!(marks[row / 32] >> (row & 31) & 1u)) store4_any(table + at, make_float4(0.f, 0.f, 0.f, 0.f));
-        } else {
+        const bool two = column + 4 > p.width, clear = !(marks[row / 32] >> (row & 31) & 1u);   // rows that the four entries are of (if p.width >= 4)
+        if (at + 4 <= to && (two ? p.width >= 4 && clear && !(marks[(row + 1) / 32] >> ((row + 1) & 31) & 1u) : clear)) {
+            store4_any(table + at, make_float4(0.f, 0.f, 0.f, 0.f));
+        } else if (two || at + 4 > to) {
             int64_t r = row, c = column;
             for (int j = 0; j < 4 && at + j < to; ++j) {
                 if (!(marks[r / 32] >> (r & 31) & 1u)) table[at + j] = 0.f;
@@ -756,7 +714,7 @@ __global__ __launch_bounds__(kFewThreads, 6) void embed_grad_few_kernel(FewArgs 
 
 // ---------------------------------------------------------------- the workspace
 struct GradSpace {
-    uint32_t *key[2], *pos[2], *counts, *named;
+    uint32_t *key[2], *pos[2], *counts;
     float *partial;
 };
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -765,10 +723,6 @@ unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)(blocks < most
 
 // Sorted entries of a chunk: 64 (fewer partial sums) where that gives wavefronts enough for the chip, else 16.
 int32_t chunk_entries(int32_t n, int64_t count, int64_t width) { return (int64_t)n * count * ceil_div(width, 512) / 64 >= 4096 ? 64 : 16; }
-
-// Whether the tables are cleared whole, beside the sort, and rows with a token written twice, or the rows without one are written beside the sums.
-// The plain clearing writes faster (6.5 TB/s against 5, 1 GB) and hides the sort, but only up to so many tokens there are few rows to write twice.
-bool clears_first(const EmbedGradArgs &p) { return !p.accumulate && p.count <= 8 * kSortThreads && 3 * p.count <= p.vocab; }
 
 // One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^25 of them.  (n, tokens, rows of 512 columns:
 // 2, 1374, 22283 of 64: 12 us, 30 by sorting; 1, 2117, 97230 of 33: 11 and 41; 14, 1033, 1327 of 1072, 2^25.4: 84 and 60.)
@@ -791,57 +745,61 @@ size_t grad_layout(int32_t n, int64_t count, int64_t vocab, int64_t width, void 
         g.pos[i] = reinterpret_cast<uint32_t *>(take(entries * sizeof(uint32_t)));
     }
     if (count > kLdsSort) g.counts = reinterpret_cast<uint32_t *>(take((size_t)n * (size_t)ceil_div(count, kTile) * kMostDigits * sizeof(uint32_t)));
-    g.named = reinterpret_cast<uint32_t *>(take((size_t)n * (size_t)ceil_div(vocab, 32) * sizeof(uint32_t)));
     g.partial = reinterpret_cast<float *>(take((size_t)n * (size_t)ceil_div(count, chunk_entries(n, count, width)) * 2 * (size_t)width * sizeof(float)));
     if (out) *out = g;
     return used;
 }
 
 template <int ITEMS>
-hipError_t sort_in_lds(const EmbedGradArgs &p, int bits, int passes, const GradSpace &g, bool clear, hipStream_t stream) {
+hipError_t sort_in_lds(const EmbedGradArgs &p, int bits, int passes, const GradSpace &g, const ClearArgs &c, hipStream_t stream) {
     constexpr size_t kBytes = (size_t)ITEMS * kSortThreads * (sizeof(uint32_t) + sizeof(uint16_t));
     static PerDeviceOnce once;
     const hipError_t st = once([] {
         return hipFuncSetAttribute(reinterpret_cast<const void *>(&sort_in_lds_kernel<ITEMS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
     });
     if (st != hipSuccess) return st;
-    ClearArgs c{p.table_grad, p.vocab * p.width, p.worker_stride, 0};
-    if (clear) c.blocks_per_worker = ceil_div(c.entries, 4 * kSortThreads);
-    hipLaunchKernelGGL(sort_in_lds_kernel<ITEMS>, dim3((unsigned)p.n + at_most((int64_t)p.n * c.blocks_per_worker, kManyBlocks)), dim3(kSortThreads), kBytes,
-                       stream, p.tokens, p.n, (int32_t)p.count, p.vocab, bits, passes, g.key[0], g.pos[0], p.accumulate || clear ? nullptr : g.named,
-                       ceil_div(p.vocab, 32), c);
+    hipLaunchKernelGGL(sort_in_lds_kernel<ITEMS>, dim3((unsigned)p.n + at_most(c.to, kManyBlocks)), dim3(kSortThreads), kBytes, stream, p.tokens, p.n, (int32_t)p.count,
+                       p.vocab, bits, passes, g.key[0], g.pos[0], c);
     return hipGetLastError();
 }
 
-// Sorts; *in: the buffer of g that holds the result.  clear: the tables are cleared too (clears_first), else the rows with a token marked.
-hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, bool clear, int *in, hipStream_t stream) {
+// Sorts, and clears the tables where they are not added to; *in: the buffer of g that holds the result.
+hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, int *in, hipStream_t stream) {
+    ClearArgs c{p.table_grad, p.vocab * p.width, p.worker_stride, 0, 0, 0};
+    if (!p.accumulate) c.blocks_per_worker = ceil_div(c.entries, 4 * kSortThreads);
+    const int64_t clears = c.to = p.n * c.blocks_per_worker;
     int key_bits = 1;                                              // of vocab, the largest key
     while (p.vocab >> key_bits) ++key_bits;
     const int passes = (key_bits + kDigitBits - 1) / kDigitBits, bits = (key_bits + passes - 1) / passes;
     *in = 0;
-    if (p.count <= 2 * kSortThreads) return sort_in_lds<2>(p, bits, passes, g, clear, stream);
-    if (p.count <= 8 * kSortThreads) return sort_in_lds<8>(p, bits, passes, g, clear, stream);
-    if (p.count <= kLdsSort) return sort_in_lds<16>(p, bits, passes, g, clear, stream);
+    if (p.count <= 2 * kSortThreads) return sort_in_lds<2>(p, bits, passes, g, c, stream);
+    if (p.count <= 8 * kSortThreads) return sort_in_lds<8>(p, bits, passes, g, c, stream);
+    if (p.count <= kLdsSort) return sort_in_lds<16>(p, bits, passes, g, c, stream);
     SortArgs a{};
     a.tokens = p.tokens;
     a.count = p.count;
     a.vocab = p.vocab;
     a.tiles = (int32_t)ceil_div(p.count, kTile);
     a.counts = g.counts;
-    const dim3 grid((unsigned)a.tiles, (unsigned)p.n);
+    a.sort_blocks = (int64_t)p.n * a.tiles;
+    // each launch clears its share
+    int64_t launch = 0;
+    const auto grid = [&] {
+        a.clear = c;
+        a.clear.from = clears * launch / (2 * passes);
+        a.clear.to = clears * ++launch / (2 * passes);
+        return dim3((unsigned)a.sort_blocks + at_most(a.clear.to - a.clear.from, kManyBlocks));
+    };
     for (int pass = 0; pass < passes; ++pass, *in = 1 - *in) {
         a.key = g.key[*in];
         a.pos = g.pos[*in];
         a.key_out = g.key[1 - *in];
         a.pos_out = g.pos[1 - *in];
         a.digit = Digit{pass * bits, bits};
-        hipLaunchKernelGGL(sort_histogram_kernel, grid, dim3(kSortThreads), 0, stream, a);
-        hipLaunchKernelGGL(sort_scatter_kernel, grid, dim3(kSortThreads), 0, stream, a);
-    }
-    if (!p.accumulate) {
-        const int64_t words = ceil_div(p.vocab, 32);
-        hipLaunchKernelGGL(mark_named_kernel, dim3((unsigned)ceil_div(words, kMarkedWords), (unsigned)p.n), dim3(kThreads), 0, stream, g.key[*in], p.count, g.named,
-                           words);
+        dim3 blocks = grid();
+        hipLaunchKernelGGL(sort_histogram_kernel, blocks, dim3(kSortThreads), 0, stream, a);
+        blocks = grid();
+        hipLaunchKernelGGL(sort_scatter_kernel, blocks, dim3(kSortThreads), 0, stream, a);
     }
     return hipGetLastError();
 }
@@ -869,7 +827,7 @@ static hipError_t embed_grad_few(const EmbedGradArgs &p, hipStream_t stream) {
     const int64_t column_tiles = ceil_div(p.width, kWave * sum_columns<T>());
     FewArgs a{p, column_tiles, 0, 0, 0, 1};
     // a wavefront per entry, or more where that gives many thousand workgroups, each of which reads all of the worker's tokens
-    const int64_t each = ceil_div(p.count, kFewWaves), wanted = ceil_div(kFewBlocks, p.n * column_tiles);
+    const int64_t each = ceil_div(p.count, kFewWaves), wanted = ceil_div(kFewBlocks / 4, p.n * column_tiles);
     a.blocks_each = (int32_t)(each < wanted ? each : wanted);
     a.sum_blocks = p.n * column_tiles * a.blocks_each;
     const int64_t all = p.vocab * p.width;
@@ -890,30 +848,21 @@ hipError_t launch_embed_grad(const EmbedGradArgs &p, void *workspace, hipStream_
     GradSpace g;
     grad_layout(p.n, p.count, p.vocab, p.width, workspace, &g);
     int in = 0;
-    const bool cleared = clears_first(p);
-    const hipError_t st = sort_tokens(p, g, cleared, &in, stream);
+    const hipError_t st = sort_tokens(p, g, &in, stream);
     if (st != hipSuccess) return st;
     SumArgs s{};
     s.p = p;
     s.key = g.key[in];
     s.pos = g.pos[in];
-    s.named = g.named;
-    s.named_words = ceil_div(p.vocab, 32);
     s.partial = g.partial;
     s.chunk = chunk_entries(p.n, p.count, p.width);
     s.chunks = ceil_div(p.count, s.chunk);
     return with_type(p.type, [&](auto type) {
         typedef typename ValueOf<decltype(type)::value>::type T;
         s.column_tiles = ceil_div(p.width, kWave * sum_columns<T>());
-        s.sum_blocks = at_most(ceil_div((int64_t)p.n * s.chunks * s.column_tiles, kThreads / kWave), kManyBlocks);
-        const int64_t wanted = (16 << 10) / (4 * p.width);         // rows of some 16 KB in all: workgroups that run together write one stretch of memory
-        s.fill_rows = wanted < 4 ? 4 : wanted;
-        s.fill_blocks_per_worker = ceil_div(p.vocab, s.fill_rows);
-        const int64_t fill = p.accumulate || cleared ? 0 : at_most((int64_t)p.n * s.fill_blocks_per_worker, 8 * kManyBlocks);
-        const dim3 grid((unsigned)(s.sum_blocks + fill));
-        if (p.accumulate) hipLaunchKernelGGL((embed_grad_kernel<T, kAdd>), grid, dim3(kThreads), 0, stream, s);
-        else if (cleared) hipLaunchKernelGGL((embed_grad_kernel<T, kStore>), grid, dim3(kThreads), 0, stream, s);
-        else hipLaunchKernelGGL((embed_grad_kernel<T, kStoreAndFill>), grid, dim3(kThreads), 0, stream, s);
+        const dim3 grid(at_most(ceil_div((int64_t)p.n * s.chunks * s.column_tiles, kThreads / kWave), kManyBlocks));
+        if (p.accumulate) hipLaunchKernelGGL((embed_grad_kernel<T, true>), grid, dim3(kThreads), 0, stream, s);
+        else hipLaunchKernelGGL((embed_grad_kernel<T, false>), grid, dim3(kThreads), 0, stream, s);
         const int64_t tiles = ceil_div(p.width, kJoinColumns);
         const dim3 join(at_most((int64_t)p.n * (s.chunks - 1) * tiles, kManyBlocks));
         if (p.accumulate) hipLaunchKernelGGL((embed_grad_join_kernel<true>), join, dim3(kJoinThreads), 0, stream, s, tiles);
