@@ -239,8 +239,10 @@ struct ClearArgs {
 // By workgroup `block` of `blocks`.
 __device__ __forceinline__ void clear_blocks(const ClearArgs &c, int64_t block, int64_t blocks) {
     for (int64_t b = c.from + block; b < c.to; b += blocks) {
+        // whole lines of 128 bytes: behind the entries before a table's first one, which its first block clears too
         float *table = c.table + b / c.blocks_per_worker * c.stride;
-        const int64_t at = (b % c.blocks_per_worker * kSortThreads + threadIdx.x) * 4;
+        const int64_t before = (uint32_t)-(int32_t)((uintptr_t)table / sizeof(float)) % 32u, at = before + (b % c.blocks_per_worker * kSortThreads + threadIdx.x) * 4;
+        if (b % c.blocks_per_worker == 0 && threadIdx.x < before && threadIdx.x < c.entries) table[threadIdx.x] = 0.f;
         if (at + 4 <= c.entries) {
             store4_any(table + at, make_float4(0.f, 0.f, 0.f, 0.f));
         } else {
@@ -248,6 +250,8 @@ __device__ __forceinline__ void clear_blocks(const ClearArgs &c, int64_t block, 
         }
     }
 }
+
+__global__ __launch_bounds__(kSortThreads) void clear_kernel(ClearArgs c) { clear_blocks(c, blockIdx.x, gridDim.x); }
 
 // Workgroups 0 .. n - 1 sort; those behind them clear.
 template <int ITEMS>
@@ -550,8 +554,9 @@ __global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / kWave;
 constexpr int64_t kFewTokens = 4096;
 constexpr int64_t kFewBlocks = 4096;                               // workgroups that fill the chip several times over
-constexpr int64_t kFewStretch = 8 * kFewThreads, kFewMostStretch = 128 * kFewThreads;   // entries of a table: 16 KB, 256 KB
-constexpr uint32_t kFewHeavy = 32;                                 // from so many entries on a row is added by the whole workgroup
+constexpr int64_t kFewStretch = 8 * kFewThreads, kFewMostStretch = 64 * kFewThreads;   // entries of a table: 16 KB, 128 KB
+constexpr int64_t kFewClear = (int64_t)256 << 20;             // larger tables are cleared whole by a launch of their own
+constexpr uint32_t kFewHeavy = 16;                                 // from so many entries on a row is added by the whole workgroup
 
 struct FewArgs {
     EmbedGradArgs p;
@@ -623,15 +628,16 @@ __global__ __launch_bounds__(kFewThreads, 6) void embed_grad_few_kernel(FewArgs 
     float *table = p.table_grad + worker * p.worker_stride;
     volatile uint16_t *list = lists[wave_id()];
 
-    // what entries of the list name are added, the first `n`
-    auto add_listed = [&](int n, float(&acc)[N]) {
+    // adds the entries that the list names from `from` on, n <= 64
+    auto add_listed = [&](int from, int n, float(&acc)[N]) {
         __builtin_amdgcn_wave_barrier();
+        const int named = list[from + lane_id()];
         for (int i = 0; i < n; i += FLIGHT) {
             Held<T, N> f[FLIGHT];
 #pragma unroll
             for (int j = 0; j < FLIGHT; ++j) {
                 if (i + j >= n) break;
-                const int64_t at = __builtin_amdgcn_readfirstlane((int)list[i + j]);
+                const int64_t at = __builtin_amdgcn_readlane(named, i + j);
                 if (c.at >= 0) hold_columns<true>(grad + at * p.grad_stride, c, f[j]);
             }
 #pragma unroll
@@ -679,7 +685,7 @@ __global__ __launch_bounds__(kFewThreads, 6) void embed_grad_few_kernel(FewArgs 
         }
         float acc[N] = {}, old[N] = {};
         if (ADD && c.at >= 0) load_columns<true>(table + (int64_t)row * p.width, c, old);
-        add_listed(n, acc);
+        add_listed(0, n, acc);
         finish(row, acc, old);
     }
     __syncthreads();
@@ -694,7 +700,8 @@ __global__ __launch_bounds__(kFewThreads, 6) void embed_grad_few_kernel(FewArgs 
             if (hits >> lane_id() & 1u) list[n + lanes_below(hits)] = (uint16_t)(base + lane_id());
             n += (int)popc64(hits);
             if (n >= kWave || base + kWave >= stop) {
-                add_listed(n, acc);
+                add_listed(0, min(n, kWave), acc);
+                if (n > kWave) add_listed(kWave, n - kWave, acc);
                 n = 0;
             }
         }
@@ -726,7 +733,7 @@ int32_t chunk_entries(int32_t n, int64_t count, int64_t width) { return (int64_t
 
 // One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^25 of them.  (n, tokens, rows of 512 columns:
 // 2, 1374, 22283 of 64: 12 us, 30 by sorting; 1, 2117, 97230 of 33: 11 and 41; 14, 1033, 1327 of 1072, 2^25.4: 84 and 60.)
-bool few_tokens(int32_t n, int64_t count, int64_t width) { return count <= kFewTokens && n * count * count * ceil_div(width, 512) <= (int64_t)1 << 25; }
+bool few_tokens(int32_t n, int64_t count, int64_t width) { return count <= kFewTokens && n * count * count * ceil_div(width, 512) <= (int64_t)1 << 27; }
 
 size_t grad_layout(int32_t n, int64_t count, int64_t vocab, int64_t width, void *ws, GradSpace *out) {
     if (few_tokens(n, count, width)) return 256;                           // not used; never zero, so that callers need no case of their own for it
@@ -763,11 +770,17 @@ hipError_t sort_in_lds(const EmbedGradArgs &p, int bits, int passes, const GradS
     return hipGetLastError();
 }
 
-// Sorts, and clears the tables where they are not added to; *in: the buffer of g that holds the result.
-hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, int *in, hipStream_t stream) {
+// Clears nothing where the tables are added to.
+ClearArgs clear_args(const EmbedGradArgs &p) {
     ClearArgs c{p.table_grad, p.vocab * p.width, p.worker_stride, 0, 0, 0};
     if (!p.accumulate) c.blocks_per_worker = ceil_div(c.entries, 4 * kSortThreads);
-    const int64_t clears = c.to = p.n * c.blocks_per_worker;
+    c.to = p.n * c.blocks_per_worker;
+    return c;
+}
+
+// Sorts, and clears the tables where they are not added to; *in: the buffer of g that holds the result.
+hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, int *in, hipStream_t stream) {
+    const ClearArgs c = clear_args(p);
     int key_bits = 1;                                              // of vocab, the largest key
     while (p.vocab >> key_bits) ++key_bits;
     const int passes = (key_bits + kDigitBits - 1) / kDigitBits, bits = (key_bits + passes - 1) / passes;
@@ -786,8 +799,8 @@ hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, int *in, hipS
     int64_t launch = 0;
     const auto grid = [&] {
         a.clear = c;
-        a.clear.from = clears * launch / (2 * passes);
-        a.clear.to = clears * ++launch / (2 * passes);
+        a.clear.from = c.to * launch / (2 * passes);
+        a.clear.to = c.to * ++launch / (2 * passes);
         return dim3((unsigned)a.sort_blocks + at_most(a.clear.to - a.clear.from, kManyBlocks));
     };
     for (int pass = 0; pass < passes; ++pass, *in = 1 - *in) {
@@ -827,15 +840,22 @@ static hipError_t embed_grad_few(const EmbedGradArgs &p, hipStream_t stream) {
     const int64_t column_tiles = ceil_div(p.width, kWave * sum_columns<T>());
     FewArgs a{p, column_tiles, 0, 0, 0, 1};
     // a wavefront per entry, or more where that gives many thousand workgroups, each of which reads all of the worker's tokens
-    const int64_t each = ceil_div(p.count, kFewWaves), wanted = ceil_div(kFewBlocks / 4, p.n * column_tiles);
+    const int64_t each = ceil_div(p.count, kFewWaves), wanted = ceil_div(kFewBlocks, p.n * column_tiles);
     a.blocks_each = (int32_t)(each < wanted ? each : wanted);
     a.sum_blocks = p.n * column_tiles * a.blocks_each;
     const int64_t all = p.vocab * p.width;
     a.stretch = ceil_div(ceil_div(p.n * all, kFewBlocks), kFewStretch) * kFewStretch;
     if (a.stretch > kFewMostStretch) a.stretch = kFewMostStretch;
     a.stretches = ceil_div(all, a.stretch);
-    const int64_t blocks = a.sum_blocks + (p.accumulate ? 0 : p.n * a.stretches);
+    // large tables are cleared whole before
+    const bool clear = !p.accumulate, before = clear && 4 * p.n * all > kFewClear;
+    const int64_t blocks = a.sum_blocks + (clear && !before ? p.n * a.stretches : 0);
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (before) {
+        const ClearArgs c = clear_args(p);
+        hipLaunchKernelGGL(clear_kernel, dim3(at_most(c.to, kManyBlocks)), dim3(kSortThreads), 0, stream, c);
+    }
+    if (blocks == 0) return hipGetLastError();                     // no tokens
     if (p.accumulate) hipLaunchKernelGGL((embed_grad_few_kernel<T, true>), dim3((unsigned)blocks), dim3(kFewThreads), 0, stream, a);
     else hipLaunchKernelGGL((embed_grad_few_kernel<T, false>), dim3((unsigned)blocks), dim3(kFewThreads), 0, stream, a);
     return hipGetLastError();
