@@ -488,7 +488,8 @@ template <class T, bool ADD>
 __global__ __launch_bounds__(kThreads, EU) void embed_grad_kernel(SumArgs s) {
     const int64_t tasks = (int64_t)s.p.n * s.chunks * s.column_tiles;
     for (int64_t task = (int64_t)blockIdx.x * (kThreads / kWave) + wave_id(); task < tasks; task += (int64_t)gridDim.x * (kThreads / kWave)) {
-        const int64_t chunk = task / s.column_tiles;
+        // the last chunks, of rare tokens, cost the most where tables are added to, and go first
+        const int64_t chunk = (ADD ? tasks - 1 - task : task) / s.column_tiles;
         sum_chunk<T, ADD>(s, chunk / s.chunks, chunk % s.chunks, task % s.column_tiles);
     }
 }
@@ -728,8 +729,12 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kManyBlocks = 1 << 20;
 unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)(blocks < most ? blocks : most); }
 
-// Sorted entries of a chunk: 64 (fewer partial sums) where that gives wavefronts enough for the chip, else 16.
-int32_t chunk_entries(int32_t n, int64_t count, int64_t width) { return (int64_t)n * count * ceil_div(width, 512) / 64 >= 4096 ? 64 : 16; }
+// Sorted entries of a chunk: 64, or 32 (fewer partial sums), where that gives wavefronts enough for the chip, else 16.  (65536 bf16 tokens of 2048: 183 us with 64, 189
+// with 32, 197 with 16; 10 x 24784 of 406: 146 with 16, 135 with 32.)
+int32_t chunk_entries(int32_t n, int64_t count, int64_t width) {
+    const int64_t wavefronts = n * count * ceil_div(width, 512);
+    return wavefronts / 64 >= 4096 ? 64 : wavefronts / 32 >= 4096 ? 32 : 16;
+}
 
 // One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^25 of them.  (n, tokens, rows of 512 columns:
 // 2, 1374, 22283 of 64: 12 us, 30 by sorting; 1, 2117, 97230 of 33: 11 and 41; 14, 1033, 1327 of 1072, 2^25.4: 84 and 60.)

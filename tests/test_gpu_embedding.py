@@ -190,3 +190,47 @@ def test_gradient_beyond_32_bits(gpu):
             want = g[i].double()[tokens[i] == v].sum(0)
             assert torch.allclose(out[i, v].double(), want, rtol=1e-6, atol=1e-6)
         assert int(out[i].count_nonzero(dim=1).count_nonzero()) == len({int(t) for t in tokens[i] if t >= 0})
+
+
+@pytest.mark.parametrize("n,count,vocab,width,dtype,kind", [(5, 60000, 700, 8, "bf16", "zipf"), (3, 50000, 3001, 12, "f16", "zipf"), (3, 50000, 3001, 12, "f32", "uniform"),
+                                                            (2, 4000, 37, 16, "f32", "zipf"), (1, 4096, 5, 700, "bf16", "uniform"), (1, 4096, 90000, 9, "f16", "outside"),
+                                                            (2, 3000, 2, 5, "f32", "one"), (1, 16384, 131071, 16, "bf16", "zipf"), (1, 16385, 131072, 16, "bf16", "zipf")])
+def test_gradient_of_many_tokens(gpu, n, count, vocab, width, dtype, kind):
+    torch, b = gpu
+    print(f"embed_grad n={n} count={count} vocab={vocab} width={width} {dtype} {kind}", flush=True)
+    rng = np.random.default_rng(count + width)
+    tokens = token_sets(rng, kind, n, count, vocab)
+    g = torch.from_numpy(rng.standard_normal((n, count, width)).astype(np.float32)).to(lm.TORCH[dtype])
+    base = torch.from_numpy(rng.standard_normal((n, vocab, width)).astype(np.float32))
+    dt = torch.from_numpy(tokens).cuda()
+    for before in (None, base):
+        out = torch.full((n, vocab, width), math.nan, device="cuda") if before is None else before.cuda()
+        got = b.ef21_embed_grad(g.cuda(), dt, vocab, 0.75, out=out, accumulate=before is not None)
+        want, bound = lm.embed_grad(g.double().numpy(), tokens, vocab, 0.75, *([] if before is None else [before.numpy()]))
+        lm.inside(as64(got), want, bound, "gradient")
+
+
+@pytest.mark.parametrize("n,count,vocab,width,shift", [(3, 100, 30001, 1003, 1), (1, 4096, 70000, 1024, 0), (2, 9, 70000, 1024, 2), (3, 0, 30001, 1003, 3), (1, 20000, 30000, 2500, 5)])
+def test_gradient_of_large_tables(gpu, n, count, vocab, width, shift):
+    """Tables of more than 256 MB, at any alignment: each row is written, and nothing between the tables or around them."""
+    torch, b = gpu
+    print(f"embed_grad n={n} count={count} vocab={vocab} width={width} shift={shift}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(count + shift)
+    tokens = torch.randint(0, vocab, (n, count), device="cuda", generator=gen)
+    if count > 4:
+        tokens[:, 0], tokens[:, 1], tokens[:, 2] = 0, vocab - 1, -1
+    grad = torch.randn(n, count, width, device="cuda", generator=gen).mul_(8).round_()   # whole numbers: their sums are exact
+    stride = vocab * width + 7
+    flat = torch.full((n * stride + shift,), 3.5, device="cuda")
+    out = flat[shift:].as_strided((n, vocab, width), (stride, width, 1))
+    b.ef21_embed_grad(grad, tokens, vocab, out=out)
+    for i in range(n):
+        want = torch.zeros(vocab, width, device="cuda")
+        ok = tokens[i] >= 0
+        want.index_add_(0, tokens[i][ok], grad[i][ok])
+        assert torch.equal(out[i], want)
+        del want
+    assert bool((flat[:shift] == 3.5).all())
+    for i in range(n):
+        end = shift + i * stride + vocab * width
+        assert bool((flat[end:end + 7] == 3.5).all())
