@@ -1,9 +1,14 @@
 // Embedding lookup, out_t = scale table[token_t], and its gradient, G_i[v] = scale sum_{t : token_it = v} grad_it for worker i.
 //
+// Both are bound by memory: the lookup by the rows it reads and writes (81920 fp32 rows of 1024 to bf16, 503 MB through the chip: 56 us), the gradient by grad_out
+// and the table rows.
+//
 // The gradient goes by sorted tokens: every worker's positions are put in the order of their tokens, and of time within a
-// token, so that the sums have a fixed order.  A wavefront then adds kChunk consecutive entries of that order, whatever tokens they
-// belong to: how often one token occurs does not matter to the balance of the work.  A token that crosses the
-// end of a chunk leaves partial sums, which a last kernel adds in order.
+// token, so that the sums have a fixed order and need no atomics.  A wavefront then adds a chunk of consecutive entries of that order, whatever tokens they
+// belong to: how often one token occurs does not matter to the balance of the work.  A token of more than 64 entries that crosses the
+// end of a chunk leaves partial sums, which a last kernel adds in order.  The sort is a chain of round trips that leaves the memory idle, so the tables are
+// cleared beside it.  (65536 bf16 tokens of 2048, added to a table: 183 us, of which the sort 33, the sums 138 for 600 MB, the join 12; narrow rows are bound by instructions, since an entry costs a
+// wavefront the same whether 6 lanes have columns or 64: 7 x 20750 fp16 tokens of 46 77 us.)  Few tokens need no sort: embed_grad_few_kernel.
 #include "device_utils.h"
 #include "kernels.h"
 #include "lm.h"
@@ -402,10 +407,7 @@ constexpr int kShort = kWave;                                      // a token of
 // in the chunk and leaves a partial sum.  Eight rows of grad_out, and with ADD the rows that they are added to, are in flight.
 template <class T, bool ADD>
 __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int64_t chunk, int64_t column_tile) {
-    #ifndef FL
-#define FL 8
-#endif
-    constexpr int N = sum_columns<T>(), FLIGHT = FL;
+        constexpr int N = sum_columns<T>(), FLIGHT = 8;
     const EmbedGradArgs &p = s.p;
     const Columns c = columns_of<N>(column_tile * (kWave * N) + lane_id() * N, p.width);
     const uint32_t *key = s.key + worker * p.count, *pos = s.pos + worker * p.count;
@@ -481,11 +483,8 @@ __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int6
     }
 }
 
-#ifndef EU
-#define EU 4
-#endif
 template <class T, bool ADD>
-__global__ __launch_bounds__(kThreads, EU) void embed_grad_kernel(SumArgs s) {
+__global__ __launch_bounds__(kThreads, 4) void embed_grad_kernel(SumArgs s) {
     const int64_t tasks = (int64_t)s.p.n * s.chunks * s.column_tiles;
     for (int64_t task = (int64_t)blockIdx.x * (kThreads / kWave) + wave_id(); task < tasks; task += (int64_t)gridDim.x * (kThreads / kWave)) {
         // the last chunks, of rare tokens, cost the most where tables are added to, and go first
@@ -554,9 +553,11 @@ __global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s
 // these workgroups are others that clear stretches of the tables around the named rows.
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / kWave;
 constexpr int64_t kFewTokens = 4096;
-constexpr int64_t kFewBlocks = 4096;                               // workgroups that fill the chip several times over
+constexpr int64_t kFewResident = 3 * 256, kFewBlocks = 4096;        // workgroups that sum, that clear
 constexpr int64_t kFewStretch = 8 * kFewThreads, kFewMostStretch = 64 * kFewThreads;   // entries of a table: 16 KB, 128 KB
-constexpr int64_t kFewClear = (int64_t)256 << 20;             // larger tables are cleared whole by a launch of their own
+// Tables of more bytes in all are cleared whole by a launch of their own, in whole lines, and rows with a token written twice (12 x 66801 rows of 238, 763 MB: 149 us, 161 with the
+// clearing around the rows; 93318 rows of 432, 161 MB: 30 and 24).
+constexpr int64_t kFewClear = (int64_t)256 << 20;
 constexpr uint32_t kFewHeavy = 16;                                 // from so many entries on a row is added by the whole workgroup
 
 struct FewArgs {
@@ -736,12 +737,13 @@ int32_t chunk_entries(int32_t n, int64_t count, int64_t width) {
     return wavefronts / 64 >= 4096 ? 64 : wavefronts / 32 >= 4096 ? 32 : 16;
 }
 
-// One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^25 of them.  (n, tokens, rows of 512 columns:
-// 2, 1374, 22283 of 64: 12 us, 30 by sorting; 1, 2117, 97230 of 33: 11 and 41; 14, 1033, 1327 of 1072, 2^25.4: 84 and 60.)
+// One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^27 of them.  (us with and without, n x tokens into rows of width,
+// and the product's logarithm: 2 x 1374 into 22283 of 64, 21.9: 12 and 30; 4 x 2982 into 1389 of 160, 25.1: 20 and 45; 12 x 2470 into 47774 of 62, 26.1: 38 and 51;
+// 10 x 4208 into 1373 of 144, 27.4: 50 and 46; 18 x 4241 into 19653 of 98, 28.3: 98 and 60.)
 bool few_tokens(int32_t n, int64_t count, int64_t width) { return count <= kFewTokens && n * count * count * ceil_div(width, 512) <= (int64_t)1 << 27; }
 
 size_t grad_layout(int32_t n, int64_t count, int64_t vocab, int64_t width, void *ws, GradSpace *out) {
-    if (few_tokens(n, count, width)) return 256;                           // not used; never zero, so that callers need no case of their own for it
+    if (few_tokens(n, count, width)) return 256;                   // not used; never zero, so that callers need no case of their own for it
     char *at = static_cast<char *>(ws);
     size_t used = 0;
     auto take = [&](size_t bytes) {
@@ -844,8 +846,9 @@ template <class T>
 static hipError_t embed_grad_few(const EmbedGradArgs &p, hipStream_t stream) {
     const int64_t column_tiles = ceil_div(p.width, kWave * sum_columns<T>());
     FewArgs a{p, column_tiles, 0, 0, 0, 1};
-    // a wavefront per entry, or more where that gives many thousand workgroups, each of which reads all of the worker's tokens
-    const int64_t each = ceil_div(p.count, kFewWaves), wanted = ceil_div(kFewBlocks, p.n * column_tiles);
+    // a wavefront per entry, or more entries where not all workgroups would be on the chip at once, each of which reads all of the worker's tokens (8 x 2048 bf16
+    // tokens of 1024: 201 us with the clearing, 212 with a wavefront per entry)
+    const int64_t each = ceil_div(p.count, kFewWaves), wanted = ceil_div(kFewResident, p.n * column_tiles);
     a.blocks_each = (int32_t)(each < wanted ? each : wanted);
     a.sum_blocks = p.n * column_tiles * a.blocks_each;
     const int64_t all = p.vocab * p.width;
