@@ -493,56 +493,77 @@ __global__ __launch_bounds__(kThreads, 4) void embed_grad_kernel(SumArgs s) {
     }
 }
 
-// The tokens of more than kShort entries that begin in a chunk and go on behind it: their partial sums in order.  A workgroup per chunk and kJoinColumns columns; of a long run
-// each quarter of the workgroup takes a quarter.
+// The tokens of more than kShort entries that begin in a chunk and go on behind it: their partial sums in order.  A workgroup per GROUP chunks, which its lanes look at side by side, and
+// kJoinColumns columns; of a long run each quarter of the workgroup takes a quarter.
 constexpr int kJoinThreads = 512, kJoinParts = 4, kJoinColumns = kJoinThreads / kJoinParts * 4;
 
-template <bool ADD>
-__global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s, int64_t tiles) {
+template <bool ADD, int GROUP>
+__global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s, int64_t tiles, int64_t groups) {
     __shared__ float lds[kJoinParts][kJoinColumns];
     const EmbedGradArgs &p = s.p;
-    const int64_t tasks = (int64_t)p.n * (s.chunks - 1) * tiles;
+    const int64_t tasks = (int64_t)p.n * groups * tiles;
     for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
-        const int64_t tile = task % tiles, chunk = task / tiles % (s.chunks - 1), worker = task / tiles / (s.chunks - 1);
+        const int64_t tile = task % tiles, group = task / tiles % groups, worker = task / tiles / groups;
         const uint32_t *key = s.key + worker * p.count;
-        const int64_t first = chunk * s.chunk, end = first + s.chunk;
-        const uint32_t k = key[end - 1], behind = key[end], begin = key[first], before = first > 0 ? key[first - 1] : kNoKey;
-        const uint32_t k_here = lane_id() < s.chunk ? key[first + lane_id()] : kNoKey, k_behind = end + lane_id() < p.count ? key[end + lane_id()] : kNoKey;
-        if (k != behind || k == (uint32_t)p.vocab) continue;                              // ends here
-        if (begin == k && before == k) continue;                                          // began before
-        if (popc64(__ballot(k_here == k)) + popc64(__ballot(k_behind == k)) <= (uint32_t)kShort) continue;
-        const int64_t last = (end + wave_lower_bound(key + end, p.count - end, k + 1u) - 1) / s.chunk;   // the chunk it ends in
-        const int64_t run = last - chunk + 1, each = run <= 8 ? run : (run + kJoinParts - 1) / kJoinParts;
-        const int quarter = (int)threadIdx.x / (kJoinThreads / kJoinParts), column = (int)threadIdx.x % (kJoinThreads / kJoinParts) * 4;
-        const int64_t from = chunk + quarter * each, to = from + each < last + 1 ? from + each : last + 1;
-        const Columns c = columns_of<4>(tile * kJoinColumns + column, p.width);
-        const float *part = s.partial + worker * s.chunks * 2 * p.width;
-        float *out = p.table_grad + worker * p.worker_stride + (int64_t)k * p.width;
-        float acc[4] = {}, old[4] = {};
-        if (c.at >= 0) {
-            if (ADD && quarter == 0) load_columns<true>(out, c, old);
+        uint32_t k_last = kNoKey, k_here = kNoKey, k_behind = kNoKey;
+        const auto goes_on = [&](int64_t chunk) {
+            const int64_t first = chunk * s.chunk, end = first + s.chunk;
+            const uint32_t behind = key[end], begin = key[first], before = first > 0 ? key[first - 1] : kNoKey;
+            k_last = key[end - 1];
+            return k_last == behind && k_last != (uint32_t)p.vocab && !(begin == k_last && before == k_last);   // not: ends here, no token, began before
+        };
+        const auto look = [&](int64_t chunk) {
+            const int64_t first = chunk * s.chunk, end = first + s.chunk;
+            k_here = lane_id() < s.chunk ? key[first + lane_id()] : kNoKey;
+            k_behind = end + lane_id() < p.count ? key[end + lane_id()] : kNoKey;
+        };
+        uint64_t left = 0;
+        if constexpr (GROUP == 1) {
+            look(group);
+            left = goes_on(group);
+        } else {
+            const int64_t mine = group * GROUP + lane_id();
+            left = __ballot(lane_id() < GROUP && mine < s.chunks - 1 && goes_on(mine));
+        }
+        for (; left != 0; left &= left - 1u) {
+            const int which = __ffsll((long long)left) - 1;
+            const int64_t chunk = group * GROUP + which, end = chunk * s.chunk + s.chunk;
+            const uint32_t k = GROUP == 1 ? k_last : __builtin_amdgcn_readlane(k_last, which);
+            if (GROUP > 1) look(chunk);
+            if (popc64(__ballot(k_here == k)) + popc64(__ballot(k_behind == k)) <= (uint32_t)kShort) continue;
+            const int64_t last = (end + wave_lower_bound(key + end, p.count - end, k + 1u) - 1) / s.chunk;   // the chunk it ends in
+            const int64_t run = last - chunk + 1, each = run <= 8 ? run : (run + kJoinParts - 1) / kJoinParts;
+            const int quarter = (int)threadIdx.x / (kJoinThreads / kJoinParts), column = (int)threadIdx.x % (kJoinThreads / kJoinParts) * 4;
+            const int64_t from = chunk + quarter * each, to = from + each < last + 1 ? from + each : last + 1;
+            const Columns c = columns_of<4>(tile * kJoinColumns + column, p.width);
+            const float *part = s.partial + worker * s.chunks * 2 * p.width;
+            float *out = p.table_grad + worker * p.worker_stride + (int64_t)k * p.width;
+            float acc[4] = {}, old[4] = {};
+            if (c.at >= 0) {
+                if (ADD && quarter == 0) load_columns<true>(out, c, old);
 #pragma unroll 8
-            for (int64_t i = from; i < to; ++i) {
-                float f[4];
-                load_columns<true>(part + (2 * i + (i == chunk ? 1 : 0)) * p.width, c, f);
+                for (int64_t i = from; i < to; ++i) {
+                    float f[4];
+                    load_columns<true>(part + (2 * i + (i == chunk ? 1 : 0)) * p.width, c, f);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] += f[j];
+                    for (int j = 0; j < 4; ++j) acc[j] += f[j];
+                }
             }
-        }
-        if (each < run) {
-            __syncthreads();
+            if (each < run) {
+                __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) lds[quarter][column + j] = acc[j];
-            __syncthreads();
-            for (int w = 1; w < kJoinParts; ++w) {
+                for (int j = 0; j < 4; ++j) lds[quarter][column + j] = acc[j];
+                __syncthreads();
+                for (int w = 1; w < kJoinParts; ++w) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] += lds[w][column + j];
+                    for (int j = 0; j < 4; ++j) acc[j] += lds[w][column + j];
+                }
             }
-        }
-        if (quarter == 0 && c.at >= 0) {
+            if (quarter == 0 && c.at >= 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = ADD ? fmaf(p.scale, acc[j], old[j]) : p.scale * acc[j];
-            store_columns(out, c, acc, true);
+                for (int j = 0; j < 4; ++j) acc[j] = ADD ? fmaf(p.scale, acc[j], old[j]) : p.scale * acc[j];
+                store_columns(out, c, acc, true);
+            }
         }
     }
 }
@@ -892,9 +913,14 @@ hipError_t launch_embed_grad(const EmbedGradArgs &p, void *workspace, hipStream_
         if (p.accumulate) hipLaunchKernelGGL((embed_grad_kernel<T, true>), grid, dim3(kThreads), 0, stream, s);
         else hipLaunchKernelGGL((embed_grad_kernel<T, false>), grid, dim3(kThreads), 0, stream, s);
         const int64_t tiles = ceil_div(p.width, kJoinColumns);
-        const dim3 join(at_most((int64_t)p.n * (s.chunks - 1) * tiles, kManyBlocks));
-        if (p.accumulate) hipLaunchKernelGGL((embed_grad_join_kernel<true>), join, dim3(kJoinThreads), 0, stream, s, tiles);
-        else hipLaunchKernelGGL((embed_grad_join_kernel<false>), join, dim3(kJoinThreads), 0, stream, s, tiles);
+        if (s.chunks == 1) return hipGetLastError();
+        // four chunks to a workgroup where there are many, most of which leave nothing to join (13 x 9905 tokens of 112: 72 us, 79 with one; 65536 of 2048: 185 and 183)
+        const bool four = p.n * (s.chunks - 1) > 4096;
+        const int64_t groups = ceil_div(s.chunks - 1, four ? 4 : 1);
+        const dim3 join(at_most((int64_t)p.n * groups * tiles, kManyBlocks));
+        const auto kernel = p.accumulate ? (four ? embed_grad_join_kernel<true, 4> : embed_grad_join_kernel<true, 1>)
+                                         : (four ? embed_grad_join_kernel<false, 4> : embed_grad_join_kernel<false, 1>);
+        hipLaunchKernelGGL(kernel, join, dim3(kJoinThreads), 0, stream, s, tiles, groups);
         return hipGetLastError();
     });
 }

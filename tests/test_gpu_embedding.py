@@ -234,3 +234,17 @@ def test_gradient_of_large_tables(gpu, n, count, vocab, width, shift):
     for i in range(n):
         end = shift + i * stride + vocab * width
         assert bool((flat[end:end + 7] == 3.5).all())
+
+
+def test_gradient_of_very_many_workers(gpu):
+    """16 tokens of each of 65535 workers: one chunk of sorted entries a worker, and 4.3e9 entries of grad_out."""
+    torch, b = gpu
+    n, count, width = 65535, 16, 4100
+    grad = torch.empty(n, count, width, dtype=torch.bfloat16, device="cuda")
+    grad.random_(-8, 9, generator=torch.Generator(device="cuda").manual_seed(2))
+    tokens = torch.zeros(n, count, dtype=torch.int32, device="cuda")
+    tokens[::3, 5], tokens[7, :] = -1, 1                               # outside a vocabulary of one
+    got = b.ef21_embed_grad(grad, tokens, 1)
+    for i in range(0, n, 4096):
+        part = grad[i:i + 4096].float() * (tokens[i:i + 4096] == 0)[..., None]
+        assert torch.equal(got[i:i + 4096, 0], part.sum(1))
