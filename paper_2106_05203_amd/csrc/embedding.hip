@@ -117,7 +117,7 @@ __device__ __forceinline__ void store_columns(T *row, const Columns &c, const fl
 }
 
 // ---------------------------------------------------------------- lookup
-// A wavefront takes 64 N columns of kRows tokens, so that so many rows are in flight.
+// A wavefront takes 64 N columns of kLookupRows tokens, so that so many rows are in flight; the table is read with ordinary loads, since frequent rows are read again from the caches.
 constexpr int kLookupRows = 4;
 
 template <class TIN, class TOUT>
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs p, int64_t co
 
 // ---------------------------------------------------------------- sorting the positions by token
 // Stable radix sort of (token, position), digit by digit from the lowest.  Up to kLdsSort entries of a worker are sorted in the LDS of one
-// workgroup in one launch; more go tile by tile, a histogram and a scatter per digit.
+// workgroup in one launch (6423 tokens, two digits: 20 us, latency of 16 wavefronts); more go tile by tile, a histogram and a scatter per digit (65536: 33 us in four launches).
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kDigitBits = 9, kMostDigits = 1 << kDigitBits;
 constexpr int kLdsSort = 16 * kSortThreads;
@@ -404,10 +404,10 @@ constexpr int sum_columns() { return 16 / (int)sizeof(T); }        // columns of
 constexpr int kShort = kWave;                                      // a token of up to so many entries is added by one wavefront
 
 // The chunk's wavefront adds the tokens that begin in the chunk, those with at most kShort entries to their end.  Of a longer token it adds what lies
-// in the chunk and leaves a partial sum.  Eight rows of grad_out, and with ADD the rows that they are added to, are in flight.
+// in the chunk and leaves a partial sum.  FLIGHT rows of grad_out, and with ADD the rows that they are added to, are in flight.
 template <class T, bool ADD>
 __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int64_t chunk, int64_t column_tile) {
-        constexpr int N = sum_columns<T>(), FLIGHT = 8;
+    constexpr int N = sum_columns<T>(), FLIGHT = ADD ? 6 : 8;      // eight and the rows to add to would not fit the registers (184 us and 182 for 65536 bf16 tokens of 2048)
     const EmbedGradArgs &p = s.p;
     const Columns c = columns_of<N>(column_tile * (kWave * N) + lane_id() * N, p.width);
     const uint32_t *key = s.key + worker * p.count, *pos = s.pos + worker * p.count;

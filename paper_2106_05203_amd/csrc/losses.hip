@@ -2,10 +2,13 @@
 //
 // Preference: for pair p with the sequences 2p (preferred) and 2p + 1,
 //   D = S(2p) - S(2p + 1),  S = the sum, or the mean, of logp - ref over a sequence's labelled rows
-//   logistic       L = -(1 - e) log sigma(beta D) - e log sigma(-beta D),   dL/dD = beta (sigma(beta D) - (1 - e))
+//   logistic       L = -(1 - e) log sigma(beta D) - e log sigma(-beta D),   dL/dD = beta (e - sigma(-beta D))
 //   least squares  L = (D - 1 / (2 beta))^2,                                dL/dD = 2 (D - 1 / (2 beta))
 // The differences logp - ref are taken per token: sums of log-probabilities of long sequences are thousands and would keep
 // little of a margin near one in fp32.  Sums over sequences in 64 bits, in a fixed order.
+//
+// Both are bound by memory.  The preference loss reads the logits twice, since a pair's margin comes before any of its gradient: 16 pairs of 1024 rows of 32768 bf16, 12288 of
+// 16384 rows with a label, 1.88 GB through the memory: 439 us.  The policy loss reads them once, with the row held in registers: 8192 rows of 131072 bf16, 4 GB: 720 us.
 //
 // Policy, per token: q = exp(logp - old), L = -min(q A, clip(q) A) + kl (exp(o) - 1 - o), o = ref - logp.
 #include "token_rows.h"
@@ -37,25 +40,12 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyArgs &p, const Tok
     return t;
 }
 
-// Sums of V[] over the workgroup, the same bits in every thread.
-constexpr int kPairThreads = 1024;
-template <int N>
-__device__ void block_sums(double (&v)[N], double (*lds)[N]) {
+constexpr int kPairThreads = 1024, kPairWaves = kPairThreads / kWave;
+// Sums of v[] over groups of LANES lanes, in every lane.
+template <int LANES, int N>
+__device__ __forceinline__ void lane_sums(double (&v)[N]) {
 #pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o, kWave);
-    }
-    __syncthreads();
-    if (lane_id() == 0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) lds[wave_id()][i] = v[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lds[lane_id() % (kPairThreads / kWave)][i];
-#pragma unroll
-    for (int o = kPairThreads / kWave / 2; o > 0; o >>= 1) {
+    for (int o = LANES / 2; o > 0; o >>= 1) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o, kWave);
     }
@@ -66,11 +56,39 @@ struct PairTerms {
     int64_t at[3];
     float loss, chosen, other;
 };
+// lds: the wavefronts' sums; the pair's loss and its two coefficients are left in their place.  By one wavefront.
+__device__ __forceinline__ void pair_loss(const PairArgs &p, double weight, double (*lds)[4]) {
+    double v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = lds[lane_id() % kPairWaves][i];
+    lane_sums<kPairWaves>(v);
+    double per[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) per[side] = p.mean && v[2 * side + 1] > 0.0 ? 1.0 / v[2 * side + 1] : 1.0;
+    const double margin = v[0] * per[0] - v[2] * per[1], beta = (double)p.beta;
+    double loss, slope;
+    if (p.loss == 0) {                                               // EF21_LOSS_LOGISTIC
+        const double z = beta * margin, e = (double)p.smoothing, soft = log1p(exp(-fabs(z)));
+        loss = soft + (z < 0.0 ? (e - 1.0) * z : e > 0.0 ? e * z : 0.0);   // -(1 - e) log sigma(z) - e log sigma(-z), of infinite z too
+        slope = beta * (e - 1.0 / (1.0 + exp(z)));
+    } else {
+        const double off = margin - 0.5 / beta;
+        loss = off * off;
+        slope = 2.0 * off;
+    }
+    slope *= weight;
+    if (lane_id() == 0) {
+        lds[0][0] = loss;
+        lds[0][1] = slope * per[0];
+        lds[0][2] = -slope * per[1];
+    }
+}
 // By a workgroup; the same in every thread.  The two sequences' rows follow one another, so one pass takes both.
 __device__ __forceinline__ PairTerms pair_terms(const PairArgs &p, int64_t pair, double (*lds)[4]) {
     PairTerms t;
 #pragma unroll
     for (int i = 0; i < 3; ++i) t.at[i] = min(max(p.seq_start[2 * pair + i], i ? t.at[i ? i - 1 : 0] : (int64_t)0), p.rows);
+    const double weight = p.weight ? (double)p.weight[pair] : 1.0 / (double)p.pairs;
     double v[4] = {0.0, 0.0, 0.0, 0.0};                              // sum and count of the first sequence, of the second one
 #pragma unroll 4
     for (int64_t r = t.at[0] + threadIdx.x; r < t.at[2]; r += kPairThreads) {
@@ -83,30 +101,24 @@ __device__ __forceinline__ PairTerms pair_terms(const PairArgs &p, int64_t pair,
         v[2] += first ? 0.0 : d;
         v[3] += first ? 0.0 : one;
     }
-    block_sums<4>(v, lds);
-    double per[2];
+    // The wavefronts' sums; then the first wavefront alone forms the terms (all sixteen at it take 3 us longer).
+    lane_sums<kWave>(v);
+    __syncthreads();
+    if (lane_id() == 0) {
 #pragma unroll
-    for (int side = 0; side < 2; ++side) per[side] = p.mean && v[2 * side + 1] > 0.0 ? 1.0 / v[2 * side + 1] : 1.0;
-    const double margin = v[0] * per[0] - v[2] * per[1], beta = (double)p.beta;
-    double loss, slope;
-    if (p.loss == 0) {                                               // EF21_LOSS_LOGISTIC
-        const double z = beta * margin, e = (double)p.smoothing, soft = log1p(exp(-fabs(z)));
-        loss = (1.0 - e) * (soft + fmax(-z, 0.0)) + e * (soft + fmax(z, 0.0));
-        slope = beta * (1.0 / (1.0 + exp(-z)) - (1.0 - e));
-    } else {
-        const double off = margin - 0.5 / beta;
-        loss = off * off;
-        slope = 2.0 * off;
+        for (int i = 0; i < 4; ++i) lds[wave_id()][i] = v[i];
     }
-    slope *= p.weight ? (double)p.weight[pair] : 1.0 / (double)p.pairs;
-    t.loss = (float)loss;
-    t.chosen = (float)(slope * per[0]);
-    t.other = (float)(-slope * per[1]);
+    __syncthreads();
+    if (wave_id() == 0) pair_loss(p, weight, lds);
+    __syncthreads();
+    t.loss = (float)lds[0][0];
+    t.chosen = (float)lds[0][1];
+    t.other = (float)lds[0][2];
     return t;
 }
 
 __global__ __launch_bounds__(kPairThreads) void preference_pairs_kernel(PairArgs p) {
-    __shared__ double lds[kPairThreads / kWave][4];
+    __shared__ double lds[kPairWaves][4];
     for (int64_t pair = blockIdx.x; pair < p.pairs; pair += gridDim.x) {
         const PairTerms t = pair_terms(p, pair, lds);
         if (threadIdx.x == 0) p.out_loss[pair] = t.loss;
@@ -121,6 +133,8 @@ struct RowSpace {
 };
 
 // ---------------------------------------------------------------- the sums, and then the gradient
+// In launches of their own: parts of the rows small enough for the last cache, in turn, take longer (550 us for 490, 1 GB of logits), since each launch's tail of long rows
+// costs more than the second read.
 // POLICY: the tokens' losses and the rows' coefficients too; else the coefficient of a row in no pair.
 template <class T, int WAVES, bool POLICY>
 __global__ __launch_bounds__(Team<WAVES>::kBlock) void loss_forward_kernel(LogitRows in, PolicyArgs pol, float *logp_out, RowSpace out) {
@@ -185,7 +199,7 @@ __global__ __launch_bounds__(kGradThreads) void loss_grad_kernel(LogitRows in, R
 // pair's workgroups take the rows before it too, the last one's those behind it (coefficient 0).
 template <class T>
 __global__ __launch_bounds__(kPairThreads) void preference_few_kernel(LogitRows in, PairArgs p, RowSpace s, LogitGrad out, int32_t share, bool short_rows) {
-    __shared__ double lds[kPairThreads / kWave][4];
+    __shared__ double lds[kPairWaves][4];
     const int64_t pair = blockIdx.x / share, part = blockIdx.x % share;
     const PairTerms t = pair_terms(p, pair, lds);
     if (part == 0 && threadIdx.x == 0) p.out_loss[pair] = t.loss;
@@ -231,7 +245,8 @@ hipError_t loss_grad(const LogitRows &in, const RowSpace &s, const LogitGrad &ou
 
 // ---------------------------------------------------------------- the policy loss with the row held in registers
 // The row stays in the team's registers between the sum and the gradient, so it is read once: thread t holds the pieces t, t + TEAM, ..., and -inf
-// behind the last one.
+// behind the last one.  One row to a team in the order of the workgroups: 1 GB of bf16 logits of 8192, 16384, 32768 and 65536 columns 355, 362, 385 and 380 us; with persistent
+// workgroups that fetch the next row's pieces as they store the gradient 437, 395, 408 and 411.  131072 columns, 16 pieces: 415, two passes 518.
 template <class T, int WAVES, int PIECES>
 __global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void policy_held_kernel(LogitRows in, PolicyArgs pol, LogitGrad out) {
     typedef Team<WAVES> G;
@@ -322,7 +337,7 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void poli
 
 // out_loss = sum_r weight[r] token_loss[r] over the rows with a label, in 64 bits and in an order that the number of rows alone fixes: slices of
 // kSumSlice rows, a workgroup each, then the slices.
-constexpr int kSumThreads = 256, kSumRows = 16, kSumSlice = kSumThreads * kSumRows;
+constexpr int kSumThreads = 1024, kSumRows = 16, kSumSlice = kSumThreads * kSumRows;
 
 __device__ __forceinline__ double block_sum(double v, double *lds) {
 #pragma unroll
@@ -334,18 +349,28 @@ __device__ __forceinline__ double block_sum(double v, double *lds) {
     return v;
 }
 
-// sums nullptr: one slice, straight to out_loss.
+// sums nullptr: one slice, straight to out_loss.  All of a thread's rows are in flight; what belongs to a row without a label is read and not used (it may be NaN).
 __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(LogitRows in, const float *token_loss, const float *weight, double *sums, float *out_loss) {
     __shared__ double lds[kSumThreads / kWave];
     const int64_t first = (int64_t)blockIdx.x * kSumSlice + threadIdx.x;
     const float even = 1.f / (float)in.rows;
     float l[kSumRows], w[kSumRows];
+    bool has[kSumRows];
 #pragma unroll
     for (int i = 0; i < kSumRows; ++i) {
         const int64_t r = first + i * kSumThreads;
-        const bool has = r < in.rows && label_of(in, r) >= 0;
-        l[i] = has ? token_loss[r] : 0.f;
-        w[i] = !has ? 0.f : weight ? weight[r] : even;
+        l[i] = w[i] = 0.f;
+        has[i] = false;
+        if (r < in.rows) {
+            l[i] = token_loss[r];
+            w[i] = weight ? weight[r] : even;
+            has[i] = label_of(in, r) >= 0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kSumRows; ++i) {
+        l[i] = has[i] ? l[i] : 0.f;
+        w[i] = has[i] ? w[i] : 0.f;
     }
     double sum = 0.0;
 #pragma unroll

@@ -398,3 +398,31 @@ def test_rows_of_every_size_and_spread(gpu, vocab, dtype):
     over = x.clone()
     b.ef21_token_logps_grad(over, dl, lse, one, out=over)
     lm.inside(as64(over), g, bound, "gradient over the logits")
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.1])
+def test_preference_of_impossible_tokens(gpu, smoothing):
+    """A reply with a token of probability zero: the margin is infinite, and the loss and its gradient have their limits; margins at which the sigmoid is within
+    an ulp of one keep their slope."""
+    torch, b = gpu
+    vocab, far = 40, 34.0
+    x = torch.zeros(6, vocab, device="cuda")
+    labels = torch.tensor([3, 4, 5, 6, 7, 8], device="cuda")
+    x[1, 4] = -math.inf                                                # pair 0: the other reply is impossible, pair 1: the preferred one
+    x[2, 5] = -math.inf
+    ref = torch.full((6,), -math.log(vocab), device="cuda")
+    ref[1], ref[2] = -4.0, -4.0
+    ref[5] += far                                                      # pair 2: a margin of `far`
+    starts = torch.arange(7, device="cuda")
+    loss, logp, grad = b.ef21_preference_loss(x, labels, starts, ref, 1.0, smoothing=smoothing, pair_weight=torch.ones(3, device="cuda"))
+    want = [math.inf if smoothing else 0.0, math.inf, math.log1p(math.exp(-far)) + smoothing * far]
+    assert logp.tolist()[1] == -math.inf and logp.tolist()[2] == -math.inf
+    slope = [smoothing, smoothing - 1.0, smoothing - 1.0 / (1.0 + math.exp(far))]
+    for p in range(3):
+        assert loss[p].item() == pytest.approx(want[p], rel=1e-5)
+        for row, sign in ((2 * p, 1.0), (2 * p + 1, -1.0)):
+            prob = torch.softmax(x[row].double(), 0)
+            hot = torch.zeros(vocab, device="cuda", dtype=torch.float64)
+            hot[labels[row]] = 1.0
+            expect = sign * slope[p] * (hot - prob)
+            assert float((grad[row].double() - expect).abs().max()) <= 1e-5 * abs(slope[p])
