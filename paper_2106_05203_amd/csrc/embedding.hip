@@ -7,8 +7,8 @@
 // token, so that the sums have a fixed order and need no atomics.  A wavefront then adds a chunk of consecutive entries of that order, whatever tokens they
 // belong to: how often one token occurs does not matter to the balance of the work.  A token of more than 64 entries that crosses the
 // end of a chunk leaves partial sums, which a last kernel adds in order.  The sort is a chain of round trips that leaves the memory idle, so the tables are
-// cleared beside it.  (65536 bf16 tokens of 2048, added to a table: 183 us, of which the sort 33, the sums 138 for 600 MB, the join 12; narrow rows are bound by instructions, since an entry costs a
-// wavefront the same whether 6 lanes have columns or 64: 7 x 20750 fp16 tokens of 46 77 us.)  Few tokens need no sort: embed_grad_few_kernel.
+// cleared beside it.  (65536 bf16 tokens of 2048, added to a table: 176 us, of which the sort 28, the sums 140 for 600 MB, the join 12; narrow rows are bound by instructions, since an entry costs a
+// wavefront the same whether 6 lanes have columns or 64: 7 x 20750 fp16 tokens of 46 65 us.)  Few tokens need no sort: embed_grad_few_kernel.
 #include "device_utils.h"
 #include "kernels.h"
 #include "lm.h"
@@ -146,11 +146,14 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs p, int64_t co
 
 // ---------------------------------------------------------------- sorting the positions by token
 // Stable radix sort of (token, position), digit by digit from the lowest.  Up to kLdsSort entries of a worker are sorted in the LDS of one
-// workgroup in one launch (6423 tokens, two digits: 20 us, latency of 16 wavefronts); more go tile by tile, a histogram and a scatter per digit (65536: 33 us in four launches).
+// workgroup in one launch (10 x 2083 tokens of 2352: 88 us in all, 101 the other way; 15 x 6172 of 384: 72 and 79); more go tile by tile, a histogram and a scatter per digit
+// (13 x 9905 of 112: 64 us, 71 in LDS; 65536, two digits: 26 us in four launches, chains of round trips).
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kDigitBits = 9, kMostDigits = 1 << kDigitBits;
-constexpr int kLdsSort = 16 * kSortThreads;
-constexpr int kTileItems = 4, kTile = kTileItems * kSortThreads;
+constexpr int kLdsSort = 8 * kSortThreads;
+// Entries of a tile, in 1024: many small tiles leave each less to do one after the other, but every tile reads the counts of all.  (65536 tokens of 2048, us for 1, 2, 4: 176, 176, 183;
+// 50299 of 96: 60, 61, 69.)
+inline int tile_items(int64_t count) { return count <= 128 * kSortThreads ? 1 : count <= 2048 * kSortThreads ? 4 : 16; }
 constexpr uint32_t kNoKey = 0xffffffffu;                           // behind every key, in every digit
 
 // Key of a token: itself, or vocab (behind all others) where it is none.
@@ -313,79 +316,87 @@ struct SortArgs {
     uint32_t *counts;                                              // [n][tiles][kMostDigits]
     Digit digit;
     ClearArgs clear;
-    int64_t sort_blocks;                                           // n tiles; workgroups behind them clear
+    int64_t tasks;                                                 // n tiles
+    uint32_t sort_blocks;                                          // workgroups that take them in turn; those behind clear
     __device__ __forceinline__ bool clears() const {
         if (blockIdx.x < sort_blocks) return false;
         clear_blocks(clear, blockIdx.x - sort_blocks, gridDim.x - sort_blocks);
         return true;
     }
-    __device__ __forceinline__ int64_t worker() const { return blockIdx.x / (uint32_t)tiles; }
-    __device__ __forceinline__ int32_t tile() const { return (int32_t)(blockIdx.x % (uint32_t)tiles); }
 };
 __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int64_t first, int64_t at) {
     return a.digit.shift == 0 ? token_key(a.tokens, first + at, a.vocab) : a.key[first + at];
 }
 
+template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void sort_histogram_kernel(SortArgs a) {
     if (a.clears()) return;
     __shared__ uint32_t hist[kMostDigits];
-    const int64_t first = a.worker() * a.count, start = (int64_t)a.tile() * kTile;
-    if (threadIdx.x < kMostDigits) hist[threadIdx.x] = 0u;
-    __syncthreads();
-    uint32_t key[kTileItems];
+    for (int64_t task = blockIdx.x; task < a.tasks; task += a.sort_blocks) {
+        const int32_t tile = (int32_t)(task % a.tiles);
+        const int64_t worker = task / a.tiles, first = worker * a.count, start = (int64_t)tile * (ITEMS * kSortThreads);
+        if (threadIdx.x < kMostDigits) hist[threadIdx.x] = 0u;
+        __syncthreads();
+        uint32_t key[ITEMS];
 #pragma unroll
-    for (int i = 0; i < kTileItems; ++i) {
-        const int64_t at = start + i * kSortThreads + threadIdx.x;
-        key[i] = at < a.count ? sort_key(a, first, at) : kNoKey;
+        for (int i = 0; i < ITEMS; ++i) {
+            const int64_t at = start + i * kSortThreads + threadIdx.x;
+            key[i] = at < a.count ? sort_key(a, first, at) : kNoKey;
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+            if (start + i * kSortThreads + threadIdx.x < a.count) atomicAdd(&hist[a.digit.of(key[i])], 1u);
+        __syncthreads();
+        if (threadIdx.x < kMostDigits) a.counts[task * kMostDigits + threadIdx.x] = hist[threadIdx.x];
     }
-#pragma unroll
-    for (int i = 0; i < kTileItems; ++i)
-        if (start + i * kSortThreads + threadIdx.x < a.count) atomicAdd(&hist[a.digit.of(key[i])], 1u);
-    __syncthreads();
-    if (threadIdx.x < kMostDigits) a.counts[(int64_t)blockIdx.x * kMostDigits + threadIdx.x] = hist[threadIdx.x];
 }
 
+template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) {
     if (a.clears()) return;
     __shared__ SortShared s;
     __shared__ uint32_t goes[kMostDigits];
-    const int64_t first = a.worker() * a.count, start = (int64_t)a.tile() * kTile;
-    uint32_t key[kTileItems], rank[kTileItems], pos[kTileItems];
+    for (int64_t task = blockIdx.x; task < a.tasks; task += a.sort_blocks) {
+        const int32_t tile = (int32_t)(task % a.tiles);
+        const int64_t worker = task / a.tiles, first = worker * a.count, start = (int64_t)tile * (ITEMS * kSortThreads);
+        uint32_t key[ITEMS], rank[ITEMS], pos[ITEMS];
 #pragma unroll
-    for (int i = 0; i < kTileItems; ++i) {
-        const int64_t at = start + item_index<kTileItems>(i);
-        const bool in = at < a.count;
-        key[i] = in ? sort_key(a, first, at) : kNoKey;
-        pos[i] = !in ? 0u : a.digit.shift == 0 ? (uint32_t)at : a.pos[first + at];
-    }
-    // where the tile's entries of a digit go: behind all of lower digits, and those of the same digit in the tiles before
-    uint32_t total = 0u, earlier = 0u;
-    if (threadIdx.x < kMostDigits) {
-        const uint32_t *c = a.counts + a.worker() * a.tiles * kMostDigits + threadIdx.x;
-#pragma unroll 8
-        for (int t = 0; t < a.tiles; ++t) {
-            const uint32_t v = c[(int64_t)t * kMostDigits];
-            total += v;
-            if (t < a.tile()) earlier += v;
+        for (int i = 0; i < ITEMS; ++i) {
+            const int64_t at = start + item_index<ITEMS>(i);
+            const bool in = at < a.count;
+            key[i] = in ? sort_key(a, first, at) : kNoKey;
+            pos[i] = !in ? 0u : a.digit.shift == 0 ? (uint32_t)at : a.pos[first + at];
         }
-    }
-    const uint32_t sum = wave_inclusive_scan(total);
-    if (lane_id() == kWave - 1) s.wave_total[wave_id()] = sum;
-    __syncthreads();
-    if (threadIdx.x < kMostDigits) {
-        uint32_t low = 0u;
-        for (int w = 0; w < wave_id(); ++w) low += s.wave_total[w];
-        goes[threadIdx.x] = low + sum - total + earlier;
-    }
-    rank_items<kTileItems>(key, rank, a.digit, s);
-    scan_digits(s);
+        // where the tile's entries of a digit go: behind all of lower digits, and those of the same digit in the tiles before
+        uint32_t total = 0u, earlier = 0u;
+        if (threadIdx.x < kMostDigits) {
+            const uint32_t *c = a.counts + worker * a.tiles * kMostDigits + threadIdx.x;
+#pragma unroll 8
+            for (int t = 0; t < a.tiles; ++t) {
+                const uint32_t v = c[(int64_t)t * kMostDigits];
+                total += v;
+                if (t < tile) earlier += v;
+            }
+        }
+        const uint32_t sum = wave_inclusive_scan(total);
+        if (lane_id() == kWave - 1) s.wave_total[wave_id()] = sum;
+        __syncthreads();
+        if (threadIdx.x < kMostDigits) {
+            uint32_t low = 0u;
+            for (int w = 0; w < wave_id(); ++w) low += s.wave_total[w];
+            goes[threadIdx.x] = low + sum - total + earlier;
+        }
+        rank_items<ITEMS>(key, rank, a.digit, s);
+        scan_digits(s);
 #pragma unroll
-    for (int i = 0; i < kTileItems; ++i) {
-        if (start + item_index<kTileItems>(i) >= a.count) continue;
-        const uint32_t d = a.digit.of(key[i]);
-        const int64_t to = first + goes[d] + s.before[wave_id()][d] + rank[i];
-        a.key_out[to] = key[i];
-        a.pos_out[to] = pos[i];
+        for (int i = 0; i < ITEMS; ++i) {
+            if (start + item_index<ITEMS>(i) >= a.count) continue;
+            const uint32_t d = a.digit.of(key[i]);
+            const int64_t to = first + goes[d] + s.before[wave_id()][d] + rank[i];
+            a.key_out[to] = key[i];
+            a.pos_out[to] = pos[i];
+        }
+        __syncthreads();
     }
 }
 
@@ -761,7 +772,9 @@ int32_t chunk_entries(int32_t n, int64_t count, int64_t width) {
 // One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^27 of them.  (us with and without, n x tokens into rows of width,
 // and the product's logarithm: 2 x 1374 into 22283 of 64, 21.9: 12 and 30; 4 x 2982 into 1389 of 160, 25.1: 20 and 45; 12 x 2470 into 47774 of 62, 26.1: 38 and 51;
 // 10 x 4208 into 1373 of 144, 27.4: 50 and 46; 18 x 4241 into 19653 of 98, 28.3: 98 and 60.)
-bool few_tokens(int32_t n, int64_t count, int64_t width) { return count <= kFewTokens && n * count * count * ceil_div(width, 512) <= (int64_t)1 << 27; }
+bool few_tokens(int32_t n, int64_t count, int64_t width) {
+    return count == 0 || (count <= kFewTokens && n * count * count * ceil_div(width, 512) <= (int64_t)1 << 27 && n * ceil_div(width, 256) <= kManyBlocks);
+}
 
 size_t grad_layout(int32_t n, int64_t count, int64_t vocab, int64_t width, void *ws, GradSpace *out) {
     if (few_tokens(n, count, width)) return 256;                   // not used; never zero, so that callers need no case of their own for it
@@ -779,7 +792,7 @@ size_t grad_layout(int32_t n, int64_t count, int64_t vocab, int64_t width, void 
         g.key[i] = reinterpret_cast<uint32_t *>(take(entries * sizeof(uint32_t)));
         g.pos[i] = reinterpret_cast<uint32_t *>(take(entries * sizeof(uint32_t)));
     }
-    if (count > kLdsSort) g.counts = reinterpret_cast<uint32_t *>(take((size_t)n * (size_t)ceil_div(count, kTile) * kMostDigits * sizeof(uint32_t)));
+    if (count > kLdsSort) g.counts = reinterpret_cast<uint32_t *>(take((size_t)n * (size_t)ceil_div(count, tile_items(count) * kSortThreads) * kMostDigits * sizeof(uint32_t)));
     g.partial = reinterpret_cast<float *>(take((size_t)n * (size_t)ceil_div(count, chunk_entries(n, count, width)) * 2 * (size_t)width * sizeof(float)));
     if (out) *out = g;
     return used;
@@ -814,22 +827,25 @@ hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, int *in, hipS
     const int passes = (key_bits + kDigitBits - 1) / kDigitBits, bits = (key_bits + passes - 1) / passes;
     *in = 0;
     if (p.count <= 2 * kSortThreads) return sort_in_lds<2>(p, bits, passes, g, c, stream);
-    if (p.count <= 8 * kSortThreads) return sort_in_lds<8>(p, bits, passes, g, c, stream);
-    if (p.count <= kLdsSort) return sort_in_lds<16>(p, bits, passes, g, c, stream);
+    if (p.count <= kLdsSort) return sort_in_lds<8>(p, bits, passes, g, c, stream);
     SortArgs a{};
     a.tokens = p.tokens;
     a.count = p.count;
     a.vocab = p.vocab;
-    a.tiles = (int32_t)ceil_div(p.count, kTile);
+    const int items = tile_items(p.count);
+    const auto histogram = items == 1 ? sort_histogram_kernel<1> : items == 4 ? sort_histogram_kernel<4> : sort_histogram_kernel<16>;
+    const auto scatter = items == 1 ? sort_scatter_kernel<1> : items == 4 ? sort_scatter_kernel<4> : sort_scatter_kernel<16>;
+    a.tiles = (int32_t)ceil_div(p.count, items * kSortThreads);
     a.counts = g.counts;
-    a.sort_blocks = (int64_t)p.n * a.tiles;
+    a.tasks = (int64_t)p.n * a.tiles;
+    a.sort_blocks = at_most(a.tasks, kManyBlocks);
     // each launch clears its share
     int64_t launch = 0;
     const auto grid = [&] {
         a.clear = c;
         a.clear.from = c.to * launch / (2 * passes);
         a.clear.to = c.to * ++launch / (2 * passes);
-        return dim3((unsigned)a.sort_blocks + at_most(a.clear.to - a.clear.from, kManyBlocks));
+        return dim3(a.sort_blocks + at_most(a.clear.to - a.clear.from, kManyBlocks));
     };
     for (int pass = 0; pass < passes; ++pass, *in = 1 - *in) {
         a.key = g.key[*in];
@@ -838,9 +854,9 @@ hipError_t sort_tokens(const EmbedGradArgs &p, const GradSpace &g, int *in, hipS
         a.pos_out = g.pos[1 - *in];
         a.digit = Digit{pass * bits, bits};
         dim3 blocks = grid();
-        hipLaunchKernelGGL(sort_histogram_kernel, blocks, dim3(kSortThreads), 0, stream, a);
+        hipLaunchKernelGGL(histogram, blocks, dim3(kSortThreads), 0, stream, a);
         blocks = grid();
-        hipLaunchKernelGGL(sort_scatter_kernel, blocks, dim3(kSortThreads), 0, stream, a);
+        hipLaunchKernelGGL(scatter, blocks, dim3(kSortThreads), 0, stream, a);
     }
     return hipGetLastError();
 }
@@ -879,7 +895,6 @@ static hipError_t embed_grad_few(const EmbedGradArgs &p, hipStream_t stream) {
     // large tables are cleared whole before
     const bool clear = !p.accumulate, before = clear && 4 * p.n * all > kFewClear;
     const int64_t blocks = a.sum_blocks + (clear && !before ? p.n * a.stretches : 0);
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
     if (before) {
         const ClearArgs c = clear_args(p);
         hipLaunchKernelGGL(clear_kernel, dim3(at_most(c.to, kManyBlocks)), dim3(kSortThreads), 0, stream, c);

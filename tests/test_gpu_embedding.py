@@ -248,3 +248,27 @@ def test_gradient_of_very_many_workers(gpu):
     for i in range(0, n, 4096):
         part = grad[i:i + 4096].float() * (tokens[i:i + 4096] == 0)[..., None]
         assert torch.equal(got[i:i + 4096, 0], part.sum(1))
+    got.fill_(math.nan)
+    b.ef21_embed_grad(grad[:, :0], tokens[:, :0].contiguous(), 1, out=got)
+    assert int(got.count_nonzero()) == 0
+    del got, part
+    # so many columns that workgroups take several tiles' worth of tokens and of sums
+    got = b.ef21_embed_grad(grad.view(n, 1, count * width), tokens[:, :1].contiguous(), 1)
+    for i in range(0, n, 4096):
+        assert torch.equal(got[i:i + 4096, 0], grad[i:i + 4096].view(-1, count * width).float() * (tokens[i:i + 4096, :1] == 0))
+
+
+@pytest.mark.parametrize("n,count,vocab,width", [(2, 200001, 500, 4), (1, 131073, 262144, 3), (1, 2200000, 3000, 1), (3, 8193, 1 << 20, 2)])
+def test_gradient_sorted_in_tiles(gpu, n, count, vocab, width):
+    """Tiles of every size, and keys of one, two and three digits."""
+    torch, b = gpu
+    print(f"embed_grad n={n} count={count} vocab={vocab} width={width}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    tokens = (torch.rand(n, count, device="cuda", generator=gen).pow_(3) * (vocab + 1)).to(torch.int32) - 1
+    grad = torch.randint(-2, 3, (n, count, width), device="cuda", generator=gen).float()   # whole numbers: their sums are exact
+    got = b.ef21_embed_grad(grad, tokens, vocab)
+    for i in range(n):
+        ok = tokens[i] >= 0
+        assert torch.equal(got[i], torch.zeros(vocab, width, device="cuda").index_add_(0, tokens[i][ok].long(), grad[i][ok]))
+    again = b.ef21_embed_grad(grad, tokens, vocab, out=got.clone(), accumulate=True)
+    assert torch.equal(again, 2 * got)
