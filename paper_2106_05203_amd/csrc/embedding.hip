@@ -5,10 +5,10 @@
 //
 // The gradient goes by sorted tokens: every worker's positions are put in the order of their tokens, and of time within a
 // token, so that the sums have a fixed order and need no atomics.  A wavefront then adds a chunk of consecutive entries of that order, whatever tokens they
-// belong to: how often one token occurs does not matter to the balance of the work.  A token of more than 64 entries that crosses the
+// belong to: how often one token occurs does not matter to the balance of the work.  A token of many entries that crosses the
 // end of a chunk leaves partial sums, which a last kernel adds in order.  The sort is a chain of round trips that leaves the memory idle, so the tables are
-// cleared beside it.  (65536 bf16 tokens of 2048, added to a table: 176 us, of which the sort 28, the sums 140 for 600 MB, the join 12; narrow rows are bound by instructions, since an entry costs a
-// wavefront the same whether 6 lanes have columns or 64: 7 x 20750 fp16 tokens of 46 65 us.)  Few tokens need no sort: embed_grad_few_kernel.
+// cleared beside it.  (65536 bf16 tokens of 2048, added to a table: 176 us, of which the sort 28, the sums 140 for 600 MB, the join 12; short rows by latency,
+// since six launches of dependent round trips do little each: 50299 fp16 tokens into 104142 rows of 96 55 us.)  Few tokens need no sort: embed_grad_few_kernel.
 #include "device_utils.h"
 #include "kernels.h"
 #include "lm.h"
@@ -407,14 +407,13 @@ struct SumArgs {
     float *partial;                                                // [n][chunks][2][width]: what a chunk has of the token that it begins with, and of the last one
     int64_t chunks, column_tiles;
     int32_t chunk;                                                 // sorted entries that a wavefront adds, at most 64
+    int32_t whole;                                                 // a token of up to so many entries, at most 64, is added by one wavefront
 };
 
 template <class T>
 constexpr int sum_columns() { return 16 / (int)sizeof(T); }        // columns of a lane
 
-constexpr int kShort = kWave;                                      // a token of up to so many entries is added by one wavefront
-
-// The chunk's wavefront adds the tokens that begin in the chunk, those with at most kShort entries to their end.  Of a longer token it adds what lies
+// The chunk's wavefront adds the tokens that begin in the chunk, those with at most s.whole entries to their end.  Of a longer token it adds what lies
 // in the chunk and leaves a partial sum.  FLIGHT rows of grad_out, and with ADD the rows that they are added to, are in flight.
 template <class T, bool ADD>
 __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int64_t chunk, int64_t column_tile) {
@@ -446,12 +445,12 @@ __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int6
     int at = 0, stop = here;
     bool open = false;                                             // the first token is a long one that began before
     if (before > 0) {
-        open = before + lead + (lead == here ? behind : 0) > kShort;
+        open = before + lead + (lead == here ? behind : 0) > s.whole;
         if (!open) at = lead;                                      // the wavefront of the chunk that it began in adds it
     }
     const bool began_here = !(before > 0 && lead == here);
     const uint64_t ends = __ballot(k != k_next);                   // entries that are the last of their token
-    if (began_here && behind > 0 && tail + behind <= kShort) stop += behind;
+    if (began_here && behind > 0 && tail + behind <= s.whole) stop += behind;
     float acc[N] = {};
     while (at < stop) {
         Held<T, N> f[FLIGHT];
@@ -504,7 +503,7 @@ __global__ __launch_bounds__(kThreads, 4) void embed_grad_kernel(SumArgs s) {
     }
 }
 
-// The tokens of more than kShort entries that begin in a chunk and go on behind it: their partial sums in order.  A workgroup per GROUP chunks, which its lanes look at side by side, and
+// The tokens of more than s.whole entries that begin in a chunk and go on behind it: their partial sums in order.  A workgroup per GROUP chunks, which its lanes look at side by side, and
 // kJoinColumns columns; of a long run each quarter of the workgroup takes a quarter.
 constexpr int kJoinThreads = 512, kJoinParts = 4, kJoinColumns = kJoinThreads / kJoinParts * 4;
 
@@ -541,7 +540,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s
             const int64_t chunk = group * GROUP + which, end = chunk * s.chunk + s.chunk;
             const uint32_t k = GROUP == 1 ? k_last : __builtin_amdgcn_readlane(k_last, which);
             if (GROUP > 1) look(chunk);
-            if (popc64(__ballot(k_here == k)) + popc64(__ballot(k_behind == k)) <= (uint32_t)kShort) continue;
+            if (popc64(__ballot(k_here == k)) + popc64(__ballot(k_behind == k)) <= (uint32_t)s.whole) continue;
             const int64_t last = (end + wave_lower_bound(key + end, p.count - end, k + 1u) - 1) / s.chunk;   // the chunk it ends in
             const int64_t run = last - chunk + 1, each = run <= 8 ? run : (run + kJoinParts - 1) / kJoinParts;
             const int quarter = (int)threadIdx.x / (kJoinThreads / kJoinParts), column = (int)threadIdx.x % (kJoinThreads / kJoinParts) * 4;
@@ -920,6 +919,7 @@ hipError_t launch_embed_grad(const EmbedGradArgs &p, void *workspace, hipStream_
     s.pos = g.pos[in];
     s.partial = g.partial;
     s.chunk = chunk_entries(p.n, p.count, p.width);
+    s.whole = 2 * s.chunk < kWave ? 2 * s.chunk : kWave;           // (2 x 25249 tokens of 392, chunks of 16: 55 us with 32 or 16, 62 with 64; 10 x 24784 of 406, of 32: 128 with 64, 132 with 32)
     s.chunks = ceil_div(p.count, s.chunk);
     return with_type(p.type, [&](auto type) {
         typedef typename ValueOf<decltype(type)::value>::type T;
