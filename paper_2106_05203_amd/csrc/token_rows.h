@@ -132,7 +132,13 @@ struct RowStat {
         constexpr double kLn2 = 0.69314718055994530942;
         return empty() ? -INFINITY : large() ? (float)((double)m + kLn2 * (double)l) : (float)((2.0 * (double)m + (double)l) * kLn2);
     }
-    __device__ float log_prob(float x) const { return empty() ? -INFINITY : (z(x) - l) * 0.693147181f; }
+    // Once a row, in 64 bits: z, z - l and the product with ln 2 would each round at the size of log p (rms error 3.3e-7, so 2.0e-7, on rows of 131072).
+    __device__ float log_prob(float x) const {
+        constexpr double kLn2 = 0.69314718055994530942;
+        if (empty()) return -INFINITY;
+        const double from = large() ? ((double)x - (double)m) * (double)kLog2E : fma((double)x, (double)kLog2E, -2.0 * (double)m);
+        return (float)((from - (double)l) * kLn2);
+    }
     // of a row whose lse is known, |lse| < 10^6
     static __device__ RowStat of(float lse) {
         const double both = (double)lse * 1.44269504088896340736;
