@@ -1,14 +1,15 @@
 // Embedding lookup, out_t = scale table[token_t], and its gradient, G_i[v] = scale sum_{t : token_it = v} grad_it for worker i.
 //
-// Both are bound by memory: the lookup by the rows it reads and writes (81920 fp32 rows of 1024 to bf16, 503 MB through the chip: 56 us), the gradient by grad_out
-// and the table rows.
+// Both are bound by memory: the lookup by the rows it reads and writes (81920 fp32 rows of 1024 to bf16, 503 MB through the chip: 56 us), the
+// gradient by grad_out and the table rows.
 //
-// The gradient goes by sorted tokens: every worker's positions are put in the order of their tokens, and of time within a
-// token, so that the sums have a fixed order and need no atomics.  A wavefront then adds a chunk of consecutive entries of that order, whatever tokens they
-// belong to: how often one token occurs does not matter to the balance of the work.  A token of many entries that crosses the
-// end of a chunk leaves partial sums, which a last kernel adds in order.  The sort is a chain of round trips that leaves the memory idle, so the tables are
-// cleared beside it.  (65536 bf16 tokens of 2048, added to a table: 176 us, of which the sort 28, the sums 140 for 600 MB, the join 12; short rows by latency,
-// since six launches of dependent round trips do little each: 50299 fp16 tokens into 104142 rows of 96 55 us.)  Few tokens need no sort: embed_grad_few_kernel.
+// The gradient goes by sorted tokens: every worker's positions are put in the order of their tokens, and of time within a token, so that the
+// sums have a fixed order and need no atomics.  A wavefront then adds a chunk of consecutive entries of that order, whatever tokens they
+// belong to: how often one token occurs does not matter to the balance of the work.  A token of many entries that crosses the end of a chunk
+// leaves partial sums, which a last kernel adds in order.  The sort is a chain of round trips that leaves the memory idle, so the tables are
+// cleared beside it.  (65536 bf16 tokens of 2048, added to a table: 176 us, of which the sort 28, the sums 140 for 600 MB, the join 12; short
+// rows by latency, since six launches of dependent round trips do little each: 50299 fp16 tokens into 104142 rows of 96 55 us.)  Few tokens
+// need no sort: embed_grad_few_kernel.
 #include "device_utils.h"
 #include "kernels.h"
 #include "lm.h"
@@ -117,7 +118,8 @@ __device__ __forceinline__ void store_columns(T *row, const Columns &c, const fl
 }
 
 // ---------------------------------------------------------------- lookup
-// A wavefront takes 64 N columns of kLookupRows tokens, so that so many rows are in flight; the table is read with ordinary loads, since frequent rows are read again from the caches.
+// A wavefront takes 64 N columns of kLookupRows tokens, so that so many rows are in flight; the table is read with ordinary loads, since
+// frequent rows are read again from the caches.
 constexpr int kLookupRows = 4;
 
 template <class TIN, class TOUT>
@@ -146,13 +148,13 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs p, int64_t co
 
 // ---------------------------------------------------------------- sorting the positions by token
 // Stable radix sort of (token, position), digit by digit from the lowest.  Up to kLdsSort entries of a worker are sorted in the LDS of one
-// workgroup in one launch (10 x 2083 tokens of 2352: 88 us in all, 101 the other way; 15 x 6172 of 384: 72 and 79); more go tile by tile, a histogram and a scatter per digit
-// (13 x 9905 of 112: 64 us, 71 in LDS; 65536, two digits: 26 us in four launches, chains of round trips).
+// workgroup in one launch (10 x 2083 tokens of 2352: 88 us in all, 101 the other way; 15 x 6172 of 384: 72 and 79); more go tile by tile, a
+// histogram and a scatter per digit (13 x 9905 of 112: 64 us, 71 in LDS; 65536, two digits: 26 us in four launches, chains of round trips).
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kDigitBits = 9, kMostDigits = 1 << kDigitBits;
 constexpr int kLdsSort = 8 * kSortThreads;
-// Entries of a tile, in 1024: many small tiles leave each less to do one after the other, but every tile reads the counts of all.  (65536 tokens of 2048, us for 1, 2, 4: 176, 176, 183;
-// 50299 of 96: 60, 61, 69.)
+// Entries of a tile, in 1024: many small tiles leave each less to do one after the other, but every tile reads the counts of all.  (65536
+// tokens of 2048, us for 1, 2, 4: 176, 176, 183; 50299 of 96: 60, 61, 69.)
 inline int tile_items(int64_t count) { return count <= 128 * kSortThreads ? 1 : count <= 2048 * kSortThreads ? 4 : 16; }
 constexpr uint32_t kNoKey = 0xffffffffu;                           // behind every key, in every digit
 
@@ -404,7 +406,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs a) 
 struct SumArgs {
     EmbedGradArgs p;
     const uint32_t *key, *pos;                                     // [n][count], sorted
-    float *partial;                                                // [n][chunks][2][width]: what a chunk has of the token that it begins with, and of the last one
+    // [n][chunks][2][width]: what a chunk has of the token that it begins with, and of the last one
+    float *partial;
     int64_t chunks, column_tiles;
     int32_t chunk;                                                 // sorted entries that a wavefront adds, at most 64
     int32_t whole;                                                 // a token of up to so many entries, at most 64, is added by one wavefront
@@ -413,11 +416,12 @@ struct SumArgs {
 template <class T>
 constexpr int sum_columns() { return 16 / (int)sizeof(T); }        // columns of a lane
 
-// The chunk's wavefront adds the tokens that begin in the chunk, those with at most s.whole entries to their end.  Of a longer token it adds what lies
-// in the chunk and leaves a partial sum.  FLIGHT rows of grad_out, and with ADD the rows that they are added to, are in flight.
+// The chunk's wavefront adds the tokens that begin in the chunk, those with at most s.whole entries to their end.  Of a longer token it adds
+// what lies in the chunk and leaves a partial sum.  FLIGHT rows of grad_out, and with ADD the rows that they are added to, are in flight.
 template <class T, bool ADD>
 __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int64_t chunk, int64_t column_tile) {
-    constexpr int N = sum_columns<T>(), FLIGHT = ADD ? 6 : 8;      // eight and the rows to add to would not fit the registers (184 us and 182 for 65536 bf16 tokens of 2048)
+    // eight and the rows to add to would not fit the registers (184 us and 182 for 65536 bf16 tokens of 2048)
+    constexpr int N = sum_columns<T>(), FLIGHT = ADD ? 6 : 8;
     const EmbedGradArgs &p = s.p;
     const Columns c = columns_of<N>(column_tile * (kWave * N) + lane_id() * N, p.width);
     const uint32_t *key = s.key + worker * p.count, *pos = s.pos + worker * p.count;
@@ -439,7 +443,8 @@ __device__ __forceinline__ void sum_chunk(const SumArgs &s, int64_t worker, int6
         q_behind = pos[mine + here];
     }
     const uint32_t k_first = __builtin_amdgcn_readfirstlane(k), k_last = __builtin_amdgcn_readlane(k, here - 1);
-    // entries of the first token before the chunk and of the last one behind it (at most 64 of each are looked at), and of the first one in the chunk
+    // entries of the first token before the chunk and of the last one behind it (at most 64 of each are looked at), and of the first one in
+    // the chunk
     const int before = (int)popc64(__ballot(k_before == k_first)), behind = (int)popc64(__ballot(k_behind == k_last));
     const int lead = (int)popc64(__ballot(k == k_first)), tail = (int)popc64(__ballot(k == k_last));
     int at = 0, stop = here;
@@ -503,8 +508,8 @@ __global__ __launch_bounds__(kThreads, 4) void embed_grad_kernel(SumArgs s) {
     }
 }
 
-// The tokens of more than s.whole entries that begin in a chunk and go on behind it: their partial sums in order.  A workgroup per GROUP chunks, which its lanes look at side by side, and
-// kJoinColumns columns; of a long run each quarter of the workgroup takes a quarter.
+// The tokens of more than s.whole entries that begin in a chunk and go on behind it: their partial sums in order.  A workgroup per GROUP
+// chunks, which its lanes look at side by side, and kJoinColumns columns; of a long run each quarter of the workgroup takes a quarter.
 constexpr int kJoinThreads = 512, kJoinParts = 4, kJoinColumns = kJoinThreads / kJoinParts * 4;
 
 template <bool ADD, int GROUP>
@@ -520,7 +525,8 @@ __global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s
             const int64_t first = chunk * s.chunk, end = first + s.chunk;
             const uint32_t behind = key[end], begin = key[first], before = first > 0 ? key[first - 1] : kNoKey;
             k_last = key[end - 1];
-            return k_last == behind && k_last != (uint32_t)p.vocab && !(begin == k_last && before == k_last);   // not: ends here, no token, began before
+            // not: ends here, no token, began before
+            return k_last == behind && k_last != (uint32_t)p.vocab && !(begin == k_last && before == k_last);
         };
         const auto look = [&](int64_t chunk) {
             const int64_t first = chunk * s.chunk, end = first + s.chunk;
@@ -579,22 +585,23 @@ __global__ __launch_bounds__(kJoinThreads) void embed_grad_join_kernel(SumArgs s
 }
 
 // ---------------------------------------------------------------- few tokens
-// One launch without a sort.  A workgroup has all of its worker's tokens in its LDS; a wavefront takes an entry and, if it is the first that names its row, looks through
-// the others and adds them in order.  A token of many entries is added by the whole workgroup, each wavefront those of a stretch of time.  Behind
-// these workgroups are others that clear stretches of the tables around the named rows.
+// One launch without a sort.  A workgroup has all of its worker's tokens in its LDS; a wavefront takes an entry and, if it is the first that
+// names its row, looks through the others and adds them in order.  A token of many entries is added by the whole workgroup, each wavefront
+// those of a stretch of time.  Behind these workgroups are others that clear stretches of the tables around the named rows.
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / kWave;
 constexpr int64_t kFewTokens = 4096;
 constexpr int64_t kFewResident = 3 * 256, kFewBlocks = 4096;        // workgroups that sum, that clear
 constexpr int64_t kFewStretch = 8 * kFewThreads, kFewMostStretch = 64 * kFewThreads;   // entries of a table: 16 KB, 128 KB
-// Tables of more bytes in all are cleared whole by a launch of their own, in whole lines, and rows with a token written twice (12 x 66801 rows of 238, 763 MB: 149 us, 161 with the
-// clearing around the rows; 93318 rows of 432, 161 MB: 30 and 24).
+// Tables of more bytes in all are cleared whole by a launch of their own, in whole lines, and rows with a token written twice (12 x 66801 rows
+// of 238, 763 MB: 149 us, 161 with the clearing around the rows; 93318 rows of 432, 161 MB: 30 and 24).
 constexpr int64_t kFewClear = (int64_t)256 << 20;
 constexpr uint32_t kFewHeavy = 16;                                 // from so many entries on a row is added by the whole workgroup
 
 struct FewArgs {
     EmbedGradArgs p;
     int64_t column_tiles, sum_blocks;
-    int32_t blocks_each;                                           // workgroups of a worker and column tile: entry t is taken by number t mod blocks_each
+    // workgroups of a worker and column tile: entry t is taken by number t mod blocks_each
+    int32_t blocks_each;
     int64_t stretch, stretches;                                    // entries of a table that a workgroup clears; so many a worker
 };
 
@@ -761,16 +768,17 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kManyBlocks = 1 << 20;
 unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)(blocks < most ? blocks : most); }
 
-// Sorted entries of a chunk: 64, or 32 (fewer partial sums), where that gives wavefronts enough for the chip, else 16.  (65536 bf16 tokens of 2048: 183 us with 64, 189
-// with 32, 197 with 16; 10 x 24784 of 406: 146 with 16, 135 with 32.)
+// Sorted entries of a chunk: 64, or 32 (fewer partial sums), where that gives wavefronts enough for the chip, else 16.  (65536 bf16 tokens of
+// 2048: 183 us with 64, 189 with 32, 197 with 16; 10 x 24784 of 406: 146 with 16, 135 with 32.)
 int32_t chunk_entries(int32_t n, int64_t count, int64_t width) {
     const int64_t wavefronts = n * count * ceil_div(width, 512);
     return wavefronts / 64 >= 4096 ? 64 : wavefronts / 32 >= 4096 ? 32 : 16;
 }
 
-// One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^27 of them.  (us with and without, n x tokens into rows of width,
-// and the product's logarithm: 2 x 1374 into 22283 of 64, 21.9: 12 and 30; 4 x 2982 into 1389 of 160, 25.1: 20 and 45; 12 x 2470 into 47774 of 62, 26.1: 38 and 51;
-// 10 x 4208 into 1373 of 144, 27.4: 50 and 46; 18 x 4241 into 19653 of 98, 28.3: 98 and 60.)
+// One launch without a sort, whose wavefronts together look through n count^2 tokens for each 512 columns: up to 2^27 of them.  (us with and
+// without, n x tokens into rows of width, and the product's logarithm: 2 x 1374 into 22283 of 64, 21.9: 12 and 30; 4 x 2982 into 1389 of 160,
+// 25.1: 20 and 45; 12 x 2470 into 47774 of 62, 26.1: 38 and 51; 10 x 4208 into 1373 of 144, 27.4: 50 and 46; 18 x 4241 into 19653 of 98, 28.3:
+// 98 and 60.)
 bool few_tokens(int32_t n, int64_t count, int64_t width) {
     return count == 0 || (count <= kFewTokens && n * count * count * ceil_div(width, 512) <= (int64_t)1 << 27 && n * ceil_div(width, 256) <= kManyBlocks);
 }
@@ -882,8 +890,8 @@ template <class T>
 static hipError_t embed_grad_few(const EmbedGradArgs &p, hipStream_t stream) {
     const int64_t column_tiles = ceil_div(p.width, kWave * sum_columns<T>());
     FewArgs a{p, column_tiles, 0, 0, 0, 1};
-    // a wavefront per entry, or more entries where not all workgroups would be on the chip at once, each of which reads all of the worker's tokens (8 x 2048 bf16
-    // tokens of 1024: 201 us with the clearing, 212 with a wavefront per entry)
+    // a wavefront per entry, or more entries where not all workgroups would be on the chip at once, each of which reads all of the worker's
+    // tokens (8 x 2048 bf16 tokens of 1024: 201 us with the clearing, 212 with a wavefront per entry)
     const int64_t each = ceil_div(p.count, kFewWaves), wanted = ceil_div(kFewResident, p.n * column_tiles);
     a.blocks_each = (int32_t)(each < wanted ? each : wanted);
     a.sum_blocks = p.n * column_tiles * a.blocks_each;
@@ -919,7 +927,8 @@ hipError_t launch_embed_grad(const EmbedGradArgs &p, void *workspace, hipStream_
     s.pos = g.pos[in];
     s.partial = g.partial;
     s.chunk = chunk_entries(p.n, p.count, p.width);
-    s.whole = 2 * s.chunk < kWave ? 2 * s.chunk : kWave;           // (2 x 25249 tokens of 392, chunks of 16: 55 us with 32 or 16, 62 with 64; 10 x 24784 of 406, of 32: 128 with 64, 132 with 32)
+    // (2 x 25249 tokens of 392, chunks of 16: 55 us with 32 or 16, 62 with 64; 10 x 24784 of 406, of 32: 128 with 64, 132 with 32)
+    s.whole = 2 * s.chunk < kWave ? 2 * s.chunk : kWave;
     s.chunks = ceil_div(p.count, s.chunk);
     return with_type(p.type, [&](auto type) {
         typedef typename ValueOf<decltype(type)::value>::type T;
@@ -929,7 +938,8 @@ hipError_t launch_embed_grad(const EmbedGradArgs &p, void *workspace, hipStream_
         else hipLaunchKernelGGL((embed_grad_kernel<T, false>), grid, dim3(kThreads), 0, stream, s);
         const int64_t tiles = ceil_div(p.width, kJoinColumns);
         if (s.chunks == 1) return hipGetLastError();
-        // four chunks to a workgroup where there are many, most of which leave nothing to join (13 x 9905 tokens of 112: 72 us, 79 with one; 65536 of 2048: 185 and 183)
+        // four chunks to a workgroup where there are many, most of which leave nothing to join (13 x 9905 tokens of 112: 72 us, 79 with one;
+        // 65536 of 2048: 185 and 183)
         const bool four = p.n * (s.chunks - 1) > 4096;
         const int64_t groups = ceil_div(s.chunks - 1, four ? 4 : 1);
         const dim3 join(at_most((int64_t)p.n * groups * tiles, kManyBlocks));

@@ -7,8 +7,9 @@
 // The differences logp - ref are taken per token: sums of log-probabilities of long sequences are thousands and would keep
 // little of a margin near one in fp32.  Sums over sequences in 64 bits, in a fixed order.
 //
-// Both are bound by memory.  The preference loss reads the logits twice, since a pair's margin comes before any of its gradient: 16 pairs of 1024 rows of 32768 bf16, 12288 of
-// 16384 rows with a label, 1.88 GB through the memory: 439 us.  The policy loss reads them once, with the row held in registers: 8192 rows of 131072 bf16, 4 GB: 720 us.
+// Both are bound by memory.  The preference loss reads the logits twice, since a pair's margin comes before any of its gradient: 16 pairs of
+// 1024 rows of 32768 bf16, 12288 of 16384 rows with a label, 1.88 GB through the memory: 439 us.  The policy loss reads them once, with the
+// row held in registers: 8192 rows of 131072 bf16, 4 GB: 720 us.
 //
 // Policy, per token: q = exp(logp - old), L = -min(q A, clip(q) A) + kl (exp(o) - 1 - o), o = ref - logp.
 #include "token_rows.h"
@@ -133,9 +134,9 @@ struct RowSpace {
 };
 
 // ---------------------------------------------------------------- the sums, and then the gradient
-// In launches of their own: parts of the rows small enough for the last cache, in turn, take longer (550 us for 490, 1 GB of logits), since each launch's tail of long rows
-// costs more than the second read.
-// POLICY: the tokens' losses and the rows' coefficients too; else the coefficient of a row in no pair.
+// In launches of their own: parts of the rows small enough for the last cache, in turn, take longer (550 us for 490, 1 GB of logits), since
+// each launch's tail of long rows costs more than the second read. POLICY: the tokens' losses and the rows' coefficients too; else the
+// coefficient of a row in no pair.
 template <class T, int WAVES, bool POLICY>
 __global__ __launch_bounds__(Team<WAVES>::kBlock) void loss_forward_kernel(LogitRows in, PolicyArgs pol, float *logp_out, RowSpace out) {
     typedef Team<WAVES> G;
@@ -244,9 +245,10 @@ hipError_t loss_grad(const LogitRows &in, const RowSpace &s, const LogitGrad &ou
 }
 
 // ---------------------------------------------------------------- the policy loss with the row held in registers
-// The row stays in the team's registers between the sum and the gradient, so it is read once: thread t holds the pieces t, t + TEAM, ..., and -inf
-// behind the last one.  One row to a team in the order of the workgroups: 1 GB of bf16 logits of 8192, 16384, 32768 and 65536 columns 355, 362, 385 and 380 us; with persistent
-// workgroups that fetch the next row's pieces as they store the gradient 437, 395, 408 and 411.  131072 columns, 16 pieces: 415, two passes 518.
+// The row stays in the team's registers between the sum and the gradient, so it is read once: thread t holds the pieces t, t + TEAM, ..., and
+// -inf behind the last one.  One row to a team in the order of the workgroups: 1 GB of bf16 logits of 8192, 16384, 32768 and 65536 columns
+// 355, 362, 385 and 380 us; with persistent workgroups that fetch the next row's pieces as they store the gradient 437, 395, 408 and 411.
+// 131072 columns, 16 pieces: 415, two passes 518.
 template <class T, int WAVES, int PIECES>
 __global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void policy_held_kernel(LogitRows in, PolicyArgs pol, LogitGrad out) {
     typedef Team<WAVES> G;
@@ -349,7 +351,8 @@ __device__ __forceinline__ double block_sum(double v, double *lds) {
     return v;
 }
 
-// sums nullptr: one slice, straight to out_loss.  All of a thread's rows are in flight; what belongs to a row without a label is read and not used (it may be NaN).
+// sums nullptr: one slice, straight to out_loss.  All of a thread's rows are in flight; what belongs to a row without a label is read and not
+// used (it may be NaN).
 __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(LogitRows in, const float *token_loss, const float *weight, double *sums, float *out_loss) {
     __shared__ double lds[kSumThreads / kWave];
     const int64_t first = (int64_t)blockIdx.x * kSumSlice + threadIdx.x;
@@ -426,8 +429,9 @@ hipError_t policy(const LogitRows &in, const PolicyArgs &p, const LogitGrad &out
 
 }  // namespace
 
-// us a call, three launches and two: 256 x 1000 bf16, 4 pairs 15.3 and 12.7; 256 x 4000 fp32 15.2 and 12.6; 8 x 32000 fp32 15.2 and 14.6; beyond, 64 x 32000 bf16 15.2 and
-// 15.8, 1024 x 4000 fp32 19.1 and 32, 8 x 131072 bf16 18.0 and 21.6.  (Rows of 8 KB by one wavefront each, 64 x 4000 bf16: 15.3 and 15.9.)
+// us a call, three launches and two: 256 x 1000 bf16, 4 pairs 15.3 and 12.7; 256 x 4000 fp32 15.2 and 12.6; 8 x 32000 fp32 15.2 and 14.6;
+// beyond, 64 x 32000 bf16 15.2 and 15.8, 1024 x 4000 fp32 19.1 and 32, 8 x 131072 bf16 18.0 and 21.6.  (Rows of 8 KB by one wavefront each, 64
+// x 4000 bf16: 15.3 and 15.9.)
 constexpr int64_t kFewBytes = (int64_t)4 << 20, kFewRowBytes = 64 << 10, kFewShortBytes = 4 << 10;
 
 size_t preference_workspace_bytes(int64_t rows) { return row_space_bytes(rows); }

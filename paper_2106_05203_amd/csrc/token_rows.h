@@ -6,13 +6,14 @@
 //
 //   lse = (M + l) ln 2,   logp = (z_label - l) ln 2,   exp(x_v - lse) = 2^(z_v - l)
 //
-// for any M: log2 e rounded to fp32 means a softmax at another temperature by 10^-8, and everything else cancels.  M only has to keep the sum in fp32's range,
-// so a running maximum is not needed: every thread takes M from the first entries that it sees and adds up; fp32 holds 2^127 of them, an entry 88 above those
-// it started from.  A sum that leaves the range after all (or a NaN) shows in the joint sum, and the row is taken again with its maximum.  That
-// is four instructions an entry (unpack, multiply-add, exponential, add) instead of six, for rows whose sums are bound by instructions as much as by memory.
+// for any M: log2 e rounded to fp32 means a softmax at another temperature by 10^-8, and everything else cancels.  M only has to keep the sum
+// in fp32's range, so a running maximum is not needed: every thread takes M from the first entries that it sees and adds up; fp32 holds 2^127
+// of them, an entry 88 above those it started from.  A sum that leaves the range after all (or a NaN) shows in the joint sum, and the row is
+// taken again with its maximum.  That is four instructions an entry (unpack, multiply-add, exponential, add) instead of six, for rows whose
+// sums are bound by instructions as much as by memory.
 //
-// A team of wavefronts takes a row and joins its threads' sums once, so that lse costs one pass.  Rows start at any address: a row is taken as 16-byte pieces between a head and
-// a tail of a few entries, which go one to a thread.
+// A team of wavefronts takes a row and joins its threads' sums once, so that lse costs one pass.  Rows start at any address: a row is taken as
+// 16-byte pieces between a head and a tail of a few entries, which go one to a thread.
 #pragma once
 #include "device_utils.h"
 #include "lm.h"
@@ -69,7 +70,8 @@ __device__ __forceinline__ Raw nothing() {
     return Raw{w, w, w, w};
 }
 
-// Non-temporal loads and stores: with plain loads 1 GB of bf16 rows takes 177 us to sum and not 155, with plain stores its gradient 342 and not 335.
+// Non-temporal loads and stores: with plain loads 1 GB of bf16 rows takes 177 us to sum and not 155, with plain stores its gradient 342 and
+// not 335.
 template <class T>
 __device__ __forceinline__ Raw load_piece(const T *p) {
     return __builtin_nontemporal_load(reinterpret_cast<const Raw *>(p));
@@ -119,9 +121,9 @@ struct ExpSum {
     }
 };
 
-// log2 sum exp of a row.  Two kinds of rows: with z = x log2 e - 2 m the sum is 2 m + l; where the numbers are so large that this product's rounding is
-// no longer small (or that it is infinite: a row of the lowest number everywhere), z = (x - m) log2 e, and it is m log2 e + l.  Which one it is shows in
-// m: half of a whole number below 2^22, or a maximum of 2.9e6 and more.  l = -inf: no entry above -inf.
+// log2 sum exp of a row.  Two kinds of rows: with z = x log2 e - 2 m the sum is 2 m + l; where the numbers are so large that this product's
+// rounding is no longer small (or that it is infinite: a row of the lowest number everywhere), z = (x - m) log2 e, and it is m log2 e + l.
+// Which one it is shows in m: half of a whole number below 2^22, or a maximum of 2.9e6 and more.  l = -inf: no entry above -inf.
 constexpr float kMostM = 4194304.f, kLargeTop = 2.9e6f;
 struct RowStat {
     float m, l;
@@ -132,7 +134,8 @@ struct RowStat {
         constexpr double kLn2 = 0.69314718055994530942;
         return empty() ? -INFINITY : large() ? (float)((double)m + kLn2 * (double)l) : (float)((2.0 * (double)m + (double)l) * kLn2);
     }
-    // Once a row, in 64 bits: z, z - l and the product with ln 2 would each round at the size of log p (rms error 3.3e-7, so 2.0e-7, on rows of 131072).
+    // Once a row, in 64 bits: z, z - l and the product with ln 2 would each round at the size of log p (rms error 3.3e-7, so 2.0e-7, on rows
+    // of 131072).
     __device__ float log_prob(float x) const {
         constexpr double kLn2 = 0.69314718055994530942;
         if (empty()) return -INFINITY;
@@ -181,7 +184,8 @@ __device__ __forceinline__ ExpSum join_wave(ExpSum e) {
 // ---------------------------------------------------------------- gradient of a row
 template <class T>
 struct GradOf {
-    // kOne: 2^(x log2 e - (2 m + l)), where that sum's rounding is far below the type's (but not for the label, where 1 - p may cancel); kTwo: 2^(z - l); kLarge: z of such a row; kZero: nothing to give
+    // kOne: 2^(x log2 e - (2 m + l)), where that sum's rounding is far below the type's (but not for the label, where 1 - p may cancel); kTwo:
+    // 2^(z - l); kLarge: z of such a row; kZero: nothing to give
     enum Way { kOne, kTwo, kLarge, kZero };
     static constexpr Way kUsual = sizeof(T) == 2 ? kOne : kTwo;
     Way way;
@@ -423,7 +427,8 @@ inline hipError_t with_team(int64_t vocab, F f) {
 
 // ---------------------------------------------------------------- the gradient from what the sums left, in tiles
 // A workgroup per kGradPieces pieces of a row.  Workgroups that are on the chip together then work on one stretch of memory of a few
-// megabytes, which the memory answers faster than as many rows at once: 1 GB of bf16 logits with 32768 columns 347 us, 391 with a workgroup per row.
+// megabytes, which the memory answers faster than as many rows at once: 1 GB of bf16 logits with 32768 columns 347 us, 391 with a workgroup
+// per row.
 constexpr int kGradThreads = 256, kGradFlight = 2, kGradPieces = kGradThreads * kGradFlight;
 
 template <class T>

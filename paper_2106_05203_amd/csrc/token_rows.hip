@@ -31,7 +31,8 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock) void token_logps_kernel(LogitR
 // Beyond this size the rounding of lse itself, 2^-25 |lse| of each exp(x - lse), would show, and the row's sum is taken again.
 constexpr float kLseExact = 64.f;
 
-// A wavefront per row of up to 512 pieces (8192 bytes); longer rows by tiles, bound by memory: 1 GB of bf16 logits read and as much written 335 us (6.4 TB/s).
+// A wavefront per row of up to 512 pieces (8192 bytes); longer rows by tiles, bound by memory: 1 GB of bf16 logits read and as much written
+// 335 us (6.4 TB/s).
 template <class T>
 __global__ __launch_bounds__(Team<1>::kBlock) void token_grad_short_kernel(LogitRows in, const float *lse, const float *coef, LogitGrad out) {
     typedef Team<1> G;
@@ -52,7 +53,8 @@ __global__ __launch_bounds__(Team<1>::kBlock) void token_grad_short_kernel(Logit
     }
 }
 
-// A row whose sum is taken again is the workgroup's of its first tile alone: it has read all of it before it writes any, over the logits if need be.
+// A row whose sum is taken again is the workgroup's of its first tile alone: it has read all of it before it writes any, over the logits if
+// need be.
 template <class T>
 __global__ __launch_bounds__(kGradThreads, 8) void token_grad_kernel(LogitRows in, const float *lse, const float *coef, LogitGrad out, int32_t tiles) {
     constexpr int WAVES = kGradThreads / kWave;
