@@ -294,14 +294,14 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void poli
                 float(&one)[N] = reinterpret_cast<float(&)[N]>(f[k * N]);
                 unpack<T>(held[i + k], one);
             }
-            if (i == 0 && c.pieces > 0) e.start(f);
+            if (i == 0 && thread < c.pieces) e.start(f);
             e.add(f);
             asm volatile("" : "+v"(e.m), "+v"(e.s));               // here and now: one group unpacked at a time
             __builtin_amdgcn_sched_barrier(0);
         }
         if (edge_at >= 0) {
             const float f[1] = {edge};
-            if (c.pieces == 0) e.start(f);
+            if (thread >= c.pieces) e.start(f);
             e.add(f);
         }
         asm volatile("" : "+v"(at_label));                         // has arrived, like all of the row, before any wavefront may write over it

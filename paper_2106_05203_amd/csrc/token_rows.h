@@ -8,9 +8,11 @@
 //
 // for any M: log2 e rounded to fp32 means a softmax at another temperature by 10^-8, and everything else cancels.  M only has to keep the sum
 // in fp32's range, so a running maximum is not needed: every thread takes M from the first entries that it sees and adds up; fp32 holds 2^127
-// of them, an entry 88 above those it started from.  A sum that leaves the range after all (or a NaN) shows in the joint sum, and the row is
-// taken again with its maximum.  That is four instructions an entry (unpack, multiply-add, exponential, add) instead of six, for rows whose
-// sums are bound by instructions as much as by memory.
+// of them, an entry 88 above those it started from.  A sum that rises out of the range (or a NaN) shows in the joint sum.  What falls out of it
+// below is nothing beside the entry that M is of; a thread whose first entries are all masked has no such entry and starts from M = 0, and
+// whether it can have lost anything shows in its own sum and the joint one (join_team).  In both cases the row is taken again with its maximum.
+// That is four instructions an entry (unpack, multiply-add, exponential, add) instead of six, for rows whose sums are bound by instructions as
+// much as by memory.
 //
 // A team of wavefronts takes a row and joins its threads' sums once, so that lse costs one pass.  Rows start at any address: a row is taken as
 // 16-byte pieces between a head and a tail of a few entries, which go one to a thread.
@@ -102,10 +104,10 @@ __device__ __forceinline__ Cut cut_row(const T *x, int32_t vocab) {
 }
 
 // ---------------------------------------------------------------- sums of exponentials
-// s 2^m
+// s 2^m; m = kLowest: of a thread that has seen no entry
 struct ExpSum {
-    float m = 0.f, s = 0.f;
-    // M from the thread's first entries.  Below kMasked they are masks rather than logits, and zero is as good a guess as any.
+    float m = kLowest, s = 0.f;
+    // M from the thread's first entries: then s >= 1/2.  Below kMasked they are masks rather than logits, and zero is a guess.
     template <int N>
     __device__ __forceinline__ void start(const float (&f)[N]) {
         constexpr float kMasked = -5000.f;
@@ -172,9 +174,11 @@ struct TeamShared {
     float m[WAVES], s[WAVES], label;
 };
 
-// A wavefront's joint sum, the same in every lane.  A thread without a sum has no say in what M is.
-__device__ __forceinline__ ExpSum join_wave(ExpSum e) {
+// A wavefront's joint sum, the same in every lane.  A thread without a sum has no say in what M is.  doubt: some thread guessed M = 0 and has no
+// sum, so all its entries are masks, or below 2^-126.
+__device__ __forceinline__ ExpSum join_wave(ExpSum e, bool &doubt) {
     ExpSum w;
+    doubt = __ballot(e.s == 0.f && e.m == 0.f) != 0;
     if (e.s == 0.f) e.m = kLowest;
     w.m = group_max<64>(e.m);
     w.s = group_sum<64>(e.s * __builtin_amdgcn_exp2f(e.m - w.m));
@@ -270,32 +274,40 @@ __device__ ExpSum stream_sum(const T *x, const Cut &c, int32_t thread) {
             float f[K * N];
 #pragma unroll
             for (int k = 0; k < K; ++k) unpack<T>(r[u * K + k], reinterpret_cast<float(&)[N]>(f[k * N]));
-            if (u == 0 && base == 0) e.start(f);
+            if (u == 0 && base == 0 && thread < c.pieces) e.start(f);
             e.add(f);
         }
     }
     if (thread < c.edges()) {
         const float f[1] = {(float)x[c.edge<T>(thread)]};
-        if (c.pieces == 0) e.start(f);
+        if (thread >= c.pieces) e.start(f);
         e.add(f);
     }
     return e;
 }
 
+// The team's joint sum; s = 0 where it cannot be relied on.  What threads that guessed M = 0 may have lost is below V 2^-126 in all.  That is
+// nothing beside a joint sum of 2^-64 and more.  A smaller one is either relative to such a guess, and then s itself is small, or relative to
+// another thread's M below -64.
+constexpr float kLeastSum = 0x1p-64f, kLeastM = -64.f;
+
 template <int WAVES>
 __device__ __forceinline__ ExpSum join_team(ExpSum e, TeamShared<WAVES> &sh) {
-    e = join_wave(e);
+    bool doubt;
+    e = join_wave(e, doubt);
     if constexpr (WAVES > 1) {
         if (lane_id() == 0) {
             sh.m[wave_id()] = e.m;
-            sh.s[wave_id()] = e.s;
+            sh.s[wave_id()] = doubt ? -e.s : e.s;                  // in the sign, also of zero
         }
         __syncthreads();
         const int w = (int)threadIdx.x & (WAVES - 1);
-        const float mw = sh.m[w];
+        const float mw = sh.m[w], sw = sh.s[w];
+        doubt = __ballot(__float_as_int(sw) < 0) != 0;
         e.m = group_max<16>(mw);
-        e.s = group_sum<16>(sh.s[w] * __builtin_amdgcn_exp2f(mw - e.m)) * ((float)WAVES / 16.f);
+        e.s = group_sum<16>(fabsf(sw) * __builtin_amdgcn_exp2f(mw - e.m)) * ((float)WAVES / 16.f);
     }
+    if (e.s < kLeastSum || (doubt && e.m < kLeastM)) e.s = 0.f;
     return e;
 }
 
