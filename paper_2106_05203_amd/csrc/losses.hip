@@ -227,7 +227,7 @@ template <class T, bool POLICY>
 hipError_t loss_forward(const LogitRows &in, const PolicyArgs &pol, float *logp, const RowSpace &s, hipStream_t stream) {
     return with_team<T>(in.vocab, [&](auto waves) {
         constexpr int W = decltype(waves)::value;
-        hipLaunchKernelGGL((loss_forward_kernel<T, W, POLICY>), dim3(grid_of(in.rows, Team<W>::kPerBlock, kManyBlocks)), dim3(Team<W>::kBlock), 0, stream, in, pol,
+        hipLaunchKernelGGL((loss_forward_kernel<T, W, POLICY>), dim3(grid_of(in.rows, Team<W>::kPerBlock, Team<W>::kBlock)), dim3(Team<W>::kBlock), 0, stream, in, pol,
                            logp, s);
         return hipGetLastError();
     });
@@ -236,10 +236,10 @@ hipError_t loss_forward(const LogitRows &in, const PolicyArgs &pol, float *logp,
 template <class T>
 hipError_t loss_grad(const LogitRows &in, const RowSpace &s, const LogitGrad &out, hipStream_t stream) {
     if (team_waves<T>(in.vocab) == 1) {
-        hipLaunchKernelGGL(loss_grad_short_kernel<T>, dim3(grid_of(in.rows, Team<1>::kPerBlock, kManyBlocks)), dim3(Team<1>::kBlock), 0, stream, in, s, out);
+        hipLaunchKernelGGL(loss_grad_short_kernel<T>, dim3(grid_of(in.rows, Team<1>::kPerBlock, Team<1>::kBlock)), dim3(Team<1>::kBlock), 0, stream, in, s, out);
     } else {
         const int32_t tiles = grad_tiles<T>(in.vocab);
-        hipLaunchKernelGGL(loss_grad_kernel<T>, dim3(grid_of(in.rows * tiles, 1, kManyBlocks)), dim3(kGradThreads), 0, stream, in, s, out, tiles);
+        hipLaunchKernelGGL(loss_grad_kernel<T>, dim3(grid_of(in.rows * tiles, 1, kGradThreads)), dim3(kGradThreads), 0, stream, in, s, out, tiles);
     }
     return hipGetLastError();
 }
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(kSumThreads) void policy_slices_kernel(const double
 template <class T, int WAVES, int PIECES>
 hipError_t policy_held(const LogitRows &in, const PolicyArgs &p, const LogitGrad &out, hipStream_t stream) {
     typedef Team<WAVES> G;
-    hipLaunchKernelGGL((policy_held_kernel<T, WAVES, PIECES>), dim3(grid_of(in.rows, G::kPerBlock, kManyBlocks)), dim3(G::kBlock), 0, stream, in, p, out);
+    hipLaunchKernelGGL((policy_held_kernel<T, WAVES, PIECES>), dim3(grid_of(in.rows, G::kPerBlock, G::kBlock)), dim3(G::kBlock), 0, stream, in, p, out);
     return hipGetLastError();
 }
 
@@ -455,7 +455,7 @@ hipError_t launch_preference(const LogitRows &in, PairArgs pairs, const LogitGra
                 return hipGetLastError();
             }
         }
-        hipLaunchKernelGGL(preference_pairs_kernel, dim3(grid_of(pairs.pairs, 1, kManyBlocks)), dim3(kPairThreads), 0, stream, pairs);
+        hipLaunchKernelGGL(preference_pairs_kernel, dim3(grid_of(pairs.pairs, 1, kPairThreads)), dim3(kPairThreads), 0, stream, pairs);
         st = hipGetLastError();
         return st != hipSuccess || !out.ptr || in.rows == 0 ? st : loss_grad<T>(in, s, out, stream);
     });

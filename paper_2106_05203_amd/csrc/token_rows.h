@@ -489,10 +489,10 @@ struct GradTile {
     }
 };
 
-inline unsigned grid_of(int64_t items, int64_t per_block, int64_t most) {
-    const int64_t blocks = (items + per_block - 1) / per_block;
+// Workgroups of `threads` threads: a launch takes fewer than 2^32 threads in all (2^30 here), and every kernel goes on to what is left.
+inline unsigned grid_of(int64_t items, int64_t per_block, int threads) {
+    const int64_t blocks = (items + per_block - 1) / per_block, most = ((int64_t)1 << 30) / threads;
     return (unsigned)(blocks < most ? blocks : most);
 }
-constexpr int64_t kManyBlocks = 1 << 22;
 
 }  // namespace ef21

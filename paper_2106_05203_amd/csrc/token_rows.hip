@@ -89,7 +89,7 @@ hipError_t launch_token_logps(const LogitRows &in, float *logp, float *lse, hipS
         typedef typename ValueOf<decltype(type)::value>::type T;
         return with_team<T>(in.vocab, [&](auto waves) {
             typedef Team<decltype(waves)::value> G;
-            hipLaunchKernelGGL((token_logps_kernel<T, decltype(waves)::value>), dim3(grid_of(in.rows, G::kPerBlock, kManyBlocks)), dim3(G::kBlock), 0, stream, in,
+            hipLaunchKernelGGL((token_logps_kernel<T, decltype(waves)::value>), dim3(grid_of(in.rows, G::kPerBlock, G::kBlock)), dim3(G::kBlock), 0, stream, in,
                                logp, lse);
             return hipGetLastError();
         });
@@ -102,10 +102,10 @@ hipError_t launch_token_grad(const LogitRows &in, const float *lse, const float 
         typedef typename ValueOf<decltype(type)::value>::type T;
         if (team_waves<T>(in.vocab) == 1) {
             typedef Team<1> G;
-            hipLaunchKernelGGL(token_grad_short_kernel<T>, dim3(grid_of(in.rows, G::kPerBlock, kManyBlocks)), dim3(G::kBlock), 0, stream, in, lse, coef, out);
+            hipLaunchKernelGGL(token_grad_short_kernel<T>, dim3(grid_of(in.rows, G::kPerBlock, G::kBlock)), dim3(G::kBlock), 0, stream, in, lse, coef, out);
         } else {
             const int32_t tiles = grad_tiles<T>(in.vocab);
-            hipLaunchKernelGGL(token_grad_kernel<T>, dim3(grid_of(in.rows * tiles, 1, kManyBlocks)), dim3(kGradThreads), 0, stream, in, lse, coef, out, tiles);
+            hipLaunchKernelGGL(token_grad_kernel<T>, dim3(grid_of(in.rows * tiles, 1, kGradThreads)), dim3(kGradThreads), 0, stream, in, lse, coef, out, tiles);
         }
         return hipGetLastError();
     });
