@@ -322,13 +322,14 @@ __device__ __forceinline__ RowStat stat_of(float whole, float s) {
     return {0.5f * (whole + k), log2f(f)};
 }
 
-// The row again, its maximum first.  By the whole team; all of the row has been read when a thread returns.
+// The row again, its maximum first.  By the whole team; all of the row has been read when a thread returns.  (Here and in entrywise_grad v is
+// unsigned: up to TEAM beyond a vocabulary of 2^31 - 1.)
 template <class T, int WAVES>
 __device__ __forceinline__ RowStat careful_stat(const T *x, int32_t vocab, int32_t thread, TeamShared<WAVES> &sh) {
     constexpr int TEAM = WAVES * kWave;
     float top = -INFINITY;
 #pragma unroll 1
-    for (int32_t v = thread; v < vocab; v += TEAM) top = fmaxf(top, (float)x[v]);
+    for (uint32_t v = (uint32_t)thread; v < (uint32_t)vocab; v += TEAM) top = fmaxf(top, (float)x[v]);
     top = group_max<64>(top);
     if constexpr (WAVES > 1) {
         __syncthreads();                                           // the sums in sh have been read
@@ -341,7 +342,7 @@ __device__ __forceinline__ RowStat careful_stat(const T *x, int32_t vocab, int32
     if (top == -INFINITY) st.m = 0.f;
     ExpSum e;
 #pragma unroll 1
-    for (int32_t v = thread; v < vocab; v += TEAM) e.s += __builtin_amdgcn_exp2f(st.z((float)x[v]));
+    for (uint32_t v = (uint32_t)thread; v < (uint32_t)vocab; v += TEAM) e.s += __builtin_amdgcn_exp2f(st.z((float)x[v]));
     float s = group_sum<64>(e.s);
     if constexpr (WAVES > 1) {
         if (lane_id() == 0) sh.s[wave_id()] = s;
@@ -400,7 +401,7 @@ __device__ void stream_grad(const T *x, T *g, const Cut &c, const GradOf<T> &d, 
 template <class T, int TEAM>
 __device__ __forceinline__ void entrywise_grad(const T *x, T *g, int32_t vocab, const GradOf<T> &d, int32_t thread) {
 #pragma unroll 1
-    for (int32_t v = thread; v < vocab; v += TEAM) g[v] = stored<T>(d.entry(v, (float)x[v]));
+    for (uint32_t v = (uint32_t)thread; v < (uint32_t)vocab; v += TEAM) g[v] = stored<T>(d.entry((int32_t)v, (float)x[v]));
 }
 
 // ---------------------------------------------------------------- teams

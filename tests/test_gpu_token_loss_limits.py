@@ -46,3 +46,37 @@ def test_more_pairs_than_a_launch_has_workgroups(gpu):
     lm.inside(as64(grad), g, bound, "gradient")
     loss[full] = math.log(2.0)
     assert float((loss.double() - math.log(2.0)).abs().max()) <= 2.0 ** -24
+
+
+@pytest.mark.parametrize("top", [2.0, 500.0])
+def test_the_longest_row(gpu, top):
+    """2^31 - 1 columns, the first and the last one not masked (500: sums that need the row's maximum, gradient entry by entry).  Both have the
+    probability 1/2, so everything is exact but for a few roundings; nothing around the row is written."""
+    torch, b = gpu
+    vocab, around = 2 ** 31 - 1, 4096
+    buf = torch.full((vocab + 2 * around,), -math.inf, dtype=torch.bfloat16, device="cuda")
+    x = buf[around:around + vocab].view(1, vocab)
+    x[0, 0], x[0, -1] = top, top
+    buf[:around], buf[around + vocab:] = 7.0, 7.0
+    label, one = torch.tensor([vocab - 1], device="cuda"), torch.ones(1, device="cuda")
+
+    def halves(g, coef, what):
+        print(f"the longest row, {top}: {what}", flush=True)
+        assert float(g[0, -1]) == coef / 2 and float(g[0, 0]) == -coef / 2
+        assert not any(int(part.count_nonzero()) for part in g[0, 1:-1].split(1 << 28))
+
+    print(f"the longest row, {top}", flush=True)
+    logp, lse = b.ef21_token_logps(x, label)
+    assert float(lse) == pytest.approx(top + math.log(2.0), rel=1e-6) and float(logp) == pytest.approx(-math.log(2.0), rel=1e-6)
+    # a margin of logp - ref = 0: the slope is -1/2
+    start, out = torch.tensor([0, 1, 1], device="cuda"), torch.full_like(x, math.nan)
+    loss, logp2, grad = b.ef21_preference_loss(x, label, start, logp, 1.0, grad=out)
+    assert torch.equal(logp2, logp) and float(loss) == pytest.approx(math.log(2.0), rel=1e-6)
+    halves(grad, -0.5, "preference loss")
+    total, _, logp3, grad = b.ef21_policy_loss(x, label, logp, one, 0.2, 0.2, grad=out)
+    assert torch.equal(logp3, logp) and float(total) == -1.0
+    halves(grad, -1.0, "policy loss")
+    del out, grad
+    b.ef21_token_logps_grad(x, label, lse, one, out=x)
+    halves(x, 1.0, "log-probability")
+    assert bool((buf[:around] == 7.0).all()) and bool((buf[around + vocab:] == 7.0).all())
