@@ -364,7 +364,8 @@ int ef21_preference_loss(const void *logits, int type, int64_t rows, int64_t voc
  *   out_loss[0]   = sum_r weight[r] token_loss[r]
  * old_logp, advantages, ref_logp, weight: fp32 [rows], read where there is a label.  ref_logp NULL: no KL term (kl must be 0);
  * weight NULL: 1 / rows.  grad_logits: the gradient of out_loss, or NULL for the loss alone; where the two sides of the
- * minimum are equal it is that of q A.  token_loss and logp: fp32 [rows], out.
+ * minimum are equal it is that of q A.  token_loss and logp: fp32 [rows], out.  With a KL term a label of probability zero
+ * (logp = -inf, ref_logp finite) has a token_loss and so an out_loss of +inf, and its row's gradient is not finite.
  * EF21_EINVAL also: clip_low outside [0, 1], clip_high or kl negative or not finite.
  * workspace: 256-byte aligned device memory of at least the bytes that ef21_policy_loss_workspace says.
  */

@@ -35,7 +35,7 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyArgs &p, const Tok
     TokenLoss t = one > two ? TokenLoss{-two, 0.f} : TokenLoss{-one, -one};   // a NaN is neither above nor dropped
     if (p.ref_logp) {
         const float off = in.ref_logp - logp, e = expm1f(off);
-        t.loss += p.kl * (e - off);
+        t.loss += p.kl * (e == INFINITY ? e : e - off);           // also of a label of probability zero, where off is infinite
         t.slope -= p.kl * e;
     }
     return t;

@@ -80,3 +80,35 @@ def test_the_longest_row(gpu, top):
     b.ef21_token_logps_grad(x, label, lse, one, out=x)
     halves(x, 1.0, "log-probability")
     assert bool((buf[:around] == 7.0).all()) and bool((buf[around + vocab:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [40, 3000, 40000, 150001])           # the row held by teams of three sizes; two passes
+def test_policy_loss_of_an_impossible_token(gpu, vocab, dtype):
+    """A label of probability zero: the ratio is zero, and a KL term is infinite, o = ref_logp - logp being so, not a NaN.  The gradient of such a row is not
+    finite: where a column has a positive probability it is the infinite slope's sign, for the label the other one.  Other rows keep theirs."""
+    torch, b = gpu
+    rng = np.random.default_rng(vocab)
+    rows = 4
+    x = torch.from_numpy(rng.standard_normal((rows, vocab)).astype(np.float32)).to(lm.TORCH[dtype]).cuda()
+    labels = rng.integers(0, vocab, rows)
+    x[1, labels[1]] = -math.inf
+    x[3] = -math.inf                                                   # nothing is left of the row: no gradient
+    dl = torch.from_numpy(labels).cuda()
+    one = torch.ones(rows, device="cuda")
+    old, adv = -2.0 * one, torch.tensor([1.0, -1.0, -1.0, 1.0], device="cuda")
+    total, tokens, logp, grad = b.ef21_policy_loss(x, dl, old, adv, 0.2, 0.2, ref_logp=old, kl=0.1)
+    assert logp.tolist()[1] == logp.tolist()[3] == -math.inf
+    assert tokens.tolist()[1] == tokens.tolist()[3] == math.inf and total.item() == math.inf
+    assert bool(torch.isfinite(tokens[[0, 2]]).all()) and bool(torch.isfinite(grad[[0, 2]].float()).all())
+    assert grad[1, labels[1]].item() == -math.inf
+    others = torch.arange(vocab, device="cuda") != labels[1]
+    assert bool((grad[1][others].float() == math.inf).all()) and not bool(grad[3].count_nonzero())
+    # without the KL term all is finite: q = 0, so min(q A, clip(q) A) is 0 for A > 0 and 0.8 A, which has no slope, for A < 0
+    total, tokens, _, grad = b.ef21_policy_loss(x, dl, old, adv, 0.2, 0.2)
+    assert tokens.tolist()[1] == pytest.approx(0.8, rel=1e-6) and tokens.tolist()[3] == 0.0 and math.isfinite(total.item())
+    assert not bool(grad[[1, 3]].count_nonzero()) and bool(torch.isfinite(grad.float()).all())
+    # a reference that is impossible as well leaves o undefined
+    ref = torch.where(torch.tensor([False, True, False, False], device="cuda"), -math.inf, old)
+    tokens = b.ef21_policy_loss(x, dl, old, adv, 0.2, 0.2, ref_logp=ref, kl=0.1)[1]
+    assert math.isnan(tokens.tolist()[1]) and tokens.tolist()[3] == math.inf
