@@ -333,7 +333,8 @@ int ef21_token_logps(const void *logits, int type, int64_t rows, int64_t vocab, 
  * The gradient of the logits from that of the log-probabilities, grad_logp [rows] (read where there is a label):
  *   grad_logits[r][v] = grad_logp[r] * ([v = label] - exp(x_v - lse[r]))
  * lse as ef21_token_logps gave it.  grad_logits has the logits' type; it may be the logits themselves (same stride) and must
- * otherwise not overlap them, here and in the calls below.
+ * otherwise not overlap them, here and in the calls below.  A row whose grad_logp (or, below, whose loss's derivative in logp) is
+ * infinite has infinities where the factor in parentheses is not zero and zero where it is.
  */
 int ef21_token_logps_grad(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
                           int label_type, const float *lse, const float *grad_logp, void *grad_logits, int64_t grad_stride,
@@ -365,7 +366,7 @@ int ef21_preference_loss(const void *logits, int type, int64_t rows, int64_t voc
  * old_logp, advantages, ref_logp, weight: fp32 [rows], read where there is a label.  ref_logp NULL: no KL term (kl must be 0);
  * weight NULL: 1 / rows.  grad_logits: the gradient of out_loss, or NULL for the loss alone; where the two sides of the
  * minimum are equal it is that of q A.  token_loss and logp: fp32 [rows], out.  With a KL term a label of probability zero
- * (logp = -inf, ref_logp finite) has a token_loss and so an out_loss of +inf, and its row's gradient is not finite.
+ * (logp = -inf, ref_logp finite) has a token_loss and so an out_loss of +inf, and an infinite derivative in logp.
  * EF21_EINVAL also: clip_low outside [0, 1], clip_high or kl negative or not finite.
  * workspace: 256-byte aligned device memory of at least the bytes that ef21_policy_loss_workspace says.
  */

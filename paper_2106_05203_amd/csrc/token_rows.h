@@ -189,23 +189,30 @@ __device__ __forceinline__ ExpSum join_wave(ExpSum e, bool &doubt) {
 template <class T>
 struct GradOf {
     // kOne: 2^(x log2 e - (2 m + l)), where that sum's rounding is far below the type's (but not for the label, where 1 - p may cancel); kTwo:
-    // 2^(z - l); kLarge: z of such a row; kZero: nothing to give
-    enum Way { kOne, kTwo, kLarge, kZero };
+    // 2^(z - l); kLarge: z of such a row; kEndless: an infinite coefficient, which gives infinities where its factor is not zero and zero, not
+    // NaN, where it is; kZero: nothing to give
+    enum Way { kOne, kTwo, kLarge, kEndless, kZero };
     static constexpr Way kUsual = sizeof(T) == 2 ? kOne : kTwo;
     Way way;
-    float m, l, both, coef;                                        // m: what z subtracts; both: m + l
+    float m, l, both, coef;                                        // m: what z subtracts; both: m + l (kEndless: whether the row is large)
     int32_t label;
     __device__ GradOf(RowStat st, float coef_, int32_t label_) : m(st.m), l(st.l), coef(coef_), label(label_) {
-        way = st.empty() ? kZero : st.large() ? kLarge : sizeof(T) == 2 && fabsf(st.m) <= 2048.f ? kOne : kTwo;
-        if (way != kLarge) m *= 2.f;
-        both = m + l;
+        way = st.empty() ? kZero : fabsf(coef_) == INFINITY ? kEndless : st.large() ? kLarge : sizeof(T) == 2 && fabsf(st.m) <= 2048.f ? kOne : kTwo;
+        if (!st.large()) m *= 2.f;
+        both = way == kEndless ? (st.large() ? 1.f : 0.f) : m + l;
     }
     template <Way WAY>
     __device__ __forceinline__ float prob(float x) const {
         if constexpr (WAY == kOne) return __builtin_amdgcn_exp2f(fmaf(x, kLog2E, -both));
         else if constexpr (WAY == kTwo) return __builtin_amdgcn_exp2f(fmaf(x, kLog2E, -m) - l);
         else if constexpr (WAY == kLarge) return __builtin_amdgcn_exp2f((x - m) * kLog2E - l);
+        else if constexpr (WAY == kEndless) return __builtin_amdgcn_exp2f((both != 0.f ? (x - m) * kLog2E : fmaf(x, kLog2E, -m)) - l);
         else return 0.f;
+    }
+    // coef times a factor
+    template <Way WAY>
+    __device__ __forceinline__ float times(float factor) const {
+        return WAY == kZero || (WAY == kEndless && factor == 0.f) ? 0.f : coef * factor;
     }
     template <Way WAY, int N>
     __device__ __forceinline__ void piece_by(uint32_t at, float (&f)[N]) const {
@@ -213,10 +220,10 @@ struct GradOf {
         if (at < (uint32_t)N) {
 #pragma unroll
             for (int i = 0; i < N; ++i) hot = (int)at == i ? f[i] : hot;
-            hot = WAY == kZero ? 0.f : coef * (1.f - prob<(WAY == kOne ? kTwo : WAY)>(hot));
+            hot = times<WAY>(1.f - prob<(WAY == kOne ? kTwo : WAY)>(hot));
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = WAY == kZero ? 0.f : -coef * prob<WAY>(f[i]);
+        for (int i = 0; i < N; ++i) f[i] = times<WAY>(-prob<WAY>(f[i]));
         if (at < (uint32_t)N) {
 #pragma unroll
             for (int i = 0; i < N; ++i) f[i] = (int)at == i ? hot : f[i];
@@ -228,6 +235,7 @@ struct GradOf {
         if (sizeof(T) == 2 && way == kOne) piece_by<kOne>(at, f);
         else if (way == kTwo) piece_by<kTwo>(at, f);
         else if (way == kLarge) piece_by<kLarge>(at, f);
+        else if (way == kEndless) piece_by<kEndless>(at, f);
         else piece_by<kZero>(at, f);
     }
     __device__ __forceinline__ float entry(int32_t v, float x) const {

@@ -112,3 +112,52 @@ def test_policy_loss_of_an_impossible_token(gpu, vocab, dtype):
     ref = torch.where(torch.tensor([False, True, False, False], device="cuda"), -math.inf, old)
     tokens = b.ef21_policy_loss(x, dl, old, adv, 0.2, 0.2, ref_logp=ref, kl=0.1)[1]
     assert math.isnan(tokens.tolist()[1]) and tokens.tolist()[3] == math.inf
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [40, 700, 9000, 40000, 150001])
+def test_infinite_slopes_leave_masked_columns_alone(gpu, vocab, dtype):
+    """A gradient is slope ([v = label] - p_v), of an infinite slope too: infinite where that factor is not zero, zero and no NaN where it is."""
+    torch, b = gpu
+    rng = np.random.default_rng(vocab)
+    inf, rows = math.inf, 5
+    values = rng.standard_normal((rows, vocab)).astype(np.float32)
+    values[3] += -6e4 if dtype == "f16" else -5e6                      # a row far from zero
+    x = torch.from_numpy(values).to(lm.TORCH[dtype]).cuda()
+    masked = torch.from_numpy(rng.random((rows, vocab)) < 0.3).cuda()
+    x[masked] = -inf
+    labels = np.array([int(rng.choice(np.flatnonzero(~masked[r].cpu().numpy()))) for r in range(rows)])
+    labels[0] = int(np.flatnonzero(masked[0].cpu().numpy())[0])       # impossible
+    x[4] = -inf
+    x[4, labels[4]] = 1.0                                              # certain
+    dl, one = torch.from_numpy(labels).cuda(), torch.ones(rows, device="cuda")
+    logp, lse = b.ef21_token_logps(x, dl)
+    p = torch.softmax(x.double(), 1)
+    hot = torch.zeros_like(p)
+    hot[torch.arange(rows), dl] = 1.0
+    factor = hot - p
+    clear = (factor == 0) | (factor.abs() > 1e-30)                     # what fp32 shows without doubt
+    clear[4, labels[4]] = False                                        # (1 - p of the certain label is a rounding)
+
+    def expect(grad, slopes, what):
+        grad = grad.double()
+        for r, slope in enumerate(slopes):
+            want = torch.where(factor[r] == 0, 0.0, slope * factor[r]) if math.isinf(slope) else None
+            if want is None:
+                assert bool(torch.isfinite(grad[r]).all()), f"{what}: row {r}"
+            else:
+                assert torch.equal(grad[r][clear[r]], want[clear[r]]), f"{what}: row {r}"
+                assert not bool(torch.isnan(grad[r]).any()), f"{what}: row {r}"
+
+    expect(b.ef21_token_logps_grad(x, dl, lse, torch.tensor([inf, -inf, 1.0, inf, -inf], device="cuda")), [inf, -inf, 1.0, inf, -inf], "log-probability")
+    # least squares: the margin of (0, 1) is -inf, of (2, 3) finite
+    start = torch.tensor([0, 1, 2, 3, 4], device="cuda")
+    loss, _, grad = b.ef21_preference_loss(x, dl, start, logp.clamp(min=-10.0), 0.5, loss=1, pair_weight=one[:2])
+    assert loss.tolist()[0] == inf and math.isfinite(loss.tolist()[1])
+    expect(grad, [-inf, inf, 1.0, 1.0, 1.0], "preference loss")
+    # the KL term of the impossible label; a ratio beyond fp32 where the advantage is negative
+    old = logp.clamp(min=-10.0) + torch.tensor([0.0, -200.0, 0.0, -200.0, -200.0], device="cuda")
+    ref = logp.clamp(min=-10.0)
+    _, tokens, _, grad = b.ef21_policy_loss(x, dl, old, -one, 0.2, 0.2, ref_logp=ref, kl=0.1, weight=one)
+    assert tokens.tolist()[0] == inf
+    expect(grad, [-inf, inf, 1.0, inf, inf], "policy loss")
