@@ -284,26 +284,30 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void poli
         const TokenIn ti = token_in(pol, r, in.rows);
         ExpSum e;
         const int32_t wave_first = __builtin_amdgcn_readfirstlane(thread);
+        const auto add_up = [&](auto first) {                          // first: e.m is taken from the row; else it is there already
 #pragma unroll
-        for (int i = 0; i < PIECES; i += K) {
-            if (wave_first >= c.pieces - i * TEAM && i > 0) break;
-            float f[K * N];
+            for (int i = 0; i < PIECES; i += K) {
+                if (wave_first >= c.pieces - i * TEAM && i > 0) break;
+                float f[K * N];
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                asm("" : "+v"(held[i + k]));                       // held as it was loaded: left alone, the compiler unpacks it first
-                float(&one)[N] = reinterpret_cast<float(&)[N]>(f[k * N]);
-                unpack<T>(held[i + k], one);
+                for (int k = 0; k < K; ++k) {
+                    asm("" : "+v"(held[i + k]));                   // held as it was loaded: left alone, the compiler unpacks it first
+                    float(&one)[N] = reinterpret_cast<float(&)[N]>(f[k * N]);
+                    unpack<T>(held[i + k], one);
+                }
+                if (first && i == 0 && c.pieces > 0) e.start(f);
+                e.add(f);
+                asm volatile("" : "+v"(e.m), "+v"(e.s));           // here and now: one group unpacked at a time
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (i == 0 && thread < c.pieces) e.start(f);
-            e.add(f);
-            asm volatile("" : "+v"(e.m), "+v"(e.s));               // here and now: one group unpacked at a time
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (edge_at >= 0) {
-            const float f[1] = {edge};
-            if (thread >= c.pieces) e.start(f);
-            e.add(f);
-        }
+            if (wave_first < c.edges()) {
+                const float f[1] = {edge};
+                if (first && c.pieces == 0) e.start(f);
+                e.add(f);
+            }
+        };
+        add_up(std::true_type());
+        if (e.again()) add_up(std::false_type());
         asm volatile("" : "+v"(at_label));                         // has arrived, like all of the row, before any wavefront may write over it
         const RowStat st = team_stat<T, WAVES>(e, x, vocab, thread, shared[turn]);
         turn ^= 1;

@@ -7,10 +7,12 @@
 //   lse = (M + l) ln 2,   logp = (z_label - l) ln 2,   exp(x_v - lse) = 2^(z_v - l)
 //
 // for any M: log2 e rounded to fp32 means a softmax at another temperature by 10^-8, and everything else cancels.  M only has to keep the sum
-// in fp32's range, so a running maximum is not needed: every thread takes M from the first entries that it sees and adds up; fp32 holds 2^127
-// of them, an entry 88 above those it started from.  A sum that rises out of the range (or a NaN) shows in the joint sum.  What falls out of it
-// below is nothing beside the entry that M is of; a thread whose first entries are all masked has no such entry and starts from M = 0, and
-// whether it can have lost anything shows in its own sum and the joint one (join_team).  In both cases the row is taken again with its maximum.
+// near the sum, so a running maximum is not needed: a wavefront takes M from its first entries (eight a lane) and adds up.
+//   A term is rounded with its z, at 2^64 by 1.3e-6 of itself.  Where a lane's sum comes out beyond that, or all of a wavefront's below 2^-64,
+// the wavefront adds up once more, with M moved to the largest sum.
+//   A sum beyond 2^127, an entry 88 above those that the wavefront started from, and a NaN show in the joint sum.  What falls out of the range
+// below is nothing beside the entry that M is of; a wavefront whose first entries are all masked has no such entry and starts from M = 0, and
+// whether all that it has may have been lost shows in the joint sum's M (join_team).  Then the row is taken again with its maximum.
 // That is four instructions an entry (unpack, multiply-add, exponential, add) instead of six, for rows whose sums are bound by instructions as
 // much as by memory.
 //
@@ -104,22 +106,48 @@ __device__ __forceinline__ Cut cut_row(const T *x, int32_t vocab) {
 }
 
 // ---------------------------------------------------------------- sums of exponentials
-// s 2^m; m = kLowest: of a thread that has seen no entry
+// The largest value of each group of 16 or 64 lanes, in every lane of the group (group_sum with another operation).
+template <int LANES>
+__device__ __forceinline__ float group_max(float v) {
+    v = fmaxf(v, dpp_move<0xB1>(v));
+    v = fmaxf(v, dpp_move<0x4E>(v));
+    v = fmaxf(v, dpp_move<0x141>(v));
+    v = fmaxf(v, dpp_move<0x140>(v));
+    if constexpr (LANES == 64) {
+        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return v;
+}
+
+// s 2^m, a lane's part of a row; m is the wavefront's, kLowest where it has seen no entry
 struct ExpSum {
     float m = kLowest, s = 0.f;
-    // M from the thread's first entries: then s >= 1/2.  Below kMasked they are masks rather than logits, and zero is a guess.
+    // M from the wavefront's first entries: then some lane has s >= 1/2.  Below kMasked they are masks rather than logits, and zero is a guess.
     template <int N>
     __device__ __forceinline__ void start(const float (&f)[N]) {
         constexpr float kMasked = -5000.f;
         float top = f[0];
 #pragma unroll
         for (int i = 1; i < N; ++i) top = fmaxf(top, f[i]);
+        top = group_max<64>(top);
         m = top > kMasked ? __builtin_rintf(top * kLog2E) : 0.f;
     }
     template <int N>
     __device__ __forceinline__ void add(const float (&f)[N]) {
 #pragma unroll
         for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f(fmaf(f[i], kLog2E, -m));
+    }
+    // Whether the wavefront has to add up again; then M is moved, and the sums begin anew.
+    __device__ __forceinline__ bool again() {
+        if (__ballot(s >= 0x1p64f) == 0 && (__ballot(s >= 0x1p-64f) != 0 || __ballot(s > 0.f) == 0)) return false;
+        const float most = group_max<64>(s);
+        if (most == INFINITY) return false;
+        m += (float)__builtin_amdgcn_frexp_expf(most);
+        s = 0.f;
+        return true;
     }
 };
 
@@ -152,37 +180,19 @@ struct RowStat {
     }
 };
 
-// The largest value of each group of 16 or 64 lanes, in every lane of the group (group_sum with another operation).
-template <int LANES>
-__device__ __forceinline__ float group_max(float v) {
-    v = fmaxf(v, dpp_move<0xB1>(v));
-    v = fmaxf(v, dpp_move<0x4E>(v));
-    v = fmaxf(v, dpp_move<0x141>(v));
-    v = fmaxf(v, dpp_move<0x140>(v));
-    if constexpr (LANES == 64) {
-        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-        r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
-    return v;
-}
-
 // What the wavefronts of a team tell each other.  Used in turn by odd and even rows, so that one barrier a row is enough.
 template <int WAVES>
 struct TeamShared {
     float m[WAVES], s[WAVES], label;
 };
 
-// A wavefront's joint sum, the same in every lane.  A thread without a sum has no say in what M is.  doubt: some thread guessed M = 0 and has no
-// sum, so all its entries are masks, or below 2^-126.
+// A wavefront's joint sum, the same in every lane; without a sum it has no say in what the team's M is.  doubt: it guessed M = 0 and has no sum,
+// so all its entries are masks, or below 2^-126.
 __device__ __forceinline__ ExpSum join_wave(ExpSum e, bool &doubt) {
-    ExpSum w;
-    doubt = __ballot(e.s == 0.f && e.m == 0.f) != 0;
+    e.s = group_sum<64>(e.s);
+    doubt = e.s == 0.f && e.m == 0.f;
     if (e.s == 0.f) e.m = kLowest;
-    w.m = group_max<64>(e.m);
-    w.s = group_sum<64>(e.s * __builtin_amdgcn_exp2f(e.m - w.m));
-    return w;
+    return e;
 }
 
 // ---------------------------------------------------------------- gradient of a row
@@ -257,47 +267,52 @@ __device__ void zero_row(T *g, int32_t vocab, int32_t thread) {
 // ---------------------------------------------------------------- one pass over a row, from memory
 // Thread t of TEAM takes the pieces t, t + TEAM, ... in groups of eight entries and then its edge, as policy_held_kernel does: a row's
 // sum has the same bits whichever kernel takes it and however many rows there are (how large a team is goes by the row's length alone).
-template <class T, int TEAM>
-__device__ ExpSum stream_sum(const T *x, const Cut &c, int32_t thread) {
+// FIRST: e.m is taken from the row; else it is there already.
+template <class T, int TEAM, bool FIRST>
+__device__ __forceinline__ void stream_pass(const T *x, const Cut &c, int32_t thread, ExpSum &e) {
     constexpr int N = Piece<T>::N, K = Piece<T>::kGroup, U = 4;    // groups in flight
-    ExpSum e;
-    const char *from = reinterpret_cast<const char *>(x + c.head);
     const uint32_t mine = (uint32_t)thread * 16u;
     const int32_t wave_first = __builtin_amdgcn_readfirstlane(thread);
-    for (int32_t base = 0; base < c.pieces; base += U * K * TEAM, from += (int64_t)U * K * TEAM * 16) {
-        Raw r[U * K];
-        if (base + U * K * TEAM <= c.pieces) {
+            const char *from = reinterpret_cast<const char *>(x + c.head);
+            for (int32_t base = 0; base < c.pieces; base += U * K * TEAM, from += (int64_t)U * K * TEAM * 16) {
+                Raw r[U * K];
+                if (base + U * K * TEAM <= c.pieces) {
 #pragma unroll
-            for (int u = 0; u < U * K; ++u) r[u] = load_piece(reinterpret_cast<const T *>(from + u * TEAM * 16 + mine));
-        } else {
+                    for (int u = 0; u < U * K; ++u) r[u] = load_piece(reinterpret_cast<const T *>(from + u * TEAM * 16 + mine));
+                } else {
 #pragma unroll
-            for (int u = 0; u < U * K; ++u) {
-                r[u] = nothing<T>();
-                if (thread < c.pieces - base - u * TEAM) r[u] = load_piece(reinterpret_cast<const T *>(from + u * TEAM * 16 + mine));
+                    for (int u = 0; u < U * K; ++u) {
+                        r[u] = nothing<T>();
+                        if (thread < c.pieces - base - u * TEAM) r[u] = load_piece(reinterpret_cast<const T *>(from + u * TEAM * 16 + mine));
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (wave_first >= c.pieces - base - u * K * TEAM) break;   // none of the wavefront's threads has more
+                    float f[K * N];
+#pragma unroll
+                    for (int k = 0; k < K; ++k) unpack<T>(r[u * K + k], reinterpret_cast<float(&)[N]>(f[k * N]));
+                    if (FIRST && u == 0 && base == 0) e.start(f);
+                    e.add(f);
+                }
             }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (wave_first >= c.pieces - base - u * K * TEAM) break;   // none of the wavefront's threads has more
-            float f[K * N];
-#pragma unroll
-            for (int k = 0; k < K; ++k) unpack<T>(r[u * K + k], reinterpret_cast<float(&)[N]>(f[k * N]));
-            if (u == 0 && base == 0 && thread < c.pieces) e.start(f);
-            e.add(f);
-        }
-    }
-    if (thread < c.edges()) {
-        const float f[1] = {(float)x[c.edge<T>(thread)]};
-        if (thread >= c.pieces) e.start(f);
-        e.add(f);
-    }
+            if (wave_first < c.edges()) {
+                const float edge[1] = {thread < c.edges() ? (float)x[c.edge<T>(thread)] : -INFINITY};
+                if (FIRST && c.pieces == 0) e.start(edge);
+                e.add(edge);
+            }
+}
+template <class T, int TEAM>
+__device__ ExpSum stream_sum(const T *x, const Cut &c, int32_t thread) {
+    ExpSum e;
+    stream_pass<T, TEAM, true>(x, c, thread, e);
+    if (e.again()) stream_pass<T, TEAM, false>(x, c, thread, e);
     return e;
 }
 
-// The team's joint sum; s = 0 where it cannot be relied on.  What threads that guessed M = 0 may have lost is below V 2^-126 in all.  That is
-// nothing beside a joint sum of 2^-64 and more.  A smaller one is either relative to such a guess, and then s itself is small, or relative to
-// another thread's M below -64.
-constexpr float kLeastSum = 0x1p-64f, kLeastM = -64.f;
+// The team's joint sum; s = 0 where it cannot be relied on.  What wavefronts that guessed M = 0 and have no sum may have lost is below V 2^-126
+// in all, which is nothing beside a joint sum of 2^-65 and more: the largest wavefront's is 2^(M - 1) at the least.
+constexpr float kLeastM = -64.f;
 
 template <int WAVES>
 __device__ __forceinline__ ExpSum join_team(ExpSum e, TeamShared<WAVES> &sh) {
@@ -305,8 +320,10 @@ __device__ __forceinline__ ExpSum join_team(ExpSum e, TeamShared<WAVES> &sh) {
     e = join_wave(e, doubt);
     if constexpr (WAVES > 1) {
         if (lane_id() == 0) {
-            sh.m[wave_id()] = e.m;
-            sh.s[wave_id()] = doubt ? -e.s : e.s;                  // in the sign, also of zero
+            // as a part in [1/2, 1) and a power of two: else a large sum beside a larger M would be lost with that power
+            const float part = __builtin_amdgcn_frexp_mantf(e.s);
+            sh.m[wave_id()] = e.m + (float)__builtin_amdgcn_frexp_expf(e.s);
+            sh.s[wave_id()] = doubt ? -part : part;                // in the sign, also of zero
         }
         __syncthreads();
         const int w = (int)threadIdx.x & (WAVES - 1);
@@ -315,7 +332,7 @@ __device__ __forceinline__ ExpSum join_team(ExpSum e, TeamShared<WAVES> &sh) {
         e.m = group_max<16>(mw);
         e.s = group_sum<16>(fabsf(sw) * __builtin_amdgcn_exp2f(mw - e.m)) * ((float)WAVES / 16.f);
     }
-    if (e.s < kLeastSum || (doubt && e.m < kLeastM)) e.s = 0.f;
+    if (doubt && e.m < kLeastM) e.s = 0.f;
     return e;
 }
 

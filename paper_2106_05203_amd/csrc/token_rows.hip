@@ -6,7 +6,7 @@ namespace {
 
 // A team per row, one pass, bound by memory: 1 GB of bf16 logits 155 us (6.9 TB/s).
 template <class T, int WAVES>
-__global__ __launch_bounds__(Team<WAVES>::kBlock) void token_logps_kernel(LogitRows in, float *logp, float *lse) {
+__global__ __launch_bounds__(Team<WAVES>::kBlock, 8) void token_logps_kernel(LogitRows in, float *logp, float *lse) {
     typedef Team<WAVES> G;
     __shared__ TeamShared<WAVES> shared[2];
     int turn = 0;

@@ -134,3 +134,56 @@ def test_a_row_moved_by_a_constant(gpu, vocab, dtype):
                        ("preference_loss", lambda y: b.ef21_preference_loss(y, dl, start, zero, 1.0, grad=False)[1]),
                        ("policy_loss", lambda y: b.ef21_policy_loss(y, dl, zero, zero, 0.2, 0.2, grad=False)[2])]:
         lm.inside(as64(logp(moved)), as64(logp(x)), bound, what)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [24, 130, 700, 5003, 20000, 50304, 150001])
+def test_entries_far_from_the_first_ones(gpu, vocab, dtype):
+    """A thread adds its part of a row relative to its first entries.  Here others lie 20 to 130 above them (in another thread's reach or not), or below
+    where the first ones are masked."""
+    torch, b = gpu
+    print(f"far entries vocab={vocab} {dtype}", flush=True)
+    rng = np.random.default_rng(vocab)
+    at, base = np.arange(vocab), rng.standard_normal(vocab)
+    kinds = [40 * base, 25 * base - 85, 100 * base + 50]
+    for up in (20.0, 30.0, 45.0, 60.0, 75.0, 85.0, 87.0):
+        one = base - 50.0
+        one[-1 - vocab // 3] += up
+        kinds.append(one)
+        two = base - 80.0                                              # one more, among the first entries of another thread
+        two[3], two[-1 - vocab // 3] = 9.0, -80.0 + up
+        kinds.append(two)
+    for height in (-80.0, -60.0, -30.0, 30.0, 60.0, 80.0):             # nothing among the first entries
+        kinds.append(np.where(at < max(vocab // 2, 4), -math.inf, height + base))
+        few = np.where(at % 7 == 5, height + 3 * base, -1e4)
+        kinds.append(few)
+    for down in (60.0, 86.5, 87.5, 88.0):                              # a few high entries: the first ones of some threads, behind low ones in others
+        for share in (0.003, 0.01, 0.03, 0.1):
+            high = rng.random(vocab) < share
+            high[[0, -2]] = True
+            kinds.append(np.where(high, 0.0, -down) + 0.1 * base)
+    kinds = kinds[1:] if len(kinds) % 2 else kinds
+    if vocab > 20000:
+        kinds = kinds[-16:] + kinds[:10]
+    x = torch.from_numpy(np.stack(kinds)).to(lm.TORCH[dtype]).cuda()
+    labels = np.argmax(as64(x), axis=1)
+    likely = np.argsort(-as64(x), axis=1)[:, : min(vocab, 4)]
+    labels[::3] = likely[::3, -1]                                      # also one that is not the largest
+    far = lm.Rows(as64(x), labels).logp < -60.0
+    labels[far] = np.argmax(as64(x), axis=1)[far]
+    check(torch, b, x, labels, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_large_sum_beside_a_guess(gpu, dtype):
+    """Four wavefronts take 6144 columns, 2048 at first.  One finds masks and then an entry at -44; the others start at -90 and one of them meets an entry at
+    -46.25: relative to what they started from 2^-63 and 2^63, and a ninth of the row's sum is the second one's."""
+    torch, b = gpu
+    vocab, entries = 6144, 4 if dtype == "f32" else 8
+    at = np.arange(vocab)
+    wave = at // entries % 256 // 64
+    row = np.where(wave == 0, -math.inf, -90.0)
+    low, high = np.flatnonzero((wave == 1) & (at > 4200))[9], np.flatnonzero((wave == 0) & (at > 4200))[20]
+    row[high], row[low] = -44.0, -46.25
+    x = torch.from_numpy(np.stack([row, row])).to(lm.TORCH[dtype]).cuda()
+    check(torch, b, x, np.array([low, high]), dtype)
