@@ -311,7 +311,8 @@ int ef21_embed(const void *table, int table_type, int64_t vocab, int64_t width, 
  * table_grad + i * worker_stride -- with worker_stride = d a block of the rows [n][d] that ef21_step takes.  accumulate != 0
  * adds to what is there (a table shared with the output layer) and leaves rows without a token untouched; 0 writes every row.
  * Tokens outside [0, vocab) contribute nothing.  The positions are sorted by token and a token's rows are added in an order
- * that the tokens alone fix.  n in [1, 65535], count and vocab below 2^31.
+ * that n, count, width and the tokens fix: the same call gives the same bits, another number of workers may round differently.
+ * n in [1, 65535], count and vocab below 2^31.
  * workspace: 256-byte aligned device memory of at least the bytes that ef21_embed_grad_workspace says.
  */
 int ef21_embed_grad_workspace(int32_t n, int64_t count, int64_t vocab, int64_t width, int64_t *bytes);
