@@ -186,12 +186,13 @@ struct TeamShared {
     float m[WAVES], s[WAVES];
 };
 
-// A wavefront's joint sum, the same in every lane; without a sum it has no say in what the team's M is.  doubt: it guessed M = 0 and has no sum,
-// so all its entries are masks, or below 2^-126.
+// A wavefront's joint sum, the same in every lane; without a sum it has no say in what the team's M is, unless its M is beyond kMostM, where z of
+// the very entry that M is of may be rounded out of range (then the team takes the row again).  doubt: it guessed M = 0 and has no sum, so all
+// its entries are masks, or below 2^-126.
 __device__ __forceinline__ ExpSum join_wave(ExpSum e, bool &doubt) {
     e.s = group_sum<64>(e.s);
     doubt = e.s == 0.f && e.m == 0.f;
-    if (e.s == 0.f) e.m = kLowest;
+    if (e.s == 0.f && e.m < kMostM) e.m = kLowest;
     return e;
 }
 

@@ -187,3 +187,18 @@ def test_a_large_sum_beside_a_guess(gpu, dtype):
     row[high], row[low] = -44.0, -46.25
     x = torch.from_numpy(np.stack([row, row])).to(lm.TORCH[dtype]).cuda()
     check(torch, b, x, np.array([low, high]), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [24, 700, 5003, 20000, 50304, 150001])
+def test_one_entry_beyond_all_scales(gpu, vocab, dtype):
+    """A row of ordinary logits with one of 10^9 to 3 10^38: x log2 e of that one is rounded by more than fp32's range of exponents."""
+    torch, b = gpu
+    print(f"one large entry vocab={vocab} {dtype}", flush=True)
+    rng = np.random.default_rng(vocab)
+    rows = 24
+    values = rng.standard_normal((rows, vocab))
+    labels = rng.integers(0, vocab, rows)
+    values[np.arange(rows), labels] = np.append(10.0 ** rng.uniform(9, 38, rows - 2), [3.3e38, 2.0 ** 127])
+    x = torch.from_numpy(values).to(lm.TORCH[dtype]).cuda()
+    check(torch, b, x, labels, dtype)
