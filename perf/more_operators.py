@@ -1,0 +1,443 @@
+"""Operators of training and scoring language models next to those of perf/operators.py, as a program calls them.
+
+Kinds of case:
+
+  stats   ef21_token_stats: lse, entropy and the k most likely tokens of each row of logits, log-probabilities of the labels where there
+          are any, and with backward=True ef21_token_stats_grad: the gradient of the logits from those of log-probabilities and entropies
+  norm    ef21_grad_norm: the norm of all gradients together, and the factor that clips it
+  adamw   AdamW.step: one step on many tensors, states in 32 bits, or in 8 with a scale per 256 entries
+
+Rows whose label is -100 are ignored; their logits hold NaN here, as memory that nobody filled would.  The tensors of norm and adamw lie in
+common buffers, each from a multiple of 256 entries on, with zeros between them; the plain form works on the buffers as a whole.
+Inputs are drawn on the GPU from the seed alone.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+IGNORE, BLOCK = -100, 256
+BETA1, BETA2, EPS, STEP, LR, DECAY = 0.9, 0.999, 1e-8, 1000, 1e-3, 0.1
+
+
+# ---------------------------------------------------------------- the cases
+def listed():
+    return [
+        # one sequence's next token, before it is drawn: no label, twenty alternatives; latency alone
+        dict(name="stats_token", kind="stats", rows=1, vocab=131072, dtype="bf16", k=20, labelled=False, ignored=0.0, padded=0, backward=False, wide=True),
+        # one decoding step of 64 sequences, with the token that was drawn: an odd vocabulary, so no two rows are aligned alike
+        dict(name="stats_decode", kind="stats", rows=64, vocab=50001, dtype="f16", k=5, labelled=True, ignored=0.0, padded=0, backward=False, wide=True),
+        # scoring given texts in fp32: a vocabulary padded by columns of -inf, an odd number of rows
+        dict(name="stats_score", kind="stats", rows=2001, vocab=32064, dtype="f32", k=8, labelled=True, ignored=0.125, padded=63, backward=False, wide=False),
+        # training with log-probabilities, entropies and the first alternatives watched
+        dict(name="stats_train", kind="stats", rows=4096, vocab=50001, dtype="f16", k=2, labelled=True, ignored=0.125, padded=0, backward=True, wide=True),
+        # the largest: a policy step with an entropy term on 8192 tokens of a large vocabulary
+        dict(name="stats_step", kind="stats", rows=8192, vocab=131072, dtype="bf16", k=0, labelled=True, ignored=0.125, padded=0, backward=True, wide=True),
+        # the gradient estimate of a problem of 50 000 coordinates, one tensor
+        dict(name="norm_small", kind="norm", tensors=1, total=50000, grad="f32", scale=1.0, mix=1),
+        # gradients of a model with a table of 131072 rows of 2048, and its smaller tensors
+        dict(name="norm_model", kind="norm", tensors=146, total=402653184, grad="bf16", scale=1.0 / 1024, mix=2),
+        # a toy model
+        dict(name="adamw_toy", kind="adamw", tensors=4, total=100100, param="f32", grad="f32", copy="", bits=32, stochastic=False, clip=False, mix=3),
+        # a model of 11.2 million entries in many tensors, as an image classifier or a small language model has them
+        dict(name="adamw_many", kind="adamw", tensors=146, total=11200000, param="f32", grad="bf16", copy="", bits=32, stochastic=False, clip=True, mix=4),
+        # fp32 parameters with the bf16 copy that the next forward pass reads
+        dict(name="adamw_master", kind="adamw", tensors=146, total=402653184, param="f32", grad="bf16", copy="bf16", bits=32, stochastic=False, clip=True, mix=5),
+        # nothing in 32 bits: bf16 parameters and 8-bit states, rounded stochastically
+        dict(name="adamw8_many", kind="adamw", tensors=146, total=11200000, param="bf16", grad="bf16", copy="", bits=8, stochastic=True, clip=True, mix=6),
+        # fp32 parameters and gradients, as the compressed step's estimate is, with 8-bit states
+        dict(name="adamw8_model", kind="adamw", tensors=146, total=201326592, param="f32", grad="f32", copy="", bits=8, stochastic=True, clip=False, mix=7),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    """A whole number in [lo, hi], uniform in its logarithm."""
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))))
+
+
+def draw(rng):
+    kind = rng.choice(["stats", "stats", "norm", "adamw", "adamw"])
+    if kind == "stats":
+        vocab = _log_int(rng, 500, 262144)
+        if rng.random() < 0.5:
+            vocab = -(-vocab // 64) * 64
+        labelled = rng.random() < 0.8
+        return dict(kind=kind, rows=_log_int(rng, 1, max(1, min(16384, 500000000 // vocab))), vocab=vocab, dtype=rng.choice(["f32", "bf16", "f16"]),
+                    k=rng.choice([0, 1, 5, 20, 64, rng.randint(1, 64)]), labelled=labelled, ignored=rng.choice([0.0, 0.125, 0.3]) if labelled else 0.0,
+                    padded=rng.choice([0, 0, vocab % 64 and 1, 17]), backward=rng.random() < 0.5, wide=rng.random() < 0.5)
+    tensors = _log_int(rng, 1, 400)
+    total = _log_int(rng, max(1000, 20 * tensors), 200000000)
+    mix, grad = rng.randrange(1 << 30), rng.choice(["f32", "bf16", "f16"])
+    if kind == "norm":
+        return dict(kind=kind, tensors=tensors, total=total, grad=grad, scale=rng.choice([1.0, 1.0 / 1024]), mix=mix)
+    param = rng.choice(["f32", "f32", "bf16", "f16"])
+    bits = rng.choice([32, 8])
+    return dict(kind=kind, tensors=tensors, total=total, param=param, grad=grad, copy=rng.choice(["", "bf16", "f16"]) if param == "f32" else "", bits=bits,
+                stochastic=(bits == 8 or param != "f32") and rng.random() < 0.7, clip=rng.random() < 0.6, mix=mix)
+
+
+def _ignored(c):
+    """Rows without a label: the same number for every seed, and never all of them."""
+    return min(c["rows"] - 1, int(round(c["ignored"] * c["rows"])))
+
+
+def _sizes(c):
+    """Entries of each tensor: a few large ones hold most of the total, every other one is odd."""
+    rng = random.Random(c["mix"])
+    share = [math.exp(rng.uniform(0.0, 8.0)) for _ in range(c["tensors"])]
+    sizes = [max(1, int(c["total"] * s / sum(share))) for s in share]
+    return [n if i % 2 else max(16, n // 16 * 16) for i, n in enumerate(sizes)]
+
+
+# ---------------------------------------------------------------- inputs
+def _generator(seed):
+    return torch.Generator(device=DEV).manual_seed(int(seed))
+
+
+def _logits(c, g):
+    """(logits, labels): normal logits with the label's raised; -inf in the padding columns; NaN in the rows without a label."""
+    rows, vocab, real = c["rows"], c["vocab"], c["vocab"] - c["padded"]
+    x = torch.randn(rows, vocab, generator=g, device=DEV, dtype=TYPES[c["dtype"]]).mul_(2.0)
+    if c["padded"]:
+        x[:, real:] = -math.inf
+    u = torch.rand(rows, generator=g, device=DEV, dtype=torch.float64)                       # Zipf's law
+    labels = ((float(real) + 1.0) ** u - 1.0).to(torch.int64).clamp_(0, real - 1)
+    x[torch.arange(rows, device=DEV), labels] += torch.rand(rows, generator=g, device=DEV).mul_(6.0).add_(4.0).to(x.dtype)
+    k = _ignored(c)
+    if k:
+        out = torch.randperm(rows, generator=g, device=DEV)[:k]
+        labels[out] = IGNORE
+        x[out] = math.nan
+    return x, labels if c["wide"] else labels.to(torch.int32)
+
+
+def _coded(x):
+    """Blocks of 256 entries in 8 bits, to nearest, and their scales, as an earlier step left them."""
+    blocks = x.view(-1, BLOCK)
+    scale = (blocks.abs().amax(1) / 448.0).clamp_(min=2.0 ** -126)
+    return (blocks / scale[:, None]).clamp_(-448.0, 448.0).to(torch.float8_e4m3fn).view(-1), scale
+
+
+def prepare(case, seed):
+    c, g = case, _generator(seed)
+    s = {"case": c}
+    randn = lambda *shape: torch.randn(*shape, generator=g, device=DEV)  # noqa: E731
+    if c["kind"] == "stats":
+        rows, k = c["rows"], c["k"]
+        s["logits"], s["labels"] = _logits(c, g)
+        if not c["labelled"]:
+            s["labels"] = None
+        s["out"] = {n: torch.empty(rows, device=DEV) for n in ("lse", "entropy")}
+        if c["labelled"]:
+            s["out"]["logp"] = torch.empty(rows, device=DEV)
+        if k:
+            s["out"]["top_tokens"], s["out"]["top_logp"] = torch.empty(rows, k, device=DEV, dtype=torch.int32), torch.empty(rows, k, device=DEV)
+        if c["backward"]:
+            size = (1024.0 if c["dtype"] == "f16" else 1.0) / rows                           # gradients in f16 go with a loss scale
+            s["grad"] = torch.empty_like(s["logits"])
+            s["grad_logp"] = randn(rows).mul_(size) if c["labelled"] else None
+            s["grad_entropy"] = randn(rows).mul_(0.1).sub_(0.2).mul_(size)
+        return s
+    sizes = _sizes(c)
+    starts, at = [], 0
+    for n in sizes:
+        starts.append(at)
+        at += -(-n // BLOCK) * BLOCK
+    of = torch.repeat_interleave(torch.arange(len(sizes), device=DEV), torch.tensor([-(-n // BLOCK) for n in sizes], device=DEV), output_size=at // BLOCK)
+    first, length = torch.tensor(starts, device=DEV), torch.tensor(sizes, device=DEV)
+    inside = torch.arange(at, device=DEV).view(-1, BLOCK) < (first + length)[of][:, None]    # else between two tensors
+    views = lambda flat: [flat[a:a + n] for a, n in zip(starts, sizes)]  # noqa: E731
+    spread = torch.exp(randn(at // BLOCK, 1))                                                # some blocks' gradients are larger than others'
+    # the gradients of a block have a common size and entries of their own
+    g0 = randn(at).view(-1, BLOCK).mul_(spread).mul_(inside)
+    s["grad"] = (g0 * (1e-3 * (1024.0 if c["grad"] == "f16" else 1.0))).to(TYPES[c["grad"]]).view(-1)
+    s["grads"] = views(s["grad"])
+    if c["kind"] == "norm":
+        s["max_norm"] = 0.5 * c["scale"] * 1e-3 * math.sqrt(sum(sizes))                      # clips
+        s["norm"], s["factor"] = torch.empty(1, device=DEV), torch.empty(1, device=DEV)
+        return s
+    s["param"] = randn(at).view(-1, BLOCK).mul_(0.02).mul_(inside).to(TYPES[c["param"]]).view(-1)
+    s["params"] = views(s["param"])
+    size = spread * 1e-3 * (1.0 if c["clip"] or c["grad"] != "f16" else 1024.0)
+    m = randn(at).view(-1, BLOCK).mul_(0.3 * size).mul_(inside)
+    v = randn(at).view(-1, BLOCK).square_().add_(0.2).mul_(size * size).mul_(inside)
+    if c["bits"] == 8:
+        (s["m"], s["m_scale"]), (s["v"], s["v_scale"]) = _coded(m), _coded(v.sqrt_())
+        in_blocks = lambda flat: [flat[a // BLOCK:a // BLOCK + -(-n // BLOCK)] for a, n in zip(starts, sizes)]  # noqa: E731
+        s["m_scales"], s["v_scales"] = in_blocks(s["m_scale"]), in_blocks(s["v_scale"])
+    else:
+        s["m"], s["v"] = m.view(-1), v.view(-1)
+    s["ms"], s["vs"] = views(s["m"]), views(s["v"])
+    if c["copy"]:
+        s["copy"] = torch.zeros(at, device=DEV, dtype=TYPES[c["copy"]])
+        s["copies"] = views(s["copy"])
+    # what clipping left: the same factor as a program would read from ef21_grad_norm
+    s["factor"] = torch.tensor([0.37 / (1024.0 if c["grad"] == "f16" else 1.0)], device=DEV) if c["clip"] else None
+    # tensors of many entries decay, the others (biases, norms) do not
+    s["decay"] = [DECAY if n >= 4096 else 0.0 for n in sizes]
+    s["decays"] = torch.tensor(s["decay"], device=DEV)[of]                                   # per block
+    s["tensor_of"], s["first"] = of, first                                                   # per block, per tensor
+    s["seed"] = 1000003 * (int(seed) % 1000003) + 12345
+    return s
+
+
+# ---------------------------------------------------------------- one pass
+def run(s):
+    return _run_own(s) if own else _run_plain(s)
+
+
+def _adamw_outputs(s):
+    return {n: s[n] for n in ("param", "m", "v", "m_scale", "v_scale", "copy") if n in s}
+
+
+def _run_own(s):
+    from paper_2106_05203_amd import binding as b
+    c = s["case"]
+    if c["kind"] == "stats":
+        got = b.ef21_token_stats(s["logits"], s["labels"], c["k"], **s["out"])
+        out = dict(s["out"])
+        if c["backward"]:
+            out["grad"] = b.ef21_token_stats_grad(s["logits"], s["labels"], got.sums, got.entropy, s["grad_logp"], s["grad_entropy"], out=s["grad"])
+        return out
+    if c["kind"] == "norm":
+        if "list" not in s:
+            s["list"] = b.TensorList(s["grads"])
+        norm, factor = b.ef21_grad_norm(s["list"], s["max_norm"], c["scale"], norm=s["norm"], factor=s["factor"])
+        return {"norm": norm, "factor": factor}
+    if "optimizer" not in s:                                                                 # a program makes it once
+        s["optimizer"] = b.AdamW(s["params"], s["grads"], betas=(BETA1, BETA2), eps=EPS, weight_decay=s["decay"], bits=c["bits"], m=s["ms"], v=s["vs"],
+                                 m_scale=s.get("m_scales"), v_scale=s.get("v_scales"), copies=s.get("copies"), stochastic=c["stochastic"], seed=s["seed"])
+    s["optimizer"].step(LR, step=STEP, grad_scale=s["factor"])
+    return _adamw_outputs(s)
+
+
+def _plain_stats(s):
+    c, x = s["case"], s["logits"]
+    if c["labelled"]:
+        labels = s["labels"].long()
+        has = labels >= 0
+        x = torch.where(has[:, None], x, 0.0)
+    x = x.float()
+    top = x.amax(1, keepdim=True)
+    z = x - top
+    p = torch.exp(z)
+    total = p.sum(1, keepdim=True)
+    p /= total
+    lse = (top + torch.log(total))[:, 0]
+    log_p = z.sub_(torch.log(total))
+    weighed = torch.where(p > 0, p * log_p, 0.0)
+    entropy = -weighed.sum(1)
+    keep = (lambda v, other=0.0: torch.where(has, v, other)) if c["labelled"] else (lambda v, other=0.0: v)
+    out = {"lse": keep(lse), "entropy": keep(entropy)}
+    if c["labelled"]:
+        at = labels.clamp(min=0)
+        out["logp"] = keep(log_p.gather(1, at[:, None])[:, 0])
+    if c["k"]:
+        # by value, ties to the lower token: value and place in one whole number (-0 and 0 are equal)
+        bits = x.view(torch.int32).long()
+        key = torch.where(bits < 0, -(bits & 0x7FFFFFFF), bits) * 2 ** 31 - torch.arange(c["vocab"], device=DEV)
+        tokens = key.topk(c["k"], 1).indices
+        top_logp = log_p.gather(1, tokens)
+        if c["labelled"]:
+            tokens, top_logp = torch.where(has[:, None], tokens, -1), torch.where(has[:, None], top_logp, 0.0)
+        out["top_tokens"], out["top_logp"] = tokens.to(torch.int32), top_logp
+    if c["backward"]:
+        a, b = s["grad_logp"], keep(s["grad_entropy"])
+        grad = weighed.addcmul_(p, entropy[:, None]).mul_(-b[:, None])
+        if c["labelled"]:
+            a = keep(a)
+            grad.addcmul_(p, a[:, None], value=-1.0)
+            grad[torch.arange(c["rows"], device=DEV), at] += a
+        out["grad"] = grad.to(s["logits"].dtype)
+    return out
+
+
+def _mix(x):
+    """A bijection of 32-bit numbers (held in 64 bits) whose outputs look random."""
+    x = x ^ (x >> 16)
+    x = (x * 0x6A09E667) & 0xFFFFFFFF
+    x = x ^ (x >> 15)
+    x = (x * 0xBB67AE85) & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def _random_bits(s, more):
+    """Sixteen bits for m, v and the parameter (if `more`) of each entry, by seed, step, tensor and place in the tensor."""
+    seed = s["seed"]
+    key = (_mix((_mix(seed & 0xFFFFFFFF) + (seed >> 32)) & 0xFFFFFFFF) + STEP) & 0xFFFFFFFF
+    key = _mix((_mix(key) + torch.arange(len(s["first"]), device=DEV)) & 0xFFFFFFFF)
+    place = (torch.arange(s["m"].numel(), device=DEV).view(-1, BLOCK) - s["first"][s["tensor_of"]][:, None])
+    h = _mix(place ^ _mix(key)[s["tensor_of"]][:, None])                                     # no tensor here has 2^32 entries
+    return h & 0xFFFF, h >> 16, _mix((h + 0x3C6EF372) & 0xFFFFFFFF) & 0xFFFF if more else None
+
+
+def _rounded(x, bits, mantissa, least):
+    """|x| to a floating type of so many mantissa bits and least exponent: down, or up with the probability of what is above."""
+    x = x.double()
+    exponent = torch.frexp(x.abs()).exponent.sub_(1).clamp_(min=least)
+    unit = torch.ldexp(torch.ones_like(x), exponent.sub_(mantissa))
+    return torch.copysign(torch.floor(x.abs() / unit + (bits + 0.5) / 65536.0) * unit, x)
+
+
+def _plain_code(x, bits):
+    """(8-bit values, scales) of blocks of 256 entries."""
+    scale = (x.abs().amax(1) / 448.0).clamp_(min=2.0 ** -126)
+    r = x / scale[:, None]
+    if bits is not None:
+        r = _rounded(r, bits, 3, -6)
+    return r.clamp_(-448.0, 448.0).float().to(torch.float8_e4m3fn), scale
+
+
+def _plain_adamw(s):
+    c = s["case"]
+    eight = c["bits"] == 8
+    block = lambda t: t.view(-1, BLOCK)  # noqa: E731
+    g, p = block(s["grad"]).float(), block(s["param"]).float()
+    if s["factor"] is not None:
+        g = g * s["factor"]
+    m, v = block(s["m"]).float(), block(s["v"]).float()
+    if eight:
+        m, v = m * s["m_scale"][:, None], (v * s["v_scale"][:, None]).square()
+    m = m * BETA1 + g * (1.0 - BETA1)
+    v = v * BETA2 + g * g * (1.0 - BETA2)
+    root = v.sqrt()
+    p = p - LR * (p * s["decays"][:, None] + m / (1.0 - BETA1 ** STEP) / (root / math.sqrt(1.0 - BETA2 ** STEP) + EPS))
+    for_m, for_v, for_p = _random_bits(s, c["param"] != "f32") if c["stochastic"] else (None, None, None)
+    if eight:
+        m, m_scale = _plain_code(m, for_m)
+        q, v_scale = _plain_code(root, for_v)
+        q = torch.where(root > 0, q.float().clamp(min=2.0 ** -9), 0.0)                       # never to zero
+        block(s["v"]).copy_(q)
+        s["m_scale"].copy_(m_scale)
+        s["v_scale"].copy_(v_scale)
+    else:
+        block(s["v"]).copy_(v)
+    block(s["m"]).copy_(m)
+    if for_p is not None:
+        p = _rounded(p, for_p, *((7, -126) if c["param"] == "bf16" else (10, -14)))
+    block(s["param"]).copy_(p)
+    if c["copy"]:
+        block(s["copy"]).copy_(p)
+    return _adamw_outputs(s)
+
+
+def _run_plain(s):
+    c = s["case"]
+    if c["kind"] == "stats":
+        return _plain_stats(s)
+    if c["kind"] == "norm":
+        norm = s["grad"].float().square().sum().sqrt() * c["scale"]
+        return {"norm": norm.view(1), "factor": (c["scale"] * torch.clamp(s["max_norm"] / norm, max=1.0)).view(1)}
+    return _plain_adamw(s)
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+def work(case):
+    c = case
+    size = lambda t: 4 if t == "f32" else 2 if t else 0  # noqa: E731
+    if c["kind"] == "stats":
+        b = size(c["dtype"])
+        read = (c["rows"] - _ignored(c)) * c["vocab"]                    # rows without a label need not be read
+        per_row = 8 + 8 * c["k"] + ((12 if c["wide"] else 8) if c["labelled"] else 0) + (8 if c["backward"] else 0)
+        return {"bytes": read * b + (c["rows"] * c["vocab"] * b if c["backward"] else 0) + c["rows"] * per_row, "flops": read * (10 if c["backward"] else 6)}
+    n = sum(_sizes(c))
+    if c["kind"] == "norm":
+        return {"bytes": n * size(c["grad"]) + 8, "flops": 2 * n}
+    state = 2 * n + 8 * sum(-(-k // BLOCK) for k in _sizes(c)) if c["bits"] == 8 else 8 * n
+    return {"bytes": n * (2 * size(c["param"]) + size(c["grad"]) + size(c["copy"])) + 2 * state, "flops": 16 * n}
+
+
+# ---------------------------------------------------------------- 64 bits
+def _exact_rounded(x, bits, mantissa, least):
+    """x [any] in 64 bits to the grid: the two neighbours, and which of them."""
+    size = x.abs()
+    e = torch.floor(torch.log2(torch.where(size > 0, size, 1.0)))
+    e = torch.where(2.0 ** e > size, e - 1, e)                            # log2 may round up to a power of two
+    e = torch.where(2.0 ** (e + 1) <= size, e + 1, e).clamp(min=least)
+    unit = 2.0 ** (e - mantissa)
+    low = torch.floor(size / unit)
+    if bits is None:
+        up = (size / unit - low > 0.5) | ((size / unit - low == 0.5) & (low % 2 == 1))
+    else:
+        up = size / unit - low + (bits.double() + 0.5) / 65536.0 >= 1.0
+    return torch.sign(x) * (low + up.double()) * unit
+
+
+def _exact_adamw(c, s):
+    keys = []
+    word = lambda v: v & 0xFFFFFFFF  # noqa: E731
+    for t in range(len(s["params"])):
+        h = _mix(word(s["seed"]))
+        for part in (s["seed"] >> 32, STEP, t):
+            h = _mix(word(h + part))
+        keys.append(_mix(h))                                              # the upper half of the place is zero
+    factor = float(s["factor"][0]) if s["factor"] is not None else 1.0
+    out = {n: torch.zeros(v.shape, device=DEV, dtype=torch.float64) for n, v in _adamw_outputs(s).items()}
+    for t, (p, g, m, v) in enumerate(zip(s["params"], s["grads"], s["ms"], s["vs"])):
+        n, a = p.numel(), int(s["first"][t])
+        blocks = -(-n // BLOCK)
+        wide = lambda x, sc: (torch.nn.functional.pad(x.double(), (0, blocks * BLOCK - n)).view(blocks, BLOCK) * sc.double()[:, None]).view(-1)[:n]  # noqa: E731
+        m, v = (wide(m, s["m_scales"][t]), wide(v, s["v_scales"][t]) ** 2) if c["bits"] == 8 else (m.double(), v.double())
+        g = g.double() * factor
+        m, v = BETA1 * m + (1 - BETA1) * g, BETA2 * v + (1 - BETA2) * g ** 2
+        p = p.double() * (1 - LR * s["decay"][t]) - LR / (1 - BETA1 ** STEP) * m / (torch.sqrt(v / (1 - BETA2 ** STEP)) + EPS)
+        h = _mix(torch.arange(n, device=DEV) ^ keys[t]) if c["stochastic"] else None
+        if c["bits"] == 8:
+            for name, x, b in (("m", m, None if h is None else h % 65536), ("v", torch.sqrt(v), None if h is None else h // 65536)):
+                whole = torch.nn.functional.pad(x, (0, blocks * BLOCK - n)).view(blocks, BLOCK)
+                scale = (whole.abs().amax(1) / 448).clamp(min=2.0 ** -126)
+                q = _exact_rounded(x / scale.repeat_interleave(BLOCK)[:n], b, 3, -6).clamp(-448, 448)
+                if name == "v":
+                    q = torch.where(x > 0, q.clamp(min=2.0 ** -9), q)
+                out[name][a:a + n], out[name + "_scale"][a // BLOCK:a // BLOCK + blocks] = q, scale
+        else:
+            out["m"][a:a + n], out["v"][a:a + n] = m, v
+        if c["copy"]:
+            out["copy"][a:a + n] = p
+        if c["param"] != "f32":
+            b = _mix(word(h + 0x3C6EF372)) % 65536 if h is not None else None
+            p = _exact_rounded(p, b, *((7, -126) if c["param"] == "bf16" else (10, -14)))
+        out["param"][a:a + n] = p
+    return out
+
+
+def exact(case, seed):
+    c, s = case, prepare(case, seed)
+    if c["kind"] == "adamw":
+        return _exact_adamw(c, s)
+    if c["kind"] == "norm":
+        norm = c["scale"] * math.sqrt(sum(float(torch.linalg.vector_norm(g.double())) ** 2 for g in s["grads"]))
+        return {k: torch.tensor([v], device=DEV, dtype=torch.float64) for k, v in (("norm", norm), ("factor", c["scale"] * min(1.0, s["max_norm"] / norm)))}
+    rows, vocab, k = c["rows"], c["vocab"], c["k"]
+    labels = s["labels"].to(torch.int64) if c["labelled"] else torch.zeros(rows, device=DEV, dtype=torch.int64)
+    f64 = dict(device=DEV, dtype=torch.float64)
+    out = {"lse": torch.zeros(rows, **f64), "entropy": torch.zeros(rows, **f64)}
+    if c["labelled"]:
+        out["logp"] = torch.zeros(rows, **f64)
+    if k:
+        out["top_tokens"], out["top_logp"] = None, torch.zeros(rows, k, **f64)
+    if c["backward"]:
+        out["grad"] = torch.zeros(rows, vocab, **f64)
+    for part in torch.nonzero(labels >= 0).view(-1).split(max(1, 100000000 // vocab)):
+        x = s["logits"][part].double()
+        log_p = torch.log_softmax(x, 1)
+        p = log_p.exp()
+        h = -torch.special.xlogy(p, p).sum(1)
+        out["lse"][part], out["entropy"][part] = torch.logsumexp(x, 1), h
+        if c["labelled"]:
+            out["logp"][part] = log_p[torch.arange(len(part), device=DEV), labels[part]]
+        if k:
+            out["top_logp"][part] = torch.sort(log_p, 1, descending=True).values[:, :k]
+        if c["backward"]:
+            d = -s["grad_entropy"][part].double()[:, None] * (torch.special.xlogy(p, p) + p * h[:, None])
+            if c["labelled"]:
+                a = s["grad_logp"][part].double()[:, None]
+                d = d.sub_(a * p).scatter_add_(1, labels[part][:, None], a)
+            out["grad"][part] = d
+    return out
