@@ -200,7 +200,7 @@ def _run_own(s):
     from paper_2106_05203_amd import binding as b
     c = s["case"]
     if c["kind"] == "stats":
-        got = b.ef21_token_stats(s["logits"], s["labels"], c["k"], **s["out"])
+        got = b.ef21_token_stats(s["logits"], s["labels"], c["k"], sums=c["backward"], **s["out"])
         out = dict(s["out"])
         if c["backward"]:
             out["grad"] = b.ef21_token_stats_grad(s["logits"], s["labels"], got.sums, got.entropy, s["grad_logp"], s["grad_entropy"], out=s["grad"])
