@@ -378,6 +378,100 @@ int ef21_policy_loss(const void *logits, int type, int64_t rows, int64_t vocab, 
                      float *logp, void *grad_logits, int64_t grad_stride, void *workspace, int64_t workspace_bytes,
                      void *hip_stream);
 
+/*
+ * What a model says about each row of logits: log-probabilities of given tokens, the entropy and the k most likely tokens,
+ *   lse[r] = log sum_v exp(x_v),  logp[r] = x_label - lse[r],  entropy[r] = -sum_v p_v log p_v with p_v = exp(x_v - lse[r])
+ *   top_tokens, top_logp [rows][k]: the k tokens of largest x_v in descending order, ties to the lower token, and x_v - lse[r]
+ * labels [rows]: rows whose label is outside [0, vocab) are ignored: they are not read, their logp, lse, entropy and top_logp are 0 and their
+ * top_tokens -1.  labels NULL (with any label_type): there are none, every row is taken, and logp must be NULL too.
+ * k in [0, 64] and at most vocab; with k = 0 top_tokens and top_logp may be NULL.  sums: fp32 [rows][2] for ef21_token_stats_grad, whose
+ * contents are that call's business, or NULL.
+ * Entries of -inf have probability zero and take no part in the entropy; they are alternatives too, behind all others, of log-probability -inf.
+ * A row with nothing above -inf has lse = logp = -inf and entropy 0.  A NaN or +inf in a row that is read makes its results NaN and its
+ * top_tokens -1.  A row's results depend on its entries and its alignment alone, not on how many rows there are.
+ * workspace: 256-byte aligned device memory of at least the bytes that ef21_token_stats_workspace says (0 where there are many rows).
+ * EF21_EINVAL also: k out of range, logp without labels or labels without logp.
+ */
+int ef21_token_stats_workspace(int type, int64_t rows, int64_t vocab, int32_t k, int64_t *bytes);
+int ef21_token_stats(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
+                     int label_type, int32_t k, float *logp, float *lse, float *entropy, int32_t *top_tokens, float *top_logp,
+                     float *sums, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * The gradient of the logits from those of the log-probabilities and of the entropies,
+ *   grad_logits[r][v] = grad_logp[r] * ([v = label] - p_v) - grad_entropy[r] * p_v * (log p_v + entropy[r])
+ * sums and entropy as ef21_token_stats gave them for these logits and labels.  grad_logp or grad_entropy may be NULL (zero); without labels
+ * grad_logp must be.  Both are finite and are read in the rows that count.  accumulate != 0 adds to what is in grad_logits (the gradient of another loss; rounded once more, and
+ * rows that are ignored stay as they are) and then grad_logits must not be the logits; else it may be.  Entries of probability zero, ignored rows and rows with
+ * nothing above -inf have a gradient of zero.
+ */
+int ef21_token_stats_grad(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
+                          int label_type, const float *sums, const float *entropy, const float *grad_logp,
+                          const float *grad_entropy, void *grad_logits, int64_t grad_stride, int accumulate, void *hip_stream);
+
+/*
+ * ---- The step of a model's parameters ----
+ * Line 3 of Algorithm 2, x <- x - gamma g, is one way to use the estimate g of the gradient; these calls are another, over many tensors at
+ * once: g may be parts of the vector that ef21_get_state gives, or any gradients.  Stateless, as the section above: nothing is allocated or
+ * synchronised, the calls may be captured, results are bitwise reproducible.  Arrays of `tensor_count` entries are HOST memory and are
+ * read before the call returns; what their pointers name is device memory, contiguous, aligned as its type is.  Tensors of count 0
+ * are allowed (their pointers may be NULL), and so is tensor_count = 0.
+ */
+
+/*
+ * The norm of many gradients together, and the factor that clips it:
+ *   norm[0] = scale * sqrt(sum over all tensors and entries of g^2),   factor[0] = scale * min(1, max_norm / norm[0])
+ * scale > 0: what the gradients still have to be multiplied by (1 / loss scale).  max_norm > 0; INFINITY clips nothing.  Squares and their sum are fp64,
+ * in an order that the counts and types fix.  Where norm[0] is not finite factor[0] is NaN, which ef21_adamw takes for a step to be skipped.
+ * workspace: 256-byte aligned device memory of at least the bytes that ef21_grad_norm_workspace says.
+ */
+int ef21_grad_norm_workspace(int32_t tensor_count, int64_t *bytes);
+int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t *counts, int32_t tensor_count, float scale,
+                   float max_norm, float *norm, float *factor, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * AdamW (decoupled weight decay) over many tensors.  For every entry, with f = grad_scale[0] (1 if NULL) and t = step:
+ *   g' = f g,   m <- beta1 m + (1 - beta1) g',   v <- beta2 v + (1 - beta2) g'^2
+ *   p <- p - lr * (weight_decay * p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * in fp32.  Where f is not finite nothing is changed.  An infinite or NaN gradient otherwise passes into m, v and p, of its entry alone with
+ * 32-bit states; of 8-bit ones an infinity makes its block NaN.
+ *   states: m, v fp32 (m_scale and v_scale NULL), or 8 bits: entry i of m stands for m_scale[i / 256] times the value of byte i as an OCP e4m3 number, and
+ *           sqrt(v) for v_scale[i / 256] times that of v's byte; the scales, ceil(count / 256) of each, are the block's largest value / 448, 2^-126 at the
+ *           least.  The update uses m and v before they are rounded to 8 bits.  A sqrt(v) above zero is never rounded to zero.
+ *   copy:   NULL, or bf16 or fp16 [count] (copy_type): receives the new parameters, rounded to nearest
+ *   stochastic != 0: what is kept in fewer than 32 bits (8-bit states, bf16 or fp16 parameters) is rounded up or down at random, with
+ *           probabilities that make it right on average; a moving average that moves by 1 - beta of itself a step, or a parameter by
+ *           less than half of its last bit, would stay where it is if it were rounded to nearest.  The choice follows from seed, step, the tensor's number
+ *           in the call and the entry's, so that the same call gives the same bits.
+ * lr_device, step_device: NULL, or fp32 [1] and int64 [1] that are read on the device in the place of lr and step (a captured call whose
+ * values change; a step below 1 counts as 1).
+ * The written arrays (param, m, v, their scales, copy) must not overlap one another or the gradients; no tensor may be listed twice.
+ * EF21_EINVAL: a count < 0, an unknown type, a NULL or misaligned pointer, one scale without the other, lr or weight_decay not finite,
+ * beta1 or beta2 outside [0, 1), eps not finite and > 0, step < 1.
+ */
+typedef struct ef21_adamw_tensor {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    void *copy;
+    int64_t count;
+    int32_t param_type, grad_type, copy_type;
+    float weight_decay;
+} ef21_adamw_tensor;
+
+typedef struct ef21_adamw_options {
+    double lr, beta1, beta2, eps;    /* 1 - 0.999 in fp32 is 1e-5 of itself off */
+    int64_t step;
+    const float *lr_device;
+    const int64_t *step_device;
+    const float *grad_scale;
+    uint64_t seed;
+    int32_t stochastic;
+} ef21_adamw_options;
+
+int ef21_adamw(const ef21_adamw_tensor *tensors, int32_t tensor_count, const ef21_adamw_options *options, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

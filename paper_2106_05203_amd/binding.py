@@ -8,7 +8,9 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import math
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -27,16 +29,33 @@ SYMBOLS = (
     "ef21_hbm_read", "ef21_hbm_copy", "ef21_get_choices", "ef21_set_loss", "ef21_set_minibatch", "ef21_theory_stepsize",
     "ef21_topk_static", "ef21_embed", "ef21_embed_grad_workspace", "ef21_embed_grad", "ef21_token_logps", "ef21_token_logps_grad",
     "ef21_preference_loss_workspace", "ef21_preference_loss", "ef21_policy_loss_workspace", "ef21_policy_loss",
+    "ef21_token_stats_workspace", "ef21_token_stats", "ef21_token_stats_grad", "ef21_grad_norm_workspace", "ef21_grad_norm", "ef21_adamw",
 )
 K_COUNT = 11
 VALUE_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # EF21_F32, EF21_BF16, EF21_F16
 TOKEN_TYPES = {torch.int32: 0, torch.int64: 1}                          # EF21_I32, EF21_I64
 
 
+STATE_BLOCK = 256                                                       # entries that share the scales of 8-bit states
+
+
 class EF21Error(RuntimeError):
     def __init__(self, code: int, text: str):
         super().__init__(f"libef21 error {code}: {text}")
         self.code = code
+
+
+class AdamwTensor(C.Structure):
+    """ef21_adamw_tensor"""
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("copy", C.c_void_p), ("count", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("copy_type", C.c_int32),
+                ("weight_decay", C.c_float)]
+
+
+class AdamwOptions(C.Structure):
+    """ef21_adamw_options"""
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64), ("lr_device", C.c_void_p),
+                ("step_device", C.c_void_p), ("grad_scale", C.c_void_p), ("seed", C.c_uint64), ("stochastic", C.c_int32)]
 
 
 _lib = None
@@ -87,6 +106,12 @@ def load_library() -> C.CDLL:
     lib.ef21_preference_loss.argtypes = [*logits, p, i32, p, f32, f32, C.c_int, C.c_int, p, p, p, p, i64, p, i64, p]
     lib.ef21_policy_loss_workspace.argtypes = [i64, p]
     lib.ef21_policy_loss.argtypes = [*logits, p, p, p, p, f32, f32, f32, p, p, p, p, i64, p, i64, p]
+    lib.ef21_token_stats_workspace.argtypes = [C.c_int, i64, i64, i32, p]
+    lib.ef21_token_stats.argtypes = [*logits, i32, p, p, p, p, p, p, p, i64, p]
+    lib.ef21_token_stats_grad.argtypes = [*logits, p, p, p, p, p, i64, C.c_int, p]
+    lib.ef21_grad_norm_workspace.argtypes = [i32, p]
+    lib.ef21_grad_norm.argtypes = [p, p, p, i32, f32, f32, p, p, p, i64, p]
+    lib.ef21_adamw.argtypes = [p, i32, p, p]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = C.c_int
     lib.ef21_kernel_name.restype = C.c_char_p
@@ -380,6 +405,260 @@ def ef21_policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch
     return out_loss, token_loss, logp, grad
 
 
+class TokenStats(NamedTuple):
+    """What ef21_token_stats returns; None where it was not asked for."""
+    logp: "torch.Tensor | None"          # [rows]
+    lse: torch.Tensor                    # [rows]
+    entropy: torch.Tensor                # [rows]
+    top_tokens: "torch.Tensor | None"    # [rows][k] int32
+    top_logp: "torch.Tensor | None"      # [rows][k]
+    sums: "torch.Tensor | None"          # [rows][2], for ef21_token_stats_grad
+
+
+@functools.lru_cache(maxsize=256)
+def ef21_token_stats_workspace(kind: int, rows: int, vocab: int, k: int) -> int:
+    """Bytes of workspace that ef21_token_stats needs for logits of type `kind` (VALUE_TYPES)."""
+    return _size(load_library().ef21_token_stats_workspace, kind, rows, vocab, k)
+
+
+def _maybe_labelled(logits, labels):
+    if labels is not None:
+        return _logit_rows(logits, labels)
+    at, kind, rows, vocab, stride = _matrix(logits, "logits")
+    return (at, kind, rows, vocab, stride, None, 0), rows
+
+
+def _shaped(t, shape, dtype, like, what: str):
+    """t, or a new tensor; contiguous and of that shape and type."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _gpu(t, what)
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise TypeError(f"{what}: expected contiguous {dtype}, got {t.dtype} (contiguous={t.is_contiguous()})")
+    if t.shape != shape:
+        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def ef21_token_stats(logits: torch.Tensor, labels: torch.Tensor | None = None, k: int = 0, logp: torch.Tensor | None = None,
+                     lse: torch.Tensor | None = None, entropy: torch.Tensor | None = None, top_tokens: torch.Tensor | None = None,
+                     top_logp: torch.Tensor | None = None, sums: "torch.Tensor | bool | None" = None,
+                     workspace: torch.Tensor | None = None) -> TokenStats:
+    """Log-probabilities of the labels (if any), lse, entropy and the k most likely tokens of each row of logits [rows][vocab]
+    (ef21_token_stats).  sums: what ef21_token_stats_grad needs: a tensor to write, True for a new one, False or None for none."""
+    lib = load_library()
+    args, rows = _maybe_labelled(logits, labels)
+    if labels is not None:
+        logp = _new(logp, rows, logits)
+    elif logp is not None:
+        raise ValueError("logp needs labels")
+    lse, entropy = _new(lse, rows, logits), _new(entropy, rows, logits)
+    if k > 0:
+        top_tokens, top_logp = _shaped(top_tokens, (rows, k), torch.int32, logits, "top_tokens"), _shaped(top_logp, (rows, k), _F32, logits, "top_logp")
+    elif top_tokens is not None or top_logp is not None:
+        raise ValueError("top_tokens and top_logp need k > 0")
+    sums = None if sums is None or sums is False else _shaped(None if sums is True else sums, (rows, 2), _F32, logits, "sums")
+    need = ef21_token_stats_workspace(args[1], rows, args[3], k)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    _check(lib.ef21_token_stats(*args, k, _optional(logp, rows, "logp"), _vector(lse, rows, "lse"), _vector(entropy, rows, "entropy"),
+                                top_tokens.data_ptr() if k > 0 else None, top_logp.data_ptr() if k > 0 else None,
+                                None if sums is None else sums.data_ptr(), None if workspace is None else workspace.data_ptr(),
+                                0 if workspace is None else workspace.nbytes,
+                                _stream_of(logits, labels, logp, lse, entropy, top_tokens, top_logp, sums, workspace)))
+    return TokenStats(logp, lse, entropy, top_tokens, top_logp, sums)
+
+
+def ef21_token_stats_grad(logits: torch.Tensor, labels: torch.Tensor | None, sums: torch.Tensor, entropy: torch.Tensor,
+                          grad_logp: torch.Tensor | None = None, grad_entropy: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                          accumulate: bool = False) -> torch.Tensor:
+    """The gradient of the logits from those of the log-probabilities and entropies (ef21_token_stats_grad).  `out` may be the logits;
+    with accumulate it is a gradient of them that is added to."""
+    lib = load_library()
+    args, rows = _maybe_labelled(logits, labels)
+    if accumulate and (out is None or out is True):
+        raise ValueError("accumulate needs the gradient to add to")
+    out, to, stride = _logit_grad(True if out is None else out, logits)
+    _shaped(sums, (rows, 2), _F32, logits, "sums")
+    _check(lib.ef21_token_stats_grad(*args, sums.data_ptr(), _vector(entropy, rows, "entropy"), _optional(grad_logp, rows, "grad_logp"),
+                                     _optional(grad_entropy, rows, "grad_entropy"), to, stride, int(accumulate),
+                                     _stream_of(logits, labels, sums, entropy, grad_logp, grad_entropy, out)))
+    return out
+
+
+# -- the step of a model's parameters
+class TensorList:
+    """Tensors that are looked at once and used in many calls: contiguous, fp32, bf16 or fp16, on one device."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.device = _one_device(self.tensors, "tensors")
+        for i, t in enumerate(self.tensors):
+            _dense(t, VALUE_TYPES, f"tensor {i}")
+        n = len(self.tensors)
+        self.addresses = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
+        self.types = (C.c_int32 * n)(*[VALUE_TYPES[t.dtype] for t in self.tensors])
+        self.counts = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _dense(t, types, what: str) -> None:
+    _gpu(t, what)
+    if t.dtype not in types or not t.is_contiguous():
+        raise TypeError(f"{what}: expected contiguous {' or '.join(str(d) for d in types)}, got {t.dtype} (contiguous={t.is_contiguous()})")
+
+
+def _one_device(tensors, what: str) -> int:
+    if not tensors:
+        raise ValueError(f"{what}: none given")
+    for t in tensors:
+        _gpu(t, what)
+    device = tensors[0].get_device()
+    if any(t.get_device() != device for t in tensors):
+        raise ValueError(f"{what}: all tensors must be on one device")
+    return device
+
+
+@functools.lru_cache(maxsize=256)
+def ef21_grad_norm_workspace(tensor_count: int) -> int:
+    """Bytes of workspace that ef21_grad_norm needs."""
+    return _size(load_library().ef21_grad_norm_workspace, tensor_count)
+
+
+def ef21_grad_norm(grads, max_norm: float = math.inf, scale: float = 1.0, norm: torch.Tensor | None = None, factor: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None):
+    """(norm [1], factor [1]) of all gradients together (ef21_grad_norm); grads: a TensorList, or tensors.  `factor` is what AdamW.step
+    takes as grad_scale."""
+    lib = load_library()
+    grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+    like = grads.tensors[0]
+    norm, factor = _new(norm, 1, like), _new(factor, 1, like)
+    if workspace is None:
+        workspace = torch.empty(ef21_grad_norm_workspace(len(grads)), dtype=torch.uint8, device=like.device)
+    _check(lib.ef21_grad_norm(grads.addresses, grads.types, grads.counts, len(grads), scale, max_norm, _vector(norm, 1, "norm"),
+                              _vector(factor, 1, "factor"), workspace.data_ptr(), workspace.nbytes, _stream_of(like, norm, factor, workspace)))
+    return norm, factor
+
+
+class AdamW:
+    """AdamW (ef21_adamw) over many tensors, with the states of each.
+
+    params, grads: contiguous tensors (grads may also be given to every step); a gradient of another type than its parameter is fine.
+    bits: 32 or 8 for the states, or a list of one or the other per tensor.  m, v, m_scale, v_scale: states to go on with (fp32, or
+    float8_e4m3fn with one fp32 scale per 256 entries), each a list per tensor; new ones otherwise, also for None in a list.
+    copies: a list of bf16 or fp16 tensors (or None) that receive the new parameters.  weight_decay: a number, or one per tensor.
+    stochastic, seed: see include/ef21.h.  The tensors stay the caller's; the object keeps them alive and works on their memory.
+    """
+
+    def __init__(self, params, grads=None, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, bits=32, m=None, v=None, m_scale=None,
+                 v_scale=None, copies=None, stochastic: bool = False, seed: int = 0):
+        self._lib = load_library()
+        self.params = list(params)
+        n = len(self.params)
+        self.device = _one_device(self.params, "params")
+        per = lambda x, what: self._per_tensor(x, n, what)  # noqa: E731
+        bits, decay = per(bits, "bits"), per(weight_decay, "weight_decay")
+        self.copies = per(copies, "copies")
+        self.m, self.v, self.m_scale, self.v_scale = per(m, "m"), per(v, "v"), per(m_scale, "m_scale"), per(v_scale, "v_scale")
+        self._table = (AdamwTensor * n)()
+        for i, p in enumerate(self.params):
+            _dense(p, VALUE_TYPES, f"params[{i}]")
+            if bits[i] not in (8, 32):
+                raise ValueError("bits must be 8 or 32")
+            kind, blocks = (torch.float8_e4m3fn, -(-p.numel() // STATE_BLOCK)) if bits[i] == 8 else (_F32, 0)
+            for states in (self.m, self.v):
+                states[i] = self._state(states[i], kind, p.shape, p, f"state {i}")
+            for scales in (self.m_scale, self.v_scale):
+                if bits[i] == 8:
+                    scales[i] = self._state(scales[i], _F32, (blocks,), p, f"scale {i}")
+                elif scales[i] is not None:
+                    raise ValueError(f"scale {i}: 32-bit states have none")
+            copy = self.copies[i]
+            if copy is not None:
+                _dense(copy, (torch.bfloat16, torch.float16), f"copies[{i}]")
+                if copy.shape != p.shape:
+                    raise ValueError(f"copies[{i}]: expected shape {tuple(p.shape)}, got {tuple(copy.shape)}")
+            at = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+            self._table[i] = AdamwTensor(at(p), None, at(self.m[i]), at(self.v[i]), at(self.m_scale[i]), at(self.v_scale[i]), at(copy), p.numel(),
+                                         VALUE_TYPES[p.dtype], 0, VALUE_TYPES[copy.dtype] if copy is not None else 0, float(decay[i]))
+        self._written = [t for group in (self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies) for t in group if t is not None]
+        _one_device(self._written, "params, states and copies")
+        self.grads = None
+        self._check_apart([])
+        if grads is not None:
+            self.grads = self._take(grads)
+        self._options = AdamwOptions(0.0, float(betas[0]), float(betas[1]), float(eps), 1, None, None, None, int(seed) & (2 ** 64 - 1), int(bool(stochastic)))
+        self.steps = 0
+
+    @staticmethod
+    def _per_tensor(x, n: int, what: str) -> list:
+        if not isinstance(x, (list, tuple)):
+            return [x] * n
+        if len(x) != n:
+            raise ValueError(f"{what}: expected {n}, got {len(x)}")
+        return list(x)
+
+    @staticmethod
+    def _state(t, kind, shape, like, what: str):
+        if t is None:
+            return torch.zeros(shape, dtype=_F32, device=like.device).to(kind)
+        _dense(t, (kind,), what)
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+        return t
+
+    def _check_apart(self, grads) -> None:
+        """What is written overlaps nothing."""
+        spans = [(t.data_ptr(), t.data_ptr() + t.nbytes, True) for t in self._written if t.nbytes]
+        spans += [(t.data_ptr(), t.data_ptr() + t.nbytes, False) for t in grads if t.nbytes]
+        end, end_written = 0, 0                                           # of all before, and of the written ones
+        for start, stop, written in sorted(spans):
+            if start < (end if written else end_written):
+                raise ValueError("parameters, states, copies and gradients must not overlap")
+            end = max(end, stop)
+            if written:
+                end_written = max(end_written, stop)
+
+    def _take(self, grads) -> list:
+        """Takes the addresses of gradients."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError(f"grads: expected {len(self.params)}, got {len(grads)}")
+        for i, (g, p) in enumerate(zip(grads, self.params)):
+            _dense(g, VALUE_TYPES, f"grads[{i}]")
+            if g.shape != p.shape:
+                raise ValueError(f"grads[{i}]: expected shape {tuple(p.shape)}, got {tuple(g.shape)}")
+            if g.get_device() != self.device:
+                raise ValueError(f"grads[{i}]: not on the parameters' device")
+        self._check_apart(grads)
+        for row, g in zip(self._table, grads):
+            row.grad, row.grad_type = g.data_ptr(), VALUE_TYPES[g.dtype]
+        return grads
+
+    def step(self, lr, step: "int | torch.Tensor | None" = None, grad_scale: torch.Tensor | None = None, grads=None) -> None:
+        """One step.  lr: a number, or an fp32 tensor [1] on the device; step: its number from 1 on, an int64 tensor [1] on the device, or None
+        for the one after the last; grad_scale: fp32 [1] on the device, such as ef21_grad_norm's factor (where it is not finite, nothing is
+        changed); grads: gradients for this step and the following ones."""
+        if grads is not None:
+            self.grads = self._take(grads)
+        if self.grads is None:
+            raise ValueError("no gradients given")
+        o, on_device = self._options, isinstance(lr, torch.Tensor)
+        o.lr, o.lr_device = (0.0, _vector(lr, 1, "lr")) if on_device else (lr, None)
+        o.grad_scale = _optional(grad_scale, 1, "grad_scale")
+        stepped = isinstance(step, torch.Tensor)
+        if stepped:
+            o.step, o.step_device = 1, _vector(step, 1, "step", torch.int64)
+        else:
+            o.step, o.step_device = (self.steps + 1 if step is None else step), None
+        _check(self._lib.ef21_adamw(self._table, len(self.params), C.byref(o),
+                                    _stream_of(self.params[0], lr if on_device else None, step if stepped else None, grad_scale)))
+        if not stepped:
+            self.steps = o.step
+
+
 class EF21:
     """Handle of the C library: state of Algorithm 2 for n workers batched on one GPU."""
 
@@ -465,6 +744,13 @@ class EF21:
         x = torch.empty(self.d, dtype=torch.float32, device=self.device)
         self._call(self._lib.ef21_get_state, x.data_ptr(), None, None)
         return x
+
+    def get_g(self, out: torch.Tensor | None = None) -> torch.Tensor:
+        """The estimate g of the gradient [d]."""
+        if out is None:
+            out = torch.empty(self.d, dtype=torch.float32, device=self.device)
+        self._call(self._lib.ef21_get_state, None, None, _dev(out, torch.float32, (self.d,)))
+        return out
 
     def get_messages(self):
         idx = torch.empty((self.n, self.k), dtype=torch.int32, device=self.device)

@@ -28,7 +28,7 @@ struct LogitRows {
     const void *x = nullptr;
     int type = kF32;
     int64_t rows = 0, vocab = 0, stride = 0;
-    Tokens labels;
+    Tokens labels;                                         // nullptr (token statistics alone): every row is read and has none
 };
 
 struct LogitGrad {                                         // [rows] rows, may be the logits themselves
@@ -41,6 +41,23 @@ hipError_t launch_token_logps(const LogitRows &in, float *logp, float *lse, hipS
 
 // grad[r][v] = coef[r] ([v = label] - exp(x - lse[r]))
 hipError_t launch_token_grad(const LogitRows &in, const float *lse, const float *coef, const LogitGrad &out, hipStream_t stream);
+
+struct StatArgs {
+    int32_t k;
+    float *logp, *lse, *entropy;                           // [rows]; logp nullptr: no labels
+    int32_t *top_tokens;                                   // [rows][k]
+    float *top_logp;                                       // [rows][k]
+    float *sums;                                           // [rows][2] (RowStat) or nullptr
+};
+size_t stats_workspace_bytes(int type, int64_t rows, int64_t vocab, int32_t k);
+hipError_t launch_token_stats(const LogitRows &in, const StatArgs &p, void *workspace, hipStream_t stream);
+
+struct StatGradArgs {
+    const float *sums, *entropy;
+    const float *grad_logp, *grad_entropy;                 // [rows] or nullptr
+    int accumulate;
+};
+hipError_t launch_token_stats_grad(const LogitRows &in, const StatGradArgs &p, const LogitGrad &out, hipStream_t stream);
 
 struct PairArgs {
     const int64_t *seq_start;                              // [2 pairs + 1]

@@ -39,13 +39,21 @@ int check_vectors(int64_t rows, std::initializer_list<const void *> arrays) {
 }
 
 int check_logits(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels, int label_type,
-                 ef21::LogitRows *out) {
+                 ef21::LogitRows *out, bool labelled = true) {
     if (!value_type(type)) return invalid("unknown type of the logits");
     if (rows < 0 || rows > kMostRows) return invalid("rows must be in [0, 2^31)");
     if (vocab < 1 || vocab > kMostRows) return invalid("vocab must be in [1, 2^31)");
     if (int rc = check_rows(logits, type, rows, vocab, stride, "logits are NULL or misaligned", "the logits' stride is too small or too large")) return rc;
-    if (int rc = check_tokens(labels, label_type, rows)) return rc;
+    if (labelled)
+        if (int rc = check_tokens(labels, label_type, rows)) return rc;
     *out = ef21::LogitRows{logits, type, rows, vocab, stride, {labels, label_type}};
+    return EF21_OK;
+}
+
+int check_stats_sizes(int64_t rows, int64_t vocab, int32_t k) {
+    if (rows < 0 || rows > kMostRows) return invalid("rows must be in [0, 2^31)");
+    if (vocab < 1 || vocab > kMostRows) return invalid("vocab must be in [1, 2^31)");
+    if (k < 0 || k > 64 || k > vocab) return invalid("k must be in [0, 64] and at most vocab");
     return EF21_OK;
 }
 
@@ -133,6 +141,45 @@ int ef21_token_logps_grad(const void *logits, int type, int64_t rows, int64_t vo
     if (int rc = check_vectors(rows, {lse, grad_logp})) return rc;
     if (int rc = check_grad(in, grad_logits, grad_stride)) return rc;
     return launched(ef21::launch_token_grad(in, lse, grad_logp, {grad_logits, grad_stride}, (hipStream_t)hip_stream), "logit gradient launch");
+}
+
+int ef21_token_stats_workspace(int type, int64_t rows, int64_t vocab, int32_t k, int64_t *bytes) {
+    if (!value_type(type)) return invalid("unknown type of the logits");
+    if (int rc = check_stats_sizes(rows, vocab, k)) return rc;
+    if (!bytes) return invalid("bytes is NULL");
+    *bytes = (int64_t)ef21::stats_workspace_bytes(type, rows, vocab, k);
+    return EF21_OK;
+}
+
+int ef21_token_stats(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
+                     int label_type, int32_t k, float *logp, float *lse, float *entropy, int32_t *top_tokens, float *top_logp,
+                     float *sums, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    ef21::LogitRows in;
+    if (int rc = check_stats_sizes(rows, vocab, k)) return rc;
+    if (int rc = check_logits(logits, type, rows, vocab, stride, labels, label_type, &in, labels != nullptr)) return rc;
+    if (rows > 0 && !labels != !logp) return invalid("logp goes with labels");
+    if (int rc = check_vectors(rows, {lse, entropy})) return rc;
+    if (!aligned(logp, 4) || !aligned(sums, 4)) return invalid("logp or sums is misaligned");
+    if (k > 0)
+        if (int rc = check_vectors(rows, {top_tokens, top_logp})) return rc;
+    if (int rc = check_workspace(workspace, workspace_bytes, ef21::stats_workspace_bytes(type, rows, vocab, k))) return rc;
+    return launched(ef21::launch_token_stats(in, {k, logp, lse, entropy, top_tokens, top_logp, sums}, workspace, (hipStream_t)hip_stream),
+                    "token statistics launch");
+}
+
+int ef21_token_stats_grad(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
+                          int label_type, const float *sums, const float *entropy, const float *grad_logp,
+                          const float *grad_entropy, void *grad_logits, int64_t grad_stride, int accumulate, void *hip_stream) {
+    ef21::LogitRows in;
+    if (int rc = check_logits(logits, type, rows, vocab, stride, labels, label_type, &in, labels != nullptr)) return rc;
+    if (int rc = check_vectors(rows, {entropy})) return rc;
+    if (rows > 0 && (!sums || !aligned(sums, 4))) return invalid("sums is NULL or misaligned");
+    if (!aligned(grad_logp, 4) || !aligned(grad_entropy, 4)) return invalid("grad_logp or grad_entropy is misaligned");
+    if (!labels && grad_logp) return invalid("grad_logp needs labels");
+    if (int rc = check_grad(in, grad_logits, grad_stride)) return rc;
+    if (accumulate && rows > 0 && grad_logits == logits) return invalid("a gradient that is added to must not be the logits");
+    return launched(ef21::launch_token_stats_grad(in, {sums, entropy, grad_logp, grad_entropy, accumulate}, {grad_logits, grad_stride}, (hipStream_t)hip_stream),
+                    "token statistics gradient launch");
 }
 
 int ef21_preference_loss_workspace(int64_t rows, int32_t pairs, int64_t *bytes) {
