@@ -433,7 +433,7 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
  * AdamW (decoupled weight decay) over many tensors.  For every entry, with f = grad_scale[0] (1 if NULL) and t = step:
  *   g' = f g,   m <- beta1 m + (1 - beta1) g',   v <- beta2 v + (1 - beta2) g'^2
  *   p <- p - lr * (weight_decay * p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
- * in fp32.  Where f is not finite nothing is changed.  An infinite or NaN gradient otherwise passes into m, v and p, of its entry alone with
+ * in fp32; with 8-bit states each product and sum of m and v is rounded by itself, so that the codes do not depend on how it is evaluated.  Where f is not finite nothing is changed.  An infinite or NaN gradient otherwise passes into m, v and p, of its entry alone with
  * 32-bit states; of 8-bit ones an infinity makes its block NaN.
  *   states: m, v fp32 (m_scale and v_scale NULL), or 8 bits: entry i of m stands for m_scale[i / 256] times the value of byte i as an OCP e4m3 number, and
  *           sqrt(v) for v_scale[i / 256] times that of v's byte; the scales, ceil(count / 256) of each, are the block's largest value / 448, 2^-126 at the
@@ -446,7 +446,7 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
  * lr_device, step_device: NULL, or fp32 [1] and int64 [1] that are read on the device in the place of lr and step (a captured call whose
  * values change; a step below 1 counts as 1).
  * The written arrays (param, m, v, their scales, copy) must not overlap one another or the gradients; no tensor may be listed twice.
- * EF21_EINVAL: a count < 0, an unknown type, a NULL or misaligned pointer, one scale without the other, lr or weight_decay not finite,
+ * EF21_EINVAL: a count < 0 or > 2^34, an unknown type, a NULL or misaligned pointer, one scale without the other, lr or weight_decay not finite,
  * beta1 or beta2 outside [0, 1), eps not finite and > 0, step < 1.
  */
 typedef struct ef21_adamw_tensor {

@@ -113,6 +113,22 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
+// The largest value of each group of 16 or 64 lanes, in every lane of the group (group_sum with another operation).
+template <int LANES>
+__device__ __forceinline__ float group_max(float v) {
+    v = fmaxf(v, dpp_move<0xB1>(v));
+    v = fmaxf(v, dpp_move<0x4E>(v));
+    v = fmaxf(v, dpp_move<0x141>(v));
+    v = fmaxf(v, dpp_move<0x140>(v));
+    if constexpr (LANES == 64) {
+        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return v;
+}
+
 // Place of the calling lane's item in a list whose length is `*counter` (LDS): the lanes of a wavefront that
 // have an item (`has`) take consecutive places with ONE atomic for the wavefront.  Every lane of the wavefront
 // must call; the result means something only where `has`.

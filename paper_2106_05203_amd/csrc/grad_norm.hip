@@ -1,77 +1,158 @@
 // The norm of many gradients together, and the factor that clips it.  Squares of fp32 numbers are exact in fp64 and neither overflow nor vanish there.
-#include "device_utils.h"
+//
+// One pass, bound by memory.  The tensors are cut into chunks of 32 KB; workgroup b of B takes the chunks b, b + B, ... of all tensors in turn, so
+// that a few long tensors and many short ones load the chip alike, and the order of the sums follows from the sizes.  A second launch of one
+// workgroup adds the workgroups' sums up; up to kFewChunks chunks one workgroup does it all.
+#include "token_rows.h"
 #include "tensors.h"
 
 namespace ef21 {
 namespace {
 
-constexpr int kThreads = 256, kItems = 128, kMostBlocks = 1024;
+constexpr int kThreads = 256, kFewThreads = 1024, kItems = 2 * kWave, kMostBlocks = 2048, kFlight = 8;
+constexpr int64_t kChunkBytes = kThreads * kFlight * 16, kFewChunks = 8;
 
 struct Item {
     const void *g;
     int64_t n;
-    int32_t type;
 };
 struct Table {
     Item item[kItems];
-    int32_t count;
+    int32_t first[kItems];                                         // chunks before its own
+    uint8_t type[kItems];
+    int32_t count, chunks;
 };
+static_assert(sizeof(Table) + 64 <= 4096, "the arguments of a kernel");
 
-__device__ __forceinline__ float entry_of(const Item &it, int64_t i) {
-    return it.type == kF32 ? static_cast<const float *>(it.g)[i]
-                           : it.type == kBF16 ? (float)static_cast<const __bf16 *>(it.g)[i] : (float)static_cast<const _Float16 *>(it.g)[i];
-}
-
-__device__ __forceinline__ double block_sum(double s, double (&part)[kThreads / kWave]) {
+template <int WAVES>
+__device__ __forceinline__ double block_sum(double s, double (&part)[WAVES]) {
     for (int o = kWave / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
     if (lane_id() == 0) part[wave_id()] = s;
     __syncthreads();
     s = 0.0;
-    for (int w = 0; w < kThreads / kWave; ++w) s += part[w];
+    for (int w = 0; w < WAVES; ++w) s += part[w];
     return s;
 }
 
-__global__ __launch_bounds__(kThreads) void square_sums_kernel(Table table, double *sums) {
-    __shared__ double part[kThreads / kWave];
-    double s = 0.0;
-    for (int t = 0; t < table.count; ++t)
-        for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < table.item[t].n; i += (int64_t)gridDim.x * kThreads) {
-            const double g = (double)entry_of(table.item[t], i);
-            s = fma(g, g, s);
-        }
-    s = block_sum(s, part);
-    if (threadIdx.x == 0) sums[blockIdx.x] = s;
+template <class T>
+__device__ __forceinline__ void add_squares(Raw r, double &s) {
+    float f[Piece<T>::N];
+    unpack<T>(r, f);
+#pragma unroll
+    for (int i = 0; i < Piece<T>::N; ++i) s = fma((double)f[i], (double)f[i], s);
 }
 
-__global__ __launch_bounds__(kThreads) void norm_kernel(const double *sums, int32_t count, NormArgs p) {
-    __shared__ double part[kThreads / kWave];
+// A workgroup's part of chunk c of a tensor, which lies anywhere.
+template <class T, int THREADS>
+__device__ __forceinline__ void add_chunk(const Item &it, int64_t c, double &s) {
+    typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
+    constexpr int N = Piece<T>::N, kPieces = (int)(kChunkBytes / 16), kEach = kPieces / THREADS;
+    const T *g = static_cast<const T *>(it.g) + c * kPieces * N;
+    const int64_t left = it.n - c * kPieces * N;
+    const auto load = [&](int i) { return Raw(__builtin_nontemporal_load(reinterpret_cast<const Loose *>(g + i * N))); };
+    Raw r[kEach];
+    if (left >= kPieces * N) {
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) r[u] = load((int)threadIdx.x + u * THREADS);
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) add_squares<T>(r[u], s);
+        return;
+    }
+    const int pieces = (int)(left / N), tail = (int)(left % N);
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        r[u] = Raw{0u, 0u, 0u, 0u};
+        if ((int)threadIdx.x + u * THREADS < pieces) r[u] = load((int)threadIdx.x + u * THREADS);
+    }
+    const float last = (int)threadIdx.x < tail ? (float)g[pieces * N + (int)threadIdx.x] : 0.f;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) add_squares<T>(r[u], s);
+    s = fma((double)last, (double)last, s);
+}
+
+template <int THREADS>
+__device__ __forceinline__ double sum_chunks(const Table &table) {
     double s = 0.0;
-    for (int32_t i = (int32_t)threadIdx.x; i < count; i += kThreads) s += sums[i];
-    s = block_sum(s, part);
-    if (threadIdx.x != 0) return;
-    const double norm = (double)p.scale * sqrt(s);
+    const int32_t lane = lane_id();
+    const int32_t low = lane < table.count ? table.first[lane] : 0x7fffffff, high = lane + kWave < table.count ? table.first[lane + kWave] : 0x7fffffff;
+    for (int32_t c = (int32_t)blockIdx.x; c < table.chunks; c += (int32_t)gridDim.x) {
+        const int t = __builtin_amdgcn_readfirstlane((int)(popc64(__ballot(low <= c)) + popc64(__ballot(high <= c))) - 1);
+        const Item it = table.item[t];
+        const int64_t at = c - table.first[t];
+        switch (table.type[t]) {
+            case kF32: add_chunk<float, THREADS>(it, at, s); break;
+            case kBF16: add_chunk<__bf16, THREADS>(it, at, s); break;
+            default: add_chunk<_Float16, THREADS>(it, at, s);
+        }
+    }
+    return s;
+}
+
+__device__ __forceinline__ void write_norm(double squares, const NormArgs &p) {
+    const double norm = (double)p.scale * sqrt(squares);
     const float rounded = (float)norm;
     p.norm[0] = rounded;
     const bool finite = fabsf(rounded) < INFINITY;
     p.factor[0] = !finite ? __int_as_float(0x7fc00000) : norm > (double)p.max_norm ? (float)((double)p.scale * ((double)p.max_norm / norm)) : p.scale;
 }
 
-int32_t launches(int32_t tensors) { return (tensors + kItems - 1) / kItems; }
+__global__ __launch_bounds__(kThreads) void square_sums_kernel(Table table, double *sums) {
+    __shared__ double part[kThreads / kWave];
+    const double s = block_sum<kThreads / kWave>(sum_chunks<kThreads>(table), part);
+    if (threadIdx.x == 0) sums[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(kFewThreads) void few_norm_kernel(Table table, NormArgs p) {
+    __shared__ double part[kFewThreads / kWave];
+    const double s = block_sum<kFewThreads / kWave>(sum_chunks<kFewThreads>(table), part);
+    if (threadIdx.x == 0) write_norm(s, p);
+}
+
+__global__ __launch_bounds__(kThreads) void norm_kernel(const double *sums, int32_t count, NormArgs p) {
+    __shared__ double part[kThreads / kWave];
+    double s = 0.0;
+    for (int32_t i = (int32_t)threadIdx.x; i < count; i += kThreads) s += sums[i];
+    s = block_sum<kThreads / kWave>(s, part);
+    if (threadIdx.x == 0) write_norm(s, p);
+}
 
 }  // namespace
 
-size_t norm_workspace_bytes(int32_t tensors) { return (size_t)launches(tensors) * kMostBlocks * sizeof(double); }
+// A launch takes kItems tensors, or 2^30 chunks if they are more than the memory of this card.
+size_t norm_workspace_bytes(int32_t tensors) { return (size_t)((tensors + kItems - 1) / kItems) * kMostBlocks * sizeof(double); }
 
 hipError_t launch_grad_norm(const void *const *grads, const int32_t *types, const int64_t *counts, int32_t tensors, const NormArgs &p, void *workspace,
                             hipStream_t stream) {
     double *sums = static_cast<double *>(workspace);
-    for (int32_t l = 0; l < launches(tensors); ++l) {
-        Table table{};
-        for (int32_t i = l * kItems; i < tensors && i < (l + 1) * kItems; ++i) table.item[table.count++] = Item{grads[i], counts[i], types[i]};
-        hipLaunchKernelGGL(square_sums_kernel, dim3(kMostBlocks), dim3(kThreads), 0, stream, table, sums + (int64_t)l * kMostBlocks);
+    int32_t written = 0, launches = 0;
+    Table table{};
+    for (int32_t i = 0; i < tensors; ++i) {
+        if (counts[i] > 0) {
+            const int64_t bytes = counts[i] * value_bytes(types[i]);
+            table.item[table.count] = Item{grads[i], counts[i]};
+            table.type[table.count] = (uint8_t)types[i];
+            table.first[table.count++] = table.chunks;
+            table.chunks += (int32_t)((bytes + kChunkBytes - 1) / kChunkBytes);
+        }
+        if (table.count < kItems || i + 1 == tensors) continue;
+        const int32_t blocks = table.chunks < kMostBlocks ? table.chunks : kMostBlocks;
+        hipLaunchKernelGGL(square_sums_kernel, dim3(blocks), dim3(kThreads), 0, stream, table, sums + written);
         if (hipError_t st = hipGetLastError()) return st;
+        written += blocks;
+        ++launches;
+        table.count = table.chunks = 0;
     }
-    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, stream, sums, launches(tensors) * kMostBlocks, p);
+    if (launches == 0 && table.chunks <= kFewChunks) {
+        hipLaunchKernelGGL(few_norm_kernel, dim3(1), dim3(kFewThreads), 0, stream, table, p);
+        return hipGetLastError();
+    }
+    if (table.count > 0) {
+        const int32_t blocks = table.chunks < kMostBlocks ? table.chunks : kMostBlocks;
+        hipLaunchKernelGGL(square_sums_kernel, dim3(blocks), dim3(kThreads), 0, stream, table, sums + written);
+        if (hipError_t st = hipGetLastError()) return st;
+        written += blocks;
+    }
+    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, stream, sums, written, p);
     return hipGetLastError();
 }
 

@@ -15,11 +15,11 @@ bool value_type(int type) { return type == EF21_F32 || type == EF21_BF16 || type
 
 bool array_of(const void *p, int64_t bytes) { return p && aligned(p, bytes); }
 
-// Entries of one tensor: a 64-bit byte offset and a 32-bit number of blocks hold them.
-constexpr int64_t kMostEntries = (int64_t)1 << 38;
+// Entries of one tensor: more than the card's memory holds, and a launch's workgroups do.
+constexpr int64_t kMostEntries = (int64_t)1 << 34;
 
 int check_tensor(const ef21_adamw_tensor &t) {
-    if (t.count < 0 || t.count > kMostEntries) return invalid("a tensor's count must be in [0, 2^38]");
+    if (t.count < 0 || t.count > kMostEntries) return invalid("a tensor's count must be in [0, 2^34]");
     if (!value_type(t.param_type) || !value_type(t.grad_type)) return invalid("unknown type of a parameter or gradient");
     if (!std::isfinite(t.weight_decay)) return invalid("weight_decay must be finite");
     if (t.count == 0) return EF21_OK;
@@ -51,7 +51,7 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
     if (tensor_count > 0 && (!grads || !types || !counts)) return invalid("grads, types or counts is NULL");
     for (int32_t i = 0; i < tensor_count; ++i) {
         if (!value_type(types[i])) return invalid("unknown type of a gradient");
-        if (counts[i] < 0 || counts[i] > kMostEntries) return invalid("a tensor's count must be in [0, 2^38]");
+        if (counts[i] < 0 || counts[i] > kMostEntries) return invalid("a tensor's count must be in [0, 2^34]");
         if (counts[i] > 0 && !array_of(grads[i], ef21::value_bytes(types[i]))) return invalid("a gradient is NULL or misaligned");
     }
     if (!(scale > 0.f) || !std::isfinite(scale)) return invalid("scale must be finite and > 0");

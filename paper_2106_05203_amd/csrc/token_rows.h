@@ -106,22 +106,6 @@ __device__ __forceinline__ Cut cut_row(const T *x, int32_t vocab) {
 }
 
 // ---------------------------------------------------------------- sums of exponentials
-// The largest value of each group of 16 or 64 lanes, in every lane of the group (group_sum with another operation).
-template <int LANES>
-__device__ __forceinline__ float group_max(float v) {
-    v = fmaxf(v, dpp_move<0xB1>(v));
-    v = fmaxf(v, dpp_move<0x4E>(v));
-    v = fmaxf(v, dpp_move<0x141>(v));
-    v = fmaxf(v, dpp_move<0x140>(v));
-    if constexpr (LANES == 64) {
-        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-        r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
-    return v;
-}
-
 // s 2^m, a lane's part of a row; m is the wavefront's, kLowest where it has seen no entry
 struct ExpSum {
     float m = kLowest, s = 0.f;
