@@ -438,7 +438,7 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
  *   states: m, v fp32 (m_scale and v_scale NULL), or 8 bits: entry i of m stands for m_scale[i / 256] times the value of byte i as an OCP e4m3 number, and
  *           sqrt(v) for v_scale[i / 256] times that of v's byte; the scales, ceil(count / 256) of each, are the block's largest value / 448, 2^-126 at the
  *           least.  The update uses m and v before they are rounded to 8 bits.  A sqrt(v) above zero is never rounded to zero.
- *   copy:   NULL, or bf16 or fp16 [count] (copy_type): receives the new parameters, rounded to nearest
+ *   copy:   NULL, or with fp32 parameters bf16 or fp16 [count] (copy_type): receives the new parameters, rounded to nearest
  *   stochastic != 0: what is kept in fewer than 32 bits (8-bit states, bf16 or fp16 parameters) is rounded up or down at random, with
  *           probabilities that make it right on average; a moving average that moves by 1 - beta of itself a step, or a parameter by
  *           less than half of its last bit, would stay where it is if it were rounded to nearest.  The choice follows from seed, step, the tensor's number
@@ -446,8 +446,8 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
  * lr_device, step_device: NULL, or fp32 [1] and int64 [1] that are read on the device in the place of lr and step (a captured call whose
  * values change; a step below 1 counts as 1).
  * The written arrays (param, m, v, their scales, copy) must not overlap one another or the gradients; no tensor may be listed twice.
- * EF21_EINVAL: a count < 0 or > 2^34, an unknown type, a NULL or misaligned pointer, one scale without the other, lr or weight_decay not finite,
- * beta1 or beta2 outside [0, 1), eps not finite and > 0, step < 1.
+ * EF21_EINVAL: a count < 0 or > 2^33, an unknown type, a NULL or misaligned pointer, one scale without the other, lr or weight_decay not finite,
+ * beta1 or beta2 outside [0, 1), eps not finite and at least 2^-126, step < 1.
  */
 typedef struct ef21_adamw_tensor {
     void *param;

@@ -548,7 +548,7 @@ class AdamW:
     params, grads: contiguous tensors (grads may also be given to every step); a gradient of another type than its parameter is fine.
     bits: 32 or 8 for the states, or a list of one or the other per tensor.  m, v, m_scale, v_scale: states to go on with (fp32, or
     float8_e4m3fn with one fp32 scale per 256 entries), each a list per tensor; new ones otherwise, also for None in a list.
-    copies: a list of bf16 or fp16 tensors (or None) that receive the new parameters.  weight_decay: a number, or one per tensor.
+    copies: a list of bf16 or fp16 tensors (or None) that receive the new fp32 parameters.  weight_decay: a number, or one per tensor.
     stochastic, seed: see include/ef21.h.  The tensors stay the caller's; the object keeps them alive and works on their memory.
     """
 
@@ -578,6 +578,8 @@ class AdamW:
             copy = self.copies[i]
             if copy is not None:
                 _dense(copy, (torch.bfloat16, torch.float16), f"copies[{i}]")
+                if p.dtype is not _F32:
+                    raise TypeError(f"copies[{i}]: copies are of fp32 parameters")
                 if copy.shape != p.shape:
                     raise ValueError(f"copies[{i}]: expected shape {tuple(p.shape)}, got {tuple(copy.shape)}")
             at = lambda t: t.data_ptr() if t is not None else None  # noqa: E731

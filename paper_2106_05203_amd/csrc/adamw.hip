@@ -13,9 +13,9 @@ namespace ef21 {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave, kVec = kBlock8 / kWave;
-constexpr float kMost8 = 448.f, kLeast8 = 0x1p-9f;
+constexpr float kMost8 = 448.f, kLeast8 = 0x1p-9f;                // e4m3's largest number and its least above zero
 
-// A launch's tensors; number: of the tensor in the call.
+// What a launch's workgroups read of a tensor.
 struct Item {
     void *p;
     const void *g;
@@ -24,15 +24,29 @@ struct Item {
     void *copy;
     int64_t n;
     float decay;
-    int32_t number, copy_type;
+    int32_t number;                                                // of the tensor in the call
 };
-constexpr int kItems = 44;
+
+// A launch's tensors, as many as its arguments hold: a launch that follows another waits for its last workgroup, which costs some 4 us.
+template <int BITS, bool COPY>
 struct Table {
-    Item item[kItems];
-    int32_t first[kItems];                                         // workgroups before its own
-    int32_t count;
+    static constexpr int kBytes = 4 * 8 + 8 + 3 * 4 + (BITS == 8 ? 2 * 8 : 0) + (COPY ? 8 : 0), kItems = (4096 - 40 - (int)sizeof(AdamwStep)) / kBytes;
+    static_assert(kItems <= 2 * kWave, "two lookups by a wavefront");
+    void *p[kItems];
+    const void *g[kItems];
+    void *m[kItems], *v[kItems];
+    float *ms[BITS == 8 ? kItems : 1], *vs[BITS == 8 ? kItems : 1];
+    void *copy[COPY ? kItems : 1];
+    int64_t n[kItems];
+    float decay[kItems];
+    int32_t number[kItems], first[kItems];                         // first: workgroups before its own
+    int32_t count, copy_type;
+
+    __device__ __forceinline__ Item item(int t) const {
+        return Item{p[t], g[t], m[t], v[t], BITS == 8 ? ms[t] : nullptr, BITS == 8 ? vs[t] : nullptr, COPY ? copy[t] : nullptr, n[t], decay[t], number[t]};
+    }
 };
-static_assert(sizeof(Table) + sizeof(AdamwStep) <= 4096 && kItems <= kWave, "the arguments of a kernel");
+static_assert(sizeof(Table<32, false>) + sizeof(AdamwStep) <= 4096 && sizeof(Table<8, true>) + sizeof(AdamwStep) <= 4096, "the arguments of a kernel");
 
 // Four entries that lie anywhere.
 template <class T>
@@ -40,10 +54,8 @@ struct Four {
     typedef T type __attribute__((ext_vector_type(kVec), aligned(sizeof(T))));
 };
 template <class T>
-__device__ __forceinline__ void load4(const void *p, int64_t i, float (&f)[kVec]) {
-    const auto r = __builtin_nontemporal_load(reinterpret_cast<const typename Four<T>::type *>(static_cast<const T *>(p) + i));
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) f[j] = (float)r[j];
+__device__ __forceinline__ typename Four<T>::type load4(const void *p, int64_t i) {
+    return __builtin_nontemporal_load(reinterpret_cast<const typename Four<T>::type *>(static_cast<const T *>(p) + i));
 }
 template <class T>
 __device__ __forceinline__ void store4(void *p, int64_t i, const float (&f)[kVec]) {
@@ -53,14 +65,40 @@ __device__ __forceinline__ void store4(void *p, int64_t i, const float (&f)[kVec
     __builtin_nontemporal_store(r, reinterpret_cast<typename Four<T>::type *>(static_cast<T *>(p) + i));
 }
 
-// x to a grid of `mantissa` bits behind the leading one and a least exponent: to the neighbour towards zero, or the one beyond it with the
-// probability of what lies above (sixteen random bits, each of which stands for the middle of its interval).
-__device__ __forceinline__ float round_up_by(float x, uint32_t bits, int mantissa, int least) {
-    const int e = max((int)(__float_as_uint(x) >> 23 & 255u) - 127, least) - mantissa;
-    const float units = ldexpf(fabsf(x), -e);                      // exact, below 2^(mantissa + 1)
-    const float low = floorf(units), above = units - low;          // exact
-    const float short_of = fmaf((float)(0x10000u - bits), 0x1p-16f, -0x1p-17f);   // exact
-    return copysignf(ldexpf(above >= short_of ? low + 1.f : low, e), x);
+// The root, correctly rounded where v >= 2^-100 (below, where the residues leave fp32's range, off by one in its last bit): the hardware's, which is
+// off by one at the most, or a neighbour.  Zero, infinity and NaN give residues that are not on the wrong side.
+__device__ __forceinline__ float root_of(float v) {
+    const float s = __builtin_amdgcn_sqrtf(v);
+    const float down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
+    const float below = fmaf(-down, s, v), above = fmaf(-up, s, v);
+    return above > 0.f ? up : below <= 0.f ? down : s;
+}
+
+// x / s correctly rounded, from the correctly rounded 1 / s (where the remainder is in fp32's range: x / s above 2^-20, say, which is far below the least code).
+__device__ __forceinline__ float quotient(float x, float s, float inverse) {
+    const float q = x * inverse;
+    return fmaf(fmaf(-q, s, x), inverse, q);
+}
+
+// Bytes of e4m3 numbers by random rounding: to the neighbour towards zero, or the one beyond it with the probability of what lies above.  Times 2^-120 the
+// least normal e4m3 number is fp32's, so that the exponent's lower four bits and three of the fraction's are the byte, below the least normal number too;
+// the sixteen random bits, each of which stands for the middle of its interval, are added to the twenty bits behind.
+__device__ __forceinline__ uint32_t random_code(float size, uint32_t bits) {
+    const uint32_t b = __float_as_uint(size * 0x1p-120f) + (bits << 4) + 8u;
+    return size == size ? min(b >> 20, 0x7eu) : 0x7fu;
+}
+
+// The same for a parameter: bf16, which is the upper half of fp32, and fp16.
+template <class T>
+__device__ __forceinline__ float random_param(float p, uint32_t bits) {
+    if constexpr (std::is_same<T, __bf16>::value) {
+        return __uint_as_float((__float_as_uint(p) + bits) & 0xffff0000u);
+    } else {
+        const int e = max((int)(__float_as_uint(p) >> 23 & 255u) - 127, -14) - 10;
+        const float units = ldexpf(fabsf(p), -e), low = floorf(units);                   // exact
+        const float short_of = fmaf((float)(0x10000u - bits), 0x1p-16f, -0x1p-17f);      // exact
+        return copysignf(ldexpf(units - low >= short_of ? low + 1.f : low, e), p);
+    }
 }
 
 // The step's numbers where they are read on the device.
@@ -77,232 +115,281 @@ __device__ __forceinline__ void read_step(AdamwStep &o) {
 __device__ __forceinline__ uint32_t key_of(const AdamwStep &o, int32_t number) { return mixed(mixed(o.seed + (uint32_t)o.step) + (uint32_t)number); }
 
 // Four entries of a lane, as they are read and written.
-template <class P, class G, int BITS>
+template <class P, class G, int BITS, bool COPY>
 struct Entries {
-    float p[kVec], g[kVec], m[kVec], v[kVec];
-    int m8, v8;                                                    // four bytes
+    typedef typename Four<float>::type State;
+    typename Four<P>::type p_in;
+    typename Four<G>::type g_in;
+    State m_in, v_in;                                              // 32 bits
+    int m8, v8;                                                    // 8 bits: four bytes
     float ms, vs;
+    float p[kVec], m[kVec], v[kVec];
 
-    __device__ __forceinline__ void load(const Item &it, int64_t i, int64_t block) {
-        load4<P>(it.p, i, p);
-        load4<G>(it.g, i, g);
+    __device__ __forceinline__ void load(const Item &it, int64_t i) {
+        p_in = load4<P>(it.p, i);
+        g_in = load4<G>(it.g, i);
         if constexpr (BITS == 8) {
             typedef int Loose __attribute__((aligned(1)));
             m8 = __builtin_nontemporal_load(reinterpret_cast<const Loose *>(static_cast<const uint8_t *>(it.m) + i));
             v8 = __builtin_nontemporal_load(reinterpret_cast<const Loose *>(static_cast<const uint8_t *>(it.v) + i));
-            ms = it.ms[block];
-            vs = it.vs[block];
         } else {
-            load4<float>(it.m, i, m);
-            load4<float>(it.v, i, v);
+            m_in = load4<float>(it.m, i);
+            v_in = load4<float>(it.v, i);
         }
     }
-    // The first n of the four; the others are zero.
-    __device__ __forceinline__ void load_some(const Item &it, int64_t i, int64_t block, int n) {
+    // What a lane has of a tensor's last block: all four entries, or n of them and zeros.
+    __device__ __forceinline__ void load_some(const Item &it, int64_t i, int n) {
+        p_in = (typename Four<P>::type)(P)0.f;
+        g_in = (typename Four<G>::type)(G)0.f;
+        m_in = v_in = (State)0.f;
         m8 = v8 = 0;
+        if (n >= kVec) {
+            load(it, i);
+        } else if (n > 0) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-            p[j] = g[j] = m[j] = v[j] = 0.f;
-            if (j >= n) continue;
-            p[j] = (float)static_cast<const P *>(it.p)[i + j];
-            g[j] = (float)static_cast<const G *>(it.g)[i + j];
-            if constexpr (BITS == 8) {
-                m8 |= static_cast<const uint8_t *>(it.m)[i + j] << 8 * j;
-                v8 |= static_cast<const uint8_t *>(it.v)[i + j] << 8 * j;
-            } else {
-                m[j] = static_cast<const float *>(it.m)[i + j];
-                v[j] = static_cast<const float *>(it.v)[i + j];
+            for (int j = 0; j < kVec - 1; ++j) {
+                if (j >= n) break;
+                p_in[j] = static_cast<const P *>(it.p)[i + j];
+                g_in[j] = static_cast<const G *>(it.g)[i + j];
+                if constexpr (BITS == 8) {
+                    m8 |= static_cast<const uint8_t *>(it.m)[i + j] << 8 * j;
+                    v8 |= static_cast<const uint8_t *>(it.v)[i + j] << 8 * j;
+                } else {
+                    m_in[j] = static_cast<const float *>(it.m)[i + j];
+                    v_in[j] = static_cast<const float *>(it.v)[i + j];
+                }
             }
         }
+    }
+    __device__ __forceinline__ void load_scales(const Item &it, int64_t block) {
         if constexpr (BITS == 8) {
             ms = it.ms[block];
             vs = it.vs[block];
         }
     }
 
-    // The step; random: sixteen bits for the parameters.  With 8-bit states every product and sum rounds by itself in the order of the formula, the
-    // quotients and the root correctly: the codes are then those of the formula in fp32 whoever evaluates it, where one entry in a million would else
-    // fall on the other side of a rounding's edge.
-    __device__ __forceinline__ void step(const Item &it, const AdamwStep &o, float scale, uint32_t key, int64_t i, int64_t block, bool stochastic) {
-        uint32_t random[kVec];
-        if (stochastic) {
-            const uint32_t upper = mixed(key + (uint32_t)(i >> 32));
+    // The step; place: the first entry's, upper: mixed with its upper half.  With 8-bit states every product and sum rounds by itself in the order of the formula,
+    // the quotients and the root correctly: the codes are then those of the formula in fp32 whoever evaluates it, where one entry in a million
+    // would else fall on the other side of a rounding's edge.
+    __device__ __forceinline__ void step(const Item &it, const AdamwStep &o, float scale, bool random, uint32_t place, uint32_t upper) {
+        uint32_t bits[kVec];
+        if (random) {
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) random[j] = mixed((uint32_t)(i + j) ^ upper);
+            for (int j = 0; j < kVec; ++j) bits[j] = mixed((place + (uint32_t)j) ^ upper);
         }
         float root[kVec];
         if constexpr (BITS == 8) {
 #pragma clang fp contract(off)
-            m[0] = __builtin_amdgcn_cvt_f32_fp8(m8, 0);
-            m[1] = __builtin_amdgcn_cvt_f32_fp8(m8, 1);
-            m[2] = __builtin_amdgcn_cvt_f32_fp8(m8, 2);
-            m[3] = __builtin_amdgcn_cvt_f32_fp8(m8, 3);
-            v[0] = __builtin_amdgcn_cvt_f32_fp8(v8, 0);
-            v[1] = __builtin_amdgcn_cvt_f32_fp8(v8, 1);
-            v[2] = __builtin_amdgcn_cvt_f32_fp8(v8, 2);
-            v[3] = __builtin_amdgcn_cvt_f32_fp8(v8, 3);
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) {
-                const float gs = g[j] * scale, old = v[j] * vs;
-                m[j] = m[j] * ms * o.beta1 + gs * o.more1;
-                v[j] = old * old * o.beta2 + gs * gs * o.more2;
-                root[j] = sqrtf(v[j]);
-            }
+            const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(m8, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8(m8, true);
+            const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8(v8, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(v8, true);
+            const float old_m[kVec] = {m01[0], m01[1], m23[0], m23[1]}, old_v[kVec] = {v01[0], v01[1], v23[0], v23[1]};
             float most_m = 0.f, most_v = 0.f;
 #pragma unroll
             for (int j = 0; j < kVec; ++j) {
+                const float g = (float)g_in[j] * scale, old = old_v[j] * vs;
+                m[j] = old_m[j] * ms * o.beta1 + g * o.more1;
+                v[j] = old * old * o.beta2 + g * g * o.more2;
+                root[j] = root_of(v[j]);
                 most_m = fmaxf(most_m, fabsf(m[j]));
                 most_v = fmaxf(most_v, root[j]);
             }
             ms = fmaxf(group_max<64>(most_m) * (1.f / kMost8), 0x1p-126f);
             vs = fmaxf(group_max<64>(most_v) * (1.f / kMost8), 0x1p-126f);
-            float qm[kVec], qv[kVec];
+            const float over_m = 1.f / ms, over_v = 1.f / vs;
+            if (random) {
+                uint32_t cm[kVec], cv[kVec];
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) {
-                qm[j] = m[j] / ms;
-                qv[j] = root[j] / vs;
-                if (stochastic) {
-                    qm[j] = qm[j] == qm[j] ? round_up_by(qm[j], random[j] & 0xffffu, 3, -6) : qm[j];
-                    qv[j] = qv[j] == qv[j] ? round_up_by(qv[j], random[j] >> 16, 3, -6) : qv[j];
+                for (int j = 0; j < kVec; ++j) {
+                    const float q = quotient(m[j], ms, over_m);
+                    cm[j] = random_code(fabsf(q), bits[j] & 0xffffu) | (__float_as_uint(q) >> 24 & 0x80u);
+                    cv[j] = max(random_code(quotient(root[j], vs, over_v), bits[j] >> 16), min(__float_as_uint(root[j]), 1u));
                 }
-                // (fmaxf and fminf would make a number of a NaN)
-                qm[j] = qm[j] > kMost8 ? kMost8 : qm[j] < -kMost8 ? -kMost8 : qm[j];
-                qv[j] = qv[j] > kMost8 ? kMost8 : root[j] > 0.f && qv[j] < kLeast8 ? kLeast8 : qv[j];
+                m8 = (int)(cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24);
+                v8 = (int)(cv[0] | cv[1] << 8 | cv[2] << 16 | cv[3] << 24);
+            } else {
+                float qm[kVec], qv[kVec];
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) {
+                    qm[j] = quotient(m[j], ms, over_m);
+                    qv[j] = quotient(root[j], vs, over_v);
+                    // (fmaxf and fminf would make a number of a NaN)
+                    qm[j] = qm[j] > kMost8 ? kMost8 : qm[j] < -kMost8 ? -kMost8 : qm[j];
+                    qv[j] = qv[j] > kMost8 ? kMost8 : root[j] > 0.f && qv[j] < kLeast8 ? kLeast8 : qv[j];
+                }
+                m8 = __builtin_amdgcn_cvt_pk_fp8_f32(qm[0], qm[1], 0, false);
+                m8 = __builtin_amdgcn_cvt_pk_fp8_f32(qm[2], qm[3], m8, true);
+                v8 = __builtin_amdgcn_cvt_pk_fp8_f32(qv[0], qv[1], 0, false);
+                v8 = __builtin_amdgcn_cvt_pk_fp8_f32(qv[2], qv[3], v8, true);
             }
-            m8 = __builtin_amdgcn_cvt_pk_fp8_f32(qm[0], qm[1], 0, false);
-            m8 = __builtin_amdgcn_cvt_pk_fp8_f32(qm[2], qm[3], m8, true);
-            v8 = __builtin_amdgcn_cvt_pk_fp8_f32(qv[0], qv[1], 0, false);
-            v8 = __builtin_amdgcn_cvt_pk_fp8_f32(qv[2], qv[3], v8, true);
         } else {
 #pragma unroll
             for (int j = 0; j < kVec; ++j) {
-                const float gs = g[j] * scale;
-                m[j] = fmaf(o.more1, gs, o.beta1 * m[j]);
-                v[j] = fmaf(o.more2 * gs, gs, o.beta2 * v[j]);
-                root[j] = sqrtf(v[j]);
+                const float g = (float)g_in[j] * scale;
+                m[j] = fmaf(o.more1, g, o.beta1 * m_in[j]);
+                v[j] = fmaf(o.more2 * g, g, o.beta2 * v_in[j]);
+                root[j] = root_of(v[j]);
             }
         }
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
-            p[j] = fmaf(-o.lr, fmaf(it.decay, p[j], m[j] * o.scale1 / fmaf(root[j], o.scale2, o.eps)), p[j]);
+            const float old = (float)p_in[j];
+            p[j] = fmaf(-o.lr, fmaf(it.decay, old, m[j] * o.scale1 * __builtin_amdgcn_rcpf(fmaf(root[j], o.scale2, o.eps))), old);
             if constexpr (sizeof(P) == 2) {
-                if (stochastic && fabsf(p[j]) < INFINITY) {
-                    const uint32_t bits = mixed(random[j] + 0x3C6EF372u) & 0xffffu;
-                    p[j] = std::is_same<P, __bf16>::value ? round_up_by(p[j], bits, 7, -126) : round_up_by(p[j], bits, 10, -14);
-                }
+                if (random && fabsf(p[j]) < INFINITY) p[j] = random_param<P>(p[j], mixed(bits[j] + 0x3C6EF372u) & 0xffffu);
             }
         }
     }
 
-    __device__ __forceinline__ void store(const Item &it, int64_t i, int64_t block) const {
+    __device__ __forceinline__ void store(const Item &it, int copy_type, int64_t i) const {
         store4<P>(it.p, i, p);
-        if (it.copy) {
-            if (it.copy_type == kBF16) store4<__bf16>(it.copy, i, p);
+        if constexpr (COPY) {
+            if (copy_type == kBF16) store4<__bf16>(it.copy, i, p);
             else store4<_Float16>(it.copy, i, p);
         }
         if constexpr (BITS == 8) {
             typedef int Loose __attribute__((aligned(1)));
             __builtin_nontemporal_store(m8, reinterpret_cast<Loose *>(static_cast<uint8_t *>(it.m) + i));
             __builtin_nontemporal_store(v8, reinterpret_cast<Loose *>(static_cast<uint8_t *>(it.v) + i));
-            store_scales(it, block);
         } else {
             store4<float>(it.m, i, m);
             store4<float>(it.v, i, v);
         }
     }
-    __device__ __forceinline__ void store_some(const Item &it, int64_t i, int64_t block, int n) const {
+    __device__ __forceinline__ void store_some(const Item &it, int copy_type, int64_t i, int n) const {
+        if (n >= kVec) {
+            store(it, copy_type, i);
+        } else if (n > 0) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-            if (j >= n) continue;
-            static_cast<P *>(it.p)[i + j] = stored<P>(p[j]);
-            if (it.copy) {
-                if (it.copy_type == kBF16) static_cast<__bf16 *>(it.copy)[i + j] = stored<__bf16>(p[j]);
-                else static_cast<_Float16 *>(it.copy)[i + j] = stored<_Float16>(p[j]);
-            }
-            if constexpr (BITS == 8) {
-                static_cast<uint8_t *>(it.m)[i + j] = (uint8_t)(m8 >> 8 * j);
-                static_cast<uint8_t *>(it.v)[i + j] = (uint8_t)(v8 >> 8 * j);
-            } else {
-                static_cast<float *>(it.m)[i + j] = m[j];
-                static_cast<float *>(it.v)[i + j] = v[j];
+            for (int j = 0; j < kVec - 1; ++j) {
+                if (j >= n) break;
+                static_cast<P *>(it.p)[i + j] = stored<P>(p[j]);
+                if constexpr (COPY) {
+                    if (copy_type == kBF16) static_cast<__bf16 *>(it.copy)[i + j] = stored<__bf16>(p[j]);
+                    else static_cast<_Float16 *>(it.copy)[i + j] = stored<_Float16>(p[j]);
+                }
+                if constexpr (BITS == 8) {
+                    static_cast<uint8_t *>(it.m)[i + j] = (uint8_t)(m8 >> 8 * j);
+                    static_cast<uint8_t *>(it.v)[i + j] = (uint8_t)(v8 >> 8 * j);
+                } else {
+                    static_cast<float *>(it.m)[i + j] = m[j];
+                    static_cast<float *>(it.v)[i + j] = v[j];
+                }
             }
         }
-        if constexpr (BITS == 8) store_scales(it, block);
     }
     __device__ __forceinline__ void store_scales(const Item &it, int64_t block) const {
-        if (lane_id() == 0) {
+        if (BITS == 8 && lane_id() == 0) {
             it.ms[block] = ms;
             it.vs[block] = vs;
         }
     }
 };
 
-// A workgroup per 4 kFlight blocks of 256 entries, a wavefront per block, four entries a lane.
-// A launch's threads stay below 2^32: 2^23 workgroups, which hold 2^33 entries and more.
+// A workgroup per 4 FLIGHT blocks of 256 entries, a wavefront per block at a time, four entries a lane.
+template <int FLIGHT>
+constexpr int kChunk = FLIGHT * kWaves * kBlock8;
+// A launch's threads stay below 2^32: 2^23 workgroups, which hold the 2^33 entries that a tensor may have.
 constexpr int64_t kMostBlocks = (int64_t)1 << 23;
-constexpr int kFlight = 4, kChunk = kFlight * kWaves * kBlock8;
 
-template <class P, class G, int BITS>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(Table table, AdamwStep o) {
+template <class P, class G, int BITS, bool COPY, int FLIGHT>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(Table<BITS, COPY> table, AdamwStep o) {
     // the tensor: the last that begins at or before this workgroup
-    const int32_t first = lane_id() < table.count ? table.first[lane_id()] : 0x7fffffff;
-    const int t = __builtin_amdgcn_readfirstlane((int)popc64(__ballot(first <= (int32_t)blockIdx.x)) - 1);
-    const Item &it = table.item[t];
+    const int32_t lane = lane_id(), here = (int32_t)blockIdx.x;
+    const int32_t low = lane < table.count ? table.first[lane] : 0x7fffffff;
+    int t = (int)popc64(__ballot(low <= here)) - 1;
+    if constexpr (Table<BITS, COPY>::kItems > kWave) {
+        const int32_t high = lane + kWave < table.count ? table.first[lane + kWave] : 0x7fffffff;
+        t += (int)popc64(__ballot(high <= here));
+    }
+    t = __builtin_amdgcn_readfirstlane(t);
+    const Item it = table.item(t);
     const float scale = o.grad_scale ? *o.grad_scale : 1.f;
     if (!(fabsf(scale) < INFINITY)) return;
     read_step(o);
-    const bool stochastic = o.stochastic != 0 && (BITS == 8 || sizeof(P) == 2);
-    const uint32_t key = stochastic ? key_of(o, it.number) : 0;
-    const int64_t chunk = (int)blockIdx.x - table.first[t], block = chunk * (kFlight * kWaves) + wave_id();
-    const int64_t i = block * kBlock8 + lane_id() * kVec;
+    const bool random = o.stochastic != 0 && (BITS == 8 || sizeof(P) == 2);
+    const uint32_t key = random ? key_of(o, it.number) : 0;
+    const int64_t chunk = here - table.first[t], block = chunk * (FLIGHT * kWaves) + wave_id();
+    const int64_t left = it.n - block * kBlock8;                   // from the wavefront's first block on; <= 0: it has none
     constexpr int kApart = kWaves * kBlock8;
-    Entries<P, G, BITS> e[kFlight];
-    if ((chunk + 1) * kChunk <= it.n) {
+    const int32_t mine = lane * kVec;
+    Entries<P, G, BITS, COPY> e[FLIGHT];
+    const bool whole = (chunk + 1) * kChunk<FLIGHT> <= it.n;
+    if (whole) {
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) e[u].load(it, i + u * kApart, block + u * kWaves);
+        for (int u = 0; u < FLIGHT; ++u) e[u].load(it, block * kBlock8 + u * kApart + mine);
+    } else {
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            e[u].step(it, o, scale, key, i + u * kApart, block + u * kWaves, stochastic);
-            e[u].store(it, i + u * kApart, block + u * kWaves);
-        }
-        return;
+        for (int u = 0; u < FLIGHT; ++u) e[u].load_some(it, block * kBlock8 + u * kApart + mine, (int)min(left - u * kApart - mine, (int64_t)kVec));
     }
-#pragma unroll 1
-    for (int u = 0; u < kFlight; ++u) {
-        const int64_t at = i + u * kApart;
-        const int64_t left = it.n - (block + u * kWaves) * kBlock8;
-        if (left <= 0) break;
-        const int n = (int)max(min(it.n - at, (int64_t)kVec), (int64_t)0);
-        if (left >= kBlock8) e[0].load(it, at, block + u * kWaves);
-        else e[0].load_some(it, at, block + u * kWaves, n);
-        e[0].step(it, o, scale, key, at, block + u * kWaves, stochastic);
-        if (left >= kBlock8) e[0].store(it, at, block + u * kWaves);
-        else e[0].store_some(it, at, block + u * kWaves, n);
+#pragma unroll
+    for (int u = 0; u < FLIGHT; ++u)
+        if (left > u * kApart) e[u].load_scales(it, block + u * kWaves);
+#pragma unroll
+    for (int u = 0; u < FLIGHT; ++u) {
+        if (left <= u * kApart) break;
+        const int64_t from = block * kBlock8 + u * kApart;
+        e[u].step(it, o, scale, random, (uint32_t)from + (uint32_t)mine, mixed(key + (uint32_t)(from >> 32)));
+        if (whole) e[u].store(it, table.copy_type, from + mine);
+        else e[u].store_some(it, table.copy_type, from + mine, (int)min(left - u * kApart - mine, (int64_t)kVec));
+        e[u].store_scales(it, block + u * kWaves);
     }
 }
 
-template <class P, class G, int BITS>
-hipError_t launch_group(const ef21_adamw_tensor *tensors, int32_t count, const AdamwStep &step, int param_type, int grad_type, hipStream_t stream) {
-    Table table{};
+// Launches for the tensors of one kind.
+struct Kind {
+    int param, grad, bits, copy;                                   // copy: its type or -1
+    bool operator==(const Kind &o) const { return param == o.param && grad == o.grad && bits == o.bits && copy == o.copy; }
+};
+Kind kind_of(const ef21_adamw_tensor &x) { return {x.param_type, x.grad_type, x.m_scale ? 8 : 32, x.copy ? x.copy_type : -1}; }
+
+template <class P, class G, int BITS, bool COPY, int FLIGHT>
+hipError_t launch_kind(const ef21_adamw_tensor *tensors, int32_t count, const AdamwStep &step, const Kind &kind, hipStream_t stream) {
+    typedef Table<BITS, COPY> Tensors;
+    Tensors table{};
+    table.copy_type = kind.copy;
     int64_t blocks = 0;
     const auto flush = [&]() {
         if (table.count == 0) return hipSuccess;
-        hipLaunchKernelGGL((adamw_kernel<P, G, BITS>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, table, step);
+        hipLaunchKernelGGL((adamw_kernel<P, G, BITS, COPY, FLIGHT>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, table, step);
         table.count = 0;
         blocks = 0;
         return hipGetLastError();
     };
     for (int32_t i = 0; i < count; ++i) {
         const ef21_adamw_tensor &x = tensors[i];
-        if (x.count == 0 || x.param_type != param_type || x.grad_type != grad_type || (x.m_scale != nullptr) != (BITS == 8)) continue;
-        const int64_t more = (x.count + kChunk - 1) / kChunk;
-        if (table.count == kItems || (table.count > 0 && blocks + more > kMostBlocks))
+        if (x.count == 0 || !(kind_of(x) == kind)) continue;
+        const int64_t more = (x.count + kChunk<FLIGHT> - 1) / kChunk<FLIGHT>;
+        if (table.count == Tensors::kItems || (table.count > 0 && blocks + more > kMostBlocks))
             if (hipError_t st = flush()) return st;
-        table.item[table.count] = Item{x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.count, x.weight_decay, i, x.copy_type};
-        table.first[table.count++] = (int32_t)blocks;
+        const int32_t t = table.count++;
+        table.p[t] = x.param;
+        table.g[t] = x.grad;
+        table.m[t] = x.m;
+        table.v[t] = x.v;
+        if constexpr (BITS == 8) {
+            table.ms[t] = x.m_scale;
+            table.vs[t] = x.v_scale;
+        }
+        if constexpr (COPY) table.copy[t] = x.copy;
+        table.n[t] = x.count;
+        table.decay[t] = x.weight_decay;
+        table.number[t] = i;
+        table.first[t] = (int32_t)blocks;
         blocks += more;
     }
     return flush();
+}
+
+// 8-bit states: two blocks in flight of a wavefront where the chip has several rounds of workgroups, 201 million entries 541 us, 560 with one and 557 with
+// four; else one, since a block takes a microsecond of instructions: 11.2 million in 146 tensors 43, 47 with two and 56 with four.  32-bit states: one,
+// 403 million entries 1888 us, with two the same and 1930 with four.
+constexpr int64_t kManyEntries = (int64_t)1 << 25;
+
+template <class P, class G, int BITS, bool COPY>
+hipError_t launch_kind(const ef21_adamw_tensor *tensors, int32_t count, const AdamwStep &step, const Kind &kind, int64_t entries, hipStream_t stream) {
+    if constexpr (BITS == 8)
+        if (entries >= kManyEntries) return launch_kind<P, G, BITS, COPY, 2>(tensors, count, step, kind, stream);
+    return launch_kind<P, G, BITS, COPY, 1>(tensors, count, step, kind, stream);
 }
 
 }  // namespace
@@ -329,18 +416,37 @@ AdamwStep adamw_step(const ef21_adamw_options &o) {
 }
 
 hipError_t launch_adamw(const ef21_adamw_tensor *tensors, int32_t count, const AdamwStep &step, hipStream_t stream) {
-    for (int param = 0; param < 3; ++param)
-        for (int grad = 0; grad < 3; ++grad) {
-            const hipError_t st = with_type(param, [&](auto p) {
-                return with_type(grad, [&](auto g) {
-                    typedef typename ValueOf<decltype(p)::value>::type P;
-                    typedef typename ValueOf<decltype(g)::value>::type G;
-                    if (hipError_t st = launch_group<P, G, 32>(tensors, count, step, param, grad, stream)) return st;
-                    return launch_group<P, G, 8>(tensors, count, step, param, grad, stream);
-                });
-            });
-            if (st != hipSuccess) return st;
+    Kind kinds[3 * 3 * 2 * 3];
+    int64_t entries[3 * 3 * 2 * 3];
+    int found = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (tensors[i].count == 0) continue;
+        const Kind kind = kind_of(tensors[i]);
+        int k = 0;
+        while (k < found && !(kinds[k] == kind)) ++k;
+        if (k == found) {
+            kinds[found++] = kind;
+            entries[k] = 0;
         }
+        entries[k] += tensors[i].count;
+    }
+    for (int k = 0; k < found; ++k) {
+        const Kind &kind = kinds[k];
+        const hipError_t st = with_type(kind.param, [&](auto param) {
+            return with_type(kind.grad, [&](auto grad) {
+                typedef typename ValueOf<decltype(param)::value>::type P;
+                typedef typename ValueOf<decltype(grad)::value>::type G;
+                if constexpr (sizeof(P) == 4) {
+                    if (kind.copy >= 0)
+                        return kind.bits == 8 ? launch_kind<P, G, 8, true>(tensors, count, step, kind, entries[k], stream)
+                                              : launch_kind<P, G, 32, true>(tensors, count, step, kind, entries[k], stream);
+                }
+                return kind.bits == 8 ? launch_kind<P, G, 8, false>(tensors, count, step, kind, entries[k], stream)
+                                      : launch_kind<P, G, 32, false>(tensors, count, step, kind, entries[k], stream);
+            });
+        });
+        if (st != hipSuccess) return st;
+    }
     return hipSuccess;
 }
 

@@ -19,7 +19,6 @@ struct Item {
 struct Table {
     Item item[kItems];
     int32_t first[kItems];                                         // chunks before its own
-    uint8_t type[kItems];
     int32_t count, chunks;
 };
 static_assert(sizeof(Table) + 64 <= 4096, "the arguments of a kernel");
@@ -50,8 +49,8 @@ __device__ __forceinline__ void add_chunk(const Item &it, int64_t c, double &s) 
     const T *g = static_cast<const T *>(it.g) + c * kPieces * N;
     const int64_t left = it.n - c * kPieces * N;
     const auto load = [&](int i) { return Raw(__builtin_nontemporal_load(reinterpret_cast<const Loose *>(g + i * N))); };
-    Raw r[kEach];
     if (left >= kPieces * N) {
+        Raw r[kEach];
 #pragma unroll
         for (int u = 0; u < kEach; ++u) r[u] = load((int)threadIdx.x + u * THREADS);
 #pragma unroll
@@ -59,31 +58,22 @@ __device__ __forceinline__ void add_chunk(const Item &it, int64_t c, double &s) 
         return;
     }
     const int pieces = (int)(left / N), tail = (int)(left % N);
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        r[u] = Raw{0u, 0u, 0u, 0u};
-        if ((int)threadIdx.x + u * THREADS < pieces) r[u] = load((int)threadIdx.x + u * THREADS);
+#pragma unroll 2
+    for (int i = (int)threadIdx.x; i < pieces; i += THREADS) add_squares<T>(load(i), s);
+    if ((int)threadIdx.x < tail) {
+        const double last = (double)(float)g[pieces * N + (int)threadIdx.x];
+        s = fma(last, last, s);
     }
-    const float last = (int)threadIdx.x < tail ? (float)g[pieces * N + (int)threadIdx.x] : 0.f;
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) add_squares<T>(r[u], s);
-    s = fma((double)last, (double)last, s);
 }
 
-template <int THREADS>
+template <class T, int THREADS>
 __device__ __forceinline__ double sum_chunks(const Table &table) {
     double s = 0.0;
     const int32_t lane = lane_id();
     const int32_t low = lane < table.count ? table.first[lane] : 0x7fffffff, high = lane + kWave < table.count ? table.first[lane + kWave] : 0x7fffffff;
     for (int32_t c = (int32_t)blockIdx.x; c < table.chunks; c += (int32_t)gridDim.x) {
         const int t = __builtin_amdgcn_readfirstlane((int)(popc64(__ballot(low <= c)) + popc64(__ballot(high <= c))) - 1);
-        const Item it = table.item[t];
-        const int64_t at = c - table.first[t];
-        switch (table.type[t]) {
-            case kF32: add_chunk<float, THREADS>(it, at, s); break;
-            case kBF16: add_chunk<__bf16, THREADS>(it, at, s); break;
-            default: add_chunk<_Float16, THREADS>(it, at, s);
-        }
+        add_chunk<T, THREADS>(table.item[t], c - table.first[t], s);
     }
     return s;
 }
@@ -96,15 +86,17 @@ __device__ __forceinline__ void write_norm(double squares, const NormArgs &p) {
     p.factor[0] = !finite ? __int_as_float(0x7fc00000) : norm > (double)p.max_norm ? (float)((double)p.scale * ((double)p.max_norm / norm)) : p.scale;
 }
 
-__global__ __launch_bounds__(kThreads) void square_sums_kernel(Table table, double *sums) {
+template <class T>
+__global__ __launch_bounds__(kThreads, 8) void square_sums_kernel(Table table, double *sums) {
     __shared__ double part[kThreads / kWave];
-    const double s = block_sum<kThreads / kWave>(sum_chunks<kThreads>(table), part);
+    const double s = block_sum<kThreads / kWave>(sum_chunks<T, kThreads>(table), part);
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
+template <class T>
 __global__ __launch_bounds__(kFewThreads) void few_norm_kernel(Table table, NormArgs p) {
     __shared__ double part[kFewThreads / kWave];
-    const double s = block_sum<kFewThreads / kWave>(sum_chunks<kFewThreads>(table), part);
+    const double s = block_sum<kFewThreads / kWave>(sum_chunks<T, kFewThreads>(table), part);
     if (threadIdx.x == 0) write_norm(s, p);
 }
 
@@ -118,40 +110,53 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const double *sums, int3
 
 }  // namespace
 
-// A launch takes kItems tensors, or 2^30 chunks if they are more than the memory of this card.
-size_t norm_workspace_bytes(int32_t tensors) { return (size_t)((tensors + kItems - 1) / kItems) * kMostBlocks * sizeof(double); }
+// A launch takes kItems tensors of one type.
+size_t norm_workspace_bytes(int32_t tensors) {
+    return tensors == 0 ? 0 : (size_t)((tensors + kItems - 1) / kItems + 2) * kMostBlocks * sizeof(double);
+}
 
 hipError_t launch_grad_norm(const void *const *grads, const int32_t *types, const int64_t *counts, int32_t tensors, const NormArgs &p, void *workspace,
                             hipStream_t stream) {
     double *sums = static_cast<double *>(workspace);
-    int32_t written = 0, launches = 0;
-    Table table{};
+    int64_t chunks = 0;
+    int kinds = 0;
+    const auto chunks_of = [&](int32_t i) { return (counts[i] * value_bytes(types[i]) + kChunkBytes - 1) / kChunkBytes; };
     for (int32_t i = 0; i < tensors; ++i) {
-        if (counts[i] > 0) {
-            const int64_t bytes = counts[i] * value_bytes(types[i]);
-            table.item[table.count] = Item{grads[i], counts[i]};
-            table.type[table.count] = (uint8_t)types[i];
-            table.first[table.count++] = table.chunks;
-            table.chunks += (int32_t)((bytes + kChunkBytes - 1) / kChunkBytes);
-        }
-        if (table.count < kItems || i + 1 == tensors) continue;
-        const int32_t blocks = table.chunks < kMostBlocks ? table.chunks : kMostBlocks;
-        hipLaunchKernelGGL(square_sums_kernel, dim3(blocks), dim3(kThreads), 0, stream, table, sums + written);
-        if (hipError_t st = hipGetLastError()) return st;
-        written += blocks;
-        ++launches;
-        table.count = table.chunks = 0;
+        chunks += chunks_of(i);
+        if (counts[i] > 0) kinds |= 1 << types[i];
     }
-    if (launches == 0 && table.chunks <= kFewChunks) {
-        hipLaunchKernelGGL(few_norm_kernel, dim3(1), dim3(kFewThreads), 0, stream, table, p);
-        return hipGetLastError();
+    const bool few = chunks <= kFewChunks && tensors <= kItems && (kinds & (kinds - 1)) == 0;
+    int32_t written = 0;
+    for (int type = kF32; type <= kF16; ++type) {
+        if (!(kinds >> type & 1)) continue;
+        const hipError_t st = with_type(type, [&](auto as) {
+            typedef typename ValueOf<decltype(as)::value>::type T;
+            Table table{};
+            const auto flush = [&]() {
+                if (table.count == 0) return hipSuccess;
+                if (few) {
+                    hipLaunchKernelGGL(few_norm_kernel<T>, dim3(1), dim3(kFewThreads), 0, stream, table, p);
+                } else {
+                    const int32_t blocks = table.chunks < kMostBlocks ? table.chunks : kMostBlocks;
+                    hipLaunchKernelGGL(square_sums_kernel<T>, dim3(blocks), dim3(kThreads), 0, stream, table, sums + written);
+                    written += blocks;
+                }
+                table.count = table.chunks = 0;
+                return hipGetLastError();
+            };
+            for (int32_t i = 0; i < tensors; ++i) {
+                if (types[i] != type || counts[i] == 0) continue;
+                if (table.count == kItems || (table.count > 0 && table.chunks + chunks_of(i) > INT32_MAX - kMostBlocks))
+                    if (hipError_t st = flush()) return st;
+                table.item[table.count] = Item{grads[i], counts[i]};
+                table.first[table.count++] = table.chunks;
+                table.chunks += (int32_t)chunks_of(i);
+            }
+            return flush();
+        });
+        if (st != hipSuccess) return st;
     }
-    if (table.count > 0) {
-        const int32_t blocks = table.chunks < kMostBlocks ? table.chunks : kMostBlocks;
-        hipLaunchKernelGGL(square_sums_kernel, dim3(blocks), dim3(kThreads), 0, stream, table, sums + written);
-        if (hipError_t st = hipGetLastError()) return st;
-        written += blocks;
-    }
+    if (few && kinds) return hipSuccess;
     hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, stream, sums, written, p);
     return hipGetLastError();
 }

@@ -16,10 +16,10 @@ bool value_type(int type) { return type == EF21_F32 || type == EF21_BF16 || type
 bool array_of(const void *p, int64_t bytes) { return p && aligned(p, bytes); }
 
 // Entries of one tensor: more than the card's memory holds, and a launch's workgroups do.
-constexpr int64_t kMostEntries = (int64_t)1 << 34;
+constexpr int64_t kMostEntries = (int64_t)1 << 33;
 
 int check_tensor(const ef21_adamw_tensor &t) {
-    if (t.count < 0 || t.count > kMostEntries) return invalid("a tensor's count must be in [0, 2^34]");
+    if (t.count < 0 || t.count > kMostEntries) return invalid("a tensor's count must be in [0, 2^33]");
     if (!value_type(t.param_type) || !value_type(t.grad_type)) return invalid("unknown type of a parameter or gradient");
     if (!std::isfinite(t.weight_decay)) return invalid("weight_decay must be finite");
     if (t.count == 0) return EF21_OK;
@@ -29,6 +29,7 @@ int check_tensor(const ef21_adamw_tensor &t) {
     if (!aligned(t.m_scale, 4) || !aligned(t.v_scale, 4)) return invalid("a scale is misaligned");
     const int64_t bytes = t.m_scale ? 1 : 4;
     if (!array_of(t.m, bytes) || !array_of(t.v, bytes)) return invalid("a state is NULL or misaligned");
+    if (t.copy && t.param_type != EF21_F32) return invalid("a copy needs fp32 parameters");
     if (t.copy && ((t.copy_type != EF21_BF16 && t.copy_type != EF21_F16) || !aligned(t.copy, 2)))
         return invalid("a copy must be bf16 or fp16 and aligned");
     return EF21_OK;
@@ -51,7 +52,7 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
     if (tensor_count > 0 && (!grads || !types || !counts)) return invalid("grads, types or counts is NULL");
     for (int32_t i = 0; i < tensor_count; ++i) {
         if (!value_type(types[i])) return invalid("unknown type of a gradient");
-        if (counts[i] < 0 || counts[i] > kMostEntries) return invalid("a tensor's count must be in [0, 2^34]");
+        if (counts[i] < 0 || counts[i] > kMostEntries) return invalid("a tensor's count must be in [0, 2^33]");
         if (counts[i] > 0 && !array_of(grads[i], ef21::value_bytes(types[i]))) return invalid("a gradient is NULL or misaligned");
     }
     if (!(scale > 0.f) || !std::isfinite(scale)) return invalid("scale must be finite and > 0");
@@ -72,7 +73,7 @@ int ef21_adamw(const ef21_adamw_tensor *tensors, int32_t tensor_count, const ef2
     const ef21_adamw_options &o = *options;
     if (!std::isfinite(o.lr)) return invalid("lr must be finite");
     if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0)) return invalid("beta1 and beta2 must be in [0, 1)");
-    if (!((float)o.eps > 0.f) || !std::isfinite((float)o.eps)) return invalid("eps must be finite and > 0");
+    if (!((float)o.eps >= 0x1p-126f) || !std::isfinite((float)o.eps)) return invalid("eps must be finite and at least 2^-126");
     if (o.step < 1) return invalid("step must be at least 1");
     if (!aligned(o.lr_device, 4) || !aligned(o.step_device, 8) || !aligned(o.grad_scale, 4)) return invalid("lr_device, step_device or grad_scale is misaligned");
     const hipError_t st = ef21::launch_adamw(tensors, tensor_count, ef21::adamw_step(o), (hipStream_t)hip_stream);

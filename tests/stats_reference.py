@@ -159,7 +159,7 @@ class Adamw:
             d_scale = most + 2 * U * scale
             s, ds = spread(scale, len(x)), spread(d_scale, len(x))
             r = x / s
-            dr = d / s + np.abs(r) * (ds / s + 3 * U)
+            dr = d / s + np.abs(r) * (ds / s + 3 * U) + 2.0 ** -30      # below 2^-6 random rounding takes r to a multiple of 2^-29 first
             low, high = (np.clip(rounded(y, "e4m3", bits), -448, 448) for y in (r - dr, r + dr))
             if name == "v":
                 floor = lambda y: np.where(self.v > 0, np.maximum(y, 2.0 ** -9), y)  # noqa: E731

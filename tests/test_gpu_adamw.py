@@ -326,7 +326,7 @@ def test_binding_refuses(gpu):
             (TypeError, lambda: b.AdamW([f(8)[::2]])), (ValueError, lambda: b.AdamW([p], [g, g])), (ValueError, lambda: b.AdamW([p], [f(5)])),
             (TypeError, lambda: b.AdamW([p], [g.long()])), (ValueError, lambda: b.AdamW([p], bits=16)), (ValueError, lambda: b.AdamW([p], bits=[8, 32])),
             (ValueError, lambda: b.AdamW([p], m_scale=[f(1)])), (TypeError, lambda: b.AdamW([p], m=[f().half()])), (ValueError, lambda: b.AdamW([p], m=[f(5)])),
-            (ValueError, lambda: b.AdamW([p], bits=8, m_scale=[f(2)])), (TypeError, lambda: b.AdamW([p], copies=[f()])),
+            (ValueError, lambda: b.AdamW([p], bits=8, m_scale=[f(2)])), (TypeError, lambda: b.AdamW([p], copies=[f()])), (TypeError, lambda: b.AdamW([p.half()], copies=[p.half()])),
             (ValueError, lambda: b.AdamW([p], copies=[f(3).half()])), (ValueError, lambda: b.AdamW([p, p])), (ValueError, lambda: b.AdamW([both[:5], both[4:]])),
             (ValueError, lambda: b.AdamW([p], [p])), (ValueError, lambda: b.AdamW([p], m=[g], v=[g])), (ValueError, lambda: b.AdamW([p], [g], m=[g])),
             (ValueError, lambda: b.AdamW([p]).step(1e-3)), (b.EF21Error, lambda: b.AdamW([p], [g]).step(math.nan)),

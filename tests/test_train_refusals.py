@@ -57,13 +57,13 @@ def options(**change):
 
 
 def test_adamw(lib, ptr):  # noqa: F811
-    for change in [dict(count=-1), dict(count=2 ** 34 + 1), dict(param_type=3), dict(grad_type=-1), dict(weight_decay=math.inf), dict(weight_decay=math.nan), dict(param=None),
+    for change in [dict(count=-1), dict(count=2 ** 33 + 1), dict(param_type=3), dict(grad_type=-1), dict(weight_decay=math.inf), dict(weight_decay=math.nan), dict(param=None),
                    dict(param=ptr + 2), dict(grad=None), dict(grad=ptr + 1), dict(m=None), dict(v=None), dict(m=ptr + 2), dict(v=ptr + 1), dict(m_scale=ptr),
                    dict(v_scale=ptr), dict(m_scale=ptr + 2, v_scale=ptr), dict(m_scale=ptr, v_scale=ptr + 1), dict(copy=ptr, copy_type=0), dict(copy=ptr, copy_type=3),
-                   dict(copy=ptr + 1, copy_type=1)]:
+                   dict(copy=ptr + 1, copy_type=1), dict(copy=ptr, copy_type=1, param_type=1)]:
         refused(lib, lib.ef21_adamw(tensor(ptr, **change), 1, options(), None))
     for change in [dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta1=math.nan), dict(beta2=1.0), dict(beta2=-1.0), dict(eps=0.0), dict(eps=-1.0),
-                   dict(eps=math.inf), dict(eps=1e-60), dict(eps=math.nan), dict(step=0), dict(step=-3), dict(lr_device=ptr + 2), dict(step_device=ptr + 4), dict(grad_scale=ptr + 1)]:
+                   dict(eps=math.inf), dict(eps=1e-60), dict(eps=1e-38), dict(eps=math.nan), dict(step=0), dict(step=-3), dict(lr_device=ptr + 2), dict(step_device=ptr + 4), dict(grad_scale=ptr + 1)]:
         refused(lib, lib.ef21_adamw(tensor(ptr), 1, options(**change), None))
     refused(lib, lib.ef21_adamw(tensor(ptr), -1, options(), None))
     refused(lib, lib.ef21_adamw(None, 1, options(), None))
@@ -76,7 +76,7 @@ def test_grad_norm(lib, ptr):  # noqa: F811
     one = lambda kind, v: (kind * 1)(v)  # noqa: E731
     good = [one(C.c_void_p, ptr), one(C.c_int32, 1), one(C.c_int64, 8), 1, 1.0, 1.0, ptr, ptr + 4, ptr + 256, size.value, None]
     for at, value in [(0, None), (0, one(C.c_void_p, None)), (0, one(C.c_void_p, ptr + 1)), (1, None), (1, one(C.c_int32, 3)), (2, None), (2, one(C.c_int64, -1)),
-                      (2, one(C.c_int64, 2 ** 34 + 1)), (3, -1), (4, 0.0), (4, -1.0), (4, math.nan), (4, math.inf), (5, 0.0), (5, math.nan), (5, -1.0), (6, None), (6, ptr + 2),
+                      (2, one(C.c_int64, 2 ** 33 + 1)), (3, -1), (4, 0.0), (4, -1.0), (4, math.nan), (4, math.inf), (5, 0.0), (5, math.nan), (5, -1.0), (6, None), (6, ptr + 2),
                       (7, None), (8, None), (8, ptr + 8), (9, size.value - 1), (9, -1)]:
         refused(lib, lib.ef21_grad_norm(*swap(good, at, value)))
     refused(lib, lib.ef21_grad_norm_workspace(-1, C.byref(size)))
