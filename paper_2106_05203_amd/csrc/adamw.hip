@@ -12,8 +12,9 @@
 namespace ef21 {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave, kVec = kBlock8 / kWave;
-constexpr float kMost8 = 448.f, kLeast8 = 0x1p-9f;                // e4m3's largest number and its least above zero
+constexpr int kVec = kBlock8 / kWave;
+constexpr float kMost8 = 448.f, kLeast8 = 0x1p-9f;                // e4m3's largest number (up to 464 the hardware rounds to it) and its least
+constexpr float kLargest = 3.402823466e38f;                        // above zero; fp32's largest
 
 // What a launch's workgroups read of a tensor.
 struct Item {
@@ -74,18 +75,35 @@ __device__ __forceinline__ float root_of(float v) {
     return above > 0.f ? up : below <= 0.f ? down : s;
 }
 
-// x / s correctly rounded, from the correctly rounded 1 / s (where the remainder is in fp32's range: x / s above 2^-20, say, which is far below the least code).
+// x / s correctly rounded but for one in millions, from 1 / s that is off by its last bit (where the remainder is in fp32's range: x / s above 2^-20, say, which is far below the least code).
 __device__ __forceinline__ float quotient(float x, float s, float inverse) {
     const float q = x * inverse;
     return fmaf(fmaf(-q, s, x), inverse, q);
 }
 
-// Bytes of e4m3 numbers by random rounding: to the neighbour towards zero, or the one beyond it with the probability of what lies above.  Times 2^-120 the
-// least normal e4m3 number is fp32's, so that the exponent's lower four bits and three of the fraction's are the byte, below the least normal number too;
-// the sixteen random bits, each of which stands for the middle of its interval, are added to the twenty bits behind.
-__device__ __forceinline__ uint32_t random_code(float size, uint32_t bits) {
-    const uint32_t b = __float_as_uint(size * 0x1p-120f) + (bits << 4) + 8u;
-    return size == size ? min(b >> 20, 0x7eu) : 0x7fu;
+// The byte of an e4m3 number by random rounding, in its place above 2^20: to the neighbour towards zero, or the one beyond it with the probability of what
+// lies above.  Times 2^-120 the least normal e4m3 number is fp32's, so that the exponent's lower four bits and three of the fraction's are the byte, below
+// the least normal number too; the sixteen random bits, each of which stands for the middle of its interval, are added to the twenty bits behind.
+// A NaN lies above 0x7f, and what is 448 up to rounding below it, whatever is added.
+__device__ __forceinline__ uint32_t random_code(float size, uint32_t bits) { return __float_as_uint(size * 0x1p-120f) + (bits << 4) + 8u; }
+__device__ __forceinline__ uint32_t byte_of(uint32_t code) { return min(code >> 20, 0x7fu); }
+
+// The largest of a wavefront's numbers, which are not negative: as whole numbers, so that an instruction does each of the first four steps.
+__device__ __forceinline__ float wave_max_size(float size) {
+    uint32_t b = __float_as_uint(size);
+    b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0xB1, 0xf, 0xf, true));
+    b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0x4E, 0xf, 0xf, true));
+    b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0x141, 0xf, 0xf, true));
+    b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0x140, 0xf, 0xf, true));
+    auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    b = max(r[0], r[1]);
+    r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return __uint_as_float(max(r[0], r[1]));
+}
+
+__device__ __forceinline__ float inverse_of(float s) {
+    const float y = __builtin_amdgcn_rcpf(s);
+    return fmaf(fmaf(-s, y, 1.f), y, y);
 }
 
 // The same for a parameter: bf16, which is the upper half of fp32, and fp16.
@@ -193,16 +211,17 @@ struct Entries {
                 most_m = fmaxf(most_m, fabsf(m[j]));
                 most_v = fmaxf(most_v, root[j]);
             }
-            ms = fmaxf(group_max<64>(most_m) * (1.f / kMost8), 0x1p-126f);
-            vs = fmaxf(group_max<64>(most_v) * (1.f / kMost8), 0x1p-126f);
-            const float over_m = 1.f / ms, over_v = 1.f / vs;
+            ms = fmaxf(wave_max_size(most_m) * (1.f / kMost8), 0x1p-126f);
+            vs = fmaxf(wave_max_size(most_v) * (1.f / kMost8), 0x1p-126f);
+            const float over_m = inverse_of(ms), over_v = inverse_of(vs);
             if (random) {
                 uint32_t cm[kVec], cv[kVec];
 #pragma unroll
                 for (int j = 0; j < kVec; ++j) {
                     const float q = quotient(m[j], ms, over_m);
-                    cm[j] = random_code(fabsf(q), bits[j] & 0xffffu) | (__float_as_uint(q) >> 24 & 0x80u);
-                    cv[j] = max(random_code(quotient(root[j], vs, over_v), bits[j] >> 16), min(__float_as_uint(root[j]), 1u));
+                    cm[j] = byte_of(random_code(fabsf(q), bits[j] & 0xffffu)) | (__float_as_uint(q) >> 24 & 0x80u);
+                    // a root above zero has 2^20 and more for its bits
+                    cv[j] = byte_of(max(random_code(quotient(root[j], vs, over_v), bits[j] >> 16), min(__float_as_uint(root[j]), 1u << 20)));
                 }
                 m8 = (int)(cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24);
                 v8 = (int)(cv[0] | cv[1] << 8 | cv[2] << 16 | cv[3] << 24);
@@ -212,9 +231,7 @@ struct Entries {
                 for (int j = 0; j < kVec; ++j) {
                     qm[j] = quotient(m[j], ms, over_m);
                     qv[j] = quotient(root[j], vs, over_v);
-                    // (fmaxf and fminf would make a number of a NaN)
-                    qm[j] = qm[j] > kMost8 ? kMost8 : qm[j] < -kMost8 ? -kMost8 : qm[j];
-                    qv[j] = qv[j] > kMost8 ? kMost8 : root[j] > 0.f && qv[j] < kLeast8 ? kLeast8 : qv[j];
+                    qv[j] = root[j] > 0.f ? fmaxf(qv[j], kLeast8) : qv[j];
                 }
                 m8 = __builtin_amdgcn_cvt_pk_fp8_f32(qm[0], qm[1], 0, false);
                 m8 = __builtin_amdgcn_cvt_pk_fp8_f32(qm[2], qm[3], m8, true);
@@ -233,7 +250,8 @@ struct Entries {
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
             const float old = (float)p_in[j];
-            p[j] = fmaf(-o.lr, fmaf(it.decay, old, m[j] * o.scale1 * __builtin_amdgcn_rcpf(fmaf(root[j], o.scale2, o.eps))), old);
+            const float under = fminf(fmaf(root[j], o.scale2, o.eps), kLargest);
+            p[j] = fmaf(-o.lr, fmaf(it.decay, old, quotient(m[j] * o.scale1, under, __builtin_amdgcn_rcpf(under))), old);
             if constexpr (sizeof(P) == 2) {
                 if (random && fabsf(p[j]) < INFINITY) p[j] = random_param<P>(p[j], mixed(bits[j] + 0x3C6EF372u) & 0xffffu);
             }
@@ -285,14 +303,26 @@ struct Entries {
     }
 };
 
-// A workgroup per 4 FLIGHT blocks of 256 entries, a wavefront per block at a time, four entries a lane.
-template <int FLIGHT>
-constexpr int kChunk = FLIGHT * kWaves * kBlock8;
-// A launch's threads stay below 2^32: 2^23 workgroups, which hold the 2^33 entries that a tensor may have.
+// A workgroup per WAVES FLIGHT blocks of 256 entries, a wavefront per block at a time, four entries a lane.
+//   32-bit states are bound by memory, and the memory answers seven streams of fewer wavefronts faster: 403 million entries with a copy in workgroups of two
+// wavefronts, three to a SIMD, 1842 us (6.1 TB/s); as many as the registers allow (eight) 2012, two 2070.  Without a copy, 134 million fp32 entries and
+// gradients, four to a SIMD 604, three 610; workgroups of four wavefronts 649, eight to a SIMD 666.
+//   8-bit states take some 90 instructions an entry, and as many wavefronts as there are: 201 million fp32 entries 536, three to a SIMD 594.  Two blocks in
+// flight of a wavefront where the chip has several rounds of workgroups: 541, with one 560, with four 557; else one, since a block takes a microsecond of
+// instructions: 11.2 million entries in 146 tensors 43, with two 47, with four 56.
+template <int BITS, bool COPY>
+struct Shape {
+    static constexpr int kWaves = BITS == 8 ? 4 : 2, kThreads = kWaves * kWave, kToSimd = BITS == 8 ? 8 : COPY ? 3 : 4;
+    template <int FLIGHT>
+    static constexpr int chunk() { return FLIGHT * kWaves * kBlock8; }
+};
+constexpr int64_t kManyEntries = (int64_t)1 << 25;
+// A launch's threads stay below 2^32: 2^24 workgroups, which hold the 2^33 entries that a tensor may have.
 constexpr int64_t kMostBlocks = (int64_t)1 << 23;
 
 template <class P, class G, int BITS, bool COPY, int FLIGHT>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(Table<BITS, COPY> table, AdamwStep o) {
+__global__ __launch_bounds__((Shape<BITS, COPY>::kThreads)) __attribute__((amdgpu_waves_per_eu(1, (Shape<BITS, COPY>::kToSimd)))) void adamw_kernel(Table<BITS, COPY> table, AdamwStep o) {
+    constexpr int kWaves = Shape<BITS, COPY>::kWaves, kChunk = Shape<BITS, COPY>::template chunk<FLIGHT>();
     // the tensor: the last that begins at or before this workgroup
     const int32_t lane = lane_id(), here = (int32_t)blockIdx.x;
     const int32_t low = lane < table.count ? table.first[lane] : 0x7fffffff;
@@ -313,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table<BITS, COPY> table
     constexpr int kApart = kWaves * kBlock8;
     const int32_t mine = lane * kVec;
     Entries<P, G, BITS, COPY> e[FLIGHT];
-    const bool whole = (chunk + 1) * kChunk<FLIGHT> <= it.n;
+    const bool whole = (chunk + 1) * kChunk <= it.n;
     if (whole) {
 #pragma unroll
         for (int u = 0; u < FLIGHT; ++u) e[u].load(it, block * kBlock8 + u * kApart + mine);
@@ -345,6 +375,7 @@ Kind kind_of(const ef21_adamw_tensor &x) { return {x.param_type, x.grad_type, x.
 template <class P, class G, int BITS, bool COPY, int FLIGHT>
 hipError_t launch_kind(const ef21_adamw_tensor *tensors, int32_t count, const AdamwStep &step, const Kind &kind, hipStream_t stream) {
     typedef Table<BITS, COPY> Tensors;
+    constexpr int kThreads = Shape<BITS, COPY>::kThreads, kChunk = Shape<BITS, COPY>::template chunk<FLIGHT>();
     Tensors table{};
     table.copy_type = kind.copy;
     int64_t blocks = 0;
@@ -358,7 +389,7 @@ hipError_t launch_kind(const ef21_adamw_tensor *tensors, int32_t count, const Ad
     for (int32_t i = 0; i < count; ++i) {
         const ef21_adamw_tensor &x = tensors[i];
         if (x.count == 0 || !(kind_of(x) == kind)) continue;
-        const int64_t more = (x.count + kChunk<FLIGHT> - 1) / kChunk<FLIGHT>;
+        const int64_t more = (x.count + kChunk - 1) / kChunk;
         if (table.count == Tensors::kItems || (table.count > 0 && blocks + more > kMostBlocks))
             if (hipError_t st = flush()) return st;
         const int32_t t = table.count++;
@@ -379,11 +410,6 @@ hipError_t launch_kind(const ef21_adamw_tensor *tensors, int32_t count, const Ad
     }
     return flush();
 }
-
-// 8-bit states: two blocks in flight of a wavefront where the chip has several rounds of workgroups, 201 million entries 541 us, 560 with one and 557 with
-// four; else one, since a block takes a microsecond of instructions: 11.2 million in 146 tensors 43, 47 with two and 56 with four.  32-bit states: one,
-// 403 million entries 1888 us, with two the same and 1930 with four.
-constexpr int64_t kManyEntries = (int64_t)1 << 25;
 
 template <class P, class G, int BITS, bool COPY>
 hipError_t launch_kind(const ef21_adamw_tensor *tensors, int32_t count, const AdamwStep &step, const Kind &kind, int64_t entries, hipStream_t stream) {
