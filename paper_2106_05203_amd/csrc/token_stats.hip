@@ -1,16 +1,36 @@
 // Entropy and the most likely tokens of rows of logits beside their log-probabilities, and the gradient (token_rows.h has the mathematics).
 //
 //   With z_v = x_v log2 e - M, s = sum 2^z_v and t = sum 2^z_v z_v:   entropy = ln 2 (log2 s - t / s)
-//   M is the row's maximum (a whole number next to it), so that no z is above 1/2: with t of one sign the difference does not cancel, and s >= 0.7.
 //   d logp / d x_v = [v = label] - p_v,   d entropy / d x_v = -p_v (log p_v + entropy)
+//
+// A row is cut into tiles of 512 pieces of 16 bytes, a wavefront's registers full.  Each tile has an M of its own, a whole number next to its maximum: no z
+// is above 1/2, so that t has one sign, the difference does not cancel and nothing leaves fp32's range, and no maximum has to be carried along.  A tile
+// leaves its M, s and t, and the tiles are joined in an order that the row's length alone fixes.
+//   The alternatives: a wavefront keeps the 64 best entries that it has met, one a lane, in order.  What the tile's maxima are needed for anyway tells it
+// whether a tile has any that is better than the k-th; those few are collected in LDS and merged 64 at a time.  The first bound is the k-th largest of the
+// 64 lanes' maxima of the first tile, which some k entries reach and not many more.
 #include "token_rows.h"
 
 namespace ef21 {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kEach = 8, kTile = kEach * kWave;                    // pieces of a lane, of a tile
+constexpr int kMostSlices = 256;
 
-// An order of entries: by value (-0 and 0 alike), then the lower token first.  A larger key comes first; 0 is no key of an entry.
+// Tiles of a row and how they are grouped: into at most 256 slices, each a wavefront's at a time.
+struct Slices {
+    int32_t count, tiles;                                          // slices, tiles of each
+};
+template <class T>
+__host__ __device__ __forceinline__ Slices slices_of(int32_t vocab) {
+    const int32_t tiles = vocab / (Piece<T>::N * kTile) + 1;       // whether a row of so many has one piece more or less
+    const int32_t each = (tiles + kMostSlices - 1) / kMostSlices;
+    return {(tiles + each - 1) / each, each};
+}
+
+// ---------------------------------------------------------------- order
+// An order of entries: by value (-0 and 0 alike), then the lower token first.  A larger key comes first; 0 is no entry's.
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t v) {
     const uint32_t bits = __float_as_uint(x + 0.f);
     const uint32_t order = bits ^ ((int32_t)bits < 0 ? 0xffffffffu : 0x80000000u);
@@ -22,105 +42,462 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 }
 __device__ __forceinline__ int32_t token_of(uint64_t key) { return (int32_t)(0xffffffffu - (uint32_t)key); }
 
-__device__ __forceinline__ uint64_t wave_max_key(uint64_t key) {
-    for (int o = kWave / 2; o > 0; o >>= 1) {
-        const uint64_t other = __shfl_xor((unsigned long long)key, o, kWave);
-        key = other > key ? other : key;
-    }
-    return key;
+__device__ __forceinline__ uint64_t read_lane(uint64_t key, int lane) {
+    const uint32_t high = (uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane), low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, lane);
+    return (uint64_t)high << 32 | low;
 }
 
-// A workgroup per row; the row is read for its maximum, for the sums and once for each alternative.
-template <class T>
-__global__ __launch_bounds__(kThreads) void token_stats_kernel(LogitRows in, StatArgs p) {
-    __shared__ float part[2][kWaves];
-    __shared__ uint64_t best[kWaves];
-    const int thread = (int)threadIdx.x;
-    const uint32_t vocab = (uint32_t)in.vocab;
-    for (int64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
-        const int32_t label = in.labels.ptr ? label_of(in, r) : 0;
-        if (label < 0) {
-            if (thread == 0) {
-                p.logp[r] = p.lse[r] = p.entropy[r] = 0.f;
-                if (p.sums) {
-                    p.sums[2 * r] = 0.f;
-                    p.sums[2 * r + 1] = -INFINITY;
-                }
-            }
-            if (thread < p.k) {
-                p.top_tokens[r * p.k + thread] = -1;
-                p.top_logp[r * p.k + thread] = 0.f;
-            }
-            continue;
+struct SelectShared {
+    uint64_t wait[2 * kWave], order[kWave];
+};
+
+// The best entries that a wavefront has met.  An entry can be among the k best if it is at least `bound` and its key above `limit`.
+struct Selection {
+    uint64_t mine = 0, limit = 0;                                  // the lane's entry, by rank; the k-th
+    float bound = -INFINITY;
+    int waiting = 0;
+
+    // The other's first n entries (by lane, in any order, all different from mine) into mine.
+    __device__ __forceinline__ void merge(uint64_t other, int n, int k, SelectShared &sh) {
+        int my_rank = lane_id(), other_rank = 0;
+        for (int i = 0; i < n; ++i) {
+            const uint64_t one = read_lane(other, i);
+            my_rank += one > mine ? 1 : 0;
+            other_rank += one > other ? 1 : 0;
+            const int before = (int)popc64(__ballot(mine > one));
+            other_rank += lane_id() == i ? before : 0;
         }
-        const T *x = static_cast<const T *>(in.x) + r * in.stride;
-        float top = -INFINITY;
-        for (uint32_t v = (uint32_t)thread; v < vocab; v += kThreads) top = fmaxf(top, (float)x[v]);
-        top = group_max<64>(top);
-        __syncthreads();
-        if (lane_id() == 0) part[0][wave_id()] = top;
-        __syncthreads();
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, part[0][w]);
-        RowStat st{fabsf(top) >= kLargeTop ? top : 0.5f * __builtin_rintf(top * kLog2E), 0.f};
-        if (top == -INFINITY) st.m = 0.f;
-        float s = 0.f, t = 0.f;
-        for (uint32_t v = (uint32_t)thread; v < vocab; v += kThreads) {
-            const float z = st.z((float)x[v]), e = __builtin_amdgcn_exp2f(z);
+        if (my_rank < kWave) sh.order[my_rank] = mine;
+        if (lane_id() < n && other_rank < kWave) sh.order[other_rank] = other;
+        mine = sh.order[lane_id()];
+        limit = read_lane(mine, k - 1);
+        if (limit != 0) bound = fmaxf(bound, value_of(limit));
+    }
+    // `has` lanes' entries.
+    __device__ __forceinline__ void offer(bool has, float x, uint32_t v, int k, SelectShared &sh) {
+        const uint64_t key = key_of(x, v);
+        const uint64_t lanes = __ballot(has && key > limit);
+        if (lanes == 0) return;
+        if (has && key > limit) sh.wait[waiting + (int)lanes_below(lanes)] = key;
+        waiting += (int)popc64(lanes);
+        if (waiting >= kWave) {
+            merge(sh.wait[lane_id()], kWave, k, sh);
+            waiting -= kWave;
+            const uint64_t rest = sh.wait[kWave + lane_id()];
+            sh.wait[lane_id()] = rest;
+        }
+    }
+    __device__ __forceinline__ void finish(int k, SelectShared &sh) {
+        if (waiting > 0) merge(lane_id() < waiting ? sh.wait[lane_id()] : 0, waiting, k, sh);
+        waiting = 0;
+    }
+    // Another wavefront's list.
+    __device__ __forceinline__ void join(uint64_t list, int k, SelectShared &sh) {
+        const int n = (int)popc64(__ballot(list > limit));
+        if (n > 0) merge(list, n, k, sh);
+    }
+    // The k-th largest of the lanes' maxima is a bound: k entries reach it.
+    __device__ __forceinline__ void raise(float most, int k) {
+        int reach = 0;
+#pragma unroll 8
+        for (int i = 0; i < kWave; ++i) reach += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(most), i)) >= most ? 1 : 0;
+        bound = fmaxf(bound, group_max<64>(reach >= k ? most : -INFINITY));
+    }
+};
+
+// ---------------------------------------------------------------- sums of a tile
+// M as RowStat holds it; s = 0: no entry above -inf.
+struct Record {
+    float m, s, t;
+};
+
+// M in base 2, exactly.
+__device__ __forceinline__ double base_of(float m) { return fabsf(m) >= kMostM / 2.f ? (double)m * (double)kLog2E : 2.0 * (double)m; }
+
+// r's sums beside an M of `base`, which is not below its own.
+__device__ __forceinline__ void rebase(const Record &r, double base, float &s, float &t) {
+    const float d = fmaxf((float)(base_of(r.m) - base), -1000.f), f = r.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(d);
+    s = f * r.s;
+    t = f * fmaf(d, r.s, r.t);
+}
+__device__ __forceinline__ Record joined(const Record &a, const Record &b) {
+    if (a.s == 0.f) return b;
+    if (b.s == 0.f) return a;
+    Record r{fmaxf(a.m, b.m), 0.f, 0.f};
+    const double base = base_of(r.m);
+    float sa, ta, sb, tb;
+    rebase(a, base, sa, ta);
+    rebase(b, base, sb, tb);
+    r.s = sa + sb;
+    r.t = ta + tb;
+    return r;
+}
+
+// Maxima by the instruction itself: fmaxf quiets its operands first, which doubles what a tile's maxima cost.  A NaN may come out or not; its row's
+// results are NaN by the sum.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float max2(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = max2(v, dpp_move<0xB1>(v));
+    v = max2(v, dpp_move<0x4E>(v));
+    v = max2(v, dpp_move<0x141>(v));
+    v = max2(v, dpp_move<0x140>(v));
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
+
+// The largest entry of a piece.
+template <class T>
+__device__ __forceinline__ float piece_max(Raw r) {
+    if constexpr (sizeof(T) == 4) {
+        return max3(max2(__uint_as_float(r[0]), __uint_as_float(r[1])), __uint_as_float(r[2]), __uint_as_float(r[3]));
+    } else if constexpr (std::is_same<T, __bf16>::value) {
+        float f[8];
+        unpack<T>(r, f);
+        return max3(max3(max3(max2(f[0], f[1]), f[2], f[3]), f[4], f[5]), f[6], f[7]);
+    } else {
+        uint32_t a, b;
+        asm("v_pk_max_f16 %0, %1, %2" : "=v"(a) : "v"(r[0]), "v"(r[1]));
+        asm("v_pk_max_f16 %0, %1, %2" : "=v"(b) : "v"(r[2]), "v"(r[3]));
+        asm("v_pk_max_f16 %0, %1, %2" : "=v"(a) : "v"(a), "v"(b));
+        typedef _Float16 H2 __attribute__((ext_vector_type(2)));
+        const H2 most = __builtin_bit_cast(H2, a);
+        return max2((float)most[0], (float)most[1]);
+    }
+}
+
+template <class T>
+struct TileOf {
+    static constexpr int N = Piece<T>::N;
+    Raw raw[kEach];
+    float edge;                                                    // an entry of the head or tail: of the row's first tile alone
+    bool edges;
+
+    __device__ __forceinline__ void load(const T *x, const Cut &c, int32_t tile) {
+        const int32_t lane = lane_id();
+        const int64_t base = (int64_t)tile * kTile;
+        const T *from = x + c.head + base * N;
+        const int32_t left = (int32_t)((int64_t)c.pieces - base);  // may be none: the last tile of a row, or a row of edges
+        if (left >= kTile) {
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) raw[u] = load_piece(from + (u * kWave + lane) * N);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                raw[u] = nothing<T>();
+                if (u * kWave + lane < left) raw[u] = load_piece(from + (u * kWave + lane) * N);
+            }
+        }
+        edges = tile == 0 && c.edges() > 0;
+        edge = edges && lane < c.edges() ? (float)x[c.edge<T>(lane)] : -INFINITY;
+    }
+
+    // GUARD: an entry of -inf (or one whose z is) takes no part in t.
+    template <bool LARGE, bool GUARD>
+    __device__ __forceinline__ void add(float m, float &s, float &t) const {
+        const auto one = [&](float x) {
+            const float z = LARGE ? (x - m) * kLog2E : fmaf(x, kLog2E, -2.f * m), e = __builtin_amdgcn_exp2f(z);
             s += e;
-            t = fmaf(e, fmaxf(z, kLowest), t);
+            t = fmaf(e, GUARD ? fmaxf(z, kLowest) : z, t);
+        };
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            float f[N];
+            unpack<T>(raw[u], f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) one(f[i]);
+        }
+        if (edges) one(edge);
+    }
+
+    __device__ __forceinline__ Record sums(float top) const {
+        Record r{fabsf(top) >= kLargeTop ? top : 0.5f * __builtin_rintf(top * kLog2E), 0.f, 0.f};
+        if (!(top > -INFINITY)) r.m = 0.f;
+        const bool large = fabsf(r.m) >= kMostM / 2.f;
+        if (large) add<true, true>(r.m, r.s, r.t);
+        else add<false, false>(r.m, r.s, r.t);
+        if (__ballot(r.t != r.t) != 0 && !large) {
+            r.s = r.t = 0.f;
+            add<false, true>(r.m, r.s, r.t);
+        }
+        r.s = group_sum<64>(r.s);
+        r.t = group_sum<64>(r.t);
+        return r;
+    }
+
+    __device__ __forceinline__ void select(const Cut &c, int32_t tile, const float (&most)[kEach], float lane_most, int k, Selection &best, SelectShared &sh) const {
+        const uint64_t some = __ballot(lane_most >= best.bound);
+        if (some == 0) return;
+        if ((int)popc64(some) >= k) best.raise(lane_most, k);
+        const int32_t first = tile * kTile + lane_id();
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            if (__ballot(most[u] >= best.bound) == 0) continue;
+            float f[N];
+            unpack<T>(raw[u], f);
+            const bool in = first + u * kWave < c.pieces;
+            const uint32_t v = (uint32_t)c.head + (uint32_t)(first + u * kWave) * N;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (__ballot(in && f[i] >= best.bound) != 0) best.offer(in && f[i] >= best.bound, f[i], v + i, k, sh);
+        }
+        if (edges) best.offer(lane_id() < c.edges() && edge >= best.bound, edge, (uint32_t)c.edge<T>(lane_id()), k, sh);
+    }
+};
+
+// A wavefront takes a slice: its sums, and its entries for the selection.
+template <class T>
+__device__ __forceinline__ Record take_slice(const T *x, const Cut &c, const Slices &cut, int32_t slice, int k, Selection &best, SelectShared &sh) {
+    Record sum{0.f, 0.f, 0.f};
+    for (int32_t i = 0; i < cut.tiles; ++i) {
+        const int32_t tile = slice * cut.tiles + i;
+        if (tile > 0 && (int64_t)tile * kTile >= c.pieces) break;  // a row that has one tile less than its length allows
+        TileOf<T> t;
+        t.load(x, c, tile);
+        float most[kEach], top = t.edge;
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            most[u] = piece_max<T>(t.raw[u]);
+            top = max2(top, most[u]);
+        }
+        const Record r = t.sums(wave_max(top));
+        sum = i == 0 ? r : joined(sum, r);
+        if (k > 0) t.select(c, tile, most, top, k, best, sh);
+    }
+    return sum;
+}
+
+// ---------------------------------------------------------------- a row's results
+struct RowOut {
+    RowStat st;
+    float entropy;
+    bool wrong;
+};
+
+// By one wavefront, from the records of all slices in LDS or memory.
+__device__ __forceinline__ RowOut row_out(const Record *records, int32_t count) {
+    float top = -INFINITY;
+    for (int32_t i = lane_id(); i < count; i += kWave) top = records[i].s != 0.f ? fmaxf(top, records[i].m) : top;
+    top = group_max<64>(top);
+    float s = 0.f, t = 0.f;
+    if (top > -INFINITY) {
+        const double base = base_of(top);
+        for (int32_t i = lane_id(); i < count; i += kWave) {
+            float more_s, more_t;
+            rebase(records[i], base, more_s, more_t);
+            s += more_s;
+            t += more_t;
         }
         s = group_sum<64>(s);
         t = group_sum<64>(t);
-        __syncthreads();
-        if (lane_id() == 0) {
-            part[0][wave_id()] = s;
-            part[1][wave_id()] = t;
-        }
-        __syncthreads();
-        s = t = 0.f;
-        for (int w = 0; w < kWaves; ++w) {
-            s += part[0][w];
-            t += part[1][w];
-        }
-        const bool wrong = s != s;
-        float entropy = 0.f;
-        if (s == 0.f) {
-            st.l = -INFINITY;
-        } else {
-            entropy = 0.69314718055994530942f * fmaxf(log2f(s) - t / s, 0.f);
-            if (wrong) entropy = s;
-            if (st.large()) st.l = log2f(s);
-            else st = stat_of(2.f * st.m, s);
-        }
-        if (thread == 0) {
-            if (p.logp) p.logp[r] = st.log_prob((float)x[label]);
-            p.lse[r] = st.lse();
-            p.entropy[r] = entropy;
-            if (p.sums) {
-                p.sums[2 * r] = st.m;
-                p.sums[2 * r + 1] = st.l;
-            }
-        }
-        uint64_t last = ~0ull;
-        for (int i = 0; i < p.k; ++i) {
-            uint64_t most = 0;
-            for (uint32_t v = (uint32_t)thread; v < vocab; v += kThreads) {
-                const uint64_t key = key_of((float)x[v], v);
-                if (key < last && key > most) most = key;
-            }
-            most = wave_max_key(most);
-            __syncthreads();
-            if (lane_id() == 0) best[wave_id()] = most;
-            __syncthreads();
-            for (int w = 0; w < kWaves; ++w) most = best[w] > most ? best[w] : most;
-            last = most;
-            if (thread == 0) {
-                p.top_tokens[r * p.k + i] = wrong ? -1 : token_of(most);
-                p.top_logp[r * p.k + i] = wrong ? s : st.log_prob(value_of(most));
-            }
+    }
+    RowOut r{{top, -INFINITY}, 0.f, !(s < INFINITY)};
+    if (r.wrong) {
+        r.st = {0.f, __int_as_float(0x7fc00000)};
+        r.entropy = __int_as_float(0x7fc00000);
+    } else if (s == 0.f) {
+        r.st.m = 0.f;
+    } else {
+        const float l = log2f(s);
+        r.entropy = 0.69314718055994530942f * fmaxf(l - t / s, 0.f);
+        if (r.st.large()) r.st.l = l;
+        else r.st = stat_of(2.f * top, s);
+    }
+    return r;
+}
+
+__device__ __forceinline__ void write_row(const StatArgs &p, int64_t r, const RowOut &out, float at_label, uint64_t key) {
+    const float nan = __int_as_float(0x7fc00000);
+    if (lane_id() == 0) {
+        if (p.logp) p.logp[r] = out.wrong ? nan : out.st.log_prob(at_label);
+        p.lse[r] = out.wrong ? nan : out.st.lse();
+        p.entropy[r] = out.entropy;
+        if (p.sums) {
+            p.sums[2 * r] = out.st.m;
+            p.sums[2 * r + 1] = out.st.l;
         }
     }
+    if (lane_id() < p.k) {
+        p.top_tokens[r * p.k + lane_id()] = out.wrong ? -1 : token_of(key);
+        p.top_logp[r * p.k + lane_id()] = out.wrong ? nan : out.st.log_prob(value_of(key));
+    }
 }
+__device__ __forceinline__ void write_ignored(const StatArgs &p, int64_t r) {
+    if (lane_id() == 0) {
+        if (p.logp) p.logp[r] = 0.f;
+        p.lse[r] = p.entropy[r] = 0.f;
+        if (p.sums) {
+            p.sums[2 * r] = 0.f;
+            p.sums[2 * r + 1] = -INFINITY;
+        }
+    }
+    if (lane_id() < p.k) {
+        p.top_tokens[r * p.k + lane_id()] = -1;
+        p.top_logp[r * p.k + lane_id()] = 0.f;
+    }
+}
+
+// Whether the row counts; its label's logit.
+template <class T>
+__device__ __forceinline__ bool row_counts(const LogitRows &in, int64_t r, float &at_label) {
+    at_label = 0.f;
+    if (!in.labels.ptr) return true;
+    const int32_t label = label_of(in, r);
+    if (label < 0) return false;
+    at_label = (float)(static_cast<const T *>(in.x) + r * in.stride)[label];
+    return true;
+}
+
+// ---------------------------------------------------------------- kernels
+// A wavefront per row.
+constexpr int kFewSlices = 4;
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void stats_short_kernel(LogitRows in, StatArgs p) {
+    __shared__ SelectShared select[kWaves];
+    __shared__ Record records[kWaves][kFewSlices];
+    const Slices cut = slices_of<T>((int32_t)in.vocab);
+    SelectShared &sh = select[wave_id()];
+    Record *mine = records[wave_id()];
+    for (int64_t r = (int64_t)blockIdx.x * kWaves + wave_id(); r < in.rows; r += (int64_t)gridDim.x * kWaves) {
+        float at_label;
+        if (!row_counts<T>(in, r, at_label)) {
+            write_ignored(p, r);
+            continue;
+        }
+        const T *x = static_cast<const T *>(in.x) + r * in.stride;
+        const Cut c = cut_row(x, (int32_t)in.vocab);
+        Selection best;
+        for (int32_t s = 0; s < cut.count; ++s) {
+            const Record record = take_slice<T>(x, c, cut, s, p.k, best, sh);
+            if (lane_id() == 0) mine[s] = record;
+        }
+        if (p.k > 0) best.finish(p.k, sh);
+        __builtin_amdgcn_wave_barrier();
+        write_row(p, r, row_out(mine, cut.count), at_label, best.mine);
+    }
+}
+
+// A workgroup per row, its wavefronts take the slices in turn.  The first wavefront joins what they found while the others begin the next row.
+template <class T>
+__global__ __launch_bounds__(kThreads) void stats_row_kernel(LogitRows in, StatArgs p) {
+    __shared__ SelectShared select[kWaves];
+    __shared__ Record records[2][kMostSlices];
+    __shared__ uint64_t lists[2][kWaves][kWave];
+    const Slices cut = slices_of<T>((int32_t)in.vocab);
+    SelectShared &sh = select[wave_id()];
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
+        float at_label;
+        if (!row_counts<T>(in, r, at_label)) {
+            if (wave_id() == 0) write_ignored(p, r);
+            continue;
+        }
+        const T *x = static_cast<const T *>(in.x) + r * in.stride;
+        const Cut c = cut_row(x, (int32_t)in.vocab);
+        Selection best;
+        for (int32_t s = wave_id(); s < cut.count; s += kWaves) {
+            const Record record = take_slice<T>(x, c, cut, s, p.k, best, sh);
+            if (lane_id() == 0) records[turn][s] = record;
+        }
+        if (p.k > 0) {
+            best.finish(p.k, sh);
+            lists[turn][wave_id()][lane_id()] = best.mine;
+        }
+        __syncthreads();
+        if (wave_id() == 0) {
+            if (p.k > 0)
+                for (int w = 1; w < kWaves; ++w) best.join(lists[turn][w][lane_id()], p.k, sh);
+            write_row(p, r, row_out(records[turn], cut.count), at_label, best.mine);
+        }
+        turn ^= 1;
+    }
+}
+
+// Few rows: a workgroup per part of a row, and a second launch that joins the parts.
+struct Parts {
+    int32_t slices, count;                                         // slices of a part, parts of a row
+    Record *records;                                               // [rows][slices of a row]
+    uint64_t *lists;                                               // [rows][parts][k]
+};
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void stats_part_kernel(LogitRows in, StatArgs p, Parts parts) {
+    __shared__ SelectShared select[kWaves];
+    __shared__ uint64_t lists[kWaves][kWave];
+    const Slices cut = slices_of<T>((int32_t)in.vocab);
+    SelectShared &sh = select[wave_id()];
+    const int64_t r = blockIdx.x / (uint32_t)parts.count;
+    const int32_t part = (int32_t)(blockIdx.x % (uint32_t)parts.count);
+    if (in.labels.ptr && label_of(in, r) < 0) return;
+    const T *x = static_cast<const T *>(in.x) + r * in.stride;
+    const Cut c = cut_row(x, (int32_t)in.vocab);
+    Selection best;
+    const int32_t end = min((part + 1) * parts.slices, cut.count);
+    for (int32_t s = part * parts.slices + wave_id(); s < end; s += kWaves) {
+        const Record record = take_slice<T>(x, c, cut, s, p.k, best, sh);
+        if (lane_id() == 0) parts.records[r * cut.count + s] = record;
+    }
+    if (p.k == 0) return;
+    best.finish(p.k, sh);
+    lists[wave_id()][lane_id()] = best.mine;
+    __syncthreads();
+    if (wave_id() != 0) return;
+    for (int w = 1; w < kWaves; ++w) best.join(lists[w][lane_id()], p.k, sh);
+    if (lane_id() < p.k) parts.lists[(r * parts.count + part) * p.k + lane_id()] = best.mine;
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void stats_join_kernel(LogitRows in, StatArgs p, Parts parts) {
+    __shared__ SelectShared select[kWaves];
+    __shared__ uint64_t lists[kWaves][kWave];
+    const Slices cut = slices_of<T>((int32_t)in.vocab);
+    SelectShared &sh = select[wave_id()];
+    const int64_t r = blockIdx.x;
+    float at_label;
+    if (!row_counts<T>(in, r, at_label)) {
+        if (wave_id() == 0) write_ignored(p, r);
+        return;
+    }
+    Selection best;
+    if (p.k > 0) {
+        for (int32_t i = wave_id(); i < parts.count; i += kWaves)
+            best.join(lane_id() < p.k ? parts.lists[(r * parts.count + i) * p.k + lane_id()] : 0, p.k, sh);
+        lists[wave_id()][lane_id()] = best.mine;
+        __syncthreads();
+    }
+    if (wave_id() != 0) return;
+    if (p.k > 0)
+        for (int w = 1; w < kWaves; ++w) best.join(lists[w][lane_id()], p.k, sh);
+    write_row(p, r, row_out(parts.records + r * cut.count, cut.count), at_label, best.mine);
+}
+
+// How a call is cut: parts.count = 1 without a second launch.
+constexpr int64_t kFewRows = 1024;
+template <class T>
+Parts parts_of(int64_t rows, int64_t vocab) {
+    const Slices cut = slices_of<T>((int32_t)vocab);
+    Parts parts{cut.count, 1, nullptr, nullptr};
+    if (rows >= kFewRows || cut.count <= kFewSlices) return parts;
+    const int64_t most = 2048 / (rows > 0 ? rows : 1);             // parts of a row
+    int64_t each = (cut.count + most - 1) / most;
+    each = (each + kWaves - 1) / kWaves * kWaves;
+    parts.slices = (int32_t)each;
+    parts.count = (int32_t)((cut.count + each - 1) / each);
+    return parts;
+}
+size_t up_to_256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // ---------------------------------------------------------------- gradient
 struct StatGrad {
@@ -158,13 +535,35 @@ __global__ __launch_bounds__(kThreads) void token_stats_grad_kernel(LogitRows in
 
 }  // namespace
 
-size_t stats_workspace_bytes(int, int64_t, int64_t, int32_t) { return 0; }
+size_t stats_workspace_bytes(int type, int64_t rows, int64_t vocab, int32_t k) {
+    size_t bytes = 0;
+    (void)with_type(type, [&](auto as) {
+        typedef typename ValueOf<decltype(as)::value>::type T;
+        const Parts parts = parts_of<T>(rows, vocab);
+        if (parts.count > 1)
+            bytes = up_to_256((size_t)rows * slices_of<T>((int32_t)vocab).count * sizeof(Record)) + (size_t)rows * parts.count * k * sizeof(uint64_t);
+        return hipSuccess;
+    });
+    return bytes;
+}
 
-hipError_t launch_token_stats(const LogitRows &in, const StatArgs &p, void *, hipStream_t stream) {
+hipError_t launch_token_stats(const LogitRows &in, const StatArgs &p, void *workspace, hipStream_t stream) {
     if (in.rows == 0) return hipSuccess;
     return with_type(in.type, [&](auto type) {
         typedef typename ValueOf<decltype(type)::value>::type T;
-        hipLaunchKernelGGL(token_stats_kernel<T>, dim3(grid_of(in.rows, 1, kThreads)), dim3(kThreads), 0, stream, in, p);
+        const Slices cut = slices_of<T>((int32_t)in.vocab);
+        Parts parts = parts_of<T>(in.rows, in.vocab);
+        if (parts.count > 1) {
+            parts.records = static_cast<Record *>(workspace);
+            parts.lists = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + up_to_256((size_t)in.rows * cut.count * sizeof(Record)));
+            hipLaunchKernelGGL(stats_part_kernel<T>, dim3((unsigned)(in.rows * parts.count)), dim3(kThreads), 0, stream, in, p, parts);
+            if (hipError_t st = hipGetLastError()) return st;
+            hipLaunchKernelGGL(stats_join_kernel<T>, dim3((unsigned)in.rows), dim3(kThreads), 0, stream, in, p, parts);
+        } else if (cut.count <= kFewSlices) {
+            hipLaunchKernelGGL(stats_short_kernel<T>, dim3(grid_of(in.rows, kWaves, kThreads)), dim3(kThreads), 0, stream, in, p);
+        } else {
+            hipLaunchKernelGGL(stats_row_kernel<T>, dim3(grid_of(in.rows, 1, kThreads)), dim3(kThreads), 0, stream, in, p);
+        }
         return hipGetLastError();
     });
 }
