@@ -500,35 +500,142 @@ Parts parts_of(int64_t rows, int64_t vocab) {
 size_t up_to_256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // ---------------------------------------------------------------- gradient
+// With y = log2 p:  a ([v = label] - p) - b p (y ln 2 + entropy) = [v = label] a - p (slope y + level).  Where p is zero y is -inf, or far below; from
+// -200 on p is zero without it.
 struct StatGrad {
-    RowStat st;
-    float a, b, h;                                                 // d logp, d entropy, entropy
-    int32_t label;
-    __device__ float entry(int32_t v, float x) const {
-        // log2 p; where p is zero the product with p has to be, too
-        const float y = fmaxf(st.z(x) - st.l, -200.f), p = __builtin_amdgcn_exp2f(y);
-        const float mixed = p * (b * fmaf(y, 0.69314718055994530942f, h));
-        return v == label ? a * (1.f - p) - mixed : -(a * p) - mixed;
+    float m, l, slope, level, a;                                   // m: what z subtracts
+    int32_t label;                                                 // none: no entry's number
+    bool large;
+    __device__ __forceinline__ StatGrad(const RowStat &st, float a_, float b, float h, int32_t label_)
+        : m(st.large() ? st.m : 2.f * st.m), l(st.l), slope(b * 0.69314718055994530942f), level(fmaf(b, h, a_)), a(a_), label(label_), large(st.large()) {}
+    template <bool LARGE>
+    __device__ __forceinline__ float of(float x) const {
+        const float y = fmaxf((LARGE ? (x - m) * kLog2E : fmaf(x, kLog2E, -m)) - l, -200.f);
+        return -(__builtin_amdgcn_exp2f(y) * fmaf(slope, y, level));
+    }
+    // A piece in which the label is entry `at`, if at < N.
+    template <int N>
+    __device__ __forceinline__ void piece(uint32_t at, float (&f)[N]) const {
+        if (large) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = of<true>(f[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = of<false>(f[i]);
+        }
+        if (at < (uint32_t)N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] += (int)at == i ? a : 0.f;
+        }
+    }
+    __device__ __forceinline__ float entry(int32_t v, float x) const {
+        float f[1] = {x};
+        piece((uint32_t)label - (uint32_t)v, f);
+        return f[0];
     }
 };
 
+// Pieces first, first + step, ... (EACH of them) of a row and, where `edges`, an entry of its head or tail for each thread.
+template <class T, bool ADD, int EACH>
+struct GradPieces {
+    static constexpr int N = Piece<T>::N;
+    typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));
+    Raw x[EACH], old[EACH];
+    __device__ __forceinline__ void load(const T *from, const T *to, const Cut &c, int32_t first, int32_t step) {
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            const int32_t i = first + u * step;
+            if (i >= c.pieces) continue;
+            x[u] = load_piece(from + c.head + i * N);
+            if constexpr (ADD) old[u] = Raw(__builtin_nontemporal_load(reinterpret_cast<const Loose *>(to + c.head + i * N)));
+        }
+    }
+    __device__ __forceinline__ void store(T *to, const Cut &c, int32_t first, int32_t step, const StatGrad &d) const {
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            const int32_t i = first + u * step;
+            if (i >= c.pieces) continue;
+            const int32_t v = c.head + i * N;
+            float f[N];
+            unpack<T>(x[u], f);
+            d.piece((uint32_t)d.label - (uint32_t)v, f);
+            if constexpr (ADD) {
+                float more[N];
+                unpack<T>(old[u], more);
+#pragma unroll
+                for (int k = 0; k < N; ++k) f[k] += more[k];
+            }
+            store_piece(to + v, f);
+        }
+    }
+};
+
+// In place of a label where there are none: no entry's number, nor within a piece of one.
+constexpr int32_t kNoLabel = -(1 << 30);
+
+// What a row's gradient is of; false: a row of zeros, or one that is left as it is.
 template <class T>
-__global__ __launch_bounds__(kThreads) void token_stats_grad_kernel(LogitRows in, StatGradArgs p, LogitGrad out) {
-    const uint32_t vocab = (uint32_t)in.vocab;
-    for (int64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
-        const int32_t label = in.labels.ptr ? label_of(in, r) : -1;
+__device__ __forceinline__ bool row_grad(const LogitRows &in, const StatGradArgs &p, int64_t r, StatGrad &d) {
+    const int32_t label = in.labels.ptr ? label_of(in, r) : kNoLabel;
+    const RowStat st{p.sums[2 * r], p.sums[2 * r + 1]};
+    d = StatGrad(st, p.grad_logp ? p.grad_logp[r] : 0.f, p.grad_entropy ? p.grad_entropy[r] : 0.f, p.entropy[r], label);
+    return label != -1 && !st.empty();
+}
+
+// A wavefront per row of up to 512 pieces.
+template <class T, bool ADD>
+__global__ __launch_bounds__(kThreads) void stats_grad_short_kernel(LogitRows in, StatGradArgs p, LogitGrad out) {
+    const int32_t vocab = (int32_t)in.vocab, lane = lane_id();
+    for (int64_t r = (int64_t)blockIdx.x * kWaves + wave_id(); r < in.rows; r += (int64_t)gridDim.x * kWaves) {
         const T *x = static_cast<const T *>(in.x) + r * in.stride;
         T *g = static_cast<T *>(out.ptr) + r * out.stride;
-        const RowStat st{p.sums[2 * r], p.sums[2 * r + 1]};
-        if ((in.labels.ptr && label < 0) || st.empty()) {
-            if (!p.accumulate)
-                for (uint32_t v = threadIdx.x; v < vocab; v += kThreads) g[v] = (T)0.f;
+        StatGrad d(RowStat{0.f, 0.f}, 0.f, 0.f, 0.f, 0);
+        if (!row_grad<T>(in, p, r, d)) {
+            if constexpr (!ADD) zero_row<T, kWave>(g, vocab, lane);
             continue;
         }
-        const StatGrad d{st, p.grad_logp ? p.grad_logp[r] : 0.f, p.grad_entropy ? p.grad_entropy[r] : 0.f, p.entropy[r], label};
-        for (uint32_t v = threadIdx.x; v < vocab; v += kThreads) {
-            const float e = d.entry((int32_t)v, (float)x[v]);
-            g[v] = stored<T>(p.accumulate ? (float)g[v] + e : e);
+        const Cut c = cut_row(x, vocab);
+        for (int32_t i = lane; i - lane < c.pieces; i += 4 * kWave) {
+            GradPieces<T, ADD, 4> t;
+            t.load(x, g, c, i, kWave);
+            t.store(g, c, i, kWave, d);
+        }
+        if (lane < c.edges()) {
+            const int32_t v = c.edge<T>(lane);
+            const float e = d.entry(v, (float)x[v]);
+            g[v] = stored<T>(ADD ? (float)g[v] + e : e);
+        }
+    }
+}
+
+// Longer rows in the tiles of token_rows.h, bound by memory.
+template <class T, bool ADD>
+__global__ __launch_bounds__(kGradThreads) void stats_grad_kernel(LogitRows in, StatGradArgs p, LogitGrad out, int32_t tiles) {
+    const int32_t vocab = (int32_t)in.vocab;
+    for (int64_t w = blockIdx.x; w < in.rows * tiles; w += gridDim.x) {
+        const int64_t r = w / tiles;
+        const int32_t tile = (int32_t)(w % tiles), first = tile * kGradPieces + (int32_t)threadIdx.x;
+        const T *x = static_cast<const T *>(in.x) + r * in.stride;
+        T *g = static_cast<T *>(out.ptr) + r * out.stride;
+        StatGrad d(RowStat{0.f, 0.f}, 0.f, 0.f, 0.f, 0);
+        if (!row_grad<T>(in, p, r, d)) {
+            if constexpr (!ADD) {
+                GradTile<T> t;
+                t.load(x, g, vocab, false, tile);
+                t.zero(g);
+            }
+            continue;
+        }
+        const Cut c = cut_row(x, vocab);
+        GradPieces<T, ADD, kGradFlight> t;
+        t.load(x, g, c, first, kGradThreads);
+        const bool edge = tile == 0 && (int32_t)threadIdx.x < c.edges();
+        const int32_t v = edge ? c.edge<T>((int32_t)threadIdx.x) : 0;
+        const float x_edge = edge ? (float)x[v] : 0.f;
+        t.store(g, c, first, kGradThreads, d);
+        if (edge) {
+            const float e = d.entry(v, x_edge);
+            g[v] = stored<T>(ADD ? (float)g[v] + e : e);
         }
     }
 }
@@ -572,8 +679,17 @@ hipError_t launch_token_stats_grad(const LogitRows &in, const StatGradArgs &p, c
     if (in.rows == 0) return hipSuccess;
     return with_type(in.type, [&](auto type) {
         typedef typename ValueOf<decltype(type)::value>::type T;
-        hipLaunchKernelGGL(token_stats_grad_kernel<T>, dim3(grid_of(in.rows, 1, kThreads)), dim3(kThreads), 0, stream, in, p, out);
-        return hipGetLastError();
+        const auto launch = [&](auto add) {
+            constexpr bool ADD = decltype(add)::value;
+            if (in.vocab <= kTile * Piece<T>::N) {
+                hipLaunchKernelGGL((stats_grad_short_kernel<T, ADD>), dim3(grid_of(in.rows, kWaves, kThreads)), dim3(kThreads), 0, stream, in, p, out);
+            } else {
+                const int32_t tiles = grad_tiles<T>(in.vocab);
+                hipLaunchKernelGGL((stats_grad_kernel<T, ADD>), dim3(grid_of(in.rows * tiles, 1, kGradThreads)), dim3(kGradThreads), 0, stream, in, p, out, tiles);
+            }
+            return hipGetLastError();
+        };
+        return p.accumulate ? launch(std::true_type()) : launch(std::false_type());
     });
 }
 
