@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kEach = 8, kTile = kEach * kWave;                    // pieces of a lane, of a tile
+constexpr int kEachShort = 2;                                      // of rows that have no more in all
 constexpr int kMostSlices = 256;
 
 // Tiles of a row and how they are grouped: into at most 256 slices, each a wavefront's at a time.
@@ -23,7 +24,10 @@ struct Slices {
     int32_t count, tiles;                                          // slices, tiles of each
 };
 template <class T>
+constexpr bool is_short(int64_t vocab) { return vocab / Piece<T>::N < kEachShort * kWave; }
+template <class T>
 __host__ __device__ __forceinline__ Slices slices_of(int32_t vocab) {
+    if (is_short<T>(vocab)) return {1, 1};
     const int32_t tiles = vocab / (Piece<T>::N * kTile) + 1;       // whether a row of so many has one piece more or less
     const int32_t each = (tiles + kMostSlices - 1) / kMostSlices;
     return {(tiles + each - 1) / each, each};
@@ -47,8 +51,65 @@ __device__ __forceinline__ uint64_t read_lane(uint64_t key, int lane) {
     return (uint64_t)high << 32 | low;
 }
 
+// The key of the lane whose number differs in the bits of MASK.
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_key(uint64_t key) {
+    const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(key >> 32), CTRL, 0xf, 0xf, true);
+    const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)key, CTRL, 0xf, 0xf, true);
+    return (uint64_t)high << 32 | low;
+}
+template <int MASK>
+__device__ __forceinline__ uint64_t other_key(uint64_t key) {
+    if constexpr (MASK == 1) return dpp_key<0xB1>(key);                // quad_perm [1,0,3,2]
+    else if constexpr (MASK == 2) return dpp_key<0x4E>(key);           // quad_perm [2,3,0,1]
+    else if constexpr (MASK == 3) return dpp_key<0x1B>(key);           // quad_perm [3,2,1,0]
+    else if constexpr (MASK == 7) return dpp_key<0x141>(key);          // row_half_mirror
+    else if constexpr (MASK == 15) return dpp_key<0x140>(key);         // row_mirror
+    else return __shfl_xor((unsigned long long)key, MASK, kWave);
+}
+// The larger of two lanes' keys goes to the lane with the smaller number.
+template <int MASK>
+__device__ __forceinline__ void exchange(uint64_t &key) {
+    constexpr int kHighest = MASK >= 32 ? 32 : MASK >= 16 ? 16 : MASK >= 8 ? 8 : MASK >= 4 ? 4 : MASK >= 2 ? 2 : 1;
+    const uint64_t other = other_key<MASK>(key);
+    if ((key < other) == ((lane_id() & kHighest) == 0)) key = other;
+}
+// Of two halves in descending order, the second from its end, one in descending order; and 64 keys in any order.
+__device__ __forceinline__ void order_halves(uint64_t &key) {
+    exchange<32>(key);
+    exchange<16>(key);
+    exchange<8>(key);
+    exchange<4>(key);
+    exchange<2>(key);
+    exchange<1>(key);
+}
+__device__ __forceinline__ void order_keys(uint64_t &key) {
+    exchange<1>(key);
+    exchange<3>(key);
+    exchange<1>(key);
+    exchange<7>(key);
+    exchange<2>(key);
+    exchange<1>(key);
+    exchange<15>(key);
+    exchange<4>(key);
+    exchange<2>(key);
+    exchange<1>(key);
+    exchange<31>(key);
+    exchange<8>(key);
+    exchange<4>(key);
+    exchange<2>(key);
+    exchange<1>(key);
+    exchange<63>(key);
+    exchange<16>(key);
+    exchange<8>(key);
+    exchange<4>(key);
+    exchange<2>(key);
+    exchange<1>(key);
+}
+
 struct SelectShared {
-    uint64_t wait[2 * kWave], order[kWave];
+    uint64_t wait[2 * kWave];
+    uint32_t piece[kWave][4], token[kWave];                        // token: of a piece's first entry
 };
 
 // The best entries that a wavefront has met.  An entry can be among the k best if it is at least `bound` and its key above `limit`.
@@ -57,51 +118,37 @@ struct Selection {
     float bound = -INFINITY;
     int waiting = 0;
 
-    // The other's first n entries (by lane, in any order, all different from mine) into mine.
-    __device__ __forceinline__ void merge(uint64_t other, int n, int k, SelectShared &sh) {
-        int my_rank = lane_id(), other_rank = 0;
-        for (int i = 0; i < n; ++i) {
-            const uint64_t one = read_lane(other, i);
-            my_rank += one > mine ? 1 : 0;
-            other_rank += one > other ? 1 : 0;
-            const int before = (int)popc64(__ballot(mine > one));
-            other_rank += lane_id() == i ? before : 0;
-        }
-        if (my_rank < kWave) sh.order[my_rank] = mine;
-        if (lane_id() < n && other_rank < kWave) sh.order[other_rank] = other;
-        mine = sh.order[lane_id()];
+    // Other entries in descending order, zeros last.
+    __device__ __forceinline__ void merge_ordered(uint64_t other, int k) {
+        const uint64_t turned = other_key<63>(other);              // the 64 best of both: the better of the first and the last, the second and the last but one, ...
+        if (turned > mine) mine = turned;
+        order_halves(mine);
         limit = read_lane(mine, k - 1);
         if (limit != 0) bound = fmaxf(bound, value_of(limit));
     }
     // `has` lanes' entries.
     __device__ __forceinline__ void offer(bool has, float x, uint32_t v, int k, SelectShared &sh) {
         const uint64_t key = key_of(x, v);
-        const uint64_t lanes = __ballot(has && key > limit);
-        if (lanes == 0) return;
-        if (has && key > limit) sh.wait[waiting + (int)lanes_below(lanes)] = key;
+        has = has && key > limit;
+        const uint64_t lanes = __ballot(has);
+        if (has) sh.wait[waiting + (int)lanes_below(lanes)] = key;
         waiting += (int)popc64(lanes);
-        if (waiting >= kWave) {
-            merge(sh.wait[lane_id()], kWave, k, sh);
-            waiting -= kWave;
-            const uint64_t rest = sh.wait[kWave + lane_id()];
-            sh.wait[lane_id()] = rest;
-        }
+        if (waiting >= kWave) take_waiting(kWave, k, sh);
+    }
+    __device__ __forceinline__ void take_waiting(int n, int k, SelectShared &sh) {
+        uint64_t other = lane_id() < n ? sh.wait[lane_id()] : 0;
+        order_keys(other);
+        merge_ordered(other, k);
+        waiting -= n;
+        const uint64_t rest = sh.wait[kWave + lane_id()];
+        sh.wait[lane_id()] = rest;
     }
     __device__ __forceinline__ void finish(int k, SelectShared &sh) {
-        if (waiting > 0) merge(lane_id() < waiting ? sh.wait[lane_id()] : 0, waiting, k, sh);
-        waiting = 0;
+        if (waiting > 0) take_waiting(waiting, k, sh);
     }
     // Another wavefront's list.
-    __device__ __forceinline__ void join(uint64_t list, int k, SelectShared &sh) {
-        const int n = (int)popc64(__ballot(list > limit));
-        if (n > 0) merge(list, n, k, sh);
-    }
-    // The k-th largest of the lanes' maxima is a bound: k entries reach it.
-    __device__ __forceinline__ void raise(float most, int k) {
-        int reach = 0;
-#pragma unroll 8
-        for (int i = 0; i < kWave; ++i) reach += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(most), i)) >= most ? 1 : 0;
-        bound = fmaxf(bound, group_max<64>(reach >= k ? most : -INFINITY));
+    __device__ __forceinline__ void join(uint64_t list, int k) {
+        if (__ballot(list > limit) != 0) merge_ordered(list, k);
     }
 };
 
@@ -177,24 +224,36 @@ __device__ __forceinline__ float piece_max(Raw r) {
     }
 }
 
+// Entry number `entry` of a piece from the word that holds it.
 template <class T>
+__device__ __forceinline__ float entry_of(uint32_t word, int entry) {
+    if constexpr (sizeof(T) == 4) {
+        return __uint_as_float(word);
+    } else {
+        const uint16_t half = (uint16_t)(entry & 1 ? word >> 16 : word);
+        return (float)__builtin_bit_cast(T, half);
+    }
+}
+
+template <class T, int EACH>
 struct TileOf {
     static constexpr int N = Piece<T>::N;
-    Raw raw[kEach];
+    Raw raw[EACH];
     float edge;                                                    // an entry of the head or tail: of the row's first tile alone
     bool edges;
+    int32_t left;                                                  // pieces from the tile's first on; may be none: a row of edges
 
     __device__ __forceinline__ void load(const T *x, const Cut &c, int32_t tile) {
         const int32_t lane = lane_id();
-        const int64_t base = (int64_t)tile * kTile;
+        const int64_t base = (int64_t)tile * (EACH * kWave);
         const T *from = x + c.head + base * N;
-        const int32_t left = (int32_t)((int64_t)c.pieces - base);  // may be none: the last tile of a row, or a row of edges
-        if (left >= kTile) {
+        left = (int32_t)((int64_t)c.pieces - base);
+        if (left >= EACH * kWave) {
 #pragma unroll
-            for (int u = 0; u < kEach; ++u) raw[u] = load_piece(from + (u * kWave + lane) * N);
+            for (int u = 0; u < EACH; ++u) raw[u] = load_piece(from + (u * kWave + lane) * N);
         } else {
 #pragma unroll
-            for (int u = 0; u < kEach; ++u) {
+            for (int u = 0; u < EACH; ++u) {
                 raw[u] = nothing<T>();
                 if (u * kWave + lane < left) raw[u] = load_piece(from + (u * kWave + lane) * N);
             }
@@ -203,77 +262,142 @@ struct TileOf {
         edge = edges && lane < c.edges() ? (float)x[c.edge<T>(lane)] : -INFINITY;
     }
 
-    // GUARD: an entry of -inf (or one whose z is) takes no part in t.
-    template <bool LARGE, bool GUARD>
-    __device__ __forceinline__ void add(float m, float &s, float &t) const {
-        const auto one = [&](float x) {
-            const float z = LARGE ? (x - m) * kLog2E : fmaf(x, kLog2E, -2.f * m), e = __builtin_amdgcn_exp2f(z);
-            s += e;
-            t = fmaf(e, GUARD ? fmaxf(z, kLowest) : z, t);
-        };
+    // The pieces' largest entries, and the lane's.
+    __device__ __forceinline__ float maxima(float (&most)[EACH]) const {
+        float top = edge;
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) {
+        for (int u = 0; u < EACH; ++u) {
+            most[u] = piece_max<T>(raw[u]);
+            top = max2(top, most[u]);
+        }
+        return top;
+    }
+
+    // An entry of -inf takes no part in t: 2^-200 is zero, and so is its product.  The pieces are unpacked anew: left to itself the compiler keeps what the
+    // maxima have unpacked, in 64 registers.
+    __device__ __forceinline__ void add(Record &r) {
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            asm("" : "+v"(raw[u]));
             float f[N];
             unpack<T>(raw[u], f);
 #pragma unroll
-            for (int i = 0; i < N; ++i) one(f[i]);
+            for (int i = 0; i < N; ++i) add_one(fmaf(f[i], kLog2E, -2.f * r.m), r);
         }
-        if (edges) one(edge);
+        if (edges) add_one(fmaf(edge, kLog2E, -2.f * r.m), r);
+    }
+    static __device__ __forceinline__ void add_one(float z, Record &r) {
+        const float e = __builtin_amdgcn_exp2f(z);
+        r.s += e;
+        r.t = fmaf(e, max2(z, -200.f), r.t);
     }
 
-    __device__ __forceinline__ Record sums(float top) const {
-        Record r{fabsf(top) >= kLargeTop ? top : 0.5f * __builtin_rintf(top * kLog2E), 0.f, 0.f};
-        if (!(top > -INFINITY)) r.m = 0.f;
-        const bool large = fabsf(r.m) >= kMostM / 2.f;
-        if (large) add<true, true>(r.m, r.s, r.t);
-        else add<false, false>(r.m, r.s, r.t);
-        if (__ballot(r.t != r.t) != 0 && !large) {
-            r.s = r.t = 0.f;
-            add<false, true>(r.m, r.s, r.t);
+    __device__ __forceinline__ Record sums(const T *x, const Cut &c, int32_t tile, float top) {
+        Record r{0.f, 0.f, 0.f};
+        if (fabsf(top) < kLargeTop || top == -INFINITY) {
+            r.m = top == -INFINITY ? 0.f : 0.5f * __builtin_rintf(top * kLog2E);
+            add(r);
+        } else if (!(top < INFINITY)) {                            // +inf or NaN
+            r.s = r.t = __int_as_float(0x7fc00000);
+        } else {                                                   // large: again from memory, piece by piece
+            r.m = top;
+            const T *from = x + c.head + (int64_t)tile * (EACH * kWave) * N;
+#pragma unroll 1
+            for (int32_t i = lane_id(); i < min(left, EACH * kWave); i += kWave) {
+                float f[N];
+                unpack<T>(load_piece(from + i * N), f);
+#pragma unroll
+                for (int j = 0; j < N; ++j) add_one((f[j] - top) * kLog2E, r);
+            }
+            if (edges) add_one((edge - top) * kLog2E, r);
         }
         r.s = group_sum<64>(r.s);
         r.t = group_sum<64>(r.t);
         return r;
     }
 
-    __device__ __forceinline__ void select(const Cut &c, int32_t tile, const float (&most)[kEach], float lane_most, int k, Selection &best, SelectShared &sh) const {
-        const uint64_t some = __ballot(lane_most >= best.bound);
-        if (some == 0) return;
-        if ((int)popc64(some) >= k) best.raise(lane_most, k);
-        const int32_t first = tile * kTile + lane_id();
+    // Piece u of the lane, which is a register's number only where it is a constant.
+    template <int W>
+    __device__ __forceinline__ void pick(int u, const float (&most)[EACH], float &most_u, Raw &piece) const {
+        if (W == 0 || u == W) {
+            most_u = most[W];
+            piece = raw[W];
+        }
+        if constexpr (W + 1 < EACH) pick<W + 1>(u, most, most_u, piece);
+    }
+
+    // most: the pieces' largest entries.  Pieces that have an entry to offer go to LDS, and from there entry by entry to the lanes.
+    __device__ __forceinline__ void select(const Cut &c, int32_t tile, const float (&most)[EACH], float lane_most, float top, int k, Selection &best,
+                                           SelectShared &sh) const {
+        if (__ballot(lane_most >= best.bound) == 0) return;
+        const auto reach = [&](float bound) {
+            int n = 0;
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) {
-            if (__ballot(most[u] >= best.bound) == 0) continue;
-            float f[N];
-            unpack<T>(raw[u], f);
-            const bool in = first + u * kWave < c.pieces;
-            const uint32_t v = (uint32_t)c.head + (uint32_t)(first + u * kWave) * N;
+            for (int u = 0; u < EACH; ++u) n += (int)popc64(__ballot(most[u] >= bound));
+            return n;
+        };
+        const int enough = k + k / 4;
+        if (reach(best.bound) > enough) {
+            // As many pieces reach the tile's bound as there are alternatives, or a few more: halve the way to the largest entry until it is so.  (From
+            // a bound that k pieces reach, k entries do; equal entries may end it early, and so may a way that cannot be halved.)
+            float high = top, step = 8.f;
+            for (int i = 0; i < 16; ++i) {
+                const float middle = best.bound > -INFINITY ? 0.5f * best.bound + 0.5f * high : high - step;
+                if (!(middle > best.bound && middle < high)) break;
+                const int n = reach(middle);
+                if (n >= k) best.bound = middle;
+                else high = middle;
+                if (n >= k && n <= enough) break;
+                step *= 4.f;
+            }
+        }
+        const int32_t first = tile * (EACH * kWave) + lane_id();
+        int staged = 0;
+        for (int u = 0; u < EACH;) {
+            float most_u;
+            Raw piece;
+            pick<0>(u, most, most_u, piece);
+            const bool has = most_u >= best.bound && first + u * kWave < c.pieces;
+            const uint64_t lanes = __ballot(has);
+            const int n = (int)popc64(lanes);
+            if (staged + n <= kWave) {
+                if (has) {
+                    const int at = staged + (int)lanes_below(lanes);
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (__ballot(in && f[i] >= best.bound) != 0) best.offer(in && f[i] >= best.bound, f[i], v + i, k, sh);
+                    for (int i = 0; i < 4; ++i) sh.piece[at][i] = piece[i];
+                    sh.token[at] = (uint32_t)c.head + (uint32_t)(first + u * kWave) * N;
+                }
+                staged += n;
+                ++u;
+                if (u < EACH) continue;
+            }
+            for (int at = 0; at < staged; at += kWave / N) {
+                const int from = at + lane_id() / N, entry = lane_id() % N;
+                const bool in = from < staged;
+                const float x = in ? entry_of<T>(sh.piece[from][entry * (int)sizeof(T) / 4], entry) : 0.f;
+                best.offer(in && x >= best.bound, x, in ? sh.token[from] + entry : 0u, k, sh);
+            }
+            staged = 0;
         }
         if (edges) best.offer(lane_id() < c.edges() && edge >= best.bound, edge, (uint32_t)c.edge<T>(lane_id()), k, sh);
     }
 };
 
 // A wavefront takes a slice: its sums, and its entries for the selection.
-template <class T>
+template <class T, int EACH, bool SELECT>
 __device__ __forceinline__ Record take_slice(const T *x, const Cut &c, const Slices &cut, int32_t slice, int k, Selection &best, SelectShared &sh) {
     Record sum{0.f, 0.f, 0.f};
     for (int32_t i = 0; i < cut.tiles; ++i) {
         const int32_t tile = slice * cut.tiles + i;
-        if (tile > 0 && (int64_t)tile * kTile >= c.pieces) break;  // a row that has one tile less than its length allows
-        TileOf<T> t;
+        if (tile > 0 && (int64_t)tile * (EACH * kWave) >= c.pieces) break;  // a row that has one tile less than its length allows
+        TileOf<T, EACH> t;
         t.load(x, c, tile);
-        float most[kEach], top = t.edge;
-#pragma unroll
-        for (int u = 0; u < kEach; ++u) {
-            most[u] = piece_max<T>(t.raw[u]);
-            top = max2(top, most[u]);
-        }
-        const Record r = t.sums(wave_max(top));
-        sum = i == 0 ? r : joined(sum, r);
-        if (k > 0) t.select(c, tile, most, top, k, best, sh);
+        float most[EACH];
+        const float top = t.maxima(most);
+        const float highest = wave_max(top);
+        const Record r = t.sums(x, c, tile, highest);
+        sum = joined(sum, r);
+        if constexpr (SELECT) t.select(c, tile, most, top, highest, k, best, sh);
     }
     return sum;
 }
@@ -360,66 +484,44 @@ __device__ __forceinline__ bool row_counts(const LogitRows &in, int64_t r, float
 }
 
 // ---------------------------------------------------------------- kernels
-// A wavefront per row.
-constexpr int kFewSlices = 4;
+constexpr int kToSimd = 4;                                         // wavefronts that the registers are shared out among
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void stats_short_kernel(LogitRows in, StatArgs p) {
-    __shared__ SelectShared select[kWaves];
-    __shared__ Record records[kWaves][kFewSlices];
+// A team of WAVES wavefronts per row, which take the slices in turn; the first joins what they found while the others begin the next row.  Teams of one
+// share a workgroup of four.
+template <class T, int EACH, int WAVES, bool SELECT>
+__global__ __launch_bounds__(Team<WAVES>::kBlock, kToSimd) void stats_row_kernel(LogitRows in, StatArgs p) {
+    typedef Team<WAVES> G;
+    constexpr int kTurns = WAVES == 1 ? 1 : 2;
+    __shared__ SelectShared select[G::kBlock / kWave];
+    __shared__ Record shared_records[kTurns * G::kPerBlock][EACH == kEach ? kMostSlices : 1];
+    __shared__ uint64_t lists[kTurns][WAVES][WAVES == 1 ? 1 : kWave];
     const Slices cut = slices_of<T>((int32_t)in.vocab);
     SelectShared &sh = select[wave_id()];
-    Record *mine = records[wave_id()];
-    for (int64_t r = (int64_t)blockIdx.x * kWaves + wave_id(); r < in.rows; r += (int64_t)gridDim.x * kWaves) {
-        float at_label;
-        if (!row_counts<T>(in, r, at_label)) {
-            write_ignored(p, r);
-            continue;
-        }
-        const T *x = static_cast<const T *>(in.x) + r * in.stride;
-        const Cut c = cut_row(x, (int32_t)in.vocab);
-        Selection best;
-        for (int32_t s = 0; s < cut.count; ++s) {
-            const Record record = take_slice<T>(x, c, cut, s, p.k, best, sh);
-            if (lane_id() == 0) mine[s] = record;
-        }
-        if (p.k > 0) best.finish(p.k, sh);
-        __builtin_amdgcn_wave_barrier();
-        write_row(p, r, row_out(mine, cut.count), at_label, best.mine);
-    }
-}
-
-// A workgroup per row, its wavefronts take the slices in turn.  The first wavefront joins what they found while the others begin the next row.
-template <class T>
-__global__ __launch_bounds__(kThreads) void stats_row_kernel(LogitRows in, StatArgs p) {
-    __shared__ SelectShared select[kWaves];
-    __shared__ Record records[2][kMostSlices];
-    __shared__ uint64_t lists[2][kWaves][kWave];
-    const Slices cut = slices_of<T>((int32_t)in.vocab);
-    SelectShared &sh = select[wave_id()];
+    const int member = WAVES == 1 ? 0 : wave_id();
     int turn = 0;
-    for (int64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
+    for (int64_t r = G::first(); r < in.rows; r += G::step()) {
         float at_label;
         if (!row_counts<T>(in, r, at_label)) {
-            if (wave_id() == 0) write_ignored(p, r);
+            if (member == 0) write_ignored(p, r);
             continue;
         }
         const T *x = static_cast<const T *>(in.x) + r * in.stride;
         const Cut c = cut_row(x, (int32_t)in.vocab);
+        Record *records = shared_records[WAVES == 1 ? G::which() : turn];
         Selection best;
-        for (int32_t s = wave_id(); s < cut.count; s += kWaves) {
-            const Record record = take_slice<T>(x, c, cut, s, p.k, best, sh);
-            if (lane_id() == 0) records[turn][s] = record;
+        for (int32_t s = member; s < cut.count; s += WAVES) {
+            const Record record = take_slice<T, EACH, SELECT>(x, c, cut, s, p.k, best, sh);
+            if (lane_id() == 0) records[s] = record;
         }
-        if (p.k > 0) {
-            best.finish(p.k, sh);
-            lists[turn][wave_id()][lane_id()] = best.mine;
+        if (SELECT) best.finish(p.k, sh);
+        if constexpr (WAVES > 1) {
+            if (SELECT) lists[turn][member][lane_id()] = best.mine;
+            __syncthreads();
         }
-        __syncthreads();
-        if (wave_id() == 0) {
-            if (p.k > 0)
-                for (int w = 1; w < kWaves; ++w) best.join(lists[turn][w][lane_id()], p.k, sh);
-            write_row(p, r, row_out(records[turn], cut.count), at_label, best.mine);
+        if (member == 0) {
+            if (WAVES > 1 && SELECT)
+                for (int w = 1; w < WAVES; ++w) best.join(lists[turn][w][lane_id()], p.k);
+            write_row(p, r, row_out(records, cut.count), at_label, best.mine);
         }
         turn ^= 1;
     }
@@ -432,8 +534,8 @@ struct Parts {
     uint64_t *lists;                                               // [rows][parts][k]
 };
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void stats_part_kernel(LogitRows in, StatArgs p, Parts parts) {
+template <class T, bool SELECT>
+__global__ __launch_bounds__(kThreads, kToSimd) void stats_part_kernel(LogitRows in, StatArgs p, Parts parts) {
     __shared__ SelectShared select[kWaves];
     __shared__ uint64_t lists[kWaves][kWave];
     const Slices cut = slices_of<T>((int32_t)in.vocab);
@@ -446,24 +548,22 @@ __global__ __launch_bounds__(kThreads) void stats_part_kernel(LogitRows in, Stat
     Selection best;
     const int32_t end = min((part + 1) * parts.slices, cut.count);
     for (int32_t s = part * parts.slices + wave_id(); s < end; s += kWaves) {
-        const Record record = take_slice<T>(x, c, cut, s, p.k, best, sh);
+        const Record record = take_slice<T, kEach, SELECT>(x, c, cut, s, p.k, best, sh);
         if (lane_id() == 0) parts.records[r * cut.count + s] = record;
     }
-    if (p.k == 0) return;
+    if constexpr (!SELECT) return;
     best.finish(p.k, sh);
     lists[wave_id()][lane_id()] = best.mine;
     __syncthreads();
     if (wave_id() != 0) return;
-    for (int w = 1; w < kWaves; ++w) best.join(lists[w][lane_id()], p.k, sh);
+    for (int w = 1; w < kWaves; ++w) best.join(lists[w][lane_id()], p.k);
     if (lane_id() < p.k) parts.lists[(r * parts.count + part) * p.k + lane_id()] = best.mine;
 }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void stats_join_kernel(LogitRows in, StatArgs p, Parts parts) {
-    __shared__ SelectShared select[kWaves];
     __shared__ uint64_t lists[kWaves][kWave];
     const Slices cut = slices_of<T>((int32_t)in.vocab);
-    SelectShared &sh = select[wave_id()];
     const int64_t r = blockIdx.x;
     float at_label;
     if (!row_counts<T>(in, r, at_label)) {
@@ -473,18 +573,20 @@ __global__ __launch_bounds__(kThreads) void stats_join_kernel(LogitRows in, Stat
     Selection best;
     if (p.k > 0) {
         for (int32_t i = wave_id(); i < parts.count; i += kWaves)
-            best.join(lane_id() < p.k ? parts.lists[(r * parts.count + i) * p.k + lane_id()] : 0, p.k, sh);
+            best.join(lane_id() < p.k ? parts.lists[(r * parts.count + i) * p.k + lane_id()] : 0, p.k);
         lists[wave_id()][lane_id()] = best.mine;
         __syncthreads();
     }
     if (wave_id() != 0) return;
     if (p.k > 0)
-        for (int w = 1; w < kWaves; ++w) best.join(lists[w][lane_id()], p.k, sh);
+        for (int w = 1; w < kWaves; ++w) best.join(lists[w][lane_id()], p.k);
     write_row(p, r, row_out(parts.records + r * cut.count, cut.count), at_label, best.mine);
 }
 
 // How a call is cut: parts.count = 1 without a second launch.
 constexpr int64_t kFewRows = 1024;
+constexpr int32_t kFewSlices = 4;
+constexpr int64_t kRowsForOne = 4096;
 template <class T>
 Parts parts_of(int64_t rows, int64_t vocab) {
     const Slices cut = slices_of<T>((int32_t)vocab);
@@ -660,18 +762,28 @@ hipError_t launch_token_stats(const LogitRows &in, const StatArgs &p, void *work
         typedef typename ValueOf<decltype(type)::value>::type T;
         const Slices cut = slices_of<T>((int32_t)in.vocab);
         Parts parts = parts_of<T>(in.rows, in.vocab);
-        if (parts.count > 1) {
-            parts.records = static_cast<Record *>(workspace);
-            parts.lists = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + up_to_256((size_t)in.rows * cut.count * sizeof(Record)));
-            hipLaunchKernelGGL(stats_part_kernel<T>, dim3((unsigned)(in.rows * parts.count)), dim3(kThreads), 0, stream, in, p, parts);
-            if (hipError_t st = hipGetLastError()) return st;
-            hipLaunchKernelGGL(stats_join_kernel<T>, dim3((unsigned)in.rows), dim3(kThreads), 0, stream, in, p, parts);
-        } else if (cut.count <= kFewSlices) {
-            hipLaunchKernelGGL(stats_short_kernel<T>, dim3(grid_of(in.rows, kWaves, kThreads)), dim3(kThreads), 0, stream, in, p);
-        } else {
-            hipLaunchKernelGGL(stats_row_kernel<T>, dim3(grid_of(in.rows, 1, kThreads)), dim3(kThreads), 0, stream, in, p);
-        }
-        return hipGetLastError();
+        const auto launch = [&](auto select) {
+            constexpr bool SELECT = decltype(select)::value;
+            if (parts.count > 1) {
+                parts.records = static_cast<Record *>(workspace);
+                parts.lists = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + up_to_256((size_t)in.rows * cut.count * sizeof(Record)));
+                hipLaunchKernelGGL((stats_part_kernel<T, SELECT>), dim3((unsigned)(in.rows * parts.count)), dim3(kThreads), 0, stream, in, p, parts);
+                if (hipError_t st = hipGetLastError()) return st;
+                hipLaunchKernelGGL(stats_join_kernel<T>, dim3((unsigned)in.rows), dim3(kThreads), 0, stream, in, p, parts);
+                return hipGetLastError();
+            }
+            const auto rows = [&](auto each, auto waves) {
+                typedef Team<decltype(waves)::value> G;
+                hipLaunchKernelGGL((stats_row_kernel<T, decltype(each)::value, decltype(waves)::value, SELECT>), dim3(grid_of(in.rows, G::kPerBlock, G::kBlock)), dim3(G::kBlock), 0,
+                                   stream, in, p);
+                return hipGetLastError();
+            };
+            const std::integral_constant<int, kEach> each;
+            if (is_short<T>(in.vocab)) return rows(std::integral_constant<int, kEachShort>(), std::integral_constant<int, 1>());
+            if (cut.count <= kFewSlices || (SELECT && in.rows >= kRowsForOne)) return rows(each, std::integral_constant<int, 1>());
+            return rows(each, std::integral_constant<int, SELECT ? 2 : 4>());
+        };
+        return p.k > 0 ? launch(std::true_type()) : launch(std::false_type());
     });
 }
 

@@ -216,6 +216,22 @@ def test_gradient_against_differences(gpu):
         assert abs((f(up) - f(down)) / 2e-5 - grad[r, v]) < 1e-5
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [3, 700, 9000])
+def test_rows_of_nan(gpu, vocab, dtype):
+    """NaN everywhere, of both kinds (a signalling one comes out of some instructions where a quiet one does not), and one beside numbers."""
+    torch, b = gpu
+    whole = {"f32": (torch.int32, 0x7F800001), "bf16": (torch.int16, 0x7F81), "f16": (torch.int16, 0x7C01)}[dtype]
+    x = torch.randn(4, vocab, device="cuda").to(lm.TORCH[dtype])
+    x[0] = math.nan
+    x[1:3].view(whole[0])[0] = whole[1]
+    x[2:3].view(whole[0])[0, vocab // 2] = whole[1]
+    st = b.ef21_token_stats(x, torch.zeros(4, dtype=torch.int64, device="cuda"), 2, sums=True)
+    for r in range(3):
+        assert all(bool(torch.isnan(t[r]).all()) for t in (st.logp, st.lse, st.entropy, st.top_logp)) and bool((st.top_tokens[r] == -1).all())
+    check(torch, b.TokenStats(st.logp[3:], st.lse[3:], st.entropy[3:], st.top_tokens[3:], st.top_logp[3:], None), ref.Stats(as64(x[3:]), np.array([0])), 2)
+
+
 def test_nothing_to_do_and_rows_that_are_all_ignored(gpu):
     torch, b = gpu
     x = torch.empty(0, 50, device="cuda")
