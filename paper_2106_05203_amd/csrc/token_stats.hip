@@ -58,21 +58,52 @@ __device__ __forceinline__ uint64_t dpp_key(uint64_t key) {
     const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)key, CTRL, 0xf, 0xf, true);
     return (uint64_t)high << 32 | low;
 }
+// Both lanes' words of lanes 16 or 32 apart, which of the two is whose left open.
+template <int MASK>
+__device__ __forceinline__ void swap_words(uint32_t word, uint32_t &a, uint32_t &b) {
+    static_assert(MASK == 16 || MASK == 32, "");
+    const auto r = MASK == 16 ? __builtin_amdgcn_permlane16_swap(word, word, false, false) : __builtin_amdgcn_permlane32_swap(word, word, false, false);
+    a = r[0];
+    b = r[1];
+}
+template <int MASK>
+__device__ __forceinline__ void both_keys(uint64_t key, uint64_t &a, uint64_t &b) {
+    uint32_t ah, bh, al, bl;
+    swap_words<MASK>((uint32_t)(key >> 32), ah, bh);
+    swap_words<MASK>((uint32_t)key, al, bl);
+    a = (uint64_t)ah << 32 | al;
+    b = (uint64_t)bh << 32 | bl;
+}
 template <int MASK>
 __device__ __forceinline__ uint64_t other_key(uint64_t key) {
     if constexpr (MASK == 1) return dpp_key<0xB1>(key);                // quad_perm [1,0,3,2]
     else if constexpr (MASK == 2) return dpp_key<0x4E>(key);           // quad_perm [2,3,0,1]
     else if constexpr (MASK == 3) return dpp_key<0x1B>(key);           // quad_perm [3,2,1,0]
+    else if constexpr (MASK == 4) return dpp_key<0x1B>(dpp_key<0x141>(key));
     else if constexpr (MASK == 7) return dpp_key<0x141>(key);          // row_half_mirror
+    else if constexpr (MASK == 8) return dpp_key<0x128>(key);          // row_ror:8
     else if constexpr (MASK == 15) return dpp_key<0x140>(key);         // row_mirror
-    else return __shfl_xor((unsigned long long)key, MASK, kWave);
+    else if constexpr (MASK == 31) return dpp_key<0x140>(other_key<16>(key));
+    else if constexpr (MASK == 63) return other_key<31>(other_key<32>(key));
+    else {                                                             // of the two the one that is not mine; mine if both are alike
+        uint64_t a, b;
+        both_keys<MASK>(key, a, b);
+        return a == key ? b : a;
+    }
 }
 // The larger of two lanes' keys goes to the lane with the smaller number.
 template <int MASK>
 __device__ __forceinline__ void exchange(uint64_t &key) {
     constexpr int kHighest = MASK >= 32 ? 32 : MASK >= 16 ? 16 : MASK >= 8 ? 8 : MASK >= 4 ? 4 : MASK >= 2 ? 2 : 1;
-    const uint64_t other = other_key<MASK>(key);
-    if ((key < other) == ((lane_id() & kHighest) == 0)) key = other;
+    const bool upper = (lane_id() & kHighest) != 0;
+    if constexpr (MASK == 16 || MASK == 32) {
+        uint64_t a, b;
+        both_keys<MASK>(key, a, b);
+        key = (a > b) != upper ? a : b;
+    } else {
+        const uint64_t other = other_key<MASK>(key);
+        if ((key < other) != upper) key = other;
+    }
 }
 // Of two halves in descending order, the second from its end, one in descending order; and 64 keys in any order.
 __device__ __forceinline__ void order_halves(uint64_t &key) {
@@ -495,6 +526,8 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, kToSimd) void stats_row_kernel
     __shared__ SelectShared select[G::kBlock / kWave];
     __shared__ Record shared_records[kTurns * G::kPerBlock][EACH == kEach ? kMostSlices : 1];
     __shared__ uint64_t lists[kTurns][WAVES][WAVES == 1 ? 1 : kWave];
+    __shared__ RowOut shared_out[kTurns];                          // by the last wavefront where the others take some time to join their lists
+    constexpr bool kApart = SELECT && WAVES > 4;
     const Slices cut = slices_of<T>((int32_t)in.vocab);
     SelectShared &sh = select[wave_id()];
     const int member = WAVES == 1 ? 0 : wave_id();
@@ -518,10 +551,25 @@ __global__ __launch_bounds__(Team<WAVES>::kBlock, kToSimd) void stats_row_kernel
             if (SELECT) lists[turn][member][lane_id()] = best.mine;
             __syncthreads();
         }
+        constexpr int kLast = WAVES > 4 ? 2 : WAVES;               // lists that the first wavefront joins alone
+        if constexpr (SELECT) {
+            if (kApart && member == WAVES - 1) {
+                const RowOut out = row_out(records, cut.count);
+                if (lane_id() == 0) shared_out[turn] = out;
+            }
+            for (int half = WAVES / 2; half >= kLast; half /= 2) {
+                if (member < half) {
+                    best.join(lists[turn][member + half][lane_id()], p.k);
+                    lists[turn][member][lane_id()] = best.mine;
+                }
+                __syncthreads();
+            }
+        }
         if (member == 0) {
-            if (WAVES > 1 && SELECT)
-                for (int w = 1; w < WAVES; ++w) best.join(lists[turn][w][lane_id()], p.k);
-            write_row(p, r, row_out(records, cut.count), at_label, best.mine);
+            if (SELECT)
+                for (int w = 1; w < kLast; ++w) best.join(lists[turn][w][lane_id()], p.k);
+            if constexpr (kApart) write_row(p, r, shared_out[turn], at_label, best.mine);
+            else write_row(p, r, row_out(records, cut.count), at_label, best.mine);
         }
         turn ^= 1;
     }
@@ -560,10 +608,13 @@ __global__ __launch_bounds__(kThreads, kToSimd) void stats_part_kernel(LogitRows
     if (lane_id() < p.k) parts.lists[(r * parts.count + part) * p.k + lane_id()] = best.mine;
 }
 
+// A workgroup per row: the last wavefront takes the sums while the others join the lists.
 template <class T>
 __global__ __launch_bounds__(kThreads) void stats_join_kernel(LogitRows in, StatArgs p, Parts parts) {
-    __shared__ uint64_t lists[kWaves][kWave];
-    const Slices cut = slices_of<T>((int32_t)in.vocab);
+    constexpr int kJoining = kWaves - 1;
+    __shared__ uint64_t lists[kJoining][kWave];
+    __shared__ RowOut out;
+    const int32_t slices = slices_of<T>((int32_t)in.vocab).count;
     const int64_t r = blockIdx.x;
     float at_label;
     if (!row_counts<T>(in, r, at_label)) {
@@ -571,27 +622,33 @@ __global__ __launch_bounds__(kThreads) void stats_join_kernel(LogitRows in, Stat
         return;
     }
     Selection best;
-    if (p.k > 0) {
-        for (int32_t i = wave_id(); i < parts.count; i += kWaves)
+    if (wave_id() == kJoining) {
+        const RowOut sums = row_out(parts.records + r * slices, slices);
+        if (lane_id() == 0) out = sums;
+    } else if (p.k > 0) {
+        for (int32_t i = wave_id(); i < parts.count; i += kJoining)
             best.join(lane_id() < p.k ? parts.lists[(r * parts.count + i) * p.k + lane_id()] : 0, p.k);
         lists[wave_id()][lane_id()] = best.mine;
-        __syncthreads();
     }
+    __syncthreads();
     if (wave_id() != 0) return;
     if (p.k > 0)
-        for (int w = 1; w < kWaves; ++w) best.join(lists[w][lane_id()], p.k);
-    write_row(p, r, row_out(parts.records + r * cut.count, cut.count), at_label, best.mine);
+        for (int w = 1; w < kJoining; ++w) best.join(lists[w][lane_id()], p.k);
+    write_row(p, r, out, at_label, best.mine);
 }
 
-// How a call is cut: parts.count = 1 without a second launch.
-constexpr int64_t kFewRows = 1024;
-constexpr int32_t kFewSlices = 4;
-constexpr int64_t kRowsForOne = 4096;
+// How a call is cut.  parts.count = 1: without a second launch, `waves` wavefronts to a row.
+constexpr int64_t kWavesInAll = 4096;
+inline int waves_of(int64_t rows, int32_t slices, bool select) {
+    int waves = select ? 1 : 4;
+    while (waves < 16 && rows * waves * 2 <= kWavesInAll && waves < slices) waves *= 2;
+    return waves;
+}
 template <class T>
 Parts parts_of(int64_t rows, int64_t vocab) {
     const Slices cut = slices_of<T>((int32_t)vocab);
     Parts parts{cut.count, 1, nullptr, nullptr};
-    if (rows >= kFewRows || cut.count <= kFewSlices) return parts;
+    if (cut.count <= 16 || rows * 16 >= kWavesInAll) return parts;
     const int64_t most = 2048 / (rows > 0 ? rows : 1);             // parts of a row
     int64_t each = (cut.count + most - 1) / most;
     each = (each + kWaves - 1) / kWaves * kWaves;
@@ -780,8 +837,13 @@ hipError_t launch_token_stats(const LogitRows &in, const StatArgs &p, void *work
             };
             const std::integral_constant<int, kEach> each;
             if (is_short<T>(in.vocab)) return rows(std::integral_constant<int, kEachShort>(), std::integral_constant<int, 1>());
-            if (cut.count <= kFewSlices || (SELECT && in.rows >= kRowsForOne)) return rows(each, std::integral_constant<int, 1>());
-            return rows(each, std::integral_constant<int, SELECT ? 2 : 4>());
+            switch (waves_of(in.rows, cut.count, SELECT)) {
+                case 1: return rows(each, std::integral_constant<int, 1>());
+                case 2: return rows(each, std::integral_constant<int, 2>());
+                case 4: return rows(each, std::integral_constant<int, 4>());
+                case 8: return rows(each, std::integral_constant<int, 8>());
+                default: return rows(each, std::integral_constant<int, 16>());
+            }
         };
         return p.k > 0 ? launch(std::true_type()) : launch(std::false_type());
     });
