@@ -361,10 +361,17 @@ struct TileOf {
     __device__ __forceinline__ void select(const Cut &c, int32_t tile, const float (&most)[EACH], float lane_most, float top, int k, Selection &best,
                                            SelectShared &sh) const {
         if (__ballot(lane_most >= best.bound) == 0) return;
+        // pieces that reach a bound; flags: which of the lanes' pieces there are any among
+        uint32_t flags = 0;
         const auto reach = [&](float bound) {
             int n = 0;
+            flags = 0;
 #pragma unroll
-            for (int u = 0; u < EACH; ++u) n += (int)popc64(__ballot(most[u] >= bound));
+            for (int u = 0; u < EACH; ++u) {
+                const uint64_t lanes = __ballot(most[u] >= bound);
+                n += (int)popc64(lanes);
+                flags |= lanes != 0 ? 1u << u : 0u;
+            }
             return n;
         };
         const int enough = k + k / 4;
@@ -381,10 +388,12 @@ struct TileOf {
                 if (n >= k && n <= enough) break;
                 step *= 4.f;
             }
+            reach(best.bound);
         }
         const int32_t first = tile * (EACH * kWave) + lane_id();
         int staged = 0;
-        for (int u = 0; u < EACH;) {
+        while (flags != 0) {
+            const int u = __builtin_ctz(flags);
             float most_u;
             Raw piece;
             pick<0>(u, most, most_u, piece);
@@ -399,8 +408,8 @@ struct TileOf {
                     sh.token[at] = (uint32_t)c.head + (uint32_t)(first + u * kWave) * N;
                 }
                 staged += n;
-                ++u;
-                if (u < EACH) continue;
+                flags &= flags - 1;
+                if (flags != 0) continue;
             }
             for (int at = 0; at < staged; at += kWave / N) {
                 const int from = at + lane_id() / N, entry = lane_id() % N;
