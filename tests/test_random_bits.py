@@ -1,4 +1,4 @@
-"""The random bits that stochastic rounding takes (tests/stats_reference.py writes the kernel's out; test_gpu_adamw.py holds the kernel to them)."""
+"""The random bits that stochastic rounding takes (tests/stats_reference.py writes the kernel's out; test_gpu_optimizer.py holds the kernel to them)."""
 import numpy as np
 
 import stats_reference as ref
