@@ -45,6 +45,8 @@ __device__ __forceinline__ float value_of(uint64_t key) {
     return __uint_as_float(order ^ ((int32_t)order < 0 ? 0x80000000u : 0xffffffffu));
 }
 __device__ __forceinline__ int32_t token_of(uint64_t key) { return (int32_t)(0xffffffffu - (uint32_t)key); }
+// The next value above a key's.
+__device__ __forceinline__ float value_above(uint64_t key) { return value_of(key + ((uint64_t)1 << 32)); }
 
 __device__ __forceinline__ uint64_t read_lane(uint64_t key, int lane) {
     const uint32_t high = (uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane), low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, lane);
@@ -156,6 +158,11 @@ struct Selection {
         order_halves(mine);
         limit = read_lane(mine, k - 1);
         if (limit != 0) bound = fmaxf(bound, value_of(limit));
+    }
+    // What an entry of a tile from token `first` on has to be: above the k-th if that is a token in front.  (Where most entries are masked, or many alike,
+    // they are not looked at again in each tile.)
+    __device__ __forceinline__ float bound_from(uint32_t first) const {
+        return limit != 0 && (uint32_t)token_of(limit) < first ? fmaxf(bound, value_above(limit)) : bound;
     }
     // `has` lanes' entries.
     __device__ __forceinline__ void offer(bool has, float x, uint32_t v, int k, SelectShared &sh) {
@@ -360,35 +367,41 @@ struct TileOf {
     // most: the pieces' largest entries.  Pieces that have an entry to offer go to LDS, and from there entry by entry to the lanes.
     __device__ __forceinline__ void select(const Cut &c, int32_t tile, const float (&most)[EACH], float lane_most, float top, int k, Selection &best,
                                            SelectShared &sh) const {
-        if (__ballot(lane_most >= best.bound) == 0) return;
+        float bound = best.bound_from((uint32_t)c.head + (uint32_t)(tile * (EACH * kWave)) * N);
+        if (__ballot(lane_most >= bound) == 0) return;
         // pieces that reach a bound; flags: which of the lanes' pieces there are any among
         uint32_t flags = 0;
-        const auto reach = [&](float bound) {
+        const auto reach = [&](float least) {
             int n = 0;
             flags = 0;
 #pragma unroll
             for (int u = 0; u < EACH; ++u) {
-                const uint64_t lanes = __ballot(most[u] >= bound);
+                const uint64_t lanes = __ballot(most[u] >= least);
                 n += (int)popc64(lanes);
                 flags |= lanes != 0 ? 1u << u : 0u;
             }
             return n;
         };
         const int enough = k + k / 4;
-        if (reach(best.bound) > enough) {
-            // As many pieces reach the tile's bound as there are alternatives, or a few more: halve the way to the largest entry until it is so.  (From
-            // a bound that k pieces reach, k entries do; equal entries may end it early, and so may a way that cannot be halved.)
+        if (reach(bound) > enough) {
+            // As many pieces reach the tile's bound as there are alternatives, or a few more: halve the way to the largest entry, or from 8 below
+            // it, until it is so.  (From a bound that k pieces reach, k entries do; equal entries may end it early, and so may a way that cannot
+            // be halved.)
             float high = top, step = 8.f;
             for (int i = 0; i < 16; ++i) {
-                const float middle = best.bound > -INFINITY ? 0.5f * best.bound + 0.5f * high : high - step;
-                if (!(middle > best.bound && middle < high)) break;
+                const float middle = fmaxf(0.5f * bound + 0.5f * high, top - step);
+                if (!(middle > bound && middle < high)) break;
                 const int n = reach(middle);
-                if (n >= k) best.bound = middle;
-                else high = middle;
-                if (n >= k && n <= enough) break;
-                step *= 4.f;
+                if (n >= k) {
+                    bound = middle;
+                    if (n <= enough) break;
+                } else {
+                    high = middle;
+                    step *= 4.f;
+                }
             }
-            reach(best.bound);
+            best.bound = fmaxf(best.bound, bound);
+            reach(bound);
         }
         const int32_t first = tile * (EACH * kWave) + lane_id();
         int staged = 0;
@@ -397,7 +410,7 @@ struct TileOf {
             float most_u;
             Raw piece;
             pick<0>(u, most, most_u, piece);
-            const bool has = most_u >= best.bound && first + u * kWave < c.pieces;
+            const bool has = most_u >= bound && first + u * kWave < c.pieces;
             const uint64_t lanes = __ballot(has);
             const int n = (int)popc64(lanes);
             if (staged + n <= kWave) {
@@ -415,7 +428,7 @@ struct TileOf {
                 const int from = at + lane_id() / N, entry = lane_id() % N;
                 const bool in = from < staged;
                 const float x = in ? entry_of<T>(sh.piece[from][entry * (int)sizeof(T) / 4], entry) : 0.f;
-                best.offer(in && x >= best.bound, x, in ? sh.token[from] + entry : 0u, k, sh);
+                best.offer(in && x >= bound, x, in ? sh.token[from] + entry : 0u, k, sh);
             }
             staged = 0;
         }

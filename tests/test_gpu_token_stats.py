@@ -152,14 +152,15 @@ def test_large_logits(gpu, offset, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("order", ["up", "down", "sawtooth", "ties", "late", "blocks"])
+@pytest.mark.parametrize("order", ["up", "down", "sawtooth", "ties", "late", "blocks", "masked", "few", "alike"])
 @pytest.mark.parametrize("rows,vocab", [(2, 50001), (300, 20003)])
 def test_orders_that_are_hard_to_select_from(gpu, rows, vocab, order, dtype):
     torch, b = gpu
     print(f"order {order} rows={rows} vocab={vocab} {dtype}", flush=True)
     v = np.arange(vocab)
     row = {"up": v / vocab * 20, "down": -v / vocab * 20, "sawtooth": (v % 4096) / 4096 * 20, "ties": (v * 7919 % 13).astype(float),
-           "late": np.where(v >= vocab - 70, 3.0 + (v % 9), -5.0 + (v % 3)), "blocks": ((v // 8) % 64 == 3) * 4.0 + (v // 512 % 3)}[order]
+           "late": np.where(v >= vocab - 70, 3.0 + (v % 9), -5.0 + (v % 3)), "blocks": ((v // 8) % 64 == 3) * 4.0 + (v // 512 % 3),
+           "masked": np.where(v * 7919 % 997 < 3, (v % 31) / 4, -np.inf), "few": np.where(v % 9973 == 5, v / vocab, -np.inf), "alike": np.full(vocab, -3.25)}[order]
     x = torch.from_numpy(np.tile(row, (rows, 1)).astype(np.float32)).to(lm.TORCH[dtype])
     x = torch.roll(x, 1, 1) if rows > 2 else x
     R = ref.Stats(x.double().numpy()[:2])
