@@ -140,6 +140,12 @@ __device__ __forceinline__ void order_keys(uint64_t &key) {
     exchange<1>(key);
 }
 
+// An entry inserted takes some 20 instructions, 64 ordered and merged 350; but the bound then rises at once, and fewer entries are met.  4096 rows of 131072 bf16
+// with 20 alternatives: 203 us so (keys of up to 3 lanes inserted 207, of 10 207), 205 where they wait across the tiles until there are 64; with 64 alternatives
+// 235 and 222.
+constexpr uint32_t kFewKeys = 6;
+constexpr int kFewBest = 32;
+
 struct SelectShared {
     uint64_t wait[2 * kWave];
     uint32_t piece[kWave][4], token[kWave];                        // token: of a piece's first entry
@@ -164,11 +170,27 @@ struct Selection {
     __device__ __forceinline__ float bound_from(uint32_t first) const {
         return limit != 0 && (uint32_t)token_of(limit) < first ? fmaxf(bound, value_above(limit)) : bound;
     }
-    // `has` lanes' entries.
+    // One entry, the same in all lanes, above limit.
+    __device__ __forceinline__ void insert(uint64_t key, int k) {
+        const uint64_t before = dpp_key<0x138>(mine);              // wave_shr:1, the lane in front's
+        const bool behind = mine < key, first = behind && !(lane_id() > 0 && before < key);
+        mine = first ? key : behind ? before : mine;
+        limit = read_lane(mine, k - 1);
+    }
+    // `has` lanes' entries: one after the other where they are few, or else to wait until there are 64, or the tile is done.
     __device__ __forceinline__ void offer(bool has, float x, uint32_t v, int k, SelectShared &sh) {
         const uint64_t key = key_of(x, v);
         has = has && key > limit;
-        const uint64_t lanes = __ballot(has);
+        uint64_t lanes = __ballot(has);
+        if (k <= kFewBest && waiting == 0 && popc64(lanes) <= kFewKeys) {
+            while (lanes != 0) {
+                const uint64_t one = read_lane(key, __builtin_ctzll(lanes));
+                if (one > limit) insert(one, k);
+                lanes &= lanes - 1;
+            }
+            if (limit != 0) bound = fmaxf(bound, value_of(limit));
+            return;
+        }
         if (has) sh.wait[waiting + (int)lanes_below(lanes)] = key;
         waiting += (int)popc64(lanes);
         if (waiting >= kWave) take_waiting(kWave, k, sh);
@@ -354,36 +376,20 @@ struct TileOf {
         return r;
     }
 
-    // Piece u of the lane, which is a register's number only where it is a constant.
-    template <int W>
-    __device__ __forceinline__ void pick(int u, const float (&most)[EACH], float &most_u, Raw &piece) const {
-        if (W == 0 || u == W) {
-            most_u = most[W];
-            piece = raw[W];
-        }
-        if constexpr (W + 1 < EACH) pick<W + 1>(u, most, most_u, piece);
-    }
-
     // most: the pieces' largest entries.  Pieces that have an entry to offer go to LDS, and from there entry by entry to the lanes.
     __device__ __forceinline__ void select(const Cut &c, int32_t tile, const float (&most)[EACH], float lane_most, float top, int k, Selection &best,
                                            SelectShared &sh) const {
         float bound = best.bound_from((uint32_t)c.head + (uint32_t)(tile * (EACH * kWave)) * N);
-        if (__ballot(lane_most >= bound) == 0) return;
-        // pieces that reach a bound; flags: which of the lanes' pieces there are any among
-        uint32_t flags = 0;
+        const uint64_t some = __ballot(lane_most >= bound);
+        if (some == 0) return;
         const auto reach = [&](float least) {
             int n = 0;
-            flags = 0;
 #pragma unroll
-            for (int u = 0; u < EACH; ++u) {
-                const uint64_t lanes = __ballot(most[u] >= least);
-                n += (int)popc64(lanes);
-                flags |= lanes != 0 ? 1u << u : 0u;
-            }
+            for (int u = 0; u < EACH; ++u) n += (int)popc64(__ballot(most[u] >= least));
             return n;
         };
         const int enough = k + k / 4;
-        if (reach(bound) > enough) {
+        if ((int)popc64(some) > k / 2 && reach(bound) > enough) {
             // As many pieces reach the tile's bound as there are alternatives, or a few more: halve the way to the largest entry, or from 8 below
             // it, until it is so.  (From a bound that k pieces reach, k entries do; equal entries may end it early, and so may a way that cannot
             // be halved.)
@@ -401,28 +407,26 @@ struct TileOf {
                 }
             }
             best.bound = fmaxf(best.bound, bound);
-            reach(bound);
         }
         const int32_t first = tile * (EACH * kWave) + lane_id();
-        int staged = 0;
-        while (flags != 0) {
-            const int u = __builtin_ctz(flags);
-            float most_u;
-            Raw piece;
-            pick<0>(u, most, most_u, piece);
-            const bool has = most_u >= bound && first + u * kWave < c.pieces;
-            const uint64_t lanes = __ballot(has);
-            const int n = (int)popc64(lanes);
-            if (staged + n <= kWave) {
+        uint32_t flags = (1u << EACH) - 1u;                        // which of the lanes' pieces are still to be looked at
+        do {
+            int staged = 0;
+#pragma unroll
+            for (int u = 0; u < EACH; ++u) {
+                const bool has = most[u] >= bound && first + u * kWave < c.pieces;
+                const uint64_t lanes = __ballot(has);
+                const int n = (int)popc64(lanes);
+                if ((flags >> u & 1u) == 0 || staged + n > kWave) continue;
+                flags &= ~(1u << u);
+                if (lanes == 0) continue;
                 if (has) {
                     const int at = staged + (int)lanes_below(lanes);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sh.piece[at][i] = piece[i];
+                    for (int i = 0; i < 4; ++i) sh.piece[at][i] = raw[u][i];
                     sh.token[at] = (uint32_t)c.head + (uint32_t)(first + u * kWave) * N;
                 }
                 staged += n;
-                flags &= flags - 1;
-                if (flags != 0) continue;
             }
             for (int at = 0; at < staged; at += kWave / N) {
                 const int from = at + lane_id() / N, entry = lane_id() % N;
@@ -430,9 +434,9 @@ struct TileOf {
                 const float x = in ? entry_of<T>(sh.piece[from][entry * (int)sizeof(T) / 4], entry) : 0.f;
                 best.offer(in && x >= bound, x, in ? sh.token[from] + entry : 0u, k, sh);
             }
-            staged = 0;
-        }
+        } while (flags != 0);
         if (edges) best.offer(lane_id() < c.edges() && edge >= best.bound, edge, (uint32_t)c.edge<T>(lane_id()), k, sh);
+        if (k <= kFewBest) best.finish(k, sh);
     }
 };
 
