@@ -10,6 +10,7 @@ import ctypes as C
 import functools
 import math
 import os
+import struct
 from typing import NamedTuple
 
 import torch
@@ -494,7 +495,7 @@ class TensorList:
         self.tensors = list(tensors)
         self.device = _one_device(self.tensors, "tensors")
         for i, t in enumerate(self.tensors):
-            _dense(t, VALUE_TYPES, f"tensor {i}")
+            _dense(t, VALUE_TYPES, "tensors", i)
         n = len(self.tensors)
         self.addresses = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         self.types = (C.c_int32 * n)(*[VALUE_TYPES[t.dtype] for t in self.tensors])
@@ -504,7 +505,10 @@ class TensorList:
         return len(self.tensors)
 
 
-def _dense(t, types, what: str) -> None:
+def _dense(t, types, what: str, i: int) -> None:
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.is_contiguous():
+        return
+    what = f"{what}[{i}]"
     _gpu(t, what)
     if t.dtype not in types or not t.is_contiguous():
         raise TypeError(f"{what}: expected contiguous {' or '.join(str(d) for d in types)}, got {t.dtype} (contiguous={t.is_contiguous()})")
@@ -513,10 +517,11 @@ def _dense(t, types, what: str) -> None:
 def _one_device(tensors, what: str) -> int:
     if not tensors:
         raise ValueError(f"{what}: none given")
-    for t in tensors:
-        _gpu(t, what)
-    device = tensors[0].get_device()
-    if any(t.get_device() != device for t in tensors):
+    if not all([isinstance(t, torch.Tensor) and t.is_cuda for t in tensors]):
+        raise TypeError(f"{what}: expected tensors in GPU memory")
+    devices = {t.get_device() for t in tensors}
+    device = devices.pop()
+    if devices:
         raise ValueError(f"{what}: all tensors must be on one device")
     return device
 
@@ -558,41 +563,54 @@ class AdamW:
         self.params = list(params)
         n = len(self.params)
         self.device = _one_device(self.params, "params")
-        per = lambda x, what: self._per_tensor(x, n, what)  # noqa: E731
-        bits, decay = per(bits, "bits"), per(weight_decay, "weight_decay")
-        self.copies = per(copies, "copies")
-        self.m, self.v, self.m_scale, self.v_scale = per(m, "m"), per(v, "v"), per(m_scale, "m_scale"), per(v_scale, "v_scale")
-        self._table = (AdamwTensor * n)()
+        per = self._per_tensor
+        bits, decay = per(bits, n, "bits"), per(weight_decay, n, "weight_decay")
+        self.copies = per(copies, n, "copies")
+        self.m, self.v, self.m_scale, self.v_scale = per(m, n, "m"), per(v, n, "v"), per(m_scale, n, "m_scale"), per(v_scale, n, "v_scale")
+        self._counts, rows, spans = [], [], []
         for i, p in enumerate(self.params):
-            _dense(p, VALUE_TYPES, f"params[{i}]")
-            if bits[i] not in (8, 32):
+            _dense(p, VALUE_TYPES, "params", i)
+            if bits[i] != 32 and bits[i] != 8:
                 raise ValueError("bits must be 8 or 32")
-            kind, blocks = (torch.float8_e4m3fn, -(-p.numel() // STATE_BLOCK)) if bits[i] == 8 else (_F32, 0)
+            eight, count, copy = bits[i] == 8, p.numel(), self.copies[i]
+            self._counts.append(count)
+            kind, size, blocks = (torch.float8_e4m3fn, count, -(-count // STATE_BLOCK)) if eight else (_F32, 4 * count, 0)
+            at = [p.data_ptr(), 0]
+            spans.append((at[0], count * p.itemsize))
             for states in (self.m, self.v):
-                states[i] = self._state(states[i], kind, p.shape, p, f"state {i}")
+                states[i] = self._state(states[i], kind, p.shape, p, "states", i)
+                at.append(states[i].data_ptr())
+                spans.append((at[-1], size))
             for scales in (self.m_scale, self.v_scale):
-                if bits[i] == 8:
-                    scales[i] = self._state(scales[i], _F32, (blocks,), p, f"scale {i}")
+                if eight:
+                    scales[i] = self._state(scales[i], _F32, (blocks,), p, "scales", i)
+                    at.append(scales[i].data_ptr())
+                    spans.append((at[-1], 4 * blocks))
                 elif scales[i] is not None:
-                    raise ValueError(f"scale {i}: 32-bit states have none")
-            copy = self.copies[i]
+                    raise ValueError(f"scales[{i}]: 32-bit states have none")
+                else:
+                    at.append(0)
             if copy is not None:
-                _dense(copy, (torch.bfloat16, torch.float16), f"copies[{i}]")
+                _dense(copy, (torch.bfloat16, torch.float16), "copies", i)
                 if p.dtype is not _F32:
                     raise TypeError(f"copies[{i}]: copies are of fp32 parameters")
                 if copy.shape != p.shape:
                     raise ValueError(f"copies[{i}]: expected shape {tuple(p.shape)}, got {tuple(copy.shape)}")
-            at = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-            self._table[i] = AdamwTensor(at(p), None, at(self.m[i]), at(self.v[i]), at(self.m_scale[i]), at(self.v_scale[i]), at(copy), p.numel(),
-                                         VALUE_TYPES[p.dtype], 0, VALUE_TYPES[copy.dtype] if copy is not None else 0, float(decay[i]))
-        self._written = [t for group in (self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies) for t in group if t is not None]
-        _one_device(self._written, "params, states and copies")
+                spans.append((copy.data_ptr(), 2 * count))
+            rows.append(self._ROW.pack(*at, copy.data_ptr() if copy is not None else 0, count, VALUE_TYPES[p.dtype], 0,
+                                       VALUE_TYPES[copy.dtype] if copy is not None else 0, float(decay[i])))
+        self._table = (AdamwTensor * n).from_buffer_copy(b"".join(rows))
+        _one_device([t for group in (self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies) for t in group if t is not None],
+                    "params, states and copies")
+        self._written = [(start, start + size) for start, size in spans if size]
         self.grads = None
         self._check_apart([])
         if grads is not None:
             self.grads = self._take(grads)
         self._options = AdamwOptions(0.0, float(betas[0]), float(betas[1]), float(eps), 1, None, None, None, int(seed) & (2 ** 64 - 1), int(bool(stochastic)))
         self.steps = 0
+
+    _ROW = struct.Struct("7Qq3if")                                       # AdamwTensor
 
     @staticmethod
     def _per_tensor(x, n: int, what: str) -> list:
@@ -603,20 +621,23 @@ class AdamW:
         return list(x)
 
     @staticmethod
-    def _state(t, kind, shape, like, what: str):
+    def _state(t, kind, shape, like, what: str, i: int):
         if t is None:
             return torch.zeros(shape, dtype=_F32, device=like.device).to(kind)
-        _dense(t, (kind,), what)
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+        _dense(t, (kind,), what, i)
+        if t.shape != shape:
+            raise ValueError(f"{what}[{i}]: expected shape {tuple(shape)}, got {tuple(t.shape)}")
         return t
 
     def _check_apart(self, grads) -> None:
-        """What is written overlaps nothing."""
-        spans = [(t.data_ptr(), t.data_ptr() + t.nbytes, True) for t in self._written if t.nbytes]
-        spans += [(t.data_ptr(), t.data_ptr() + t.nbytes, False) for t in grads if t.nbytes]
-        end, end_written = 0, 0                                           # of all before, and of the written ones
-        for start, stop, written in sorted(spans):
+        """What is written overlaps nothing; grads: their (start, stop), which may overlap one another."""
+        # spans are apart where, in order, each ends before the next begins
+        both = self._written + grads
+        starts, stops = sorted([start for start, _ in both]), sorted([stop for _, stop in both])
+        if all(stop <= start for stop, start in zip(stops, starts[1:])):
+            return
+        end = end_written = 0                                            # of all before, and of the written ones
+        for start, stop, written in sorted([(*span, True) for span in self._written] + [(*span, False) for span in grads]):
             if start < (end if written else end_written):
                 raise ValueError("parameters, states, copies and gradients must not overlap")
             end = max(end, stop)
@@ -625,18 +646,22 @@ class AdamW:
 
     def _take(self, grads) -> list:
         """Takes the addresses of gradients."""
-        grads = list(grads)
+        grads, spans, taken = list(grads), [], []
         if len(grads) != len(self.params):
             raise ValueError(f"grads: expected {len(self.params)}, got {len(grads)}")
-        for i, (g, p) in enumerate(zip(grads, self.params)):
-            _dense(g, VALUE_TYPES, f"grads[{i}]")
+        for i, (g, p, count) in enumerate(zip(grads, self.params, self._counts)):
+            _dense(g, VALUE_TYPES, "grads", i)
             if g.shape != p.shape:
                 raise ValueError(f"grads[{i}]: expected shape {tuple(p.shape)}, got {tuple(g.shape)}")
-            if g.get_device() != self.device:
-                raise ValueError(f"grads[{i}]: not on the parameters' device")
-        self._check_apart(grads)
-        for row, g in zip(self._table, grads):
-            row.grad, row.grad_type = g.data_ptr(), VALUE_TYPES[g.dtype]
+            at = g.data_ptr()
+            taken.append((at, VALUE_TYPES[g.dtype]))
+            if count:
+                spans.append((at, at + count * g.itemsize))
+        if _one_device(grads, "grads") != self.device:
+            raise ValueError("grads: not on the parameters' device")
+        self._check_apart(spans)
+        for row, (at, kind) in zip(self._table, taken):
+            row.grad, row.grad_type = at, kind
         return grads
 
     def step(self, lr, step: "int | torch.Tensor | None" = None, grad_scale: torch.Tensor | None = None, grads=None) -> None:
