@@ -9,7 +9,7 @@
 namespace ef21 {
 namespace {
 
-constexpr int kThreads = 256, kFewThreads = 1024, kItems = 2 * kWave, kMostBlocks = 2048, kFlight = 8;
+constexpr int kThreads = 256, kFewThreads = 1024, kLookups = 3, kItems = kLookups * kWave, kMostBlocks = 2048, kFlight = 8;
 constexpr int64_t kChunkBytes = kThreads * kFlight * 16, kFewChunks = 8;
 
 struct Item {
@@ -69,10 +69,14 @@ __device__ __forceinline__ void add_chunk(const Item &it, int64_t c, double &s) 
 template <class T, int THREADS>
 __device__ __forceinline__ double sum_chunks(const Table &table) {
     double s = 0.0;
-    const int32_t lane = lane_id();
-    const int32_t low = lane < table.count ? table.first[lane] : 0x7fffffff, high = lane + kWave < table.count ? table.first[lane + kWave] : 0x7fffffff;
+    int32_t first[kLookups];
+#pragma unroll
+    for (int i = 0; i < kLookups; ++i) first[i] = lane_id() + i * kWave < table.count ? table.first[lane_id() + i * kWave] : 0x7fffffff;
     for (int32_t c = (int32_t)blockIdx.x; c < table.chunks; c += (int32_t)gridDim.x) {
-        const int t = __builtin_amdgcn_readfirstlane((int)(popc64(__ballot(low <= c)) + popc64(__ballot(high <= c))) - 1);
+        int t = -1;                                                // the last that begins at or before the chunk
+#pragma unroll
+        for (int i = 0; i < kLookups; ++i) t += (int)popc64(__ballot(first[i] <= c));
+        t = __builtin_amdgcn_readfirstlane(t);
         add_chunk<T, THREADS>(table.item[t], c - table.first[t], s);
     }
     return s;
@@ -100,11 +104,13 @@ __global__ __launch_bounds__(kFewThreads) void few_norm_kernel(Table table, Norm
     if (threadIdx.x == 0) write_norm(s, p);
 }
 
-__global__ __launch_bounds__(kThreads) void norm_kernel(const double *sums, int32_t count, NormArgs p) {
-    __shared__ double part[kThreads / kWave];
+// (a thread of 1024 has two or three sums, all on their way at once)
+__global__ __launch_bounds__(kFewThreads) void norm_kernel(const double *sums, int32_t count, NormArgs p) {
+    __shared__ double part[kFewThreads / kWave];
     double s = 0.0;
-    for (int32_t i = (int32_t)threadIdx.x; i < count; i += kThreads) s += sums[i];
-    s = block_sum<kThreads / kWave>(s, part);
+#pragma unroll 4
+    for (int32_t i = (int32_t)threadIdx.x; i < count; i += kFewThreads) s += sums[i];
+    s = block_sum<kFewThreads / kWave>(s, part);
     if (threadIdx.x == 0) write_norm(s, p);
 }
 
@@ -157,7 +163,7 @@ hipError_t launch_grad_norm(const void *const *grads, const int32_t *types, cons
         if (st != hipSuccess) return st;
     }
     if (few && kinds) return hipSuccess;
-    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, stream, sums, written, p);
+    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kFewThreads), 0, stream, sums, written, p);
     return hipGetLastError();
 }
 
