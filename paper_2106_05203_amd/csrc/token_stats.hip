@@ -223,7 +223,8 @@ __device__ __forceinline__ double base_of(float m) { return fabsf(m) >= kMostM /
 
 // r's sums beside an M of `base`, which is not below its own.
 __device__ __forceinline__ void rebase(const Record &r, double base, float &s, float &t) {
-    const float d = fmaxf((float)(base_of(r.m) - base), -1000.f), f = r.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(d);
+    // (without entries its M is zero, and may be infinitely far above)
+    const float d = fminf(fmaxf((float)(base_of(r.m) - base), -1000.f), 0.f), f = r.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(d);
     s = f * r.s;
     t = f * fmaf(d, r.s, r.t);
 }
@@ -666,8 +667,9 @@ __global__ __launch_bounds__(kThreads) void stats_join_kernel(LogitRows in, Stat
 // How a call is cut.  parts.count = 1: without a second launch, `waves` wavefronts to a row.
 constexpr int64_t kWavesInAll = 4096;
 inline int waves_of(int64_t rows, int32_t slices, bool select) {
-    int waves = select ? 1 : 4;
-    while (waves < 16 && rows * waves * 2 <= kWavesInAll && waves < slices) waves *= 2;
+    const int least = select ? 1 : 4;
+    int waves = 1;
+    while (waves < 16 && (waves < least || rows * waves * 2 <= kWavesInAll) && waves * 2 <= slices) waves *= 2;
     return waves;
 }
 template <class T>

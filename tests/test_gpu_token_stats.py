@@ -152,6 +152,25 @@ def test_large_logits(gpu, offset, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [600, 9000, 70000])
+def test_lowest_entries_beside_masked_ones(gpu, vocab, dtype):
+    """Tiles of nothing beside tiles of the type's lowest value, or of its largest: M of the one is infinitely far from that of the other."""
+    torch, b = gpu
+    low, most = torch.finfo(lm.TORCH[dtype]).min, torch.finfo(lm.TORCH[dtype]).max
+    x = torch.full((4, vocab), -math.inf, dtype=lm.TORCH[dtype])
+    x[0, vocab // 2:] = low
+    x[1, : vocab // 3] = low
+    x[2, vocab // 2:] = most
+    x[3, ::1000] = low
+    R = ref.Stats(x.double().numpy(), np.array([vocab - 1, 0, vocab - 1, 0]))
+    labels = torch.tensor([vocab - 1, 0, vocab - 1, 0], device="cuda")
+    dx, one = x.cuda(), torch.ones(4, device="cuda")
+    st = b.ef21_token_stats(dx, labels, 5, sums=True)
+    check(torch, st, R, 5)
+    lm.inside(as64(b.ef21_token_stats_grad(dx, labels, st.sums, st.entropy, one, one)), *R.stats_grad(np.ones(4), np.ones(4), dtype), "gradient")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("order", ["up", "down", "sawtooth", "ties", "late", "blocks", "masked", "few", "alike"])
 @pytest.mark.parametrize("rows,vocab", [(2, 50001), (300, 20003)])
 def test_orders_that_are_hard_to_select_from(gpu, rows, vocab, order, dtype):
