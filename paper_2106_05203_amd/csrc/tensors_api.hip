@@ -75,7 +75,8 @@ int ef21_adamw(const ef21_adamw_tensor *tensors, int32_t tensor_count, const ef2
     if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0)) return invalid("beta1 and beta2 must be in [0, 1)");
     if (!((float)o.eps >= 0x1p-126f) || !std::isfinite((float)o.eps)) return invalid("eps must be finite and at least 2^-126");
     if (o.step < 1) return invalid("step must be at least 1");
-    if (!aligned(o.lr_device, 4) || !aligned(o.step_device, 8) || !aligned(o.grad_scale, 4)) return invalid("lr_device, step_device or grad_scale is misaligned");
+    if (!aligned(o.lr_device, 4) || !aligned(o.step_device, 8) || !aligned(o.grad_scale, 4))
+        return invalid("lr_device, step_device or grad_scale is misaligned");
     const hipError_t st = ef21::launch_adamw(tensors, tensor_count, ef21::adamw_step(o), (hipStream_t)hip_stream);
     return st == hipSuccess ? EF21_OK : ef21::report_hip_error(st, "AdamW launch");
 }

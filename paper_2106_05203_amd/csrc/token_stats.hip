@@ -6,9 +6,15 @@
 // A row is cut into tiles of 512 pieces of 16 bytes, a wavefront's registers full.  Each tile has an M of its own, a whole number next to its maximum: no z
 // is above 1/2, so that t has one sign, the difference does not cancel and nothing leaves fp32's range, and no maximum has to be carried along.  A tile
 // leaves its M, s and t, and the tiles are joined in an order that the row's length alone fixes.
-//   The alternatives: a wavefront keeps the 64 best entries that it has met, one a lane, in order.  What the tile's maxima are needed for anyway tells it
-// whether a tile has any that is better than the k-th; those few are collected in LDS and merged 64 at a time.  The first bound is the k-th largest of the
-// 64 lanes' maxima of the first tile, which some k entries reach and not many more.
+//   The alternatives: a wavefront keeps the 64 best entries that it has met, one a lane, in order.  The pieces' maxima, which M needs anyway, tell which
+// pieces have an entry above the k-th.  Those few go through LDS, an entry a lane; an entry that is better is inserted, or ordered and merged with others.
+// Where more pieces qualify than there are alternatives (the first tiles of a row, rising rows), the bound is raised first: halving finds a value that
+// some k pieces' maxima reach.
+//
+// Measured (a plain read of this card's memory: 7.1 TB/s).  8192 rows of 131072 bf16, one in eight ignored, without alternatives: 277 us, 6.8 TB/s; 4096
+// rows with 20: 204 us, 5.3 TB/s, bound by the vector instructions of the sums (a product, an exponential, a maximum and two sums an entry) and by the
+// selection's latency.  2001 rows of 32064 fp32 with 8: 46 us, 4.9 TB/s: one turn of the card's wavefronts, whose last tiles are waited for.  One row of
+// 131072: 13 us, two launches' latency.
 #include "token_rows.h"
 
 namespace ef21 {
@@ -16,7 +22,8 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kEach = 8, kTile = kEach * kWave;                    // pieces of a lane, of a tile
-constexpr int kEachShort = 2;                                      // of rows that have no more in all
+constexpr int kEachShort = 2;                                      // of rows that have no more in all: 16384 rows of 1000 bf16, k = 5, with their
+                                                                   // gradient 43 us, where eight of which most are empty take 71
 constexpr int kMostSlices = 256;
 
 // Tiles of a row and how they are grouped: into at most 256 slices, each a wavefront's at a time.
@@ -140,9 +147,9 @@ __device__ __forceinline__ void order_keys(uint64_t &key) {
     exchange<1>(key);
 }
 
-// An entry inserted takes some 20 instructions, 64 ordered and merged 350; but the bound then rises at once, and fewer entries are met.  4096 rows of 131072 bf16
-// with 20 alternatives: 203 us so (keys of up to 3 lanes inserted 207, of 10 207), 205 where they wait across the tiles until there are 64; with 64 alternatives
-// 235 and 222.
+// An entry inserted takes some 20 instructions, 64 ordered and merged 350; but the bound then rises at once, and fewer entries are met.  4096 rows of 131072
+// bf16 with 20 alternatives: 203 us so (keys of up to 3 lanes inserted 207, of 10 207), 205 where they wait across the tiles until there are 64; with 64
+// alternatives 235 and 222.
 constexpr uint32_t kFewKeys = 6;
 constexpr int kFewBest = 32;
 
@@ -159,7 +166,7 @@ struct Selection {
 
     // Other entries in descending order, zeros last.
     __device__ __forceinline__ void merge_ordered(uint64_t other, int k) {
-        const uint64_t turned = other_key<63>(other);              // the 64 best of both: the better of the first and the last, the second and the last but one, ...
+        const uint64_t turned = other_key<63>(other);              // the 64 best of both: the better of the first and the last, of the second and ...
         if (turned > mine) mine = turned;
         order_halves(mine);
         limit = read_lane(mine, k - 1);
@@ -377,7 +384,8 @@ struct TileOf {
         return r;
     }
 
-    // most: the pieces' largest entries.  Pieces that have an entry to offer go to LDS, and from there entry by entry to the lanes.
+    // most: the pieces' largest entries.  Pieces that have an entry to offer go to LDS, and from there entry by entry to the lanes.  (Read again from memory
+    // instead, with the next tile's loads under way meanwhile: 512 rows of 131072, k = 20: 45 us for 40.)
     __device__ __forceinline__ void select(const Cut &c, int32_t tile, const float (&most)[EACH], float lane_most, float top, int k, Selection &best,
                                            SelectShared &sh) const {
         float bound = best.bound_from((uint32_t)c.head + (uint32_t)(tile * (EACH * kWave)) * N);
@@ -391,9 +399,8 @@ struct TileOf {
         };
         const int enough = k + k / 4;
         if ((int)popc64(some) > k / 2 && reach(bound) > enough) {
-            // As many pieces reach the tile's bound as there are alternatives, or a few more: halve the way to the largest entry, or from 8 below
-            // it, until it is so.  (From a bound that k pieces reach, k entries do; equal entries may end it early, and so may a way that cannot
-            // be halved.)
+            // More pieces reach the bound than there are alternatives: halve the way to the largest entry, or from 8 below it, until a few more do.
+            // (Where k pieces' maxima reach a bound, k entries do; equal entries may end it early, and so may a way that cannot be halved.)
             float high = top, step = 8.f;
             for (int i = 0; i < 16; ++i) {
                 const float middle = fmaxf(0.5f * bound + 0.5f * high, top - step);
@@ -542,7 +549,10 @@ __device__ __forceinline__ bool row_counts(const LogitRows &in, int64_t r, float
 }
 
 // ---------------------------------------------------------------- kernels
-constexpr int kToSimd = 4;                                         // wavefronts that the registers are shared out among
+// Wavefronts that a SIMD's registers are shared out among: 128 registers hold a tile and the selection.  With 5 and 6 (the tile spills, or is loaded in
+// parts) 8192 rows of 131072 with their gradient take 946 and 1009 us for 937, 4096 rows with 20 alternatives 215 and 262 for 215, and 2048 rows of 50000
+// with 57 and 65 for 47.
+constexpr int kToSimd = 4;
 
 // A team of WAVES wavefronts per row, which take the slices in turn; the first joins what they found while the others begin the next row.  Teams of one
 // share a workgroup of four.
@@ -665,13 +675,19 @@ __global__ __launch_bounds__(kThreads) void stats_join_kernel(LogitRows in, Stat
 }
 
 // How a call is cut.  parts.count = 1: without a second launch, `waves` wavefronts to a row.
+//   Wavefronts in all: four times the card's SIMDs, as many as are resident.  512 rows of 131072, k = 20: 40 us so, 49 with half as many, 46 with twice
+// (each begins a selection of its own); 1024 rows: 66, 84 and 74.
+//   Beyond those rows an alternative's bound is worth most where one wavefront sees the whole row; sums alone gain from four that read neighbouring tiles of
+// one row, if it is long: 8192 rows of 131072 937 us (with gradient) for 974, 16384 of 65536 332 for 345; but 50000 274 for 267, and 16000 99 for 91.
 constexpr int64_t kWavesInAll = 4096;
 inline int waves_of(int64_t rows, int32_t slices, bool select) {
-    const int least = select ? 1 : 4;
+    const int least = select || slices < 16 ? 1 : 4;
     int waves = 1;
     while (waves < 16 && (waves < least || rows * waves * 2 <= kWavesInAll) && waves * 2 <= slices) waves *= 2;
     return waves;
 }
+// By parts where a workgroup of 16 wavefronts would take more than one turn and the rows leave the card empty: one row of 131072, k = 20: 13.8 us for 20.3.
+// 16 rows of 32000, one turn: 11.9 us by a workgroup each, 13.6 by parts.
 template <class T>
 Parts parts_of(int64_t rows, int64_t vocab) {
     const Slices cut = slices_of<T>((int32_t)vocab);
@@ -795,7 +811,8 @@ __global__ __launch_bounds__(kThreads) void stats_grad_short_kernel(LogitRows in
     }
 }
 
-// Longer rows in the tiles of token_rows.h, bound by memory.
+// Longer rows in the tiles of token_rows.h, bound by memory: 8192 rows of 131072 bf16, one in eight ignored, in 655 us: 6.15 TB/s, where a plain kernel
+// that reads and writes neighbouring stretches reaches 6.4.
 template <class T, bool ADD>
 __global__ __launch_bounds__(kGradThreads) void stats_grad_kernel(LogitRows in, StatGradArgs p, LogitGrad out, int32_t tiles) {
     const int32_t vocab = (int32_t)in.vocab;
@@ -859,8 +876,8 @@ hipError_t launch_token_stats(const LogitRows &in, const StatArgs &p, void *work
             }
             const auto rows = [&](auto each, auto waves) {
                 typedef Team<decltype(waves)::value> G;
-                hipLaunchKernelGGL((stats_row_kernel<T, decltype(each)::value, decltype(waves)::value, SELECT>), dim3(grid_of(in.rows, G::kPerBlock, G::kBlock)), dim3(G::kBlock), 0,
-                                   stream, in, p);
+                hipLaunchKernelGGL((stats_row_kernel<T, decltype(each)::value, decltype(waves)::value, SELECT>),
+                                   dim3(grid_of(in.rows, G::kPerBlock, G::kBlock)), dim3(G::kBlock), 0, stream, in, p);
                 return hipGetLastError();
             };
             const std::integral_constant<int, kEach> each;

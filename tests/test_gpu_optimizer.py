@@ -300,6 +300,23 @@ def test_norm_of_odd_values(gpu):
     assert float(norm) == 0.0 and float(factor) == 0.5
 
 
+def test_memory_is_held(gpu):
+    """A tensor whose .data is exchanged: what it had is kept, read and written, and no memory that others have by now."""
+    torch, b = gpu
+    n = 1 << 20
+    p, g = torch.ones(n, device="cuda"), torch.full((n,), 2.0, device="cuda")
+    memory = p.detach()
+    opt, grads = b.AdamW([p], [g], weight_decay=0.0), b.TensorList([g])
+    p.data, g.data = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    others = [torch.zeros(n, device="cuda") for _ in range(4)]
+    opt.step(0.5)
+    norm, _ = b.ef21_grad_norm(grads, 1.0)
+    assert float(norm) == 2048.0                                   # the root of 2^20 times four
+    # m / (1 - beta1) = 2, the root of v / (1 - beta2) = 2: a step of 0.5, but for fp32's roundings, two ulp of which are 2^-22
+    assert float((memory - 0.5).abs().max()) <= 2.0 ** -20
+    assert all(float(o.abs().max()) == 0.0 for o in others) and float(p) == 0.0
+
+
 def test_large_tensors(gpu):
     """Beyond 2^31 entries and bytes: the last entries are reached, by their own random bits."""
     torch, b = gpu
