@@ -557,8 +557,8 @@ class AdamW:
     float8_e4m3fn with one fp32 scale per 256 entries), each a list per tensor; new ones otherwise, also for None in a list.
     copies: a list of bf16 or fp16 tensors (or None) that receive the new fp32 parameters.  weight_decay: a number, or one per tensor.
     stochastic, seed: see include/ef21.h.  The tensors stay the caller's; the object keeps them alive and works on the memory
-    that they have when they are given, also if their .data is another's later on.  Steps of one object follow each other: in one thread,
-    and on one stream or on streams that wait for each other.
+    that they have when they are given, also if the .data of a parameter, gradient or copy is another's later on (that of states must not be
+    exchanged).  Steps of one object follow each other: in one thread, and on one stream or on streams that wait for each other.
     """
 
     def __init__(self, params, grads=None, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, bits=32, m=None, v=None, m_scale=None,
@@ -607,7 +607,7 @@ class AdamW:
         _one_device([t for group in (self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies) for t in group if t is not None],
                     "params, states and copies")
         self._written = [(start, start + size) for start, size in spans if size]
-        self._held = [t.detach() for group in (self.params, self.m, self.v, self.m_scale, self.v_scale, self.copies) for t in group if t is not None]
+        self._held = [t.detach() for group in (self.params, self.copies) for t in group if t is not None]
         self.grads = None
         self._check_apart([])
         if grads is not None:
