@@ -680,13 +680,15 @@ __global__ __launch_bounds__(kThreads) void stats_join_kernel(LogitRows in, Stat
 // How a call is cut.  parts.count = 1: without a second launch, `waves` wavefronts to a row.
 //   Wavefronts in all: four times the card's SIMDs, as many as are resident.  512 rows of 131072, k = 20: 40 us so, 49 with half as many, 46 with twice
 // (each begins a selection of its own); 1024 rows: 66, 84 and 74.
+//   A tile to a wavefront where there are enough of them, even if some have none: 64 rows of 20000 fp16 (five tiles), k = 5 11.0 us by eight, 12.7 by four,
+// k = 40 11.8 and 16.1.
 //   Beyond those rows an alternative's bound is worth most where one wavefront sees the whole row; sums alone gain from four that read neighbouring tiles of
 // one row, if it is long: 8192 rows of 131072 937 us (with gradient) for 974, 16384 of 65536 332 for 345; but 50000 274 for 267, and 16000 99 for 91.
 constexpr int64_t kWavesInAll = 4096;
 inline int waves_of(int64_t rows, int32_t slices, bool select) {
     const int least = select || slices < 16 ? 1 : 4;
     int waves = 1;
-    while (waves < 16 && (waves < least || rows * waves * 2 <= kWavesInAll) && waves * 2 <= slices) waves *= 2;
+    while (waves < 16 && (waves < least || rows * waves * 2 <= kWavesInAll) && waves < slices) waves *= 2;
     return waves;
 }
 // By parts where a workgroup of 16 wavefronts would take more than one turn and the rows leave the card empty: one row of 131072, k = 20: 13.8 us for 20.3.
