@@ -499,12 +499,22 @@ class TensorList:
         _all_dense(self.tensors, VALUE_TYPES, "tensors")
         n = len(self.tensors)
         self._held = [t.untyped_storage() for t in self.tensors]
+        self._spaces = {}                                                # by stream: calls on two of them may overlap
         self.addresses = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         self.types = (C.c_int32 * n)(*[VALUE_TYPES[t.dtype] for t in self.tensors])
         self.counts = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
 
     def __len__(self):
         return len(self.tensors)
+
+    def workspace(self, stream: int, bytes_of: int) -> torch.Tensor:
+        """A workspace for ef21_grad_norm on a stream: zeros at first, which each call leaves as it found them.  A captured call has one of its own."""
+        space = self._spaces.get(stream)
+        if space is None or torch.cuda.is_current_stream_capturing():
+            space = torch.zeros(bytes_of, dtype=torch.uint8, device=self.tensors[0].device)
+            if not torch.cuda.is_current_stream_capturing():
+                self._spaces[stream] = space
+        return space
 
 
 def _dense(t, types, what: str, i: int) -> None:
@@ -557,15 +567,16 @@ def ef21_grad_norm_workspace(tensor_count: int) -> int:
 def ef21_grad_norm(grads, max_norm: float = math.inf, scale: float = 1.0, norm: torch.Tensor | None = None, factor: torch.Tensor | None = None,
                    workspace: torch.Tensor | None = None):
     """(norm [1], factor [1]) of all gradients together (ef21_grad_norm); grads: a TensorList, or tensors.  `factor` is what AdamW.step
-    takes as grad_scale."""
+    takes as grad_scale.  workspace: zeros before the first call with it; calls that share one follow each other."""
     lib = load_library()
     grads = grads if isinstance(grads, TensorList) else TensorList(grads)
     like = grads.tensors[0]
     norm, factor = _new(norm, 1, like), _new(factor, 1, like)
+    stream = _stream_of(like, norm, factor, workspace)
     if workspace is None:
-        workspace = torch.empty(ef21_grad_norm_workspace(len(grads)), dtype=torch.uint8, device=like.device)
+        workspace = grads.workspace(stream, ef21_grad_norm_workspace(len(grads)))
     _check(lib.ef21_grad_norm(grads.addresses, grads.types, grads.counts, len(grads), scale, max_norm, _vector(norm, 1, "norm"),
-                              _vector(factor, 1, "factor"), workspace.data_ptr(), workspace.nbytes, _stream_of(like, norm, factor, workspace)))
+                              _vector(factor, 1, "factor"), workspace.data_ptr(), workspace.nbytes, stream))
     return norm, factor
 
 

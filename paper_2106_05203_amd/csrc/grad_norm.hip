@@ -1,10 +1,13 @@
 // The norm of many gradients together, and the factor that clips it.  Squares of fp32 numbers are exact in fp64 and neither overflow nor vanish there.
 //
 // One pass, bound by memory.  The tensors are cut into chunks of 32 KB; workgroup b of B takes the chunks b, b + B, ... of all tensors in turn, so
-// that a few long tensors and many short ones load the chip alike, and the order of the sums follows from the sizes.  A second launch of one
-// workgroup adds the workgroups' sums up; up to kFewChunks chunks one workgroup does it all.
-// 403 million bf16 entries in 146 tensors: 122 us, 6.6 TB/s, both launches included (a plain read: 7.1).  50000 fp32 entries: 7.7 us by one workgroup,
-// 10.9 by two launches.
+// that a few long tensors and many short ones load the chip alike, and the order of the sums follows from the sizes.  Up to kFewChunks chunks one
+// workgroup does it all; else the last of few workgroups adds their sums up (nobody waits: one that is not the last ends), or a second launch of one
+// workgroup those of many.
+// 403 million bf16 entries in 146 tensors: 121 us, 6.7 TB/s, both launches included (a plain read: 7.1).  50000 fp32 entries: 7.0 us, most of it the
+// host's part of the call.
+#include <algorithm>
+
 #include "token_rows.h"
 #include "tensors.h"
 
@@ -13,6 +16,10 @@ namespace {
 
 constexpr int kThreads = 256, kFewThreads = 1024, kLookups = 3, kItems = kLookups * kWave, kMostBlocks = 2048, kFlight = 8;
 constexpr int64_t kChunkBytes = kThreads * kFlight * 16, kFewChunks = 8;
+// Up to so many chunks of the last launch go to so many workgroups, of which the last adds up: 1 million fp32 entries 7.4 us, 2 million 9.3, with a launch
+// of its own for the sums 10.5 either way.  Beyond, tickets queue up: 4 million 12.1 for 10.7, and one for each of 2048 workgroups triples the time.
+constexpr int32_t kTicketChunks = 256, kMostTickets = 128;
+constexpr size_t kCounterBytes = 256;
 
 struct Item {
     const void *g;
@@ -92,11 +99,26 @@ __device__ __forceinline__ void write_norm(double squares, const NormArgs &p) {
     p.factor[0] = !finite ? __int_as_float(0x7fc00000) : norm > (double)p.max_norm ? (float)((double)p.scale * ((double)p.max_norm / norm)) : p.scale;
 }
 
+// The workgroups' sums added up, by a workgroup.
+template <int THREADS>
+__device__ __forceinline__ void add_up(const double *sums, int32_t count, const NormArgs &p, double (&part)[THREADS / kWave]) {
+    double s = 0.0;
+#pragma unroll 4
+    for (int32_t i = (int32_t)threadIdx.x; i < count; i += THREADS) s += sums[i];
+    s = block_sum<THREADS / kWave>(s, part);
+    if (threadIdx.x == 0) write_norm(s, p);
+}
+
+// sums: of this launch's workgroups; `before` in front of them are those of earlier launches.  tickets: workgroups that draw one, or 0.
 template <class T>
-__global__ __launch_bounds__(kThreads, 8) void square_sums_kernel(Table table, double *sums) {
+__global__ __launch_bounds__(kThreads, 8) void square_sums_kernel(Table table, double *sums, int32_t before, uint32_t *counter, uint32_t tickets, NormArgs p) {
     __shared__ double part[kThreads / kWave];
+    __shared__ uint32_t last;
     const double s = block_sum<kThreads / kWave>(sum_chunks<T, kThreads>(table), part);
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
+    if (tickets == 0 || !draw_ticket(counter, tickets, &last)) return;
+    if (threadIdx.x == 0) *counter = 0;
+    add_up<kThreads>(sums - before, before + (int32_t)tickets, p, part);
 }
 
 template <class T>
@@ -106,35 +128,34 @@ __global__ __launch_bounds__(kFewThreads) void few_norm_kernel(Table table, Norm
     if (threadIdx.x == 0) write_norm(s, p);
 }
 
-// (a thread of 1024 has two or three sums, all on their way at once)
 __global__ __launch_bounds__(kFewThreads) void norm_kernel(const double *sums, int32_t count, NormArgs p) {
     __shared__ double part[kFewThreads / kWave];
-    double s = 0.0;
-#pragma unroll 4
-    for (int32_t i = (int32_t)threadIdx.x; i < count; i += kFewThreads) s += sums[i];
-    s = block_sum<kFewThreads / kWave>(s, part);
-    if (threadIdx.x == 0) write_norm(s, p);
+    add_up<kFewThreads>(sums, count, p, part);
 }
 
 }  // namespace
 
 // A launch takes kItems tensors of one type.
 size_t norm_workspace_bytes(int32_t tensors) {
-    return tensors == 0 ? 0 : (size_t)((tensors + kItems - 1) / kItems + 2) * kMostBlocks * sizeof(double);
+    return tensors == 0 ? 0 : kCounterBytes + (size_t)((tensors + kItems - 1) / kItems + 2) * kMostBlocks * sizeof(double);
 }
 
 hipError_t launch_grad_norm(const void *const *grads, const int32_t *types, const int64_t *counts, int32_t tensors, const NormArgs &p, void *workspace,
                             hipStream_t stream) {
-    double *sums = static_cast<double *>(workspace);
+    uint32_t *counter = static_cast<uint32_t *>(workspace);
+    double *sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + kCounterBytes);
     int64_t chunks = 0;
+    int32_t left = 0;                                              // tensors that no launch has taken yet
     int kinds = 0;
     const auto chunks_of = [&](int32_t i) { return (counts[i] * value_bytes(types[i]) + kChunkBytes - 1) / kChunkBytes; };
     for (int32_t i = 0; i < tensors; ++i) {
         chunks += chunks_of(i);
+        left += counts[i] > 0;
         if (counts[i] > 0) kinds |= 1 << types[i];
     }
     const bool few = chunks <= kFewChunks && tensors <= kItems && (kinds & (kinds - 1)) == 0;
     int32_t written = 0;
+    bool done = few && kinds;
     for (int type = kF32; type <= kF16; ++type) {
         if (!(kinds >> type & 1)) continue;
         const hipError_t st = with_type(type, [&](auto as) {
@@ -145,8 +166,11 @@ hipError_t launch_grad_norm(const void *const *grads, const int32_t *types, cons
                 if (few) {
                     hipLaunchKernelGGL(few_norm_kernel<T>, dim3(1), dim3(kFewThreads), 0, stream, table, p);
                 } else {
-                    const int32_t blocks = table.chunks < kMostBlocks ? table.chunks : kMostBlocks;
-                    hipLaunchKernelGGL(square_sums_kernel<T>, dim3(blocks), dim3(kThreads), 0, stream, table, sums + written);
+                    left -= table.count;
+                    done = left == 0 && table.chunks <= kTicketChunks;
+                    const int32_t blocks = std::min(table.chunks, done ? kMostTickets : kMostBlocks);
+                    hipLaunchKernelGGL(square_sums_kernel<T>, dim3(blocks), dim3(kThreads), 0, stream, table, sums + written, written, counter,
+                                       done ? (uint32_t)blocks : 0u, p);
                     written += blocks;
                 }
                 table.count = table.chunks = 0;
@@ -164,7 +188,7 @@ hipError_t launch_grad_norm(const void *const *grads, const int32_t *types, cons
         });
         if (st != hipSuccess) return st;
     }
-    if (few && kinds) return hipSuccess;
+    if (done) return hipSuccess;
     hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kFewThreads), 0, stream, sums, written, p);
     return hipGetLastError();
 }

@@ -194,7 +194,7 @@ def test_numbers_read_on_the_device_and_graphs(gpu):
         one, two = (optimizer(b, part, eight, 0.1, stochastic=True, seed=99) for part in (xs, ys))
         lr, step = torch.tensor([1e-3], device="cuda"), torch.tensor([1], device="cuda")
         norm, factor = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
-        grads, space = b.TensorList([x["g"].t for x in xs]), torch.empty(b.ef21_grad_norm_workspace(3), dtype=torch.uint8, device="cuda")
+        grads, space = b.TensorList([x["g"].t for x in xs]), torch.zeros(b.ef21_grad_norm_workspace(3), dtype=torch.uint8, device="cuda")
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         first = [expected(x, np.float64(np.float32(0.1)), 1, on_device=True) for x in xs]
@@ -280,6 +280,58 @@ def test_norm(gpu, dtype):
                 assert abs(float(factor) - clipped) <= 2 * U * clipped
             again = b.ef21_grad_norm(b.TensorList(gs), limit, scale)
             assert float(again[0]) == float(norm) and float(again[1]) == float(factor)
+
+
+@pytest.mark.parametrize("sizes", [(5,), (300000,), (1000003, 70000), (1500000,), (3000000,), (1,) * 200 + (50000,) * 10, (20000,) * 500])
+def test_norm_of_the_same_list_again_and_again(gpu, sizes):
+    """A list's workspace is left as it was found: calls in a row, on two streams at once, and two graphs of the list replayed in turn, all on new contents."""
+    torch, b = gpu
+    g = torch.Generator(device="cuda").manual_seed(sum(sizes))
+    xs = [torch.randn(n, generator=g, device="cuda") for n in sizes]
+    lists = b.TensorList(xs)
+    outs = [(torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")) for _ in range(4)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+
+    def want():
+        return math.sqrt(sum(float((x.double() ** 2).sum()) for x in xs))
+
+    def near(out, norm):
+        # fp64 sums, a root and one rounding to fp32; the factor with a product and a quotient in fp64
+        assert abs(float(out[0]) - norm) <= 2.0 ** -24 * 1.001 * norm and abs(float(out[1]) - min(1.0, 2.0 / norm)) <= 2.0 ** -24 * 1.001 * min(1.0, 2.0 / norm)
+
+    graphs = []
+    for out, stream in zip(outs[2:], streams):
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            b.ef21_grad_norm(lists, 2.0, norm=out[0], factor=out[1])
+        stream.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            b.ef21_grad_norm(lists, 2.0, norm=out[0], factor=out[1])
+    for turn in range(4):
+        for x in xs[:3]:
+            x.mul_(1.5)
+        torch.cuda.synchronize()
+        for out, stream in zip(outs, streams):
+            with torch.cuda.stream(stream):
+                for _ in range(5):
+                    out[0].zero_()
+                    b.ef21_grad_norm(lists, 2.0, norm=out[0], factor=out[1])
+        torch.cuda.synchronize()
+        for out in outs[2:]:
+            out[0].zero_()
+        for graph, stream in zip(graphs, streams[::-1]):
+            with torch.cuda.stream(stream):
+                graph.replay()
+                graph.replay()
+        torch.cuda.synchronize()
+        for out in outs:
+            near(out, want())
+        assert len({(float(a), float(c)) for a, c in outs}) == 1
+    space = torch.zeros(b.ef21_grad_norm_workspace(len(xs)), dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        near(b.ef21_grad_norm(lists, 2.0, workspace=space), want())
+        assert int(space[:4].max()) == 0
 
 
 def test_norm_of_odd_values(gpu):

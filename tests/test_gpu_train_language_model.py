@@ -136,7 +136,7 @@ def test_a_step_of_everything_captured(lm):
         s["step"] = torch.zeros(1, dtype=torch.int64, device="cuda")
         s["optimizer"] = b.AdamW([s["table"]], [s["grad"][0]], bits=8, stochastic=True, seed=5)
         s["list"] = b.TensorList([s["grad"]])
-        s["space"] = {n: torch.empty(size, dtype=torch.uint8, device="cuda") for n, size in (
+        s["space"] = {n: torch.zeros(size, dtype=torch.uint8, device="cuda") for n, size in (
             ("stats", max(1, b.ef21_token_stats_workspace(1, rows, vocab, 0))), ("policy", max(1, b.ef21_policy_loss_workspace(rows))),
             ("embed", b.ef21_embed_grad_workspace(1, rows, vocab, width)), ("norm", b.ef21_grad_norm_workspace(1)))}
         return s
