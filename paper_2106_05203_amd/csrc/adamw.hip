@@ -5,7 +5,7 @@
 // 8 bits: e4m3 numbers of m / s_m and sqrt(v) / s_v, s = the largest of the block / 448.  The root, not v: in powers of two its range is half of v's,
 // and the update needs it anyway.  sqrt(v) > 0 is stored as 2^-9 s_v at the least: as zero it would divide the next m by eps alone.
 //
-// Measured: 403 million fp32 parameters with a bf16 copy, bf16 gradients, 32 bits: 1838 us, 6.1 TB/s; 201 million fp32 parameters and gradients, 8 bits:
+// Measured: 403 million fp32 parameters with a bf16 copy, bf16 gradients, 32 bits: 1790 us, 6.3 TB/s; 201 million fp32 parameters and gradients, 8 bits:
 // 531 us, 6.1 TB/s, bound by memory.  11.2 million bf16 parameters in 146 tensors, 8 bits: 36.5 us where memory needs 18: three launches, and some 86
 // instructions an entry.
 #include <cmath>
@@ -310,20 +310,21 @@ struct Entries {
 };
 
 // A workgroup per WAVES FLIGHT blocks of 256 entries, a wavefront per block at a time, four entries a lane.
-//   32-bit states are bound by memory, and the memory answers seven streams of fewer wavefronts faster: 403 million entries with a copy in workgroups of two
-// wavefronts, three to a SIMD, 1842 us (6.1 TB/s); as many as the registers allow (eight) 2012, two 2070.  Without a copy, 134 million fp32 entries and
-// gradients, four to a SIMD 604, three 610; workgroups of four wavefronts 649, eight to a SIMD 666.
+//   32-bit states are bound by memory, and the memory answers seven streams of fewer wavefronts faster, the less they run in step: 403 million entries with
+// a copy, workgroups of one wavefront, four to a SIMD, 1790 us (6.3 TB/s); three 1805, five 1842; workgroups of two, three to a SIMD, 1842, eight 2012; two
+// blocks in flight 1908.  Without a copy, 134 million fp32 entries and gradients: 578, five to a SIMD 591, workgroups of two 604, of four 649.  11.2 million
+// in 146 tensors: 53.8, workgroups of two 55.6.
 //   8-bit states take some 90 instructions an entry, and as many wavefronts as there are: 201 million fp32 entries 536, three to a SIMD 594.  Two blocks in
 // flight of a wavefront where the chip has several rounds of workgroups: 541, with one 560, with four 557; else one, since a block takes a microsecond of
 // instructions: 11.2 million entries in 146 tensors 43, with two 47, with four 56.
 template <int BITS, bool COPY>
 struct Shape {
-    static constexpr int kWaves = BITS == 8 ? 4 : 2, kThreads = kWaves * kWave, kToSimd = BITS == 8 ? 8 : COPY ? 3 : 4;
+    static constexpr int kWaves = BITS == 8 ? 4 : 1, kThreads = kWaves * kWave, kToSimd = BITS == 8 ? 8 : 4;
     template <int FLIGHT>
     static constexpr int chunk() { return FLIGHT * kWaves * kBlock8; }
 };
 constexpr int64_t kManyEntries = (int64_t)1 << 25;
-// A launch's threads stay below 2^32: 2^24 workgroups, which hold the 2^33 entries that a tensor may have.
+// A launch's threads stay below 2^32: the 2^33 entries that a tensor may have are 2^25 workgroups of 64.
 constexpr int64_t kMostBlocks = (int64_t)1 << 23;
 
 template <class P, class G, int BITS, bool COPY, int FLIGHT>
