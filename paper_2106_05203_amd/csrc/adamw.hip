@@ -310,7 +310,7 @@ struct Entries {
 };
 
 // A workgroup per WAVES FLIGHT blocks of 256 entries, a wavefront per block at a time, four entries a lane.
-//   32-bit states are bound by memory, and the memory answers seven streams of fewer wavefronts faster, the less they run in step: 403 million entries with
+//   32-bit states are bound by memory, and the memory answers seven streams of fewer wavefronts, each a workgroup, faster: 403 million entries with
 // a copy, workgroups of one wavefront, four to a SIMD, 1790 us (6.3 TB/s); three 1805, five 1842; workgroups of two, three to a SIMD, 1842, eight 2012; two
 // blocks in flight 1908.  Without a copy, 134 million fp32 entries and gradients: 578, five to a SIMD 591, workgroups of two 604, of four 649.  11.2 million
 // in 146 tensors: 53.8, workgroups of two 55.6.

@@ -1,6 +1,6 @@
 // The norm of many gradients together, and the factor that clips it.  Squares of fp32 numbers are exact in fp64 and neither overflow nor vanish there.
 //
-// One pass, bound by memory.  The tensors are cut into chunks of 32 KB; workgroup b of B takes the chunks b, b + B, ... of all tensors in turn, so
+// One pass, bound by memory.  The tensors are cut into chunks of 64 KB; workgroup b of B takes the chunks b, b + B, ... of all tensors in turn, so
 // that a few long tensors and many short ones load the chip alike, and the order of the sums follows from the sizes.  Up to kFewChunks chunks one
 // workgroup does it all; else the last of few workgroups adds their sums up (nobody waits: one that is not the last ends), or a second launch of one
 // workgroup those of many.
@@ -14,11 +14,12 @@
 namespace ef21 {
 namespace {
 
-constexpr int kThreads = 256, kFewThreads = 1024, kLookups = 3, kItems = kLookups * kWave, kMostBlocks = 2048, kFlight = 8;
-constexpr int64_t kChunkBytes = kThreads * kFlight * 16, kFewChunks = 8;
-// Up to so many chunks of the last launch go to so many workgroups, of which the last adds up: 1 million fp32 entries 7.4 us, 2 million 9.3, with a launch
-// of its own for the sums 10.5 either way.  Beyond, tickets queue up: 4 million 12.1 for 10.7, and one for each of 2048 workgroups triples the time.
-constexpr int32_t kTicketChunks = 256, kMostTickets = 128;
+constexpr int kThreads = 512, kFewThreads = 1024, kLookups = 3, kItems = kLookups * kWave, kMostBlocks = 2048, kFlight = 8;
+constexpr int64_t kChunkBytes = kThreads * kFlight * 16, kFewChunks = 4;
+// Up to so many workgroups draw tickets, and the last adds up: 1 million fp32 entries 6.9 us (the host's part of the call), 1.5 million 7.7, 2 million 8.4,
+// with a launch of its own for the sums 10.3 (chunks of 32 KB: 7.4, 10.2, 9.3).  Beyond, tickets queue up: 3 million 11.7 for 9.9, and one for each of
+// 2048 workgroups triples the time of 403 million.
+constexpr int32_t kMostTickets = 128;
 constexpr size_t kCounterBytes = 256;
 
 struct Item {
@@ -167,8 +168,8 @@ hipError_t launch_grad_norm(const void *const *grads, const int32_t *types, cons
                     hipLaunchKernelGGL(few_norm_kernel<T>, dim3(1), dim3(kFewThreads), 0, stream, table, p);
                 } else {
                     left -= table.count;
-                    done = left == 0 && table.chunks <= kTicketChunks;
-                    const int32_t blocks = std::min(table.chunks, done ? kMostTickets : kMostBlocks);
+                    done = left == 0 && table.chunks <= kMostTickets;
+                    const int32_t blocks = std::min(table.chunks, kMostBlocks);
                     hipLaunchKernelGGL(square_sums_kernel<T>, dim3(blocks), dim3(kThreads), 0, stream, table, sums + written, written, counter,
                                        done ? (uint32_t)blocks : 0u, p);
                     written += blocks;
