@@ -12,6 +12,7 @@ import math
 import operator
 import os
 import struct
+import threading
 from typing import NamedTuple
 
 import torch
@@ -499,7 +500,7 @@ class TensorList:
         _all_dense(self.tensors, VALUE_TYPES, "tensors")
         n = len(self.tensors)
         self._held = [t.untyped_storage() for t in self.tensors]
-        self._spaces = {}                                                # by stream: calls on two of them may overlap
+        self._spaces, self._lock = {}, threading.Lock()                  # by stream: calls on two of them may overlap; and one thread's at a time
         self.addresses = (C.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         self.types = (C.c_int32 * n)(*[VALUE_TYPES[t.dtype] for t in self.tensors])
         self.counts = (C.c_int64 * n)(*[t.numel() for t in self.tensors])
@@ -573,10 +574,11 @@ def ef21_grad_norm(grads, max_norm: float = math.inf, scale: float = 1.0, norm: 
     like = grads.tensors[0]
     norm, factor = _new(norm, 1, like), _new(factor, 1, like)
     stream = _stream_of(like, norm, factor, workspace)
-    if workspace is None:
-        workspace = grads.workspace(stream, ef21_grad_norm_workspace(len(grads)))
-    _check(lib.ef21_grad_norm(grads.addresses, grads.types, grads.counts, len(grads), scale, max_norm, _vector(norm, 1, "norm"),
-                              _vector(factor, 1, "factor"), workspace.data_ptr(), workspace.nbytes, stream))
+    args = grads.addresses, grads.types, grads.counts, len(grads), scale, max_norm, _vector(norm, 1, "norm"), _vector(factor, 1, "factor")
+    with grads._lock:
+        if workspace is None:
+            workspace = grads.workspace(stream, ef21_grad_norm_workspace(len(grads)))
+        _check(lib.ef21_grad_norm(*args, workspace.data_ptr(), workspace.nbytes, stream))
     return norm, factor
 
 

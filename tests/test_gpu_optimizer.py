@@ -2,6 +2,7 @@
 derived).  8-bit codes and stochastically rounded numbers have to lie between the roundings of the two ends of the bound, by the same random bits."""
 import ctypes as C
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -332,6 +333,29 @@ def test_norm_of_the_same_list_again_and_again(gpu, sizes):
     for _ in range(3):
         near(b.ef21_grad_norm(lists, 2.0, workspace=space), want())
         assert int(space[:4].max()) == 0
+
+
+def test_norm_of_one_list_by_two_threads(gpu):
+    """Calls of several launches each, on the same stream and list, from two threads."""
+    torch, b = gpu
+    lists = b.TensorList([torch.full((2000,), 0.5, device="cuda") for _ in range(400)] + [torch.full((200000,), 0.5, device="cuda")])
+    got, failed = [], []
+
+    def work():
+        try:
+            outs = [b.ef21_grad_norm(lists, 1.0) for _ in range(50)]
+            got.extend(norm for norm, _ in outs)
+        except Exception as e:                                          # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed and len(got) == 100
+    assert all(float(x) == 500.0 for x in got)                          # the root of a million quarters
 
 
 def test_norm_of_odd_values(gpu):
