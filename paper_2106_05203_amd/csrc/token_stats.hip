@@ -4,7 +4,7 @@
 //   d logp / d x_v = [v = label] - p_v,   d entropy / d x_v = -p_v (log p_v + entropy)
 //
 // A row is cut into tiles of 512 pieces of 16 bytes, a wavefront's registers full.  Each tile has an M of its own, a whole number next to its maximum: no z
-// is above 1/2, so that t has one sign, the difference does not cancel and nothing leaves fp32's range, and no maximum has to be carried along.  A tile
+// is above 1/2, so that t's terms have one sign but for the largest entries', nothing leaves fp32's range and no maximum has to be carried along.  A tile
 // leaves its M, s and t, and the tiles are joined in an order that the row's length alone fixes.
 //   The alternatives: a wavefront keeps the 64 best entries that it has met, one a lane, in order.  The pieces' maxima, which M needs anyway, tell which
 // pieces have an entry above the k-th.  Those few go through LDS, an entry a lane; an entry that is better is inserted, or ordered and merged with others.
