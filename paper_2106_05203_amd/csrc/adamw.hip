@@ -71,13 +71,31 @@ __device__ __forceinline__ void store4(void *p, int64_t i, const float (&f)[kVec
     __builtin_nontemporal_store(r, reinterpret_cast<typename Four<T>::type *>(static_cast<T *>(p) + i));
 }
 
-// The root, correctly rounded where v >= 2^-100 (below, where the residues leave fp32's range, off by one in its last bit): the hardware's, which is
-// off by one at the most, or a neighbour.  Zero, infinity and NaN give residues that are not on the wrong side.
-__device__ __forceinline__ float root_of(float v) {
+// The root, correctly rounded: the hardware's, which is off by one at the most, or a neighbour.  Zero, infinity and NaN give residues that are not on the
+// wrong side.  Not for 0 < v < kLowSquare: the residues leave fp32's range, and of numbers below 2^-126 the hardware's root is zero.
+constexpr float kLowSquare = 0x1p-96f;
+__device__ __forceinline__ float root_above(float v) {
     const float s = __builtin_amdgcn_sqrtf(v);
     const float down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
     const float below = fmaf(-down, s, v), above = fmaf(-up, s, v);
     return above > 0.f ? up : below <= 0.f ? down : s;
+}
+// The roots of a lane's entries, those of low ones of 2^64 v: exact on both sides, since v is 2^-149 at the least.
+__device__ __forceinline__ void roots_of(const float (&v)[kVec], float (&root)[kVec]) {
+    float least = v[0];
+#pragma unroll
+    for (int j = 1; j < kVec; ++j) least = fminf(least, v[j]);
+    if (least < kLowSquare) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+            const bool low = v[j] < kLowSquare;
+            const float r = root_above(low ? v[j] * 0x1p64f : v[j]);
+            root[j] = low ? r * 0x1p-32f : r;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) root[j] = root_above(v[j]);
+    }
 }
 
 // x / s correctly rounded but for one in millions, from 1 / s that is off by its last bit, where the remainder is in fp32's range (x / s above 2^-20, say,
@@ -213,10 +231,11 @@ struct Entries {
                 const float g = (float)g_in[j] * scale, old = old_v[j] * vs;
                 m[j] = old_m[j] * ms * o.beta1 + g * o.more1;
                 v[j] = old * old * o.beta2 + g * g * o.more2;
-                root[j] = root_of(v[j]);
                 most_m = fmaxf(most_m, fabsf(m[j]));
-                most_v = fmaxf(most_v, root[j]);
             }
+            roots_of(v, root);
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) most_v = fmaxf(most_v, root[j]);
             ms = fmaxf(wave_max_size(most_m) * (1.f / kMost8), 0x1p-126f);
             vs = fmaxf(wave_max_size(most_v) * (1.f / kMost8), 0x1p-126f);
             const float over_m = inverse_of(ms), over_v = inverse_of(vs);
@@ -250,8 +269,8 @@ struct Entries {
                 const float g = (float)g_in[j] * scale;
                 m[j] = fmaf(o.more1, g, o.beta1 * m_in[j]);
                 v[j] = fmaf(o.more2 * g, g, o.beta2 * v_in[j]);
-                root[j] = root_of(v[j]);
             }
+            roots_of(v, root);
         }
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {

@@ -1,0 +1,63 @@
+"""AdamW at the ends of fp32's range and beyond them, in 64 bits beside the kernel."""
+import math
+
+import numpy as np
+import pytest
+
+import stats_reference as ref
+from lm_reference import U
+from test_gpu_optimizer import BETAS, as64, make, states
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+    from paper_2106_05203_amd import binding
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    binding.load_library()
+    return torch, binding
+
+
+@pytest.mark.parametrize("size", [1e-17, 1e-18, 1e-19, 1e-20])
+def test_roots_below_the_least_normal_number(gpu, size):
+    """Gradients whose v lies below 2^-126, with an eps far below their roots.  v is two products and a sum: 7 u of itself and, below 2^-126 where fp32's
+    numbers are 2^-149 apart, half of that for its product and its sum; the root is correctly rounded, and counted with 2 u; the rest as in
+    stats_reference.  The bounds of v go through the root and the quotient as they are, not to first order."""
+    torch, b = gpu
+    eps, lr, step = 1e-25, 1e-3, 5
+    x = make(torch, 600, "f32", "f32", False, seed=2, size=size)
+    p, g, m, v = as64(x["p"].t), as64(x["g"].t), states(x, "m"), states(x, "v")
+    b.AdamW([x["p"].t], [x["g"].t], betas=BETAS, eps=eps, weight_decay=0.0, m=[x["m"].t], v=[x["v"].t]).step(lr, step=step)
+    b1, b2 = BETAS
+    new_m, new_v = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    d_m, d_v = 5 * U * (np.abs(b1 * m) + np.abs((1 - b1) * g)), 7 * U * new_v + 2.0 ** -149
+    ref.between(as64(x["v"].t), new_v - d_v, new_v + d_v, "v")
+    c1, c2 = 1 / (1 - b1 ** step), 1 / math.sqrt(1 - b2 ** step)
+    least = np.sqrt(np.maximum(new_v - d_v, 0.0)) * (1 - 2 * U) * c2 + eps
+    most = np.sqrt(new_v + d_v) * (1 + 2 * U) * c2 + eps
+    q = np.stack([(new_m + s * d_m) * c1 / den for s in (-1, 1) for den in (least, most)])
+    q_low, q_high = q.min(0), q.max(0)
+    slack = 16 * U * np.maximum(np.abs(q_low), np.abs(q_high))
+    end = 4 * U * np.abs(p) + lr * 4 * U * np.abs(q).max(0)
+    ref.between(as64(x["p"].t), p - lr * (q_high + slack) - end, p - lr * (q_low - slack) + end, "parameters")
+    # and they are updates of the order of lr, but for the two entries that had no v before
+    moved = np.abs(as64(x["p"].t) - p)
+    assert np.delete(moved, [3, 4]).max() < 10 * lr
+
+
+@pytest.mark.parametrize("stochastic", [False, True])
+def test_a_tiny_root_beside_large_ones_is_not_rounded_to_zero(gpu, stochastic):
+    """8-bit blocks with one gradient of 1 and others of 1e-20, whose v of 1e-43 is 71 of fp32's least steps: stored as the least number above zero.
+    The first step is lr but for v's two roundings, each half a step of 71, half of which the root has; 2 % is far beyond that."""
+    torch, b = gpu
+    g = torch.full((1000,), 1e-20, device="cuda")
+    g[::256] = 1.0
+    p = torch.zeros(1000, device="cuda")
+    opt = b.AdamW([p], [g], betas=BETAS, eps=1e-25, weight_decay=0.0, bits=8, stochastic=stochastic, seed=3)
+    opt.step(1e-3)
+    v = as64(opt.v[0])
+    assert np.all(v[::256] == 448.0)
+    assert np.all(np.delete(v, np.arange(0, 1000, 256)) == 2.0 ** -9), "a root above zero was stored as something else than the least number"
+    assert np.all(np.abs(as64(p) + 1e-3) <= 0.02 * 1e-3)
