@@ -61,3 +61,22 @@ def test_a_tiny_root_beside_large_ones_is_not_rounded_to_zero(gpu, stochastic):
     assert np.all(v[::256] == 448.0)
     assert np.all(np.delete(v, np.arange(0, 1000, 256)) == 2.0 ** -9), "a root above zero was stored as something else than the least number"
     assert np.all(np.abs(as64(p) + 1e-3) <= 0.02 * 1e-3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("stochastic", [False, True])
+def test_a_nan_of_any_sign_and_payload_passes_into_8_bits(gpu, stochastic, dtype):
+    """A gradient of all ones (memory filled with 0xFF) and the ordinary NaN, of both signs: m, v and p of the entry are NaN, its neighbours are not."""
+    torch, b = gpu
+    kind, whole = {"f32": (torch.int32, torch.float32), "bf16": (torch.int16, torch.bfloat16), "f16": (torch.int16, torch.float16)}[dtype]
+    quiet = {"f32": 0x7fc00000, "bf16": 0x7fc0, "f16": 0x7e00}[dtype]
+    g = torch.full((600,), 1e-3, device="cuda").to(whole)
+    where = {5: -1, 300: torch.iinfo(kind).max, 301: quiet, 599: quiet + torch.iinfo(kind).min}
+    for at, word in where.items():
+        g.view(kind)[at] = word
+    p = torch.ones(600, device="cuda")
+    opt = b.AdamW([p], [g], betas=BETAS, weight_decay=0.0, bits=8, stochastic=stochastic, seed=3)
+    for _ in range(3):                                                 # (other random bits)
+        opt.step(1e-3)
+        for name, t in (("p", p), ("m", opt.m[0]), ("v", opt.v[0])):
+            assert np.flatnonzero(np.isnan(as64(t))).tolist() == sorted(where), name
