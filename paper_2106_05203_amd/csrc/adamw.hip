@@ -256,7 +256,7 @@ struct Entries {
                 for (int j = 0; j < kVec; ++j) {
                     qm[j] = quotient(m[j], ms, over_m);
                     qv[j] = quotient(root[j], vs, over_v);
-                    qv[j] = root[j] > 0.f ? fmaxf(qv[j], kLeast8) : qv[j];
+                    qv[j] = root[j] > 0.f ? __builtin_elementwise_maximum(qv[j], kLeast8) : qv[j];  // NaN where the scale is infinite, which fmaxf would hide
                 }
                 m8 = __builtin_amdgcn_cvt_pk_fp8_f32(qm[0], qm[1], 0, false);
                 m8 = __builtin_amdgcn_cvt_pk_fp8_f32(qm[2], qm[3], m8, true);
@@ -275,7 +275,8 @@ struct Entries {
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
             const float old = (float)p_in[j];
-            const float under = fminf(fmaf(root[j], o.scale2, o.eps), kLargest);
+            // (an infinite root divides to zero, by the largest number; one that is NaN stays so, which fminf would hide)
+            const float under = __builtin_elementwise_minimum(fmaf(root[j], o.scale2, o.eps), kLargest);
             p[j] = fmaf(-o.lr, fmaf(it.decay, old, quotient(m[j] * o.scale1, under, __builtin_amdgcn_rcpf(under))), old);
             if constexpr (sizeof(P) == 2) {
                 if (random && fabsf(p[j]) < INFINITY) p[j] = random_param<P>(p[j], mixed(bits[j] + 0x3C6EF372u) & 0xffffu);

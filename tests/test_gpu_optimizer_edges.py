@@ -80,3 +80,29 @@ def test_a_nan_of_any_sign_and_payload_passes_into_8_bits(gpu, stochastic, dtype
         opt.step(1e-3)
         for name, t in (("p", p), ("m", opt.m[0]), ("v", opt.v[0])):
             assert np.flatnonzero(np.isnan(as64(t))).tolist() == sorted(where), name
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_a_v_that_is_not_a_number_passes_into_the_parameter(gpu, eight):
+    """v is NaN where m is not: as a state that is given, and after a finite gradient whose square is beyond fp32, which makes an 8-bit block's v infinite
+    and so NaN, or a 32-bit v infinite (which divides m to zero)."""
+    torch, b = gpu
+    x = make(torch, 600, "f32", "f32", eight, seed=9)
+    more = dict(m_scale=[x["m_scale"].t], v_scale=[x["v_scale"].t]) if eight else {}
+    x["v"].t[300] = math.nan
+    opt = b.AdamW([x["p"].t], [x["g"].t], betas=BETAS, weight_decay=0.0, bits=8 if eight else 32, m=[x["m"].t], v=[x["v"].t], **more)
+    opt.step(1e-3)
+    assert np.flatnonzero(np.isnan(as64(x["p"].t))).tolist() == [300] and np.isnan(as64(x["v"].t)[300]) and not np.isnan(as64(x["m"].t)[300])
+    # (1e20)^2 is beyond fp32, where 8-bit states round it by itself; 1e-3 (1e20)^2 = 1e37 is not, in 32 bits' one product and sum; that of 1e22 is
+    for huge in (1e20, 1e22):
+        infinite = eight or huge > 1e21
+        p, g = torch.ones(600, device="cuda"), torch.full((600,), 1e-3, device="cuda")
+        g[7] = huge
+        opt = b.AdamW([p], [g], betas=BETAS, weight_decay=0.0, bits=8 if eight else 32)
+        opt.step(1e-3)
+        assert bool(torch.isfinite(p).all()) and (float(p[7]) == 1.0) == infinite
+        after = float(p[7])
+        g[7] = 1e-3
+        opt.step(1e-3)
+        assert np.flatnonzero(np.isnan(as64(p))).tolist() == (list(range(256)) if eight else [])
+        assert eight or (float(p[7]) == after) == infinite
