@@ -477,6 +477,14 @@ typedef struct ef21_adamw_options {
 
 int ef21_adamw(const ef21_adamw_tensor *tensors, int32_t tensor_count, const ef21_adamw_options *options, void *hip_stream);
 
+/*
+ * The same with the step's number counted on the device, where the host does not know which steps are skipped: counter is 16 bytes of device
+ * memory, 8-byte aligned, that begin with the int64 number of the last step taken (0 at first, below 0 counts as 0; the caller may set it between
+ * calls) and are otherwise the call's own.  Where f is finite the number goes up by one and is the step's; where it is not, it stays.  A captured
+ * call counts at every replay.  options->step is not read, and options->step_device must be NULL.
+ */
+int ef21_adamw_counted(const ef21_adamw_tensor *tensors, int32_t tensor_count, const ef21_adamw_options *options, void *counter, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

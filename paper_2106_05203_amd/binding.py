@@ -33,6 +33,7 @@ SYMBOLS = (
     "ef21_topk_static", "ef21_embed", "ef21_embed_grad_workspace", "ef21_embed_grad", "ef21_token_logps", "ef21_token_logps_grad",
     "ef21_preference_loss_workspace", "ef21_preference_loss", "ef21_policy_loss_workspace", "ef21_policy_loss",
     "ef21_token_stats_workspace", "ef21_token_stats", "ef21_token_stats_grad", "ef21_grad_norm_workspace", "ef21_grad_norm", "ef21_adamw",
+    "ef21_adamw_counted",
 )
 K_COUNT = 11
 VALUE_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # EF21_F32, EF21_BF16, EF21_F16
@@ -115,6 +116,7 @@ def load_library() -> C.CDLL:
     lib.ef21_grad_norm_workspace.argtypes = [i32, p]
     lib.ef21_grad_norm.argtypes = [p, p, p, i32, f32, f32, p, p, p, i64, p]
     lib.ef21_adamw.argtypes = [p, i32, p, p]
+    lib.ef21_adamw_counted.argtypes = [p, i32, p, p, p]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = C.c_int
     lib.ef21_kernel_name.restype = C.c_char_p
@@ -589,7 +591,7 @@ class AdamW:
     bits: 32 or 8 for the states, or a list of one or the other per tensor.  m, v, m_scale, v_scale: states to go on with (fp32, or
     float8_e4m3fn with one fp32 scale per 256 entries), each a list per tensor; new ones otherwise, also for None in a list.
     copies: a list of bf16 or fp16 tensors (or None) that receive the new fp32 parameters.  weight_decay: a number, or one per tensor.
-    stochastic, seed: see include/ef21.h.  The tensors stay the caller's; the object keeps them alive and works on the memory
+    stochastic, seed: see include/ef21.h.  steps: the number of the last step that was taken, which may be set.  The tensors stay the caller's; the object keeps them alive and works on the memory
     that they have when they are given, also if their .data is another's later on.  Steps of one object follow each other: in one thread,
     and on one stream or on streams that wait for each other.
     """
@@ -656,7 +658,31 @@ class AdamW:
         else:
             self._check_apart(([], []))
         self._options = AdamwOptions(0.0, float(betas[0]), float(betas[1]), float(eps), 1, None, None, None, int(seed) & (2 ** 64 - 1), int(bool(stochastic)))
-        self.steps = 0
+        # The number of the last step: the host's, or counted on the device once a step might be skipped there (`_counted`: what the counter is
+        # known to hold); None if a tensor of the caller's has it.
+        self._steps, self._counting, self._counted = 0, False, 0
+        self._counter = torch.zeros(2, dtype=torch.int64, device=self.params[0].device)
+
+    @property
+    def steps(self) -> "int | None":
+        """The number of the last step that was taken (waits for the device where it is counted there); None where the caller's tensor has it."""
+        return int(self._counter[0]) if self._counting else self._steps
+
+    @steps.setter
+    def steps(self, number: int) -> None:
+        if number < 0:
+            raise ValueError("steps must not be negative")
+        self._counter[:1].fill_(number)
+        self._steps = self._counted = number
+
+    def _count(self) -> None:
+        """From here on the device counts."""
+        if self._counting or self._counted == self._steps:
+            return
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError("a captured step=None goes on from a number on the device: set `steps` before the capture, or give a tensor")
+        self._counter[:1].fill_(self._steps)
+        self._counted = self._steps
 
     _ROW = struct.Struct("7Qq3if")                                       # AdamwTensor
     _GRAD, _GRAD_TYPE = 1, 9                                             # its columns of gradients
@@ -719,9 +745,10 @@ class AdamW:
         return grads
 
     def step(self, lr, step: "int | torch.Tensor | None" = None, grad_scale: torch.Tensor | None = None, grads=None) -> None:
-        """One step.  lr: a number, or an fp32 tensor [1] on the device; step: its number from 1 on, an int64 tensor [1] on the device, or None
-        for the one after the last; grad_scale: fp32 [1] on the device, such as ef21_grad_norm's factor (where it is not finite, nothing is
-        changed); grads: gradients for this step and the following ones."""
+        """One step.  lr: a number, or an fp32 tensor [1] on the device; grad_scale: fp32 [1] on the device, such as ef21_grad_norm's factor (where it
+        is not finite the step is skipped: nothing is changed); grads: gradients for this step and the following ones.
+        step: its number from 1 on, an int64 tensor [1] on the device, or None for the one after the last that was taken: with grad_scale, or captured,
+        the device counts (at each replay), and a skipped step does not count.  A number that is given does, and after a tensor's one has to be given."""
         if grads is not None:
             self.grads = self._take(grads)
         if self.grads is None:
@@ -732,12 +759,23 @@ class AdamW:
         stepped = isinstance(step, torch.Tensor)
         if stepped:
             o.step, o.step_device = 1, _vector(step, 1, "step", torch.int64)
+        elif step is None and self._steps is None:
+            raise ValueError("the last step's number was on the device: give this one's")
         else:
-            o.step, o.step_device = (self.steps + 1 if step is None else step), None
-        _check(self._lib.ef21_adamw(self._table, len(self.params), C.byref(o),
-                                    _stream_of(self.params[0], lr if on_device else None, step if stepped else None, grad_scale)))
-        if not stepped:
-            self.steps = o.step
+            o.step, o.step_device = (1 if self._counting else self._steps + 1) if step is None else step, None
+        stream = _stream_of(self.params[0], lr if on_device else None, step if stepped else None, grad_scale)
+        if step is None and (self._counting or grad_scale is not None or torch.cuda.is_current_stream_capturing()):
+            self._count()
+            _check(self._lib.ef21_adamw_counted(self._table, len(self.params), C.byref(o), self._counter.data_ptr(), stream))
+            self._counting = True
+            return
+        _check(self._lib.ef21_adamw(self._table, len(self.params), C.byref(o), stream))
+        if stepped:
+            self._steps, self._counting, self._counted = None, False, None
+        elif self._counting:
+            self._counter[:1].fill_(o.step)
+        else:
+            self._steps = o.step
 
 
 class EF21:

@@ -146,6 +146,11 @@ __device__ __forceinline__ float random_param(float p, uint32_t bits) {
 // The step's numbers where they are read on the device.
 __device__ __forceinline__ void read_step(AdamwStep &o) {
     if (o.lr_device) o.lr = *o.lr_device;
+    if (o.counter) {
+        o.step = o.counter->number;
+        o.scale1 = o.counter->scale1;
+        o.scale2 = o.counter->scale2;
+    }
     if (o.step_device) {
         o.step = max(*o.step_device, (int64_t)1);
         const float t = (float)o.step;
@@ -153,6 +158,10 @@ __device__ __forceinline__ void read_step(AdamwStep &o) {
         o.scale2 = o.log_beta2 == -INFINITY ? 1.f : 1.f / sqrtf(-expm1f(t * o.log_beta2));
     }
 }
+
+// 1 / (1 - beta1^t) and 1 / sqrt(1 - beta2^t)
+__host__ __device__ inline float bias1(double beta, int64_t step) { return (float)(1.0 / (1.0 - pow(beta, (double)step))); }
+__host__ __device__ inline float bias2(double beta, int64_t step) { return (float)(1.0 / sqrt(1.0 - pow(beta, (double)step))); }
 
 __device__ __forceinline__ uint32_t key_of(const AdamwStep &o, int32_t number) { return mixed(mixed(o.seed + (uint32_t)o.step) + (uint32_t)number); }
 
@@ -393,6 +402,16 @@ void adamw_kernel(Table<BITS, COPY> table, AdamwStep o) {
     }
 }
 
+// A launch of its own in front of the step's: each of their workgroups reads the number, so none of them can write it.  It costs 2.4 us of a step of 146
+// tensors with 11.1 million entries (58.0 for 55.5), and 3.2 of one of four small ones.
+__global__ void count_step_kernel(StepCounter *counter, const float *grad_scale, double beta1, double beta2) {
+    if (grad_scale && !(fabsf(*grad_scale) < INFINITY)) return;
+    const int64_t number = max(counter->number, (int64_t)0) + 1;
+    counter->number = number;
+    counter->scale1 = bias1(beta1, number);
+    counter->scale2 = bias2(beta2, number);
+}
+
 // Launches for the tensors of one kind.
 struct Kind {
     int param, grad, bits, copy;                                   // copy: its type or -1
@@ -458,8 +477,8 @@ AdamwStep adamw_step(const ef21_adamw_options &o) {
     s.eps = (float)o.eps;
     s.log_beta1 = (float)std::log(o.beta1);
     s.log_beta2 = (float)std::log(o.beta2);
-    s.scale1 = (float)(1.0 / (1.0 - std::pow(o.beta1, (double)o.step)));
-    s.scale2 = (float)(1.0 / std::sqrt(1.0 - std::pow(o.beta2, (double)o.step)));
+    s.scale1 = bias1(o.beta1, o.step);
+    s.scale2 = bias2(o.beta2, o.step);
     s.step = o.step;
     s.lr_device = o.lr_device;
     s.step_device = o.step_device;
@@ -467,6 +486,11 @@ AdamwStep adamw_step(const ef21_adamw_options &o) {
     s.seed = mixed(mixed((uint32_t)o.seed) + (uint32_t)(o.seed >> 32));
     s.stochastic = o.stochastic;
     return s;
+}
+
+hipError_t launch_count_step(StepCounter *counter, const ef21_adamw_options &o, hipStream_t stream) {
+    hipLaunchKernelGGL(count_step_kernel, dim3(1), dim3(1), 0, stream, counter, o.grad_scale, o.beta1, o.beta2);
+    return hipGetLastError();
 }
 
 hipError_t launch_adamw(const ef21_adamw_tensor *tensors, int32_t count, const AdamwStep &step, hipStream_t stream) {

@@ -8,6 +8,12 @@ namespace ef21 {
 
 constexpr int kBlock8 = 256;                               // entries that share the scales of 8-bit states
 
+// A step's number on the device, and what the step takes from it.
+struct StepCounter {
+    int64_t number;                                        // of the last step that was taken
+    float scale1, scale2;                                  // as in AdamwStep
+};
+
 struct AdamwStep {
     float lr, beta1, more1, beta2, more2, eps;             // more: 1 - beta
     float log_beta1, log_beta2;                            // for a step read on the device
@@ -16,11 +22,14 @@ struct AdamwStep {
     const float *lr_device;
     const int64_t *step_device;
     const float *grad_scale;
+    const StepCounter *counter;                            // or nullptr: the number, in the place of both above
     uint32_t seed;                                         // of both halves of the caller's
     int32_t stochastic;
 };
 AdamwStep adamw_step(const ef21_adamw_options &o);
 hipError_t launch_adamw(const ef21_adamw_tensor *tensors, int32_t count, const AdamwStep &step, hipStream_t stream);
+// One more step in the counter, unless it is to be skipped.
+hipError_t launch_count_step(StepCounter *counter, const ef21_adamw_options &o, hipStream_t stream);
 
 struct NormArgs {
     float scale, max_norm;

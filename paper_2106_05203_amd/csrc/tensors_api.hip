@@ -35,6 +35,22 @@ int check_tensor(const ef21_adamw_tensor &t) {
     return EF21_OK;
 }
 
+// All but the number of the step.
+int check_adamw(const ef21_adamw_tensor *tensors, int32_t tensor_count, const ef21_adamw_options *options) {
+    if (tensor_count < 0) return invalid("tensor_count must not be negative");
+    if ((tensor_count > 0 && !tensors) || !options) return invalid("tensors or options is NULL");
+    for (int32_t i = 0; i < tensor_count; ++i)
+        if (int rc = check_tensor(tensors[i])) return rc;
+    const ef21_adamw_options &o = *options;
+    if (!std::isfinite(o.lr)) return invalid("lr must be finite");
+    if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0)) return invalid("beta1 and beta2 must be in [0, 1)");
+    if (!((float)o.eps >= 0x1p-126f) || !std::isfinite((float)o.eps)) return invalid("eps must be finite and at least 2^-126");
+    if (!aligned(o.lr_device, 4) || !aligned(o.grad_scale, 4)) return invalid("lr_device or grad_scale is misaligned");
+    return EF21_OK;
+}
+
+int launched(hipError_t st) { return st == hipSuccess ? EF21_OK : ef21::report_hip_error(st, "AdamW launch"); }
+
 }  // namespace
 
 extern "C" {
@@ -66,19 +82,24 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
 }
 
 int ef21_adamw(const ef21_adamw_tensor *tensors, int32_t tensor_count, const ef21_adamw_options *options, void *hip_stream) {
-    if (tensor_count < 0) return invalid("tensor_count must not be negative");
-    if ((tensor_count > 0 && !tensors) || !options) return invalid("tensors or options is NULL");
-    for (int32_t i = 0; i < tensor_count; ++i)
-        if (int rc = check_tensor(tensors[i])) return rc;
+    if (int rc = check_adamw(tensors, tensor_count, options)) return rc;
     const ef21_adamw_options &o = *options;
-    if (!std::isfinite(o.lr)) return invalid("lr must be finite");
-    if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0)) return invalid("beta1 and beta2 must be in [0, 1)");
-    if (!((float)o.eps >= 0x1p-126f) || !std::isfinite((float)o.eps)) return invalid("eps must be finite and at least 2^-126");
     if (o.step < 1) return invalid("step must be at least 1");
-    if (!aligned(o.lr_device, 4) || !aligned(o.step_device, 8) || !aligned(o.grad_scale, 4))
-        return invalid("lr_device, step_device or grad_scale is misaligned");
-    const hipError_t st = ef21::launch_adamw(tensors, tensor_count, ef21::adamw_step(o), (hipStream_t)hip_stream);
-    return st == hipSuccess ? EF21_OK : ef21::report_hip_error(st, "AdamW launch");
+    if (!aligned(o.step_device, 8)) return invalid("step_device is misaligned");
+    return launched(ef21::launch_adamw(tensors, tensor_count, ef21::adamw_step(o), (hipStream_t)hip_stream));
+}
+
+int ef21_adamw_counted(const ef21_adamw_tensor *tensors, int32_t tensor_count, const ef21_adamw_options *options, void *counter, void *hip_stream) {
+    if (int rc = check_adamw(tensors, tensor_count, options)) return rc;
+    if (options->step_device) return invalid("a step that is counted has no step_device");
+    if (!array_of(counter, 8)) return invalid("counter is NULL or misaligned");
+    ef21_adamw_options o = *options;
+    o.step = 1;                                                    // not read
+    ef21::AdamwStep step = ef21::adamw_step(o);
+    ef21::StepCounter *number = static_cast<ef21::StepCounter *>(counter);
+    step.counter = number;
+    const hipError_t st = ef21::launch_count_step(number, o, (hipStream_t)hip_stream);
+    return launched(st != hipSuccess ? st : ef21::launch_adamw(tensors, tensor_count, step, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"
