@@ -403,7 +403,8 @@ int ef21_token_stats(const void *logits, int type, int64_t rows, int64_t vocab, 
  * sums and entropy as ef21_token_stats gave them for these logits and labels.  grad_logp or grad_entropy may be NULL (zero); without labels
  * grad_logp must be.  Both are finite and are read in the rows that count.  accumulate != 0 adds to what is in grad_logits (the gradient of
  * another loss; rounded once more, and rows that are ignored stay as they are) and then grad_logits must not be the logits; else it may be.
- * Entries of probability zero, ignored rows and rows with nothing above -inf have a gradient of zero.
+ * Ignored rows and rows with nothing above -inf have a gradient of zero, and so have entries of probability zero but for the label's: as the
+ * formula says, that has grad_logp[r], also where it is -inf itself.
  */
 int ef21_token_stats_grad(const void *logits, int type, int64_t rows, int64_t vocab, int64_t stride, const void *labels,
                           int label_type, const float *sums, const float *entropy, const float *grad_logp,
