@@ -425,8 +425,8 @@ int ef21_token_stats_grad(const void *logits, int type, int64_t rows, int64_t vo
  * scale > 0: what the gradients still have to be multiplied by (1 / loss scale).  max_norm > 0; INFINITY clips nothing.  Squares and their
  * sum are fp64, in an order that the counts and types fix.  Where norm[0] is not finite factor[0] is NaN, which ef21_adamw takes for a step
  * to be skipped.
- * workspace: 256-byte aligned device memory of at least the bytes that ef21_grad_norm_workspace says, whose first four bytes (a counter of
- * workgroups that are done) are zero when a call begins; every call leaves them so.  Calls that share it must follow each other.
+ * workspace: 256-byte aligned device memory of at least the bytes that ef21_grad_norm_workspace says.  It may hold anything; a call that follows
+ * another with the same workspace finds its counter of workgroups ready.  Calls that share it must follow each other.
  */
 int ef21_grad_norm_workspace(int32_t tensor_count, int64_t *bytes);
 int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t *counts, int32_t tensor_count, float scale,

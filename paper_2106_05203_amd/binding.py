@@ -511,10 +511,10 @@ class TensorList:
         return len(self.tensors)
 
     def workspace(self, stream: int, bytes_of: int) -> torch.Tensor:
-        """A workspace for ef21_grad_norm on a stream: zeros at first, which each call leaves as it found them.  A captured call has one of its own."""
+        """A workspace for ef21_grad_norm on a stream.  A captured call has one of its own."""
         space = self._spaces.get(stream)
         if space is None or torch.cuda.is_current_stream_capturing():
-            space = torch.zeros(bytes_of, dtype=torch.uint8, device=self.tensors[0].device)
+            space = torch.empty(bytes_of, dtype=torch.uint8, device=self.tensors[0].device)
             if not torch.cuda.is_current_stream_capturing():
                 self._spaces[stream] = space
         return space
@@ -570,7 +570,7 @@ def ef21_grad_norm_workspace(tensor_count: int) -> int:
 def ef21_grad_norm(grads, max_norm: float = math.inf, scale: float = 1.0, norm: torch.Tensor | None = None, factor: torch.Tensor | None = None,
                    workspace: torch.Tensor | None = None):
     """(norm [1], factor [1]) of all gradients together (ef21_grad_norm); grads: a TensorList, or tensors.  `factor` is what AdamW.step
-    takes as grad_scale.  workspace: zeros before the first call with it; calls that share one follow each other."""
+    takes as grad_scale.  Calls that share a workspace follow each other."""
     lib = load_library()
     grads = grads if isinstance(grads, TensorList) else TensorList(grads)
     like = grads.tensors[0]

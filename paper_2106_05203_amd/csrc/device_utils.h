@@ -147,24 +147,47 @@ __device__ __forceinline__ void lds_add(float *p, float v) {
     __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
-// All threads of the workgroup call.  Publishes what the workgroup has stored, draws a ticket of `counter`, and
+// All threads of the workgroup call.  Publishes what the workgroup has stored, draws a ticket by `draw`, a thread's, and
 // returns true in the workgroup that drew the last of `tickets` (it may then read what the others published).  flag: LDS.
 // Every wavefront waits until its own stores and atomics have reached the L2 cache before the barrier: a barrier orders them, in the
 // compiler's terms, by the caches that the workgroup shares, and is emitted without that wait.  One thread then fences for the
 // workgroup: the device-scope fences write back and invalidate caches that the whole workgroup shares, so one of each is
 // enough and sixteen wavefronts' worth would only queue up (one launch per iteration, us a step: n = 4, m = 250, d = 100 7.6 so, 10.8 with a
 // fence by every wavefront; n = 20, m = 400, d = 300 19 and 84).
-__device__ __forceinline__ bool draw_ticket(uint32_t *counter, uint32_t tickets, uint32_t *flag) {
+template <class Draw>
+__device__ __forceinline__ bool draw_ticket_by(Draw draw, uint32_t tickets, uint32_t *flag) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();                                     // release
-        const uint32_t drawn = atomicAdd(counter, 1u);
+        const uint32_t drawn = draw();
         __threadfence();                                     // acquire
         *flag = drawn == tickets - 1u ? 1u : 0u;
     }
     __syncthreads();
     return *flag != 0u;
+}
+// The same of a counter that is zero before the first.
+__device__ __forceinline__ bool draw_ticket(uint32_t *counter, uint32_t tickets, uint32_t *flag) {
+    return draw_ticket_by([&] { return atomicAdd(counter, 1u); }, tickets, flag);
+}
+
+// The same of a counter in memory that may hold anything: it counts in its lower half once its upper half is kCounts, and what else is there is replaced by
+// the first that draws.  A drawing ends: it is tried again only where another workgroup has changed what was no count, which each does twice at the
+// most.  (Of all that 64 bits may hold `tickets` in 2^64 look like a count.)  The last of all leaves kCounts << 32.
+constexpr uint64_t kCounts = 0x6A09E667u;
+__device__ __forceinline__ uint32_t draw_any(unsigned long long *counter, uint32_t tickets) {
+    const auto counts = [&](unsigned long long seen) { return seen >> 32 == kCounts && (uint32_t)seen < tickets; };
+    for (;;) {
+        unsigned long long seen = atomicAdd(counter, 1ull);
+        if (counts(seen)) return (uint32_t)seen;
+        ++seen;
+        while (!counts(seen)) {
+            const unsigned long long was = atomicCAS(counter, seen, (unsigned long long)(kCounts << 32 | 1u));
+            if (was == seen) return 0u;
+            seen = was;
+        }
+    }
 }
 
 __device__ __forceinline__ uint32_t wave_inclusive_scan(uint32_t v) {

@@ -112,13 +112,14 @@ __device__ __forceinline__ void add_up(const double *sums, int32_t count, const 
 
 // sums: of this launch's workgroups; `before` in front of them are those of earlier launches.  tickets: workgroups that draw one, or 0.
 template <class T>
-__global__ __launch_bounds__(kThreads, 8) void square_sums_kernel(Table table, double *sums, int32_t before, uint32_t *counter, uint32_t tickets, NormArgs p) {
+__global__ __launch_bounds__(kThreads, 8) void square_sums_kernel(Table table, double *sums, int32_t before, unsigned long long *counter, uint32_t tickets,
+                                                                     NormArgs p) {
     __shared__ double part[kThreads / kWave];
     __shared__ uint32_t last;
     const double s = block_sum<kThreads / kWave>(sum_chunks<T, kThreads>(table), part);
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
-    if (tickets == 0 || !draw_ticket(counter, tickets, &last)) return;
-    if (threadIdx.x == 0) *counter = 0;
+    if (tickets == 0 || !draw_ticket_by([&] { return draw_any(counter, tickets); }, tickets, &last)) return;
+    if (threadIdx.x == 0) *counter = kCounts << 32;
     add_up<kThreads>(sums - before, before + (int32_t)tickets, p, part);
 }
 
@@ -143,7 +144,7 @@ size_t norm_workspace_bytes(int32_t tensors) {
 
 hipError_t launch_grad_norm(const void *const *grads, const int32_t *types, const int64_t *counts, int32_t tensors, const NormArgs &p, void *workspace,
                             hipStream_t stream) {
-    uint32_t *counter = static_cast<uint32_t *>(workspace);
+    unsigned long long *counter = static_cast<unsigned long long *>(workspace);
     double *sums = reinterpret_cast<double *>(static_cast<char *>(workspace) + kCounterBytes);
     int64_t chunks = 0;
     int32_t left = 0;                                              // tensors that no launch has taken yet
