@@ -108,8 +108,10 @@ __device__ __forceinline__ float quotient(float x, float s, float inverse) {
 // The byte of an e4m3 number by random rounding, in its place above 2^20: to the neighbour towards zero, or the one beyond it with the probability of what
 // lies above.  Times 2^-120 the least normal e4m3 number is fp32's, so that the exponent's lower four bits and three of the fraction's are the byte, below
 // the least normal number too; the sixteen random bits, each of which stands for the middle of its interval, are added to the twenty bits behind.
-// A NaN lies above 0x7f, its sign taken off (with it the sum could pass 2^32), and what is 448 up to rounding below it, whatever is added.
-__device__ __forceinline__ uint32_t random_code(float x, uint32_t bits) { return (__float_as_uint(x * 0x1p-120f) & 0x7fffffffu) + (bits << 4) + 8u; }
+// A NaN lies above 0x7f, also one whose sign is set, since the sum ends at 2^32 - 1; and what is 448 up to rounding below it, whatever is added.
+__device__ __forceinline__ uint32_t random_code(float size, uint32_t bits) {
+    return __builtin_elementwise_add_sat(__float_as_uint(size * 0x1p-120f), bits << 4 | 8u);
+}
 __device__ __forceinline__ uint32_t byte_of(uint32_t code) { return min(code >> 20, 0x7fu); }
 
 // The largest of a wavefront's numbers, which are not negative: as whole numbers, so that an instruction does each of the first four steps.
@@ -253,7 +255,7 @@ struct Entries {
 #pragma unroll
                 for (int j = 0; j < kVec; ++j) {
                     const float q = quotient(m[j], ms, over_m);
-                    cm[j] = byte_of(random_code(q, bits[j] & 0xffffu)) | (__float_as_uint(q) >> 24 & 0x80u);
+                    cm[j] = byte_of(random_code(fabsf(q), bits[j] & 0xffffu)) | (__float_as_uint(q) >> 24 & 0x80u);
                     // a root above zero has 2^20 and more for its bits
                     cv[j] = byte_of(max(random_code(quotient(root[j], vs, over_v), bits[j] >> 16), min(__float_as_uint(root[j]), 1u << 20)));
                 }
