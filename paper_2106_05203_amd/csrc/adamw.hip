@@ -5,9 +5,9 @@
 // 8 bits: e4m3 numbers of m / s_m and sqrt(v) / s_v, s = the largest of the block / 448.  The root, not v: in powers of two its range is half of v's,
 // and the update needs it anyway.  sqrt(v) > 0 is stored as 2^-9 s_v at the least: as zero it would divide the next m by eps alone.
 //
-// Measured: 403 million fp32 parameters with a bf16 copy, bf16 gradients, 32 bits: 1790 us, 6.3 TB/s; 201 million fp32 parameters and gradients, 8 bits:
-// 531 us, 6.1 TB/s, bound by memory.  11.2 million bf16 parameters in 146 tensors, 8 bits: 36.5 us where memory needs 18: three launches, and some 86
-// instructions an entry.
+// Measured: 403 million fp32 parameters with a bf16 copy, bf16 gradients, 32 bits: 1790 us, 6.3 TB/s.  201 million fp32 parameters and gradients, 8 bits:
+// 530 us, 6.1 TB/s, where memory needs 505 and the 77 vector instructions an entry some 400 (64 lanes a cycle and CU at 2.4 GHz).  11.2 million bf16 parameters
+// in 146 tensors, 8 bits: 37.3 us where memory needs 18 and 91 instructions an entry 26: three launches, each with a start and a tail.
 #include <cmath>
 
 #include "device_utils.h"
@@ -32,8 +32,8 @@ struct Item {
     int32_t number;                                                // of the tensor in the call
 };
 
-// A launch's tensors, as many as its 4 KB of arguments hold (83 in 32 bits, 58 in 8): a launch that follows another waits for its last workgroup, which
-// costs some 4 us.
+// A launch's tensors, as many as its 4 KB of arguments hold (76 in 32 bits, 58 in 8; with a copy 66 and 52): a launch that follows another waits for its
+// last workgroup, which costs some 4 us.
 template <int BITS, bool COPY>
 struct Table {
     static constexpr int kBytes = 4 * 8 + 8 + 3 * 4 + (BITS == 8 ? 2 * 8 : 0) + (COPY ? 8 : 0), kItems = (4096 - 40 - (int)sizeof(AdamwStep)) / kBytes;
@@ -52,6 +52,7 @@ struct Table {
         return Item{p[t], g[t], m[t], v[t], BITS == 8 ? ms[t] : nullptr, BITS == 8 ? vs[t] : nullptr, COPY ? copy[t] : nullptr, n[t], decay[t], number[t]};
     }
 };
+static_assert(Table<32, false>::kItems == 76 && Table<8, false>::kItems == 58 && Table<32, true>::kItems == 66 && Table<8, true>::kItems == 52, "as said");
 static_assert(sizeof(Table<32, false>) + sizeof(AdamwStep) <= 4096 && sizeof(Table<8, true>) + sizeof(AdamwStep) <= 4096, "the arguments of a kernel");
 
 // Four entries that lie anywhere.
@@ -345,9 +346,10 @@ struct Entries {
 // a copy, workgroups of one wavefront, four to a SIMD, 1790 us (6.3 TB/s); three 1805, five 1842; workgroups of two, three to a SIMD, 1842, eight 2012; two
 // blocks in flight 1908.  Without a copy, 134 million fp32 entries and gradients: 578, five to a SIMD 591, workgroups of two 604, of four 649.  11.2 million
 // in 146 tensors: 53.8, workgroups of two 55.6.
-//   8-bit states take some 90 instructions an entry, and as many wavefronts as there are: 201 million fp32 entries 536, three to a SIMD 594.  Two blocks in
-// flight of a wavefront where the chip has several rounds of workgroups: 541, with one 560, with four 557; else one, since a block takes a microsecond of
-// instructions: 11.2 million entries in 146 tensors 43, with two 47, with four 56.
+//   8-bit states take 77 to 91 instructions an entry, and as many wavefronts as there are: 201 million fp32 entries 531, three to a SIMD 558; 11.2 million
+// bf16 in 146 tensors (by the same clock) 41 and 53.  Two blocks in flight of a wavefront where the chip has several rounds of workgroups, for parameters in
+// 16 bits: 134 million bf16 300 us, with one 313, fp16 to nearest 229 and 264; 33 million 77 and 80, 62 and 69.  fp32 parameters do not gain by it: 134
+// million 359 and 343, 33 million 93 and 92; with four all lose (201 million 543, 11.2 million 46).  Fewer entries: one, since 11.2 million take 41 either way.
 template <int BITS, bool COPY>
 struct Shape {
     static constexpr int kWaves = BITS == 8 ? 4 : 1, kThreads = kWaves * kWave, kToSimd = BITS == 8 ? 8 : 4;

@@ -25,8 +25,9 @@ constexpr int kThreads = 256, kWaves = kThreads / kWave;
 // us for 204, 2001 rows of 32064 fp32 with 8 48.5 for 45.7.  The next tile on its way in registers of its own costs more than it hides: 8 pieces 210 and
 // 57, 8 with 3 wavefronts a SIMD 236 and 59, 4 with 5 227 and 49.
 constexpr int kEach = 8, kTile = kEach * kWave;
-constexpr int kEachShort = 2;                                      // of rows that have no more in all: 16384 rows of 1000 bf16, k = 5, with their
-                                                                   // gradient 43 us, where eight of which most are empty take 71
+// Of rows that have no more in all, where most of eight would be empty.  16384 rows of 300 to 1020 bf16 columns 13 us for 26, with 5 alternatives 26 for 44
+// (behind, 1030 columns by eight: 27 and 45); of 300 to 508 fp32 columns 11 for 17 and 22 for 36 (600 columns by eight: 18 and 36).
+constexpr int kEachShort = 2;
 constexpr int kMostSlices = 256;
 
 // Tiles of a row and how they are grouped: into at most 256 slices, each a wavefront's at a time.
