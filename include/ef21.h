@@ -439,7 +439,7 @@ int ef21_grad_norm(const void *const *grads, const int32_t *types, const int64_t
  * in fp32; with 8-bit states each product and sum of m and v is rounded by itself, so that the codes do not depend on how it is evaluated.
  * Where f is not finite nothing is changed.  An infinite or NaN gradient otherwise passes into m, v and p, of its entry alone with 32-bit
  * states; of 8-bit ones an infinity makes its block NaN (from the next step on where it is v's alone: that of a finite g' from 1.9e19 on, whose square
- * is rounded by itself).  A v that is NaN makes its p NaN.
+ * is rounded by itself).  A v that is NaN makes its p NaN, and so does a quotient beyond fp32.
  *   states: m, v fp32 (m_scale and v_scale NULL), or 8 bits: entry i of m stands for m_scale[i / 256] times the value of byte i as an OCP
  *           e4m3 number, and sqrt(v) for v_scale[i / 256] times that of v's byte; the scales, ceil(count / 256) of each, are the block's
  *           largest value / 448, 2^-126 at the least.  The update uses m and v before they are rounded to 8 bits.  A sqrt(v) above zero is
